@@ -174,6 +174,28 @@ int mixattn_append_kv_rope(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, cons
                            const int32_t* n_new, const void* k, const void* v, float rope_theta,
                            void* stream);
 
+/* Shaped attention scores of one layer, from the next call on.  (The paper's models use plain
+ * scores; models served beside them cap their scores or bias them by distance instead of, or
+ * next to, a rotary embedding.)  With s = softmax_scale * q . k of a query at position i and a key
+ * at position j:
+ *     a = softcap * tanh(s / softcap)   (softcap > 0; softcap = 0: a = s)
+ *     b = a - slopes[h] * (i - j)       (h = query head; slopes = NULL: b = a)
+ * and the softmax runs on b; masks and windows are applied after it.  Holds for mixattn_decode,
+ * _decode_layers, _decode_static_scratch, _prefill and _attend_chunk of that layer, for every
+ * dtype and kv_format, and for that layer alone (a layer that reuses a cache has scores of its
+ * own).  softcap = 0 with slopes = NULL restores plain scores.
+ *   slopes   host, n_q_heads values in [0, MIXATTN_SLOPE_MAX], copied
+ * The cap is evaluated to about six fp32 roundings (the fp32 mode: tanhf).  Keys and values of the
+ * attended tokens must be finite; what lies behind a sequence's last token does not matter.
+ * Errors: INVALID_ARG (layer, a softcap that is neither 0 nor in [MIXATTN_SOFTCAP_MIN,
+ * MIXATTN_SOFTCAP_MAX], a slope out of range or NaN), UNSUPPORTED (slopes with more than
+ * MIXATTN_MAX_SLOPE_HEADS query heads).  A call that fails changes nothing. */
+#define MIXATTN_SOFTCAP_MIN 1e-3f
+#define MIXATTN_SOFTCAP_MAX 1e6f
+#define MIXATTN_SLOPE_MAX 1024.f
+#define MIXATTN_MAX_SLOPE_HEADS 128
+int mixattn_set_layer_scores(mixattn_ctx* ctx, int32_t layer, float softcap, const float* slopes);
+
 /* One decode step of `layer` for n_seqs sequences (Section 3).  With n the
  * number of tokens in the cache the layer reads (its owner's, after this
  * step's append) the query sits at position n-1 and attends to keys
@@ -279,6 +301,63 @@ int mixattn_set_chunk_gather_reuse(mixattn_ctx* ctx, int32_t enable);
  * Errors: INVALID_ARG for a null context. */
 int mixattn_set_chunk_ring_direct(mixattn_ctx* ctx, int32_t enable);
 
+/* Copies sequences: every dst[i] becomes what src[i] was before the call, in every cache (Section 3
+ * keeps one cache per owner layer; generating with several hypotheses needs them copied and
+ * reordered).  All assignments happen at once, so dst = the slots of a beam group and src = the
+ * slots of the chosen parents reorders the group; a sequence may be the source of several copies,
+ * and src[i] == dst[i] leaves it alone.  What dst[i] held before is dropped as by
+ * mixattn_seq_reset.
+ *   src, dst   host, n sequence ids each; dst distinct
+ * A source that is itself overwritten hands its storage to its first copy without moving
+ * anything.  Every other copy shares the source's pages that are full in all full-attention
+ * owners (a page is free again when the last sequence that holds it lets go), and gets its own
+ * copy of the pages that are not and of the rings.  The overwritten sequences' pages return to
+ * the FIFO tail first (in call order, blocks in order); the copies then take theirs from its
+ * head, in call order.
+ * Errors: BAD_SEQ, INVALID_ARG (null, n < 0, dst not distinct), OUT_OF_PAGES (nothing changed),
+ * CUDA. */
+int mixattn_fork_seqs(mixattn_ctx* ctx, int32_t n, const int32_t* src, const int32_t* dst, void* stream);
+
+/* Copies cached keys and values out as plain tensors, e.g. to move a sequence elsewhere (append_kv
+ * is the way back) or to inspect a cache.
+ *   first_pos  host, first position per sequence; NULL = the oldest token stored
+ *   n_tokens   host, tokens per sequence (>= 0); NULL = up to the newest
+ *   k, v       device, [sum n_tokens, n_kv_heads, head_dim], sequences in call order, 16-byte
+ *              aligned, context dtype: the bits that were stored (after a fused rotary embedding),
+ *              or element * 2^X from a quantised cache
+ * Errors: BAD_SEQ, INVALID_ARG (null, unaligned, a range that is not stored -- a sliding-window
+ * cache holds the last `window` tokens), CUDA. */
+int mixattn_read_kv(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32_t* seq_ids,
+                    const int32_t* first_pos, const int32_t* n_tokens, void* k, void* v, void* stream);
+
+/* One step of beam search over n_groups groups of n_beams beams: scores every continuation
+ * (beam, token) of a group as
+ *     scores[beam] + logits[beam][token] - log(sum over t of exp(logits[beam][t]))
+ * and returns the n_out best in descending order, equal ones by the lower beam * vocab + token.
+ * The beams' sequences are then put in place with mixattn_fork_seqs.
+ *   logits      device, n_groups * n_beams rows of `vocab` elements of logits_dtype (MIXATTN_F32 or
+ *               MIXATTN_BF16), rows row_stride elements apart (any alignment)
+ *   scores      device, [n_groups, n_beams] sums of log-probabilities so far
+ *   finished    device, [n_groups, n_beams] or NULL: a beam with a non-zero entry has one
+ *               continuation, eos_token, at its own score; its logits are not read
+ *   out_scores, out_beams, out_tokens
+ *               device, [n_groups, n_out]; must not overlap the inputs.  Places without a
+ *               continuation hold -infinity, -1 and -1
+ * Only finite logits count (|x| < 2^126): a token with an infinite or NaN logit is no continuation
+ * and adds nothing to the sum.  A beam whose score is not finite has no continuation, so the first
+ * step of a group is scores = 0, -inf, -inf, ...  Sums and scores are formed in fp32 and double
+ * precision; the outputs are rounded to fp32 once.  Uses the context's workspace (one stream at a
+ * time, like every call).
+ * Errors: INVALID_ARG (null, n_beams outside 1 .. MIXATTN_MAX_BEAMS, n_out outside 1 ..
+ * MIXATTN_MAX_BEAM_OUT, vocab < 1 or n_beams * vocab beyond 2^31 - 1, row_stride < vocab, eos_token
+ * outside the vocabulary while `finished` is given), CUDA. */
+#define MIXATTN_MAX_BEAMS 64
+#define MIXATTN_MAX_BEAM_OUT 64
+int mixattn_beam_select(mixattn_ctx* ctx, int32_t n_groups, int32_t n_beams, int32_t vocab,
+                        int32_t logits_dtype, const void* logits, int64_t row_stride, const float* scores,
+                        const uint8_t* finished, int32_t eos_token, int32_t n_out, float* out_scores,
+                        int32_t* out_beams, int32_t* out_tokens, void* stream);
+
 /* Size of the static device array behind mixattn_decode_static_scratch. */
 #define MIXATTN_STATIC_SCRATCH_BYTES (8u << 20)
 
@@ -375,7 +454,10 @@ enum {
   MIXATTN_K_PREFILL_FULL = 4,
   MIXATTN_K_PREFILL_SLIDING = 5,
   MIXATTN_K_GATHER = 6,         /* copy of cached + chunk keys ahead of a chunk's attention */
-  MIXATTN_K_COUNT = 7
+  MIXATTN_K_FORK = 7,           /* copies of a fork                                         */
+  MIXATTN_K_READ = 8,           /* mixattn_read_kv                                          */
+  MIXATTN_K_SELECT = 9,         /* beam selection                                           */
+  MIXATTN_K_COUNT = 10
 };
 
 /* enable != 0: from now on every kernel launch is bracketed by CUDA events on

@@ -28,7 +28,7 @@ ERR_UNSUPPORTED = -7
 ERR_CUDA = -8
 ERR_TOO_LARGE = -9
 
-K_APPEND, K_DECODE_FULL, K_DECODE_SLIDING, K_COMBINE, K_PREFILL_FULL, K_PREFILL_SLIDING, K_GATHER = range(7)
+K_APPEND, K_DECODE_FULL, K_DECODE_SLIDING, K_COMBINE, K_PREFILL_FULL, K_PREFILL_SLIDING, K_GATHER, K_FORK, K_READ, K_SELECT = range(10)
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmixattn.so")
 
@@ -88,6 +88,10 @@ def _load() -> C.CDLL:
         "mixattn_debug_read_kv": [vp, i32, i32, i32, vp, vp],
         "mixattn_debug_read_kv_fp8": [vp, i32, i32, i32, vp, vp, vp, vp],
         "mixattn_get_device_status": [vp, p32],
+        "mixattn_set_layer_scores": [vp, i32, C.c_float, C.POINTER(C.c_float)],
+        "mixattn_fork_seqs": [vp, i32, p32, p32, vp],
+        "mixattn_read_kv": [vp, i32, i32, p32, p32, p32, vp, vp, vp],
+        "mixattn_beam_select": [vp, i32, i32, i32, i32, vp, C.c_int64, vp, vp, i32, i32, vp, vp, vp, vp],
         "mixattn_set_split_tokens": [vp, i32],
         "mixattn_set_chunk_gather_reuse": [vp, i32],
         "mixattn_set_chunk_ring_direct": [vp, i32],
@@ -108,7 +112,7 @@ lib = _load()
 EXPORTS = [
     "mixattn_arena_bytes", "mixattn_cache_bytes", "mixattn_create", "mixattn_destroy",
     "mixattn_seq_reset", "mixattn_append_kv", "mixattn_append_kv_rope", "mixattn_decode", "mixattn_decode_static_scratch", "mixattn_decode_layers", "mixattn_prefill",
-    "mixattn_attend_chunk",
+    "mixattn_attend_chunk", "mixattn_set_layer_scores", "mixattn_fork_seqs", "mixattn_read_kv", "mixattn_beam_select",
     "mixattn_get_len", "mixattn_get_block_table", "mixattn_get_n_free_pages",
     "mixattn_get_ring_state", "mixattn_locate", "mixattn_debug_read_kv", "mixattn_debug_read_kv_fp8",
     "mixattn_get_device_status", "mixattn_set_split_tokens", "mixattn_set_chunk_gather_reuse",
@@ -203,6 +207,7 @@ class Context:
             raise MixAttnError(rc, "mixattn_create")
         self.h = h
         self.n_q_heads, self.n_kv_heads, self.head_dim, self.dtype = n_q_heads, n_kv_heads, head_dim, dtype
+        self.layers = [(int(kind), int(window)) for kind, window, _ in layout]
 
     def close(self):
         if getattr(self, "h", None):
@@ -296,6 +301,99 @@ class Context:
         rc = self.rc_attend_chunk(layer, seq_ids, seq_lens, q, k, v, out, stream)
         if rc:
             raise MixAttnError(rc, "mixattn_attend_chunk")
+
+    def rc_set_layer_scores(self, layer, softcap=0.0, slopes=None) -> int:
+        a = None
+        if slopes is not None:
+            a = np.ascontiguousarray(slopes, dtype=np.float32)
+            if a.shape != (self.n_q_heads,):
+                return ERR_INVALID_ARG
+            a = a.ctypes.data_as(C.POINTER(C.c_float))
+        return lib.mixattn_set_layer_scores(self.h, layer, float(softcap), a)
+
+    def set_layer_scores(self, layer, softcap=0.0, slopes=None):
+        """Caps the layer's scores (softcap * tanh(s / softcap)) and / or biases them by distance
+        (- slopes[h] * (i - j), one slope per query head); the defaults restore plain scores."""
+        rc = self.rc_set_layer_scores(layer, softcap, slopes)
+        if rc:
+            raise MixAttnError(rc, "mixattn_set_layer_scores")
+
+    def rc_fork_seqs(self, src, dst, stream=None) -> int:
+        s, d = _i32(src), _i32(dst)
+        if len(s) != len(d):
+            return ERR_INVALID_ARG
+        return lib.mixattn_fork_seqs(self.h, len(s), _p32(s), _p32(d), _stream(stream))
+
+    def fork_seqs(self, src, dst, stream=None):
+        """Every sequence dst[i] becomes a copy of what src[i] was before the call (all at once)."""
+        rc = self.rc_fork_seqs(src, dst, stream)
+        if rc:
+            raise MixAttnError(rc, "mixattn_fork_seqs")
+
+    def read_kv(self, layer, seq_ids, first_pos=None, n_tokens=None, stream=None):
+        """Returns (K, V), the cached tokens [sum n_tokens, Hkv, D] of the sequences, oldest first
+        (default: everything stored).  The tensors are allocated on torch's current stream."""
+        import torch
+        s = _i32(seq_ids)
+        p = None if first_pos is None else _i32(first_pos)
+        n = None if n_tokens is None else _i32(n_tokens)
+        if (p is not None and len(p) != len(s)) or (n is not None and len(n) != len(s)):
+            raise MixAttnError(ERR_INVALID_ARG, "mixattn_read_kv")
+        rows = 0
+        for i, seq in enumerate(s.tolist()):
+            if n is not None:
+                rows += max(0, int(n[i]))
+            elif p is not None:
+                rows += max(0, self.get_len(layer, seq) - int(p[i]))
+            else:
+                rows += self._stored(layer, seq)
+        k = torch.empty(2, rows, self.n_kv_heads, self.head_dim,
+                        dtype=torch.bfloat16 if self.dtype == BF16 else torch.float32, device=self._device())
+        k, v = k[0], k[1]
+        rc = lib.mixattn_read_kv(self.h, layer, len(s), _p32(s), _p32(p), _p32(n), _dev(k), _dev(v), _stream(stream))
+        if rc:
+            raise MixAttnError(rc, "mixattn_read_kv")
+        return k, v
+
+    def _stored(self, layer, seq) -> int:
+        n = self.get_len(layer, seq)
+        kind, window = self.layers[layer]
+        return min(n, window) if kind == SLIDING else n
+
+    def _device(self):
+        return "cpu" if self.arena is None else self.arena.device
+
+    def rc_beam_select(self, logits, scores, n_out, out_scores, out_beams, out_tokens, finished=None, eos_token=0,
+                       stream=None) -> int:
+        """logits [groups, beams, vocab] (fp32 or bf16, last dimension dense, rows evenly spaced)."""
+        import torch
+        g, b, v = logits.shape
+        if logits.dtype not in (torch.float32, torch.bfloat16) or (v > 1 and logits.stride(2) != 1):
+            return ERR_INVALID_ARG
+        stride = logits.stride(1) if b > 1 else (logits.stride(0) if g > 1 else v)
+        if g > 1 and b > 1 and logits.stride(0) != b * stride:
+            return ERR_INVALID_ARG
+        for t, dt, n in ((scores, torch.float32, g * b), (finished, torch.uint8, g * b), (out_scores, torch.float32, g * n_out),
+                         (out_beams, torch.int32, g * n_out), (out_tokens, torch.int32, g * n_out)):
+            if t is not None and (t.dtype != dt or t.numel() != n or not t.is_contiguous()):
+                return ERR_INVALID_ARG
+        return lib.mixattn_beam_select(self.h, g, b, v, BF16 if logits.dtype == torch.bfloat16 else F32, _dev(logits),
+                                       max(stride, v) if g * b == 1 else stride, _dev(scores), _dev(finished),
+                                       int(eos_token), int(n_out), _dev(out_scores), _dev(out_beams), _dev(out_tokens),
+                                       _stream(stream))
+
+    def beam_select(self, logits, scores, n_out, finished=None, eos_token=0, stream=None):
+        """The n_out best continuations of every group: (scores fp32, beams int32, tokens int32),
+        [groups, n_out] each, allocated on torch's current stream."""
+        import torch
+        g = logits.shape[0]
+        s = torch.empty(g, n_out, dtype=torch.float32, device=logits.device)
+        b = torch.empty(g, n_out, dtype=torch.int32, device=logits.device)
+        t = torch.empty(g, n_out, dtype=torch.int32, device=logits.device)
+        rc = self.rc_beam_select(logits, scores, n_out, s, b, t, finished, eos_token, stream)
+        if rc:
+            raise MixAttnError(rc, "mixattn_beam_select")
+        return s, b, t
 
     def seq_reset(self, seq):
         rc = lib.mixattn_seq_reset(self.h, seq)

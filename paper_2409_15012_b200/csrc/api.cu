@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <atomic>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "cache_manager.hpp"
@@ -16,6 +17,7 @@ using namespace mixattn;
 namespace {
 
 constexpr size_t kAlign = 256;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSplitTokens = 4096;    // automatic split length of long caches (keys)
 constexpr int kMinSplitTokens = 1024; // single-wave splitting never makes splits shorter than this
 constexpr double kL2FitsShare = 0.55;  // a re-read ring up to this share of the L2 is cached whole
@@ -68,6 +70,13 @@ ArenaPlan plan_arena(const CacheManager& cm, const mixattn_config& cfg) {
   return pl;
 }
 
+// mixattn_set_layer_scores of one layer
+struct LayerScores {
+  float softcap = 0.f;
+  std::vector<float> slopes;   // per query head; empty = no bias
+  bool plain() const { return softcap == 0.f && slopes.empty(); }
+};
+
 struct ProfileRecord {
   int cls;
   cudaEvent_t start, stop;
@@ -86,6 +95,7 @@ struct mixattn_ctx {
   int sm_count = 148;
   int64_t l2_bytes = 0;
   float scale = 0.f;
+  std::vector<LayerScores> scores;   // per layer
   int32_t split_tokens = 0;
   int64_t launches = 0;
   bool profiling = false;
@@ -192,7 +202,7 @@ int enqueue_append(mixattn_ctx* c, int layer, int n_seqs, const int32_t* seq_ids
     for (size_t a = 0; a < grants.size(); a += kTableSetMax) {
       const size_t n = grants.size() - a < (size_t)kTableSetMax ? grants.size() - a : (size_t)kTableSetMax;
       for (size_t i = 0; i < n; ++i) {
-        tp.idx[i] = grants[a + i].seq * stride + grants[a + i].block;
+        tp.idx[i] = c->cm.slot(grants[a + i].seq) * stride + grants[a + i].block;
         tp.page[i] = grants[a + i].page;
       }
       tp.n = (int32_t)n;
@@ -219,16 +229,16 @@ int enqueue_append(mixattn_ctx* c, int layer, int n_seqs, const int32_t* seq_ids
     for (int j = 0; j < nb; ++j) {
       const int i = i0 + j;
       AppendEntry& e = p.e[j];
-      e.seq = seq_ids[i];
+      e.seq = c->cm.slot(seq_ids[i]);
       e.start_pos = start_pos[i];
       e.n_new = n_new ? n_new[i] : 1;
       e.src_row0 = row;
       e.page_hint = -1;
       e.tbl_idx = -1;
       if (!ring && single) {
-        e.page_hint = c->cm.table_row(e.seq)[e.start_pos / kPage];
+        e.page_hint = c->cm.table_row(seq_ids[i])[e.start_pos / kPage];
         // grants are in call order: at most one per sequence in single-token mode
-        if (gi < grants.size() && grants[gi].seq == e.seq) {
+        if (gi < grants.size() && grants[gi].seq == seq_ids[i]) {
           e.tbl_idx = e.seq * stride + grants[gi].block;
           ++gi;
         }
@@ -283,6 +293,7 @@ int mixattn_create(const mixattn_config* cfg, mixattn_ctx** out) {
   c->geom = make_geom(cfg->n_kv_heads, cfg->head_dim, cfg->dtype, cfg->kv_format);
   c->plan = plan_arena(c->cm, *cfg);
   c->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / sqrtf((float)cfg->head_dim);
+  c->scores.resize(cfg->n_layers);
   c->host_only = cfg->device < 0;
   c->device = cfg->device;
   if (!c->host_only) {
@@ -327,6 +338,201 @@ int mixattn_seq_reset(mixattn_ctx* c, int32_t seq) {
   if (!c->cm.valid_seq(seq)) return MIXATTN_ERR_BAD_SEQ;
   c->cm.seq_reset(seq);
   ++c->cache_epoch;
+  return MIXATTN_OK;
+}
+
+// Device side of the copies a fork made (see CacheManager::apply_fork).
+static int enqueue_fork(mixattn_ctx* c, const std::vector<ForkCopy>& copies, cudaStream_t st) {
+  ForkParams p;
+  p.arena = c->arena;
+  p.table = c->dev_table();
+  p.table_stride = c->cm.max_blocks();
+  p.n_segs = p.n_rows = 0;
+  auto flush = [&]() {
+    if (p.n_segs + p.n_rows == 0) return cudaSuccess;
+    cudaError_t e = launch_recorded(c, MIXATTN_K_FORK, st, [&] { return launch_fork_copy(p, st); });
+    p.n_segs = p.n_rows = 0;
+    return e;
+  };
+  auto add_seg = [&](size_t src, size_t dst, int64_t bytes) {
+    cudaError_t e = p.n_segs == kForkSegs ? flush() : cudaSuccess;
+    p.seg[p.n_segs++] = CopySeg{(int64_t)src, (int64_t)dst, (uint32_t)(bytes / 16)};
+    return e;
+  };
+  const int64_t page_bytes = c->geom.page_bytes;
+  // a segment's length is counted in 32 bits of 16-byte units; rings longer than that are cut
+  const int64_t max_bytes = (int64_t)1 << 34;
+  for (const ForkCopy& f : copies) {
+    for (size_t o = 0; o < c->cm.owners().size(); ++o) {
+      const LayerInfo& li = c->cm.layer(c->cm.owners()[o]);
+      const size_t pool = c->plan.owner_off[o];
+      if (li.kind == MIXATTN_FULL) {
+        for (size_t b = 0; b < f.src_pages.size(); ++b)
+          if (add_seg(pool + (size_t)f.src_pages[b] * page_bytes, pool + (size_t)f.dst_pages[b] * page_bytes, page_bytes) != cudaSuccess)
+            return MIXATTN_ERR_CUDA;
+        continue;
+      }
+      const int32_t n = c->cm.slot_len((int)o, f.dst_slot), valid = n < li.window ? n : li.window;
+      const size_t ring = (size_t)ring_pages_of(li.window) * page_bytes;
+      const int64_t bytes = (int64_t)ring_pages_of(valid) * page_bytes;
+      for (int64_t a = 0; a < bytes; a += max_bytes)
+        if (add_seg(pool + f.src_slot * ring + a, pool + f.dst_slot * ring + a, std::min(max_bytes, bytes - a)) != cudaSuccess)
+          return MIXATTN_ERR_CUDA;
+    }
+    int32_t set0 = f.n_shared, left = (int32_t)f.dst_pages.size();
+    bool first = true;
+    while ((first && f.n_shared > 0) || left > 0) {
+      if (p.n_rows == kForkRows && flush() != cudaSuccess) return MIXATTN_ERR_CUDA;
+      TableRow& r = p.row[p.n_rows++];
+      r.src_slot = f.src_slot;
+      r.dst_slot = f.dst_slot;
+      r.n_copy = first ? f.n_shared : 0;
+      r.set0 = set0;
+      r.n_set = left < kRowPages ? left : kRowPages;
+      for (int i = 0; i < r.n_set; ++i) r.page[i] = f.dst_pages[f.dst_pages.size() - left + i];
+      set0 += r.n_set;
+      left -= r.n_set;
+      first = false;
+    }
+  }
+  return flush() == cudaSuccess ? MIXATTN_OK : MIXATTN_ERR_CUDA;
+}
+
+int mixattn_fork_seqs(mixattn_ctx* c, int32_t n, const int32_t* src, const int32_t* dst, void* stream) {
+  if (c == nullptr) return MIXATTN_ERR_INVALID_ARG;
+  bool moved = false;
+  try {
+    int rc = c->cm.check_fork(n, src, dst);
+    if (rc != MIXATTN_OK) return rc;
+    if (!c->host_only && c->sticky_cuda_error) return MIXATTN_ERR_CUDA;
+    DeviceGuard g(c->host_only ? -1 : c->device);
+    if (!c->host_only && !g.ok) return MIXATTN_ERR_CUDA;
+    std::vector<ForkCopy> copies;
+    moved = true;
+    rc = c->cm.apply_fork(n, src, dst, &copies);
+    if (rc != MIXATTN_OK) return rc;
+    ++c->cache_epoch;
+    return c->host_only ? MIXATTN_OK : enqueue_fork(c, copies, static_cast<cudaStream_t>(stream));
+  } catch (const std::bad_alloc&) {   // no host memory: the bookkeeping may have moved, so the context is done
+    if (moved) c->sticky_cuda_error = true;
+    return MIXATTN_ERR_CUDA;
+  }
+}
+
+int mixattn_read_kv(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t* seq_ids, const int32_t* first_pos,
+                    const int32_t* n_tokens, void* k, void* v, void* stream) {
+  if (c == nullptr || !c->cm.valid_layer(layer) || n_seqs < 0 || (n_seqs > 0 && seq_ids == nullptr))
+    return MIXATTN_ERR_INVALID_ARG;
+  const LayerInfo& li = c->cm.layer(layer);
+  const bool ring = li.kind == MIXATTN_SLIDING;
+  // range of sequence i: [first, first + n) inside the stored tokens
+  auto range = [&](int i, int32_t* first, int32_t* n) {
+    const int32_t end = c->cm.len(layer, seq_ids[i]), oldest = end - c->cm.n_attended(layer, seq_ids[i]);
+    *first = first_pos ? first_pos[i] : oldest;
+    *n = n_tokens ? n_tokens[i] : end - *first;
+    return *first >= oldest && *n >= 0 && *first <= end && *n <= end - *first;
+  };
+  int64_t total = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    int32_t first, n;
+    if (!c->cm.valid_seq(seq_ids[i])) return MIXATTN_ERR_BAD_SEQ;
+    if (!range(i, &first, &n)) return MIXATTN_ERR_INVALID_ARG;
+    total += n;
+  }
+  if (total > INT32_MAX) return MIXATTN_ERR_INVALID_ARG;
+  if (c->host_only || c->sticky_cuda_error) return MIXATTN_ERR_CUDA;
+  if (total == 0) return MIXATTN_OK;
+  if (k == nullptr || v == nullptr || ((((size_t)k) | ((size_t)v)) & 15)) return MIXATTN_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return MIXATTN_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  GatherParams p;
+  p.k_chunk = p.v_chunk = nullptr;
+  p.k_out = k;
+  p.v_out = v;
+  p.pool = c->owner_storage(layer);
+  p.table = c->dev_table();
+  p.table_stride = c->cm.max_blocks();
+  p.is_ring = ring;
+  p.window = ring ? li.window : 0;
+  p.ring_pages = ring ? ring_pages_of(li.window) : 0;
+  p.geom = c->geom;
+  int32_t row = 0;
+  for (int i0 = 0; i0 < n_seqs; i0 += kMaxCallSeqs) {
+    int longest = 0;
+    p.n_entries = std::min(n_seqs - i0, kMaxCallSeqs);
+    for (int j = 0; j < p.n_entries; ++j) {
+      GatherEntry& e = p.e[j];
+      range(i0 + j, &e.pos0, &e.n_prefix);
+      e.seq = c->cm.slot(seq_ids[i0 + j]);
+      e.n_chunk = e.src_row0 = 0;
+      e.dst_row0 = row;
+      row += e.n_prefix;
+      longest = std::max(longest, e.n_prefix);
+    }
+    if (longest == 0) continue;
+    if (launch_recorded(c, MIXATTN_K_READ, st, [&] { return launch_read_kv(p, longest, st); }) != cudaSuccess)
+      return MIXATTN_ERR_CUDA;
+  }
+  return MIXATTN_OK;
+}
+
+int mixattn_beam_select(mixattn_ctx* c, int32_t n_groups, int32_t n_beams, int32_t vocab, int32_t logits_dtype,
+                        const void* logits, int64_t row_stride, const float* scores, const uint8_t* finished,
+                        int32_t eos_token, int32_t n_out, float* out_scores, int32_t* out_beams,
+                        int32_t* out_tokens, void* stream) {
+  if (c == nullptr || n_groups < 0 || n_beams < 1 || n_beams > MIXATTN_MAX_BEAMS || vocab < 1 || n_out < 1 ||
+      n_out > MIXATTN_MAX_BEAM_OUT || (logits_dtype != MIXATTN_F32 && logits_dtype != MIXATTN_BF16) ||
+      row_stride < vocab)
+    return MIXATTN_ERR_INVALID_ARG;
+  if ((int64_t)n_beams * vocab > INT32_MAX || (int64_t)n_groups * n_beams > INT32_MAX) return MIXATTN_ERR_INVALID_ARG;
+  if (finished != nullptr && (eos_token < 0 || eos_token >= vocab)) return MIXATTN_ERR_INVALID_ARG;
+  if (c->host_only || c->sticky_cuda_error) return MIXATTN_ERR_CUDA;
+  if (n_groups == 0) return MIXATTN_OK;
+  const int elem = logits_dtype == MIXATTN_BF16 ? 2 : 4;
+  if (logits == nullptr || scores == nullptr || out_scores == nullptr || out_beams == nullptr || out_tokens == nullptr ||
+      (size_t)logits % elem != 0)
+    return MIXATTN_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return MIXATTN_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  BeamParams p;
+  p.row_stride = row_stride;
+  p.n_beams = n_beams;
+  p.vocab = vocab;
+  p.n_out = n_out;
+  p.eos = eos_token;
+  // the chunks' results live in the split-KV workspace; groups that do not fit it together run
+  // one batch after the other
+  const size_t room = c->plan.status_off - c->plan.part_o_off;
+  const size_t per_chunk = sizeof(float2) + (size_t)n_out * sizeof(uint64_t);
+  const int64_t rows = (int64_t)n_groups * n_beams;
+  p.n_chunks = beam_chunks((int)rows, vocab, elem, c->sm_count, &p.chunk_granules);
+  if ((size_t)n_beams * p.n_chunks * per_chunk > room) {   // one group must fit: fewer chunks (the workspace holds MIXATTN_MAX_BEAMS rows of one)
+    const int64_t fit = (int64_t)(room / (n_beams * per_chunk));
+    const int64_t granules = (int64_t)p.n_chunks * p.chunk_granules;
+    p.chunk_granules = (int)((granules + fit - 1) / fit);
+    p.n_chunks = (int)((granules + p.chunk_granules - 1) / p.chunk_granules);
+  }
+  const size_t per_group = (size_t)n_beams * p.n_chunks * per_chunk;
+  int64_t batch = (int64_t)(room / per_group);
+  batch = std::min<int64_t>(batch, 65535 / n_beams);
+  char* ws = c->arena + c->plan.part_o_off;
+  for (int64_t g0 = 0; g0 < n_groups; g0 += batch) {
+    const int64_t r0 = g0 * n_beams;
+    p.n_groups = (int32_t)std::min<int64_t>(batch, n_groups - g0);
+    p.logits = static_cast<const char*>(logits) + r0 * row_stride * elem;
+    p.scores = scores + r0;
+    p.finished = finished ? finished + r0 : nullptr;
+    p.out_scores = out_scores + g0 * n_out;
+    p.out_beams = out_beams + g0 * n_out;
+    p.out_tokens = out_tokens + g0 * n_out;
+    p.part_keys = reinterpret_cast<uint64_t*>(ws);
+    p.part_sums = reinterpret_cast<float2*>(ws + (size_t)p.n_groups * n_beams * p.n_chunks * n_out * sizeof(uint64_t));
+    cudaError_t e = launch_recorded(c, MIXATTN_K_SELECT, st, [&] { return launch_beam_scan(p, elem, st); });
+    if (e == cudaSuccess) e = launch_recorded(c, MIXATTN_K_SELECT, st, [&] { return launch_beam_merge(p, st); });
+    if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
+  }
   return MIXATTN_OK;
 }
 
@@ -388,6 +594,34 @@ static void set_l2_policy(const mixattn_ctx* c, int layer, DecodeParams* p) {
   p->l2_keep_bytes = (uint32_t)(window <= fits ? window : room);
 }
 
+// Kernel parameters of a layer's shaped scores; false = plain scores (nothing to pass).
+static bool score_shape_of(const mixattn_ctx* c, int layer, ScoreShape* sh) {
+  const LayerScores& ls = c->scores[layer];
+  if (ls.plain()) return false;
+  sh->pre = ls.softcap > 0.f ? c->scale / ls.softcap : c->scale * kLog2e;
+  sh->post = ls.softcap * kLog2e;
+  sh->biased = !ls.slopes.empty();
+  for (size_t h = 0; h < ls.slopes.size(); ++h) sh->slope[h] = ls.slopes[h] * kLog2e;
+  return true;
+}
+
+// Where the keys of a decode launch sit relative to the query (sequences ids[0 .. nb)).
+static void set_distances(const mixattn_ctx* c, int layer, const int32_t* ids, int nb, ShapedDecodeParams* p) {
+  const LayerInfo& li = c->cm.layer(layer);
+  p->wrap = li.kind == MIXATTN_SLIDING ? li.window : 0;
+  for (int j = 0; j < nb; ++j) {
+    const int32_t n = c->cm.len(layer, ids[j]);
+    p->newest[j] = p->wrap ? (n - 1) % p->wrap : n - 1;
+  }
+}
+
+// The split pass of a decode launch; `shaped`: the layer's scores are shaped.
+static cudaError_t launch_split_pass(const mixattn_ctx* c, const ShapedDecodeParams& p, bool shaped, cudaStream_t st) {
+  const ShapedDecodeParams* sp = shaped ? &p : nullptr;
+  return c->cfg.dtype == MIXATTN_BF16 ? launch_decode_split_bf16(p, sp, c->sm_count, st)
+                                      : launch_decode_split_f32(p, sp, st);
+}
+
 // Split plan of one decode launch over sequences ids[0 .. nb): fills the per-sequence fields of
 // *p (seq_id, n_eff, chunk_len, chunk_base, n_seqs, total_items; group and head_chunks must be
 // set) and returns the number of split slots the launch writes; *any_split tells whether a
@@ -401,7 +635,7 @@ static int plan_splits(const mixattn_ctx* c, int layer, const int32_t* ids, int 
   const int Hkv = c->cfg.n_kv_heads;
   int64_t total = 0;
   for (int j = 0; j < nb; ++j) {
-    p->seq_id[j] = ids[j];
+    p->seq_id[j] = c->cm.slot(ids[j]);
     p->n_eff[j] = c->cm.n_attended(layer, ids[j]);
     total += p->n_eff[j];
   }
@@ -457,7 +691,8 @@ int mixattn_decode(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t*
   const int Hq = c->cfg.n_q_heads, Hkv = c->cfg.n_kv_heads, D = c->cfg.head_dim;
   const size_t esz = c->geom.elem_bytes;
 
-  DecodeParams p;
+  ShapedDecodeParams p;
+  const bool shaped = score_shape_of(c, layer, &p.shape);
   p.pool = c->owner_storage(layer);
   p.table = ring ? nullptr : c->dev_table();
   p.table_stride = c->cm.max_blocks();
@@ -466,7 +701,7 @@ int mixattn_decode(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t*
   p.n_q_heads = Hq;
   p.group = Hq / Hkv;
   p.head_chunks = (p.group + kMaxGroupRows - 1) / kMaxGroupRows;
-  p.scale_log2e = c->scale * 1.4426950408889634f;
+  p.scale_log2e = c->scale * kLog2e;
   p.part_o = reinterpret_cast<float*>(c->arena + c->plan.part_o_off);
   p.part_ml = reinterpret_cast<float2*>(c->arena + c->plan.part_ml_off);
   p.status = c->dev_status();
@@ -477,13 +712,11 @@ int mixattn_decode(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t*
     bool any_split = false;
     const int base = plan_splits(c, layer, seq_ids + i0, nb, &p, &any_split);
     if (base > kWsChunks) return MIXATTN_ERR_UNSUPPORTED;   // (cannot happen: the plan is bounded by the workspace)
+    if (shaped) set_distances(c, layer, seq_ids + i0, nb, &p);
     p.q = static_cast<const char*>(q) + (size_t)i0 * Hq * D * esz;
     p.out = static_cast<char*>(out) + (size_t)i0 * Hq * D * esz;
     const int cls = ring ? MIXATTN_K_DECODE_SLIDING : MIXATTN_K_DECODE_FULL;
-    cudaError_t e = launch_recorded(c, cls, st, [&] {
-      return c->cfg.dtype == MIXATTN_BF16 ? launch_decode_split_bf16(p, c->sm_count, st)
-                                          : launch_decode_split_f32(p, st);
-    });
+    cudaError_t e = launch_recorded(c, cls, st, [&] { return launch_split_pass(c, p, shaped, st); });
     if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
     if (any_split) {
       e = launch_recorded(c, MIXATTN_K_COMBINE, st,
@@ -550,11 +783,13 @@ int mixattn_prefill(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t
   const int Hq = c->cfg.n_q_heads, Hkv = c->cfg.n_kv_heads, D = c->cfg.head_dim;
   const size_t esz = c->geom.elem_bytes;
   PrefillParams p;
+  ScoreShape shape;
+  if (score_shape_of(c, layer, &shape)) p.shape = &shape;
   p.n_q_heads = Hq;
   p.n_kv_heads = Hkv;
   p.head_dim = D;
   p.window = li.kind == MIXATTN_SLIDING ? li.window : 0;
-  p.scale_log2e = c->scale * 1.4426950408889634f;
+  p.scale_log2e = c->scale * kLog2e;
   p.status = c->dev_status();
   int64_t row = 0;
   for (int i0 = 0; i0 < n_seqs; i0 += kMaxCallSeqs) {
@@ -647,11 +882,13 @@ int mixattn_attend_chunk(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const in
   gp.ring_pages = ring ? ring_pages_of(li.window) : 0;
   gp.geom = c->geom;
   PrefillParams p;
+  ScoreShape shape;
+  if (score_shape_of(c, layer, &shape)) p.shape = &shape;
   p.n_q_heads = Hq;
   p.n_kv_heads = Hkv;
   p.head_dim = D;
   p.window = ring ? li.window : 0;
-  p.scale_log2e = c->scale * 1.4426950408889634f;
+  p.scale_log2e = c->scale * kLog2e;
   p.status = c->dev_status();
   p.k = ks;
   p.v = vs;
@@ -699,7 +936,7 @@ int mixattn_attend_chunk(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const in
       const int rows = n_prefix[i] + seq_lens[i];
       if (krow + rows > scratch) break;
       GatherEntry& e = gp.e[nb];
-      e.seq = seq_ids[i];
+      e.seq = c->cm.slot(seq_ids[i]);
       e.n_prefix = n_prefix[i];
       e.pos0 = c->cm.len(layer, seq_ids[i]) - n_prefix[i];
       e.n_chunk = seq_lens[i];
@@ -709,7 +946,7 @@ int mixattn_attend_chunk(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const in
       p.krow0[nb] = direct ? qrow : krow;
       p.prefix[nb] = direct ? c->cm.len(layer, seq_ids[i]) : n_prefix[i];
       p.cached[nb] = p.prefix[nb];
-      p.ring_page0[nb] = seq_ids[i] * ring_pages_of(li.window);
+      p.ring_page0[nb] = c->cm.slot(seq_ids[i]) * ring_pages_of(li.window);
       krow += rows;
       qrow += seq_lens[i];
       if (seq_lens[i] > mlen) mlen = seq_lens[i];
@@ -799,12 +1036,12 @@ static int stored_page_of(mixattn_ctx* c, int layer, int seq, int pos, int64_t* 
   const LayerInfo& li = c->cm.layer(layer);
   if (li.kind == MIXATTN_FULL) {
     int32_t dev_page = -1;
-    if (cudaMemcpy(&dev_page, c->dev_table() + (size_t)seq * c->cm.max_blocks() + pos / kPage,
+    if (cudaMemcpy(&dev_page, c->dev_table() + (size_t)c->cm.slot(seq) * c->cm.max_blocks() + pos / kPage,
                    sizeof(int32_t), cudaMemcpyDeviceToHost) != cudaSuccess)
       return MIXATTN_ERR_CUDA;
     *phys = dev_page;
   } else {
-    *phys = (int64_t)seq * ring_pages_of(li.window) + *slot / kPage;
+    *phys = (int64_t)c->cm.slot(seq) * ring_pages_of(li.window) + *slot / kPage;
     *slot = *slot % kPage;
   }
   return MIXATTN_OK;
@@ -921,6 +1158,22 @@ int mixattn_get_device_status(mixattn_ctx* c, int32_t* status) {
   return MIXATTN_OK;
 }
 
+int mixattn_set_layer_scores(mixattn_ctx* c, int32_t layer, float softcap, const float* slopes) {
+  if (c == nullptr || !c->cm.valid_layer(layer)) return MIXATTN_ERR_INVALID_ARG;
+  if (!(softcap == 0.f || (softcap >= MIXATTN_SOFTCAP_MIN && softcap <= MIXATTN_SOFTCAP_MAX))) return MIXATTN_ERR_INVALID_ARG;
+  const int Hq = c->cfg.n_q_heads;
+  if (slopes != nullptr) {
+    for (int h = 0; h < Hq; ++h)
+      if (!(slopes[h] >= 0.f && slopes[h] <= MIXATTN_SLOPE_MAX)) return MIXATTN_ERR_INVALID_ARG;
+    if (Hq > kMaxSlopeHeads) return MIXATTN_ERR_UNSUPPORTED;
+  }
+  LayerScores ls;
+  ls.softcap = softcap;
+  if (slopes != nullptr) ls.slopes.assign(slopes, slopes + Hq);
+  c->scores[layer] = std::move(ls);
+  return MIXATTN_OK;
+}
+
 int mixattn_set_split_tokens(mixattn_ctx* c, int32_t tokens) {
   if (c == nullptr || tokens < 0) return MIXATTN_ERR_INVALID_ARG;
   c->split_tokens = tokens;
@@ -1023,7 +1276,9 @@ int mixattn_decode_static_scratch(mixattn_ctx* c, int32_t layer, int32_t n_seqs,
   const bool ring = li.kind == MIXATTN_SLIDING;
   const int Hq = c->cfg.n_q_heads, Hkv = c->cfg.n_kv_heads, D = c->cfg.head_dim;
 
-  DecodeParams p;
+  ShapedDecodeParams p;
+  const bool shaped = score_shape_of(c, layer, &p.shape);
+  if (shaped) set_distances(c, layer, seq_ids, n_seqs, &p);
   p.group = Hq / Hkv;
   p.head_chunks = (p.group + kMaxGroupRows - 1) / kMaxGroupRows;
   // the split plan of mixattn_decode (one function), so both calls add the partial results in
@@ -1050,7 +1305,7 @@ int mixattn_decode_static_scratch(mixattn_ctx* c, int32_t layer, int32_t n_seqs,
   p.ring_pages = ring ? ring_pages_of(li.window) : 0;
   p.geom = c->geom;
   p.n_q_heads = Hq;
-  p.scale_log2e = c->scale * 1.4426950408889634f;
+  p.scale_log2e = c->scale * kLog2e;
   set_l2_policy(c, layer, &p);
   // every partial slot that the combine pass reads is written by the split pass of the
   // same call first, so nothing in the array has to start at zero
@@ -1058,10 +1313,7 @@ int mixattn_decode_static_scratch(mixattn_ctx* c, int32_t layer, int32_t n_seqs,
   p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(scratch) + part_o_bytes);
   p.status = c->dev_status();
   const int cls = ring ? MIXATTN_K_DECODE_SLIDING : MIXATTN_K_DECODE_FULL;
-  cudaError_t e = launch_recorded(c, cls, st, [&] {
-    return c->cfg.dtype == MIXATTN_BF16 ? launch_decode_split_bf16(p, c->sm_count, st)
-                                        : launch_decode_split_f32(p, st);
-  });
+  cudaError_t e = launch_recorded(c, cls, st, [&] { return launch_split_pass(c, p, shaped, st); });
   if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
   if (any_split) {
     e = launch_recorded(c, MIXATTN_K_COMBINE, st, [&] { return launch_decode_combine(p, c->cfg.dtype, st); });

@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include <deque>
+#include <utility>
 #include <vector>
 
 #include "mixattn.h"
@@ -26,6 +27,15 @@ struct PageGrant {     // a block-table entry set during an append
   int32_t seq;
   int32_t block;
   int32_t page;
+};
+
+// What a fork has to move on the device for one copy that could not simply take over its
+// source's slot.  Blocks [0, n_shared) of the source's block table are shared (their pages gain
+// a reference); the blocks from n_shared on, which an append may still write to, are copied.
+struct ForkCopy {
+  int32_t src_slot, dst_slot;
+  int32_t n_shared;
+  std::vector<int32_t> src_pages, dst_pages;   // blocks n_shared .. of the source and of the copy
 };
 
 class CacheManager {
@@ -88,6 +98,9 @@ class CacheManager {
     if (allocate) {
       table_.assign((size_t)max_seqs_ * max_blocks_, -1);
       n_blocks_.assign(max_seqs_, 0);
+      refs_.assign(n_pages_, 0);
+      slot_.resize(max_seqs_);
+      for (int i = 0; i < max_seqs_; ++i) slot_[i] = i;
       len_.assign(owners_.size() * (size_t)max_seqs_, 0);
     }
     return MIXATTN_OK;
@@ -105,11 +118,16 @@ class CacheManager {
   bool valid_layer(int l) const { return l >= 0 && l < (int)layers_.size(); }
   bool valid_seq(int s) const { return s >= 0 && s < max_seqs_; }
 
+  // Storage slot of a sequence: the row of the device block table and the ring of every
+  // sliding-window owner that hold its tokens.  Lengths and tables are kept per slot, so that a
+  // fork hands a sequence on by renaming its slot.
+  int32_t slot(int seq) const { return slot_[seq]; }
   int32_t len(int layer, int seq) const {
-    return len_[(size_t)layers_[layer].owner_slot * max_seqs_ + seq];
+    return len_[(size_t)layers_[layer].owner_slot * max_seqs_ + slot_[seq]];
   }
-  int32_t n_blocks(int seq) const { return n_blocks_[seq]; }
-  const int32_t* table_row(int seq) const { return &table_[(size_t)seq * max_blocks_]; }
+  int32_t slot_len(int owner_slot, int slot) const { return len_[(size_t)owner_slot * max_seqs_ + slot]; }
+  int32_t n_blocks(int seq) const { return n_blocks_[slot_[seq]]; }
+  const int32_t* table_row(int seq) const { return &table_[(size_t)slot_[seq] * max_blocks_]; }
 
   // Keys a decode of `layer` attends to for `seq`: all of them, or the last `window`.
   int32_t n_attended(int layer, int seq) const {
@@ -137,7 +155,7 @@ class CacheManager {
       if (end > max_seq_len_) return MIXATTN_ERR_INVALID_ARG;
       if (li.kind == MIXATTN_FULL) {
         int64_t blocks = (end + kPageSize - 1) / kPageSize;
-        if (blocks > n_blocks_[s]) need += blocks - n_blocks_[s];
+        if (blocks > n_blocks(s)) need += blocks - n_blocks(s);
       }
     }
     if (need > (int64_t)free_.size()) return MIXATTN_ERR_OUT_OF_PAGES;
@@ -151,17 +169,16 @@ class CacheManager {
                     std::vector<PageGrant>* grants) {
     const LayerInfo& li = layers_[layer];
     for (int i = 0; i < n_seqs; ++i) {
-      int s = seq_ids[i];
+      const int s = slot_[seq_ids[i]];
       int32_t n = n_new ? n_new[i] : 1;
       int32_t& L = len_[(size_t)li.owner_slot * max_seqs_ + s];
       int32_t end = L + n;
       if (li.kind == MIXATTN_FULL) {
         int32_t blocks = (end + kPageSize - 1) / kPageSize;
         while (n_blocks_[s] < blocks) {
-          int32_t pg = free_.front();
-          free_.pop_front();
+          const int32_t pg = take_page();
           table_[(size_t)s * max_blocks_ + n_blocks_[s]] = pg;
-          if (grants) grants->push_back(PageGrant{s, n_blocks_[s], pg});
+          if (grants) grants->push_back(PageGrant{seq_ids[i], n_blocks_[s], pg});
           ++n_blocks_[s];
         }
       }
@@ -169,13 +186,104 @@ class CacheManager {
     }
   }
 
-  void seq_reset(int seq) {
-    for (size_t o = 0; o < owners_.size(); ++o) len_[o * max_seqs_ + seq] = 0;
-    for (int b = 0; b < n_blocks_[seq]; ++b) {
-      free_.push_back(table_[(size_t)seq * max_blocks_ + b]);
-      table_[(size_t)seq * max_blocks_ + b] = -1;
+  void seq_reset(int seq) { release_slot(slot_[seq]); }
+
+  // Checks a fork call (see apply_fork) apart from the pages it needs; nothing changes.
+  int check_fork(int n, const int32_t* src, const int32_t* dst) const {
+    if (n < 0 || (n > 0 && (src == nullptr || dst == nullptr))) return MIXATTN_ERR_INVALID_ARG;
+    std::vector<char> seen(max_seqs_, 0);
+    for (int i = 0; i < n; ++i) {
+      if (!valid_seq(src[i]) || !valid_seq(dst[i])) return MIXATTN_ERR_BAD_SEQ;
+      if (seen[dst[i]]) return MIXATTN_ERR_INVALID_ARG;
+      seen[dst[i]] = 1;
     }
-    n_blocks_[seq] = 0;
+    return MIXATTN_OK;
+  }
+
+  // Every dst[i] becomes what src[i] was before the call (all assignments at once).  A source
+  // that the call overwrites hands its slot to its first copy; every other copy gets the slot of
+  // an overwritten sequence without copies, shares the source's pages that are full in every
+  // full-attention owner (no append writes to those any more) and takes fresh pages for the
+  // rest.  Order of the page movements: the overwritten sequences' pages return to the FIFO
+  // tail in call order, then the copies take theirs from its head in call order.
+  // Returns MIXATTN_OK, or OUT_OF_PAGES with nothing changed.
+  int apply_fork(int n, const int32_t* src, const int32_t* dst, std::vector<ForkCopy>* copies) {
+    std::vector<int32_t> from(n), to(n, -1);              // slots before and after, per entry
+    std::vector<char> held(max_seqs_, 0);                 // slots that keep their contents
+    std::vector<char> overwritten(max_seqs_, 0);          // sequences the call replaces
+    for (int i = 0; i < n; ++i) {
+      from[i] = slot_[src[i]];
+      overwritten[dst[i]] = src[i] != dst[i];
+    }
+    for (int i = 0; i < n; ++i)                           // sources that stay (or map to themselves)
+      if (!overwritten[src[i]]) {
+        held[from[i]] = 1;
+        if (src[i] == dst[i]) to[i] = from[i];
+      }
+    for (int i = 0; i < n; ++i)                           // an overwritten source: its first copy takes over
+      if (to[i] < 0 && !held[from[i]]) {
+        held[from[i]] = 1;
+        to[i] = from[i];
+      }
+    // slots whose contents die, in call order, and the copies that move in: a copy stays in the
+    // slot its sequence had where it can
+    std::vector<int32_t> dead;
+    for (int i = 0; i < n; ++i)
+      if (!held[slot_[dst[i]]]) dead.push_back(slot_[dst[i]]);
+    std::vector<char> taken(max_seqs_, 0);
+    for (int i = 0; i < n; ++i)
+      if (to[i] < 0 && !held[slot_[dst[i]]]) {
+        to[i] = slot_[dst[i]];
+        taken[to[i]] = 1;
+      }
+    size_t at = 0;
+    for (int i = 0; i < n; ++i)
+      if (to[i] < 0) {
+        while (taken[dead[at]]) ++at;
+        to[i] = dead[at++];
+      }
+    // shared pages gain their references before the dead slots lose theirs; the pages needed are
+    // counted first, so that a call that cannot be served changes nothing
+    auto row = [&](int slot) { return &table_[(size_t)slot * max_blocks_]; };
+    int64_t need = 0, freed = 0;
+    for (int i = 0; i < n; ++i)
+      if (to[i] != from[i]) {
+        const int shared = n_shared(from[i]);
+        need += n_blocks_[from[i]] - shared;
+        for (int b = 0; b < shared; ++b) ++refs_[row(from[i])[b]];
+      }
+    for (int s : dead)
+      for (int b = 0; b < n_blocks_[s]; ++b) freed += --refs_[row(s)[b]] == 0;
+    for (int s : dead)                                    // (back as they were: release_slot does it for good)
+      for (int b = 0; b < n_blocks_[s]; ++b) ++refs_[row(s)[b]];
+    if (need > (int64_t)free_.size() + freed) {
+      for (int i = 0; i < n; ++i)
+        if (to[i] != from[i])
+          for (int b = 0; b < n_shared(from[i]); ++b) --refs_[row(from[i])[b]];
+      return MIXATTN_ERR_OUT_OF_PAGES;
+    }
+    for (int s : dead) release_slot(s);
+    for (int i = 0; i < n; ++i) {
+      if (to[i] == from[i]) continue;
+      ForkCopy c;
+      c.src_slot = from[i];
+      c.dst_slot = to[i];
+      c.n_shared = n_shared(from[i]);
+      for (int b = 0; b < n_blocks_[from[i]]; ++b) {
+        int32_t pg = row(from[i])[b];
+        if (b >= c.n_shared) {
+          c.src_pages.push_back(pg);
+          pg = take_page();
+          c.dst_pages.push_back(pg);
+        }
+        row(to[i])[b] = pg;
+      }
+      n_blocks_[to[i]] = n_blocks_[from[i]];
+      for (size_t o = 0; o < owners_.size(); ++o) len_[o * max_seqs_ + to[i]] = len_[o * max_seqs_ + from[i]];
+      copies->push_back(std::move(c));
+    }
+    for (int i = 0; i < n; ++i) slot_[dst[i]] = to[i];
+    return MIXATTN_OK;
   }
 
   // Page and slot of a stored token; false if it is not stored (any more).
@@ -185,7 +293,7 @@ class CacheManager {
     int32_t lo = li.kind == MIXATTN_SLIDING && n > li.window ? n - li.window : 0;
     if (pos < lo || pos >= n) return false;
     if (li.kind == MIXATTN_FULL) {
-      *page = table_[(size_t)seq * max_blocks_ + pos / kPageSize];
+      *page = table_row(seq)[pos / kPageSize];
       *slot = pos % kPageSize;
     } else {
       *page = -1;
@@ -195,6 +303,33 @@ class CacheManager {
   }
 
  private:
+  // Blocks of a slot whose 16 tokens are stored in every full-attention owner.
+  int n_shared(int slot) const {
+    int n = n_blocks_[slot];
+    for (size_t o = 0; o < owners_.size(); ++o)
+      if (layers_[owners_[o]].kind == MIXATTN_FULL) {
+        const int full = len_[o * max_seqs_ + slot] / kPageSize;
+        if (full < n) n = full;
+      }
+    return n;
+  }
+  int32_t take_page() {
+    const int32_t pg = free_.front();
+    free_.pop_front();
+    refs_[pg] = 1;
+    return pg;
+  }
+  // Empties a slot; a page returns to the FIFO tail when its last reference goes.
+  void release_slot(int slot) {
+    for (size_t o = 0; o < owners_.size(); ++o) len_[o * max_seqs_ + slot] = 0;
+    int32_t* row = &table_[(size_t)slot * max_blocks_];
+    for (int b = 0; b < n_blocks_[slot]; ++b) {
+      if (--refs_[row[b]] == 0) free_.push_back(row[b]);
+      row[b] = -1;
+    }
+    n_blocks_[slot] = 0;
+  }
+
   std::vector<LayerInfo> layers_;
   std::vector<int> owners_;
   int n_full_owners_ = 0;
@@ -202,7 +337,9 @@ class CacheManager {
   std::deque<int32_t> free_;
   std::vector<int32_t> table_;
   std::vector<int32_t> n_blocks_;
-  std::vector<int32_t> len_;
+  std::vector<int32_t> len_;        // per owner and slot
+  std::vector<int32_t> refs_;       // block tables that hold the page
+  std::vector<int32_t> slot_;       // storage slot of each sequence
 };
 
 }  // namespace mixattn

@@ -45,7 +45,10 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "internal.h"
+#include "score_shape.cuh"
 
 namespace mixattn {
 
@@ -241,15 +244,19 @@ __device__ __forceinline__ void cluster_share(Item& x, int crank) {
 // ingests K/V at a fixed rate, so a short launch that leaves SMs idle is halved this way
 // without a second launch.  The grid then holds exactly one cluster per item.
 // KV8 = 1: the cache holds FP8 E4M3 rows with shared exponents (see the top of the file).
+// SH = 1: the layer's scores are capped and / or biased by distance (score_shape.cuh).
 // Producer warps of a variant.  With more than one, the ring length must be a multiple of their
 // number (checked by the launcher): a stage then always belongs to the same producer, whose
 // program order keeps its waits on that stage's barriers one phase apart.  (A producer that
 // waited for a phase two ahead of the barrier's would be answered "complete" by the parity test.)
 __host__ __device__ constexpr int producer_warps(int ncw, int kv8) { return (kv8 && ncw == 8) ? 4 : 1; }
 
-template <int D, int NCW, int CL, int KV8>
+template <int SH>
+using LaunchParams = std::conditional_t<SH != 0, ShapedDecodeParams, DecodeParams>;
+
+template <int D, int NCW, int CL, int KV8, int SH>
 __global__ void __launch_bounds__((NCW + producer_warps(NCW, KV8)) * 32, NCW == 4 ? 2 : 1)
-decode_split_bf16_kernel(const __grid_constant__ DecodeParams p, const int n_stages) {
+decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n_stages) {
   constexpr int kConsumerWarps = NCW;
   constexpr int kProducerWarps = producer_warps(NCW, KV8);
   constexpr int kGroups = NCW / kGroupWarps;
@@ -421,6 +428,13 @@ decode_split_bf16_kernel(const __grid_constant__ DecodeParams p, const int n_sta
         qb[ks][1] = pack_f16(__low2float(b), __high2float(b));
       }
     }
+    float slope[2] = {0.f, 0.f};   // of this thread's two heads (SH)
+    if constexpr (SH) {
+      if (p.shape.biased) {
+        slope[0] = fcol < rows ? p.shape.slope[h0 + fcol] : 0.f;
+        slope[1] = fcol + 1 < rows ? p.shape.slope[h0 + fcol + 1] : 0.f;
+      }
+    }
     float m[2] = {-INFINITY, -INFINITY};
     float l[2] = {0.f, 0.f};
     float o[D / 16][4];   // O^T: rows = channels 16 jt + frow (+8), cols = the thread's two heads
@@ -451,7 +465,7 @@ decode_split_bf16_kernel(const __grid_constant__ DecodeParams p, const int n_sta
             mma_bf16(st2, b, qb[ks + 1][0], qb[ks + 1][1]);
           }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) st[e] = (st[e] + st2[e]) * p.scale_log2e;
+          for (int e = 0; e < 4; ++e) st[e] = SH ? st[e] + st2[e] : (st[e] + st2[e]) * p.scale_log2e;
         } else {
           // one ldmatrix.x4 = (tile rows 0-7 | 8-15) x (16-byte chunk 2j | 2j+1) = two 16-channel steps
 #pragma unroll
@@ -467,12 +481,27 @@ decode_split_bf16_kernel(const __grid_constant__ DecodeParams p, const int n_sta
           }
           // the shared exponents of the page's rows sit behind its K and V elements
           const unsigned char* xs = stages + (size_t)s * kStageBytes + wig * kBlkBytes + 2 * kPage * kRowBytes;
-          const float ks0 = exp_byte_to_float(xs[key0]) * p.scale_log2e;
-          const float ks1 = exp_byte_to_float(xs[key0 + 2]) * p.scale_log2e;
+          const float ks0 = SH ? exp_byte_to_float(xs[key0]) : exp_byte_to_float(xs[key0]) * p.scale_log2e;
+          const float ks1 = SH ? exp_byte_to_float(xs[key0 + 2]) : exp_byte_to_float(xs[key0 + 2]) * p.scale_log2e;
           vscale0 = exp_byte_to_float(xs[kPage + key0]);
           vscale1 = exp_byte_to_float(xs[kPage + key0 + 2]);
           st[0] = (st[0] + st2[0]) * ks0; st[1] = (st[1] + st2[1]) * ks0;
           st[2] = (st[2] + st2[2]) * ks1; st[3] = (st[3] + st2[3]) * ks1;
+        }
+        if constexpr (SH) {   // this thread's two keys and two heads
+          float d0 = 0.f, d1 = 0.f;
+          if (p.shape.biased) {
+            int b0 = p.newest[x.i] - tok_base - (KV8 ? key0 : frow);
+            int b1 = b0 - (KV8 ? 2 : 8);
+            if (b0 < 0) b0 += p.wrap;
+            if (b1 < 0) b1 += p.wrap;
+            d0 = -(float)b0;
+            d1 = -(float)b1;
+          }
+          st[0] = shaped_score(st[0], p.shape, slope[0] * d0);
+          st[1] = shaped_score(st[1], p.shape, slope[1] * d0);
+          st[2] = shaped_score(st[2], p.shape, slope[0] * d1);
+          st[3] = shaped_score(st[3], p.shape, slope[1] * d1);
         }
         if (tok_base + kPage > x.t1) {  // ragged end of the split: this thread's two keys (tile rows frow, frow + 8)
           const int lim = x.t1 - tok_base;
@@ -518,6 +547,20 @@ decode_split_bf16_kernel(const __grid_constant__ DecodeParams p, const int n_sta
             o[jt][0] *= a0; o[jt][1] *= a1;
             o[jt][2] *= a0; o[jt][3] *= a1;
           }
+          if constexpr (SH) {
+            // the last page's rows behind the sequence hold what its previous owner left there:
+            // a weight of 0 does not silence an infinity or a NaN, so those elements are cleared
+            if (tok_base + kPage > x.t1) {
+              const int lim = x.t1 - tok_base;
+              const uint32_t keep0 = (fcol < lim ? 0xffffu : 0u) | (fcol + 1 < lim ? 0xffff0000u : 0u);
+              const uint32_t keep1 = (fcol + 8 < lim ? 0xffffu : 0u) | (fcol + 9 < lim ? 0xffff0000u : 0u);
+#pragma unroll
+              for (int jt = 0; jt < D / 16; ++jt) {
+                va[jt][0] &= keep0; va[jt][1] &= keep0;
+                va[jt][2] &= keep1; va[jt][3] &= keep1;
+              }
+            }
+          }
 #pragma unroll
           for (int jt = 0; jt < D / 16; ++jt) mma_bf16(o[jt], va[jt], ph0, ph1);
 #pragma unroll
@@ -538,10 +581,18 @@ decode_split_bf16_kernel(const __grid_constant__ DecodeParams p, const int n_sta
           // V^T rows are channels, 16 key bytes each: one ldmatrix.x4 = 32 channels; a register
           // holds keys 4t .. 4t+3 of a channel, which are the contraction indices 2t, 2t+1 and
           // 2t+8, 2t+9 in the key order of the tile rows above
+          uint32_t keep = 0xffffffffu;   // (SH: as above; a register holds four keys of a channel)
+          if constexpr (SH) {
+            if (tok_base + kPage > x.t1) {
+              const int left = x.t1 - tok_base - 2 * fcol;   // keys 4t .. 4t + 3 that belong to the sequence
+              keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+            }
+          }
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) {
             uint32_t r[4], a[4], b[4];
             ldsm_x4(vb + (32 * j + lane) * kPage, r[0], r[1], r[2], r[3]);
+            if constexpr (SH) { r[0] &= keep; r[1] &= keep; r[2] &= keep; r[3] &= keep; }
             e4m3x4_to_f16x2x2(r[0], a[0], a[2]);
             e4m3x4_to_f16x2x2(r[1], a[1], a[3]);
             e4m3x4_to_f16x2x2(r[2], b[0], b[2]);
@@ -654,21 +705,51 @@ size_t smem_bytes(int D, int group, int n_stages, int ncw, int cl, int kv8) {
 
 }  // namespace
 
-cudaError_t prepare_decode_bf16() {
-  cudaError_t e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 8, 1, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<64, 8, 1, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 4, 1, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, 113 * 1024);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<64, 4, 1, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, 113 * 1024);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 8, 2, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<64, 8, 2, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+namespace {
+
+template <int SH>
+cudaError_t prepare_variants() {
+  constexpr auto kAttr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 8, 1, 0, SH>, kAttr, 227 * 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<64, 8, 1, 0, SH>, kAttr, 227 * 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 4, 1, 0, SH>, kAttr, 113 * 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<64, 4, 1, 0, SH>, kAttr, 113 * 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 8, 2, 0, SH>, kAttr, 227 * 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<64, 8, 2, 0, SH>, kAttr, 227 * 1024);
   // quantised cache: head_dim 128 only
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 8, 1, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 4, 1, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 113 * 1024);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 8, 2, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 8, 1, 1, SH>, kAttr, 227 * 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 4, 1, 1, SH>, kAttr, 113 * 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_split_bf16_kernel<128, 8, 2, 1, SH>, kAttr, 227 * 1024);
   return e;
 }
 
-cudaError_t launch_decode_split_bf16(const DecodeParams& p, int sm_count, cudaStream_t st) {
+template <int SH>
+cudaError_t launch_variant(const cudaLaunchConfig_t& cfg, const LaunchParams<SH>& p, bool paired, bool small, int n_stages) {
+  const int D = p.geom.head_dim;
+  if (p.geom.fp8) {
+    if (paired) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 8, 2, 1, SH>, p, n_stages);
+    if (small) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 4, 1, 1, SH>, p, n_stages);
+    return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 8, 1, 1, SH>, p, n_stages);
+  }
+  if (D == 128) {
+    if (paired) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 8, 2, 0, SH>, p, n_stages);
+    if (small) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 4, 1, 0, SH>, p, n_stages);
+    return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 8, 1, 0, SH>, p, n_stages);
+  }
+  if (paired) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<64, 8, 2, 0, SH>, p, n_stages);
+  if (small) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<64, 4, 1, 0, SH>, p, n_stages);
+  return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<64, 8, 1, 0, SH>, p, n_stages);
+}
+
+}  // namespace
+
+cudaError_t prepare_decode_bf16() {
+  cudaError_t e = prepare_variants<0>();
+  return e == cudaSuccess ? prepare_variants<1>() : e;
+}
+
+cudaError_t launch_decode_split_bf16(const DecodeParams& p, const ShapedDecodeParams* shaped, int sm_count,
+                                     cudaStream_t st) {
   const int D = p.geom.head_dim;
   if (p.total_items <= 0) return cudaSuccess;
   // Few, short items (more than one but at most two per SM, e.g. one 1024-key window per
@@ -714,19 +795,8 @@ cudaError_t launch_decode_split_bf16(const DecodeParams& p, int sm_count, cudaSt
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = paired ? 2 : 1;
-  if (kv8) {
-    if (paired) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 8, 2, 1>, p, n_stages);
-    if (small) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 4, 1, 1>, p, n_stages);
-    return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 8, 1, 1>, p, n_stages);
-  }
-  if (D == 128) {
-    if (paired) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 8, 2, 0>, p, n_stages);
-    if (small) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 4, 1, 0>, p, n_stages);
-    return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<128, 8, 1, 0>, p, n_stages);
-  }
-  if (paired) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<64, 8, 2, 0>, p, n_stages);
-  if (small) return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<64, 4, 1, 0>, p, n_stages);
-  return cudaLaunchKernelEx(&cfg, decode_split_bf16_kernel<64, 8, 1, 0>, p, n_stages);
+  return shaped != nullptr ? launch_variant<1>(cfg, *shaped, paired, small, n_stages)
+                           : launch_variant<0>(cfg, p, paired, small, n_stages);
 }
 
 }  // namespace mixattn

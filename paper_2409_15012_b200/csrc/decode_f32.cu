@@ -6,7 +6,10 @@
 // HBM with one warp per key and warp-shuffle reductions.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "internal.h"
+#include "score_shape.cuh"
 
 namespace mixattn {
 
@@ -16,8 +19,10 @@ constexpr int kWarps = 4;
 constexpr int kRowsPerPass = 4;  // query heads kept in registers per pass over the keys
 
 // one work item = (split, KV head, chunk of 16 heads); grid.x = total_items
-template <int D>
-__global__ void __launch_bounds__(kWarps * 32) decode_split_f32_kernel(const __grid_constant__ DecodeParams p) {
+// SH = 1: the layer's scores are capped and / or biased by distance (score_shape.cuh)
+template <int D, int SH>
+__global__ void __launch_bounds__(kWarps * 32)
+decode_split_f32_kernel(const __grid_constant__ std::conditional_t<SH != 0, ShapedDecodeParams, DecodeParams> p) {
   constexpr int V = D / 32;  // floats per lane per row
   __shared__ float sm_o[kWarps][kRowsPerPass][D];
   __shared__ float sm_ml[kWarps][kRowsPerPass][2];
@@ -77,7 +82,17 @@ __global__ void __launch_bounds__(kWarps * 32) decode_split_f32_kernel(const __g
         for (int e = 0; e < V; ++e) s = fmaf(q[r][e], kv[e], s);
 #pragma unroll
         for (int sh = 16; sh > 0; sh >>= 1) s += __shfl_xor_sync(0xffffffffu, s, sh);
-        s *= p.scale_log2e;
+        if constexpr (SH) {
+          float bias = 0.f;
+          if (p.shape.biased) {
+            int back = p.newest[i] - t;
+            if (back < 0) back += p.wrap;
+            bias = r < nr ? -p.shape.slope[h0 + r0 + r] * (float)back : 0.f;
+          }
+          s = shaped_score_exact(s, p.shape, bias);
+        } else {
+          s *= p.scale_log2e;
+        }
         const float mn = fmaxf(m[r], s);
         const float a = exp2f(m[r] - mn);
         const float pe = exp2f(s - mn);
@@ -147,12 +162,16 @@ __global__ void decode_combine_kernel(const __grid_constant__ DecodeParams p) {
 
 }  // namespace
 
-cudaError_t launch_decode_split_f32(const DecodeParams& p, cudaStream_t st) {
+cudaError_t launch_decode_split_f32(const DecodeParams& p, const ShapedDecodeParams* shaped, cudaStream_t st) {
   if (p.total_items <= 0) return cudaSuccess;
-  if (p.geom.head_dim == 128)
-    decode_split_f32_kernel<128><<<p.total_items, kWarps * 32, 0, st>>>(p);
-  else
-    decode_split_f32_kernel<64><<<p.total_items, kWarps * 32, 0, st>>>(p);
+  const int grid = p.total_items, threads = kWarps * 32;
+  if (p.geom.head_dim == 128) {
+    if (shaped != nullptr) decode_split_f32_kernel<128, 1><<<grid, threads, 0, st>>>(*shaped);
+    else decode_split_f32_kernel<128, 0><<<grid, threads, 0, st>>>(p);
+  } else {
+    if (shaped != nullptr) decode_split_f32_kernel<64, 1><<<grid, threads, 0, st>>>(*shaped);
+    else decode_split_f32_kernel<64, 0><<<grid, threads, 0, st>>>(p);
+  }
   return cudaGetLastError();
 }
 

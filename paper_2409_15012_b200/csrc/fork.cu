@@ -1,0 +1,99 @@
+// Forking of cached sequences and reading a cache back as plain tensors.
+//
+// Paper, Section 3: the caches a layer stack keeps are a paged pool per standard owner and a ring
+// per sliding-window owner.  A copy of a sequence shares the pages no append writes to any more
+// (host bookkeeping, cache_manager.hpp); what is left to move are the partly filled page of each
+// paged pool, the rings and the sequence's row of the block table.  Both kernels are HBM-bound
+// copies with 16-byte accesses.
+#include "internal.h"
+
+namespace mixattn {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnroll = 8;                            // 16-byte loads in flight per thread
+constexpr int kBlock16 = kThreads * kUnroll;          // 16-byte units per block: 32 KB
+
+__global__ void __launch_bounds__(kThreads) fork_copy_kernel(const __grid_constant__ ForkParams p) {
+  const int y = blockIdx.y;
+  if (y < p.n_segs) {
+    const CopySeg& s = p.seg[y];
+    const uint32_t u0 = blockIdx.x * (uint32_t)kBlock16 + threadIdx.x;
+    if (u0 - threadIdx.x >= s.n16) return;
+    const int4* src = reinterpret_cast<const int4*>(p.arena + s.src);
+    int4* dst = reinterpret_cast<int4*>(p.arena + s.dst);
+    int4 v[kUnroll];
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i)
+      if (u0 + i * kThreads < s.n16) v[i] = src[u0 + i * kThreads];
+#pragma unroll
+    for (int i = 0; i < kUnroll; ++i)
+      if (u0 + i * kThreads < s.n16) dst[u0 + i * kThreads] = v[i];
+    return;
+  }
+  if (blockIdx.x > 0) return;
+  const TableRow& r = p.row[y - p.n_segs];
+  const int32_t* src = p.table + (int64_t)r.src_slot * p.table_stride;
+  int32_t* dst = p.table + (int64_t)r.dst_slot * p.table_stride;
+  for (int b = threadIdx.x; b < r.n_copy; b += kThreads) dst[b] = src[b];
+  if ((int)threadIdx.x < r.n_set) dst[r.set0 + threadIdx.x] = r.page[threadIdx.x];
+}
+
+// One block: kThreads / chunks tokens; a thread owns one 16-byte chunk of a token's rows and
+// walks the KV heads, so the page lookup is made once per thread and every warp reads and
+// writes whole rows.
+__global__ void __launch_bounds__(kThreads) read_kv_kernel(const __grid_constant__ GatherParams p) {
+  const GatherEntry& e = p.e[blockIdx.y];
+  const KvGeom& ge = p.geom;
+  const int chunks = ge.row_bytes / 16;                // 8, 16 or 32
+  const int tokens = kThreads / chunks;
+  const int t = blockIdx.x * tokens + (int)threadIdx.x / chunks;
+  const int chunk = (int)threadIdx.x % chunks;
+  if (t >= e.n_prefix) return;
+  const int pos = e.pos0 + t;
+  int64_t page;
+  int slot;
+  if (p.is_ring) {
+    const int rs = pos % p.window;
+    page = (int64_t)e.seq * p.ring_pages + rs / kPage;
+    slot = rs % kPage;
+  } else {
+    page = p.table[(int64_t)e.seq * p.table_stride + pos / kPage];
+    slot = pos % kPage;
+  }
+  const char* k = p.pool + kv_chunk_offset(ge, page, 0, 0, slot, chunk);
+  const char* v = k + (int64_t)kPage * ge.st_row_bytes;
+  const int64_t out = (int64_t)(e.dst_row0 + t) * ge.n_kv_heads * ge.row_bytes + chunk * 16;
+  char* ko = static_cast<char*>(p.k_out) + out;
+  char* vo = static_cast<char*>(p.v_out) + out;
+#pragma unroll 4
+  for (int g = 0; g < ge.n_kv_heads; ++g) {
+    const int4 a = *reinterpret_cast<const int4*>(k + (int64_t)g * ge.blk_bytes);
+    const int4 b = *reinterpret_cast<const int4*>(v + (int64_t)g * ge.blk_bytes);
+    *reinterpret_cast<int4*>(ko + (int64_t)g * ge.row_bytes) = a;
+    *reinterpret_cast<int4*>(vo + (int64_t)g * ge.row_bytes) = b;
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_fork_copy(const ForkParams& p, cudaStream_t st) {
+  if (p.n_segs + p.n_rows <= 0) return cudaSuccess;
+  uint32_t longest = 0;
+  for (int i = 0; i < p.n_segs; ++i) longest = p.seg[i].n16 > longest ? p.seg[i].n16 : longest;
+  unsigned bx = (longest + kBlock16 - 1) / kBlock16;
+  if (bx < 1) bx = 1;
+  fork_copy_kernel<<<dim3(bx, p.n_segs + p.n_rows), kThreads, 0, st>>>(p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_read_kv(const GatherParams& p, int max_rows, cudaStream_t st) {
+  if (p.geom.fp8) return launch_gather(p, max_rows, st);   // dequantises
+  if (p.n_entries <= 0 || max_rows <= 0) return cudaSuccess;
+  const int tokens = kThreads / (p.geom.row_bytes / 16);
+  read_kv_kernel<<<dim3((max_rows + tokens - 1) / tokens, p.n_entries), kThreads, 0, st>>>(p);
+  return cudaGetLastError();
+}
+
+}  // namespace mixattn

@@ -84,8 +84,19 @@ __host__ __device__ inline int64_t kv_exp_offset(const KvGeom& ge, int64_t page,
 // ---------------------------------------------------------------------------
 // kernel parameter blocks (passed by value: no per-call metadata copy)
 // ---------------------------------------------------------------------------
+
+// How a layer's scores are shaped (mixattn_set_layer_scores; the formulas are in score_shape.cuh).
+// Kernels come in two instantiations: layers with plain scores carry none of this.
+constexpr int kMaxSlopeHeads = MIXATTN_MAX_SLOPE_HEADS;
+struct ScoreShape {
+  float pre;        // factor on q . k: scale / cap with a cap, scale * log2(e) without
+  float post;       // cap * log2(e); 0 = no cap
+  int32_t biased;   // 1: the slopes below apply
+  float slope[kMaxSlopeHeads];   // per query head, times log2(e)
+};
+
 struct AppendEntry {
-  int32_t seq;        // sequence slot
+  int32_t seq;        // storage slot of the sequence (row of the block table, ring)
   int32_t start_pos;  // position of the first new token
   int32_t n_new;      // tokens appended
   int32_t src_row0;   // row of the first new token in k / v
@@ -128,10 +139,18 @@ struct DecodeParams {
   int32_t* status;        // device error word (0 = fine)
   int32_t n_seqs;
   int32_t total_items;    // chunks * Hkv * head_chunks
-  int32_t seq_id[kMaxCallSeqs];
+  int32_t seq_id[kMaxCallSeqs];          // storage slots of the sequences
   int32_t n_eff[kMaxCallSeqs];           // keys attended: min(len, window) or len
   int32_t chunk_len[kMaxCallSeqs];       // keys per split of this sequence (multiple of 16)
   int32_t chunk_base[kMaxCallSeqs + 1];  // first split index of each sequence
+};
+
+// A decode launch of a layer with shaped scores.  The key in cache position / ring slot t is
+// newest - t tokens behind the query, plus `wrap` (the window of a ring) where that is negative.
+struct ShapedDecodeParams : DecodeParams {
+  ScoreShape shape;
+  int32_t newest[kMaxCallSeqs];
+  int32_t wrap;
 };
 
 struct PrefillParams {
@@ -157,12 +176,13 @@ struct PrefillParams {
   int32_t ring_pages;               // pages per sequence in the ring (a multiple of 8)
   int64_t ring_total_pages;         // pages in ring_pool
   KvGeom geom;
+  const ScoreShape* shape = nullptr;   // host; nullptr = plain scores
 };
 
 // Copies the cached keys a chunk of queries needs, followed by the chunk's own keys, into
 // plain [rows, Hkv, D] tensors (the layout the prompt kernels read).
 struct GatherEntry {
-  int32_t seq;        // sequence slot
+  int32_t seq;        // storage slot of the sequence
   int32_t pos0;       // position of the first cached token copied
   int32_t n_prefix;   // cached tokens copied (positions pos0 .. pos0 + n_prefix - 1)
   int32_t n_chunk;    // tokens taken from the chunk tensors after them
@@ -195,6 +215,45 @@ struct TableSetParams {
   int32_t page[kTableSetMax];
 };
 
+// Device side of a fork: byte ranges of the arena to copy (whole pages: partly filled pages of the
+// paged pools, the used part of rings), and rows of the block table.
+struct CopySeg {
+  int64_t src, dst;   // byte offsets from the arena's start, multiples of 16
+  uint32_t n16;       // 16-byte units
+};
+constexpr int kRowPages = 4;
+struct TableRow {
+  int32_t src_slot, dst_slot;
+  int32_t n_copy;     // entries [0, n_copy) are copied from the source's row
+  int32_t set0;       // entries set0 .. set0 + n_set - 1 become page[]
+  int32_t n_set;
+  int32_t page[kRowPages];
+};
+constexpr int kForkSegs = 96, kForkRows = 48;   // (both lists of a launch stay below 4 KB of parameters)
+struct ForkParams {
+  char* arena;
+  int32_t* table;
+  int32_t table_stride;
+  int32_t n_segs, n_rows;
+  CopySeg seg[kForkSegs];
+  TableRow row[kForkRows];
+};
+
+// Beam selection.  part_sums and part_keys are the scan's results per (beam, chunk).
+struct BeamParams {
+  const void* logits;        // [n_groups * n_beams] rows of `vocab`, row_stride elements apart
+  int64_t row_stride;
+  const float* scores;       // [n_groups * n_beams]
+  const uint8_t* finished;   // the same, or nullptr
+  float* out_scores;         // [n_groups, n_out]
+  int32_t* out_beams;
+  int32_t* out_tokens;
+  float2* part_sums;         // [rows, n_chunks] (maximum, sum of e^(x - maximum))
+  uint64_t* part_keys;       // [rows, n_chunks, n_out] descending, 0 = none
+  int32_t n_groups, n_beams, vocab, n_out, eos;
+  int32_t n_chunks, chunk_granules;
+};
+
 // device status codes written to the status word
 enum { kDevOk = 0, kDevWaitTimeout = 1 };
 
@@ -202,9 +261,16 @@ enum { kDevOk = 0, kDevWaitTimeout = 1 };
 cudaError_t launch_append(const AppendParams& p, int max_n_new, cudaStream_t st);
 cudaError_t launch_table_set(const TableSetParams& p, cudaStream_t st);
 cudaError_t launch_gather(const GatherParams& p, int max_rows, cudaStream_t st);
+cudaError_t launch_fork_copy(const ForkParams& p, cudaStream_t st);
+cudaError_t launch_read_kv(const GatherParams& p, int max_rows, cudaStream_t st);   // entries without chunk rows
+int beam_chunks(int rows, int vocab, int elem_bytes, int sm_count, int* chunk_granules);
+cudaError_t launch_beam_scan(const BeamParams& p, int elem_bytes, cudaStream_t st);
+cudaError_t launch_beam_merge(const BeamParams& p, cudaStream_t st);
 cudaError_t prepare_decode_bf16();
-cudaError_t launch_decode_split_bf16(const DecodeParams& p, int sm_count, cudaStream_t st);   // native or quantised cache
-cudaError_t launch_decode_split_f32(const DecodeParams& p, cudaStream_t st);
+// (a launch whose layer has shaped scores passes its block as both p and shaped; else shaped = nullptr)
+cudaError_t launch_decode_split_bf16(const DecodeParams& p, const ShapedDecodeParams* shaped, int sm_count,
+                                     cudaStream_t st);   // native or quantised cache
+cudaError_t launch_decode_split_f32(const DecodeParams& p, const ShapedDecodeParams* shaped, cudaStream_t st);
 cudaError_t launch_decode_combine(const DecodeParams& p, int dtype, cudaStream_t st);
 cudaError_t launch_prefill_simple(const PrefillParams& p, int dtype, int max_len, cudaStream_t st);
 bool prefill_tc_supported(int dtype, int head_dim, const void* q, const void* k, const void* v);

@@ -9,7 +9,10 @@
 // tiles outside the band are skipped.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "internal.h"
+#include "score_shape.cuh"
 
 namespace mixattn {
 
@@ -22,8 +25,12 @@ __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162flo
 __device__ __forceinline__ void store_out(float* p, float x) { *p = x; }
 __device__ __forceinline__ void store_out(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) prefill_simple_kernel(const __grid_constant__ PrefillParams p) {
+struct Plain {};   // plain scores: no further parameters
+
+// SH: Plain, or ScoreShape for a layer whose scores are capped and / or biased by distance
+template <typename T, int D, typename SH>
+__global__ void __launch_bounds__(kThreads)
+prefill_simple_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ SH shape) {
   extern __shared__ float sm[];
   float* Qs = sm;                      // [kBM][D + 1]
   float* Ks = Qs + kBM * (D + 1);      // [kBN][D + 1]
@@ -74,7 +81,10 @@ __global__ void __launch_bounds__(kThreads) prefill_simple_kernel(const __grid_c
       float acc = 0.f;
       for (int d = 0; d < D; ++d) acc = fmaf(Qs[r * (D + 1) + d], Ks[(c + 4 * jj) * (D + 1) + d], acc);
       const bool seen = j <= i && row_ok && (p.window == 0 || i - j < p.window);
-      s[jj] = seen ? acc * p.scale_log2e : -INFINITY;
+      if constexpr (std::is_same_v<SH, ScoreShape>)
+        s[jj] = seen ? shaped_score_exact(acc, shape, shape.biased ? -shape.slope[h] * (float)(i - j) : 0.f) : -INFINITY;
+      else
+        s[jj] = seen ? acc * p.scale_log2e : -INFINITY;
       mx = fmaxf(mx, s[jj]);
     }
     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
@@ -110,15 +120,20 @@ __global__ void __launch_bounds__(kThreads) prefill_simple_kernel(const __grid_c
   }
 }
 
-template <typename T, int D>
-cudaError_t launch(const PrefillParams& p, int max_len, cudaStream_t st) {
+template <typename T, int D, typename SH>
+cudaError_t launch(const PrefillParams& p, const SH& shape, int max_len, cudaStream_t st) {
   const size_t smem = (size_t)(kBM * (D + 1) + kBN * (D + 1) + kBN * D + kBM * (kBN + 1)) * 4;
-  cudaError_t e = cudaFuncSetAttribute(prefill_simple_kernel<T, D>,
+  cudaError_t e = cudaFuncSetAttribute(prefill_simple_kernel<T, D, SH>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   dim3 grid((max_len + kBM - 1) / kBM, p.n_q_heads, p.n_seqs);
-  prefill_simple_kernel<T, D><<<grid, kThreads, smem, st>>>(p);
+  prefill_simple_kernel<T, D, SH><<<grid, kThreads, smem, st>>>(p, shape);
   return cudaGetLastError();
+}
+template <typename T, int D>
+cudaError_t launch(const PrefillParams& p, int max_len, cudaStream_t st) {
+  return p.shape != nullptr ? launch<T, D, ScoreShape>(p, *p.shape, max_len, st)
+                            : launch<T, D, Plain>(p, Plain{}, max_len, st);
 }
 
 }  // namespace

@@ -43,6 +43,7 @@
 #include <type_traits>
 
 #include "internal.h"
+#include "score_shape.cuh"
 
 namespace mixattn {
 
@@ -89,6 +90,9 @@ struct TcParams {
   int32_t cached[kMaxCallSeqs];     // the first so many of them live in a ring cache, not in k / v
   int32_t ring_page0[kMaxCallSeqs]; // first page of the sequence's ring
   int32_t ring_pages;               // pages per sequence in the ring (a multiple of 8)
+};
+struct ShapedTcParams : TcParams {
+  ScoreShape shape;
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -284,22 +288,30 @@ __device__ __forceinline__ WorkItem get_item(const TcParams& p, int id) {
   return w;
 }
 
-// key tile (index along the sequence's keys) of entry j of an item's tile list
+// key tile (index along the sequence's keys) of entry x of an item's tile list
 template <bool kRing>
-__device__ __forceinline__ int tile_of(const WorkItem& w, int j) {
-  return kRing ? w.jt_lo + j - (j >= w.dup ? 1 : 0) : w.jt_lo + j;
+__device__ __forceinline__ int tile_of(const WorkItem& w, int x) {
+  return kRing ? w.jt_lo + x - (x >= w.dup ? 1 : 0) : w.jt_lo + x;
 }
+// Entry that an item visits j-th: oldest keys first, or, with shaped scores, the newest first.  A
+// distance bias lifts the scores tile by tile towards the query, so from the oldest tile on a
+// steep head would have to move its exponent reference at every tile.
+template <bool kShape>
+__device__ __forceinline__ int entry_at(const WorkItem& w, int j) { return kShape ? w.n_tiles - 1 - j : j; }
 
 // kRing: some sequences have cached keys in a ring (a separate instantiation, so that the
 // ordinary launches carry none of its code)
 // kD: head_dim, 128 or 64.  With 64 channels an operand tile is one [128 x 64] block instead of
 // two (the buffers keep their size), the score product takes four steps of 16 channels, the
 // P V products write 64 accumulator columns, and the softmax warps do exactly the same work.
-template <bool kRing, int kD>
+// kShape: the layer's scores are capped and / or biased by distance (score_shape.cuh).  The softmax
+// warps turn each raw score into its shaped base-2 score in place right after the load, before the
+// masks; from there on nothing differs but the missing scale.
+template <bool kRing, int kD, bool kShape>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                   const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_ring,
-                  const __grid_constant__ TcParams p) {
+                  const __grid_constant__ std::conditional_t<kShape, ShapedTcParams, TcParams> p) {
   static_assert(kD == 128 || kD == 64, "head_dim");
   constexpr uint32_t kOpBytes = kD == 128 ? kTileBytes : kHalfBytes;   // bytes of one Q / K / V tile
   constexpr int kSteps = kD / 16;                                        // 16-channel steps of the score product
@@ -372,12 +384,13 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           ++q_issued;
           for (int j = 0; j < w.n_tiles && ok; ++j) {
             const int Gj = G + j;
-            const int jt = tile_of<kRing>(w, j);
+            const int x = entry_at<kShape>(w, j);
+            const int jt = tile_of<kRing>(w, x);
             // A tile of cached keys is eight whole pages of the sequence's ring: the page rows are
             // stored with the 16-byte chunks already permuted the way the MMA expects a
             // 128-byte-swizzled tile, so an unswizzled copy of (8 pages x 16 tokens x 128 bytes)
             // is that tile.  All other tiles come from k / v, whose row 0 is key w.cached.
-            const bool from_ring = kRing && jt * kBN < w.cached && j != w.dup;
+            const bool from_ring = kRing && jt * kBN < w.cached && x != w.dup;
             const int row = w.krow_base + jt * kBN - w.cached;   // (negative rows of the tile shared with the ring read as zeros)
             const int page = w.ring_page0 + (jt * (kBN / kPage)) % p.ring_pages;
             const int ks = Gj % kKStages, ku = Gj / kKStages;
@@ -576,6 +589,14 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       const int i = w.pos0 + r;           // query position among the sequence's keys
       float m_ref = -INFINITY, l = 0.f;
       uint32_t sv[64];
+      float slope = 0.f;                  // kShape: of this head, base-2 units per token
+      if constexpr (kShape) slope = p.shape.biased ? p.shape.slope[w.h] : 0.f;
+      const float scale = kShape ? 1.f : p.scale_log2e;
+      // weight of a score: 2^(score - reference)
+      auto weight = [&](uint32_t sc, float neg_m) {
+        if constexpr (kShape) return ex2_approx(__uint_as_float(sc) + neg_m);
+        else return ex2_approx(fmaf(__uint_as_float(sc), p.scale_log2e, neg_m));
+      };
       {
         if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SF + (G & 1)), (G >> 1) & 1, abort_flag))) { ok = false; break; }
         tc_fence_after();
@@ -591,21 +612,38 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         constexpr bool kLo = decltype(lo_tag)::value;
         for (int j = 0; j < w.n_tiles; ++j) {
           const int Gj = G + j, sb = Gj & 1;
-          const int j0 = tile_of<kRing>(w, j) * kBN + hs * 64;   // first key of this stream's columns
+          const int x = entry_at<kShape>(w, j);
+          const int j0 = tile_of<kRing>(w, x) * kBN + hs * 64;   // first key of this stream's columns
           const uint32_t s_addr = lane_base + kColS + sb * 128 + hs * 64;
           // band edges: causal (keys after the query) and window (keys older than i - window); and
           // the two visits of the tile in which the cached keys end
           const bool edge = (j0 + 63 > w.pos0) || (p.window > 0 && j0 <= w.pos0 + kBM - 1 - p.window) ||
-                            (kRing && (j + 1 == w.dup || j == w.dup));
+                            (kRing && (x + 1 == w.dup || x == w.dup));
           auto mask_edges = [&]() {
             int k_max = i - j0;                                      // columns <= k_max are causal-visible
             int k_min = p.window > 0 ? i - p.window + 1 - j0 : 0;    // columns >= k_min are inside the window
-            if (kRing && j + 1 == w.dup) k_max = min(k_max, w.cached - 1 - j0);   // this visit: the cached keys only
-            if (kRing && j == w.dup) k_min = max(k_min, w.cached - j0);           // this visit: the keys from k / v only
+            if (kRing && x + 1 == w.dup) k_max = min(k_max, w.cached - 1 - j0);   // this visit: the cached keys only
+            if (kRing && x == w.dup) k_min = max(k_min, w.cached - j0);           // this visit: the keys from k / v only
   #pragma unroll
             for (int e = 0; e < 64; ++e)
               if (e > k_max || e < k_min) sv[e] = 0xff800000u;             // -inf
           };
+          auto shape_scores = [&]() {
+            if constexpr (kShape) {
+              const float base = -slope * (float)(i - j0);   // bias of column 0; column e is e tokens nearer
+              if (p.shape.post > 0.f) {
+  #pragma unroll
+                for (int e = 0; e < 64; ++e)
+                  sv[e] = __float_as_uint(fmaf(tanh_fast(__uint_as_float(sv[e]) * p.shape.pre), p.shape.post,
+                                               fmaf(slope, (float)e, base)));
+              } else {
+  #pragma unroll
+                for (int e = 0; e < 64; ++e)
+                  sv[e] = __float_as_uint(fmaf(__uint_as_float(sv[e]), p.shape.pre, fmaf(slope, (float)e, base)));
+              }
+            }
+          };
+          shape_scores();
           if (edge) mask_edges();
           // a row that has not seen a key yet takes its reference from this tile
           const bool fresh = m_ref == -INFINITY;
@@ -616,7 +654,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               mx0 = fmax3(mx0, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
               mx1 = fmax3(mx1, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
             }
-            if (fresh) m_ref = fmaxf(mx0, mx1) * p.scale_log2e;
+            if (fresh) m_ref = fmaxf(mx0, mx1) * scale;
           }
           float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;   // no visible key yet: weights 0, no NaN
           // probe the next tile's scores now; the answer is read after the exponentials
@@ -627,10 +665,10 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           if constexpr (!kLo) {
   #pragma unroll
             for (int e = 0; e < 64; e += 4) {
-              const float p0 = ex2_approx(fmaf(__uint_as_float(sv[e]), p.scale_log2e, neg_m));
-              const float p1 = ex2_approx(fmaf(__uint_as_float(sv[e + 1]), p.scale_log2e, neg_m));
-              const float p2 = ex2_approx(fmaf(__uint_as_float(sv[e + 2]), p.scale_log2e, neg_m));
-              const float p3 = ex2_approx(fmaf(__uint_as_float(sv[e + 3]), p.scale_log2e, neg_m));
+              const float p0 = weight(sv[e], neg_m);
+              const float p1 = weight(sv[e + 1], neg_m);
+              const float p2 = weight(sv[e + 2], neg_m);
+              const float p3 = weight(sv[e + 3], neg_m);
               sum0 += p0 + p2;
               sum1 += p1 + p3;
               pk[e >> 1] = pack_bf16(p0, p1);
@@ -639,8 +677,8 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           } else {
   #pragma unroll
             for (int e = 0; e < 64; e += 2) {
-              const float p0 = ex2_approx(fmaf(__uint_as_float(sv[e]), p.scale_log2e, neg_m));
-              const float p1 = ex2_approx(fmaf(__uint_as_float(sv[e + 1]), p.scale_log2e, neg_m));
+              const float p0 = weight(sv[e], neg_m);
+              const float p1 = weight(sv[e + 1], neg_m);
               sum0 += p0;
               sum1 += p1;
               split_bf16(p0, p1, pk[e >> 1], pl[e >> 1]);
@@ -658,6 +696,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
             tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
             tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+            shape_scores();
             if (edge) mask_edges();
             float mxa = -INFINITY, mxb = -INFINITY;
   #pragma unroll
@@ -665,7 +704,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               mxa = fmax3(mxa, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
               mxb = fmax3(mxb, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
             }
-            const float mt = fmaxf(mxa, mxb) * p.scale_log2e;
+            const float mt = fmaxf(mxa, mxb) * scale;
             const bool far = mt > m_ref + kMaxLead;
             const float alpha = far ? ex2_approx(m_ref - mt) : 1.f;
             if (j > 0) {   // the O row holds earlier tiles: rescale it once this stream's previous P V has landed
@@ -690,8 +729,8 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             sum1 = 0.f;
   #pragma unroll
             for (int e = 0; e < 64; e += 2) {
-              const float p0 = ex2_approx(fmaf(__uint_as_float(sv[e]), p.scale_log2e, neg_m));
-              const float p1 = ex2_approx(fmaf(__uint_as_float(sv[e + 1]), p.scale_log2e, neg_m));
+              const float p0 = weight(sv[e], neg_m);
+              const float p1 = weight(sv[e + 1], neg_m);
               sum0 += p0;
               sum1 += p1;
               if constexpr (kLo) split_bf16(p0, p1, pk[e >> 1], pl[e >> 1]);
@@ -803,10 +842,15 @@ bool prefill_tc_supported(int dtype, int head_dim, const void* q, const void* k,
 }
 
 cudaError_t prepare_prefill_tc() {
-  cudaError_t e = cudaFuncSetAttribute(prefill_tc_kernel<false, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<false, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  constexpr auto kAttr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(prefill_tc_kernel<false, 128, false>, kAttr, kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 128, false>, kAttr, kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<false, 64, false>, kAttr, kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 64, false>, kAttr, kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<false, 128, true>, kAttr, kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 128, true>, kAttr, kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<false, 64, true>, kAttr, kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 64, true>, kAttr, kSmemBytes);
   return e;
 }
 
@@ -833,7 +877,8 @@ cudaError_t launch_prefill_tc(const PrefillParams& pp, int max_len, int sm_count
   } else {
     tring = tk;   // never read
   }
-  TcParams p;
+  ShapedTcParams p;   // (plain scores: the kernel is handed the TcParams part)
+  if (pp.shape != nullptr) p.shape = *pp.shape;
   p.n_q_heads = pp.n_q_heads;
   p.group = pp.n_q_heads / pp.n_kv_heads;
   p.window = pp.window;
@@ -853,13 +898,19 @@ cudaError_t launch_prefill_tc(const PrefillParams& pp, int max_len, int sm_count
   const int64_t n_ids = (int64_t)p.max_qt * pp.n_seqs * pp.n_q_heads;
   const int grid = (int)(n_ids < sm_count ? n_ids : sm_count);   // persistent: one CTA per SM
   const bool ring = pp.ring_pool != nullptr;
-  if (D == 128) {
-    if (ring) prefill_tc_kernel<true, 128><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, p);
-    else prefill_tc_kernel<false, 128><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, p);
-  } else {
-    if (ring) prefill_tc_kernel<true, 64><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, p);
-    else prefill_tc_kernel<false, 64><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, p);
-  }
+  auto launch = [&](auto d_tag) {
+    constexpr int kD = decltype(d_tag)::value;
+    const TcParams& plain = p;
+    if (pp.shape != nullptr) {
+      if (ring) prefill_tc_kernel<true, kD, true><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, p);
+      else prefill_tc_kernel<false, kD, true><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, p);
+    } else {
+      if (ring) prefill_tc_kernel<true, kD, false><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, plain);
+      else prefill_tc_kernel<false, kD, false><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, plain);
+    }
+  };
+  if (D == 128) launch(std::integral_constant<int, 128>{});
+  else launch(std::integral_constant<int, 64>{});
   return cudaGetLastError();
 }
 
