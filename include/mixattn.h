@@ -401,6 +401,10 @@ int mixattn_decode_static_scratch(mixattn_ctx* ctx, int32_t layer, int32_t n_seq
 /* Tokens appended so far to the cache `layer` reads, for sequence `seq`. */
 int mixattn_get_len(mixattn_ctx* ctx, int32_t layer, int32_t seq, int32_t* len);
 
+/* Tokens the cache `layer` reads still holds of each sequence: its length, at most the window
+ * for a sliding-window layer.  out: host, n_seqs entries. */
+int mixattn_get_stored(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32_t* seq_ids, int32_t* out);
+
 /* Copies the sequence's block table (page id per logical block) to out[0..cap)
  * (host) and writes the number of blocks in use to *n_blocks (even if > cap). */
 int mixattn_get_block_table(mixattn_ctx* ctx, int32_t seq, int32_t* out, int32_t cap,

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from typing import Optional, Sequence
 
 import numpy as np
@@ -90,6 +91,7 @@ def _load() -> C.CDLL:
         "mixattn_get_device_status": [vp, p32],
         "mixattn_set_layer_scores": [vp, i32, C.c_float, C.POINTER(C.c_float)],
         "mixattn_fork_seqs": [vp, i32, p32, p32, vp],
+        "mixattn_get_stored": [vp, i32, i32, p32, p32],
         "mixattn_read_kv": [vp, i32, i32, p32, p32, p32, vp, vp, vp],
         "mixattn_beam_select": [vp, i32, i32, i32, i32, vp, C.c_int64, vp, vp, i32, i32, vp, vp, vp, vp],
         "mixattn_set_split_tokens": [vp, i32],
@@ -113,6 +115,7 @@ EXPORTS = [
     "mixattn_arena_bytes", "mixattn_cache_bytes", "mixattn_create", "mixattn_destroy",
     "mixattn_seq_reset", "mixattn_append_kv", "mixattn_append_kv_rope", "mixattn_decode", "mixattn_decode_static_scratch", "mixattn_decode_layers", "mixattn_prefill",
     "mixattn_attend_chunk", "mixattn_set_layer_scores", "mixattn_fork_seqs", "mixattn_read_kv", "mixattn_beam_select",
+    "mixattn_get_stored",
     "mixattn_get_len", "mixattn_get_block_table", "mixattn_get_n_free_pages",
     "mixattn_get_ring_state", "mixattn_locate", "mixattn_debug_read_kv", "mixattn_debug_read_kv_fp8",
     "mixattn_get_device_status", "mixattn_set_split_tokens", "mixattn_set_chunk_gather_reuse",
@@ -138,6 +141,22 @@ def _i32(a) -> np.ndarray:
 
 def _p32(a: Optional[np.ndarray]):
     return None if a is None else a.ctypes.data_as(C.POINTER(C.c_int32))
+
+
+def _ints(a):
+    """(ctypes int32 array or None, length) of a host sequence; short lists are a step of a
+    generation loop's cost, and this is several times faster than going through numpy."""
+    if a is None:
+        return None, 0
+    if type(a) is list:
+        try:
+            b = array("i", a)
+        except TypeError:
+            b = np.array(a, dtype=np.int32)
+    else:
+        b = np.array(a, dtype=np.int32)
+    n = len(b)
+    return ((C.c_int32 * n).from_buffer(b) if n else (C.c_int32 * 1)()), n
 
 
 def _dev(t) -> Optional[int]:
@@ -207,7 +226,6 @@ class Context:
             raise MixAttnError(rc, "mixattn_create")
         self.h = h
         self.n_q_heads, self.n_kv_heads, self.head_dim, self.dtype = n_q_heads, n_kv_heads, head_dim, dtype
-        self.layers = [(int(kind), int(window)) for kind, window, _ in layout]
 
     def close(self):
         if getattr(self, "h", None):
@@ -244,8 +262,8 @@ class Context:
             raise MixAttnError(rc, "mixattn_append_kv_rope")
 
     def rc_decode(self, layer, seq_ids, q, out, stream=None) -> int:
-        s = _i32(seq_ids)
-        return lib.mixattn_decode(self.h, layer, len(s), _p32(s), _dev(q), _dev(out), _stream(stream))
+        s, n = _ints(seq_ids)
+        return lib.mixattn_decode(self.h, layer, n, s, _dev(q), _dev(out), _stream(stream))
 
     def decode(self, layer, seq_ids, q, out, stream=None):
         rc = self.rc_decode(layer, seq_ids, q, out, stream)
@@ -283,9 +301,8 @@ class Context:
             raise MixAttnError(rc, "mixattn_decode_layers")
 
     def rc_prefill(self, layer, seq_ids, seq_lens, q, k, v, out, stream=None) -> int:
-        s, n = _i32(seq_ids), _i32(seq_lens)
-        return lib.mixattn_prefill(self.h, layer, len(s), _p32(s), _p32(n), _dev(q), _dev(k), _dev(v),
-                                   _dev(out), _stream(stream))
+        (s, n), (lens, _) = _ints(seq_ids), _ints(seq_lens)
+        return lib.mixattn_prefill(self.h, layer, n, s, lens, _dev(q), _dev(k), _dev(v), _dev(out), _stream(stream))
 
     def prefill(self, layer, seq_ids, seq_lens, q, k, v, out, stream=None):
         rc = self.rc_prefill(layer, seq_ids, seq_lens, q, k, v, out, stream)
@@ -293,9 +310,8 @@ class Context:
             raise MixAttnError(rc, "mixattn_prefill")
 
     def rc_attend_chunk(self, layer, seq_ids, seq_lens, q, k, v, out, stream=None) -> int:
-        s, n = _i32(seq_ids), _i32(seq_lens)
-        return lib.mixattn_attend_chunk(self.h, layer, len(s), _p32(s), _p32(n), _dev(q), _dev(k), _dev(v),
-                                        _dev(out), _stream(stream))
+        (s, n), (lens, _) = _ints(seq_ids), _ints(seq_lens)
+        return lib.mixattn_attend_chunk(self.h, layer, n, s, lens, _dev(q), _dev(k), _dev(v), _dev(out), _stream(stream))
 
     def attend_chunk(self, layer, seq_ids, seq_lens, q, k, v, out, stream=None):
         rc = self.rc_attend_chunk(layer, seq_ids, seq_lens, q, k, v, out, stream)
@@ -319,10 +335,10 @@ class Context:
             raise MixAttnError(rc, "mixattn_set_layer_scores")
 
     def rc_fork_seqs(self, src, dst, stream=None) -> int:
-        s, d = _i32(src), _i32(dst)
-        if len(s) != len(d):
+        (s, n), (d, m) = _ints(src), _ints(dst)
+        if n != m:
             return ERR_INVALID_ARG
-        return lib.mixattn_fork_seqs(self.h, len(s), _p32(s), _p32(d), _stream(stream))
+        return lib.mixattn_fork_seqs(self.h, n, s, d, _stream(stream))
 
     def fork_seqs(self, src, dst, stream=None):
         """Every sequence dst[i] becomes a copy of what src[i] was before the call (all at once)."""
@@ -334,31 +350,35 @@ class Context:
         """Returns (K, V), the cached tokens [sum n_tokens, Hkv, D] of the sequences, oldest first
         (default: everything stored).  The tensors are allocated on torch's current stream."""
         import torch
-        s = _i32(seq_ids)
-        p = None if first_pos is None else _i32(first_pos)
-        n = None if n_tokens is None else _i32(n_tokens)
-        if (p is not None and len(p) != len(s)) or (n is not None and len(n) != len(s)):
+        (s, m), (p, mp), (n, mn) = _ints(seq_ids), _ints(first_pos), _ints(n_tokens)
+        if (p is not None and mp != m) or (n is not None and mn != m):
             raise MixAttnError(ERR_INVALID_ARG, "mixattn_read_kv")
-        rows = 0
-        for i, seq in enumerate(s.tolist()):
-            if n is not None:
-                rows += max(0, int(n[i]))
-            elif p is not None:
-                rows += max(0, self.get_len(layer, seq) - int(p[i]))
-            else:
-                rows += self._stored(layer, seq)
-        k = torch.empty(2, rows, self.n_kv_heads, self.head_dim,
-                        dtype=torch.bfloat16 if self.dtype == BF16 else torch.float32, device=self._device())
-        k, v = k[0], k[1]
-        rc = lib.mixattn_read_kv(self.h, layer, len(s), _p32(s), _p32(p), _p32(n), _dev(k), _dev(v), _stream(stream))
+        if n is None:
+            stored = (C.c_int32 * max(m, 1))()
+            rc = lib.mixattn_get_stored(self.h, layer, m, s, stored)
+            if rc:
+                raise MixAttnError(rc, "mixattn_read_kv")
+            rows = sum(stored[:m])
+            if p is not None:
+                rows = sum(max(0, self.get_len(layer, seq) - first) for seq, first in zip(s[:m], p[:m]))
+        else:
+            rows = sum(max(0, x) for x in n[:m])
+        kv = torch.empty((2, rows, self.n_kv_heads, self.head_dim),
+                         dtype=torch.bfloat16 if self.dtype == BF16 else torch.float32, device=self._device())
+        k, v = kv.unbind(0)
+        rc = lib.mixattn_read_kv(self.h, layer, m, s, p, n, _dev(k), _dev(v), _stream(stream))
         if rc:
             raise MixAttnError(rc, "mixattn_read_kv")
         return k, v
 
-    def _stored(self, layer, seq) -> int:
-        n = self.get_len(layer, seq)
-        kind, window = self.layers[layer]
-        return min(n, window) if kind == SLIDING else n
+    def get_stored(self, layer, seq_ids):
+        """Tokens the layer's cache holds of each sequence: its length, or at most the window."""
+        s, n = _ints(seq_ids)
+        out = (C.c_int32 * max(n, 1))()
+        rc = lib.mixattn_get_stored(self.h, layer, n, s, out)
+        if rc:
+            raise MixAttnError(rc, "mixattn_get_stored")
+        return out[:n]
 
     def _device(self):
         return "cpu" if self.arena is None else self.arena.device
@@ -368,32 +388,50 @@ class Context:
         """logits [groups, beams, vocab] (fp32 or bf16, last dimension dense, rows evenly spaced)."""
         import torch
         g, b, v = logits.shape
-        if logits.dtype not in (torch.float32, torch.bfloat16) or (v > 1 and logits.stride(2) != 1):
-            return ERR_INVALID_ARG
-        stride = logits.stride(1) if b > 1 else (logits.stride(0) if g > 1 else v)
-        if g > 1 and b > 1 and logits.stride(0) != b * stride:
-            return ERR_INVALID_ARG
-        for t, dt, n in ((scores, torch.float32, g * b), (finished, torch.uint8, g * b), (out_scores, torch.float32, g * n_out),
-                         (out_beams, torch.int32, g * n_out), (out_tokens, torch.int32, g * n_out)):
-            if t is not None and (t.dtype != dt or t.numel() != n or not t.is_contiguous()):
+        o = g * n_out
+        for t, dt in ((out_scores, torch.float32), (out_beams, torch.int32), (out_tokens, torch.int32)):
+            if t.dtype is not dt or t.numel() != o or not t.is_contiguous():
                 return ERR_INVALID_ARG
-        return lib.mixattn_beam_select(self.h, g, b, v, BF16 if logits.dtype == torch.bfloat16 else F32, _dev(logits),
-                                       max(stride, v) if g * b == 1 else stride, _dev(scores), _dev(finished),
-                                       int(eos_token), int(n_out), _dev(out_scores), _dev(out_beams), _dev(out_tokens),
-                                       _stream(stream))
+        return self._beam_select(logits, scores, n_out, out_scores.data_ptr(), out_beams.data_ptr(), out_tokens.data_ptr(),
+                                 finished, eos_token, stream)
+
+    def _beam_select(self, logits, scores, n_out, out_scores, out_beams, out_tokens, finished, eos_token, stream) -> int:
+        import torch
+        g, b, v = logits.shape
+        sg, sb, sv = logits.stride()
+        dt = logits.dtype
+        if dt is torch.bfloat16:
+            dt = BF16
+        elif dt is torch.float32:
+            dt = F32
+        else:
+            return ERR_INVALID_ARG
+        if b == 1:
+            sb = sg                              # one beam per group: the groups are the rows
+        if g * b <= 1:
+            sb = v
+        if (v > 1 and sv != 1) or (g > 1 and sg != b * sb):
+            return ERR_INVALID_ARG
+        if scores.dtype is not torch.float32 or scores.numel() != g * b or not scores.is_contiguous():
+            return ERR_INVALID_ARG
+        if finished is not None and (finished.dtype is not torch.uint8 or finished.numel() != g * b or
+                                     not finished.is_contiguous()):
+            return ERR_INVALID_ARG
+        return lib.mixattn_beam_select(self.h, g, b, v, dt, logits.data_ptr(), sb, scores.data_ptr(), _dev(finished),
+                                       eos_token, n_out, out_scores, out_beams, out_tokens, _stream(stream))
 
     def beam_select(self, logits, scores, n_out, finished=None, eos_token=0, stream=None):
         """The n_out best continuations of every group: (scores fp32, beams int32, tokens int32),
         [groups, n_out] each, allocated on torch's current stream."""
         import torch
         g = logits.shape[0]
-        s = torch.empty(g, n_out, dtype=torch.float32, device=logits.device)
-        b = torch.empty(g, n_out, dtype=torch.int32, device=logits.device)
-        t = torch.empty(g, n_out, dtype=torch.int32, device=logits.device)
-        rc = self.rc_beam_select(logits, scores, n_out, s, b, t, finished, eos_token, stream)
+        out = torch.empty((3, g, n_out), dtype=torch.int32, device=logits.device)
+        s, b, t = out.unbind(0)
+        at, step = out.data_ptr(), 4 * g * n_out
+        rc = self._beam_select(logits, scores, n_out, at, at + step, at + 2 * step, finished, eos_token, stream)
         if rc:
             raise MixAttnError(rc, "mixattn_beam_select")
-        return s, b, t
+        return s.view(torch.float32), b, t
 
     def seq_reset(self, seq):
         rc = lib.mixattn_seq_reset(self.h, seq)

@@ -304,11 +304,16 @@ int mixattn_create(const mixattn_config* cfg, mixattn_ctx** out) {
     }
     c->arena = static_cast<char*>(cfg->arena);
     DeviceGuard g(c->device);
-    cudaDeviceProp prop;
-    if (!g.ok || cudaGetDeviceProperties(&prop, c->device) != cudaSuccess) { delete c; return MIXATTN_ERR_CUDA; }
-    c->sm_count = prop.multiProcessorCount;
-    c->l2_bytes = prop.l2CacheSize;
-    if (prepare_decode_bf16() != cudaSuccess || prepare_prefill_tc() != cudaSuccess) { delete c; return MIXATTN_ERR_CUDA; }
+    int sms = 0, l2 = 0;   // (single attributes: filling the whole property block takes milliseconds)
+    if (!g.ok || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, c->device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&l2, cudaDevAttrL2CacheSize, c->device) != cudaSuccess) {
+      delete c;
+      return MIXATTN_ERR_CUDA;
+    }
+    c->sm_count = sms;
+    c->l2_bytes = l2;
+    if (prepare_decode_bf16() != cudaSuccess || prepare_prefill_tc() != cudaSuccess ||
+        prepare_beam_scan() != cudaSuccess) { delete c; return MIXATTN_ERR_CUDA; }
     if (cudaMemsetAsync(c->arena, 0, c->plan.total, 0) != cudaSuccess ||
         cudaStreamSynchronize(0) != cudaSuccess) {
       delete c;
@@ -497,6 +502,7 @@ int mixattn_beam_select(mixattn_ctx* c, int32_t n_groups, int32_t n_beams, int32
   if (!g.ok) return MIXATTN_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   BeamParams p;
+  p.status = c->dev_status();
   p.row_stride = row_stride;
   p.n_beams = n_beams;
   p.vocab = vocab;
@@ -991,6 +997,15 @@ int mixattn_get_len(mixattn_ctx* c, int32_t layer, int32_t seq, int32_t* len) {
   if (c == nullptr || len == nullptr || !c->cm.valid_layer(layer)) return MIXATTN_ERR_INVALID_ARG;
   if (!c->cm.valid_seq(seq)) return MIXATTN_ERR_BAD_SEQ;
   *len = c->cm.len(layer, seq);
+  return MIXATTN_OK;
+}
+
+int mixattn_get_stored(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t* seq_ids, int32_t* out) {
+  if (c == nullptr || !c->cm.valid_layer(layer) || n_seqs < 0 || (n_seqs > 0 && (seq_ids == nullptr || out == nullptr)))
+    return MIXATTN_ERR_INVALID_ARG;
+  for (int i = 0; i < n_seqs; ++i)
+    if (!c->cm.valid_seq(seq_ids[i])) return MIXATTN_ERR_BAD_SEQ;
+  for (int i = 0; i < n_seqs; ++i) out[i] = c->cm.n_attended(layer, seq_ids[i]);
   return MIXATTN_OK;
 }
 

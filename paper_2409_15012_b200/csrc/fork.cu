@@ -71,8 +71,8 @@ __global__ void __launch_bounds__(kThreads) read_kv_kernel(const __grid_constant
   for (int g = 0; g < ge.n_kv_heads; ++g) {
     const int4 a = *reinterpret_cast<const int4*>(k + (int64_t)g * ge.blk_bytes);
     const int4 b = *reinterpret_cast<const int4*>(v + (int64_t)g * ge.blk_bytes);
-    *reinterpret_cast<int4*>(ko + (int64_t)g * ge.row_bytes) = a;
-    *reinterpret_cast<int4*>(vo + (int64_t)g * ge.row_bytes) = b;
+    __stcs(reinterpret_cast<int4*>(ko + (int64_t)g * ge.row_bytes), a);   // (not read again here: shared pages and rings are)
+    __stcs(reinterpret_cast<int4*>(vo + (int64_t)g * ge.row_bytes), b);
   }
 }
 

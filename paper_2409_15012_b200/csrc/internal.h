@@ -252,6 +252,7 @@ struct BeamParams {
   uint64_t* part_keys;       // [rows, n_chunks, n_out] descending, 0 = none
   int32_t n_groups, n_beams, vocab, n_out, eos;
   int32_t n_chunks, chunk_granules;
+  int32_t* status;           // device error word
 };
 
 // device status codes written to the status word
@@ -264,6 +265,7 @@ cudaError_t launch_gather(const GatherParams& p, int max_rows, cudaStream_t st);
 cudaError_t launch_fork_copy(const ForkParams& p, cudaStream_t st);
 cudaError_t launch_read_kv(const GatherParams& p, int max_rows, cudaStream_t st);   // entries without chunk rows
 int beam_chunks(int rows, int vocab, int elem_bytes, int sm_count, int* chunk_granules);
+cudaError_t prepare_beam_scan();
 cudaError_t launch_beam_scan(const BeamParams& p, int elem_bytes, cudaStream_t st);
 cudaError_t launch_beam_merge(const BeamParams& p, cudaStream_t st);
 cudaError_t prepare_decode_bf16();
