@@ -606,6 +606,7 @@ static bool score_shape_of(const mixattn_ctx* c, int layer, ScoreShape* sh) {
   if (ls.plain()) return false;
   sh->pre = ls.softcap > 0.f ? c->scale / ls.softcap : c->scale * kLog2e;
   sh->post = ls.softcap * kLog2e;
+  for (int i = 0; i < 6; ++i) sh->poly[i] = sh->post * tanh_coefficient(i);
   sh->biased = !ls.slopes.empty();
   for (size_t h = 0; h < ls.slopes.size(); ++h) sh->slope[h] = ls.slopes[h] * kLog2e;
   return true;

@@ -30,6 +30,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "f32x2.cuh"
 #include "internal.h"
 
 namespace mixattn {
@@ -87,27 +88,6 @@ __device__ __forceinline__ int keep_best(const Key* keys, int m, Key* best, int 
   return m < n ? m : n;
 }
 
-typedef unsigned long long f32x2;   // two packed floats
-__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
-  f32x2 d;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
-  return d;
-}
-__device__ __forceinline__ float2 unpack2(f32x2 a) {
-  float2 d;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(a));
-  return d;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-  f32x2 d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-  f32x2 d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 __device__ __forceinline__ float fmax3(float a, float b, float c) {   // one instruction; NaN operands are ignored
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));

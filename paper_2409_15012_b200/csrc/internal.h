@@ -88,9 +88,14 @@ __host__ __device__ inline int64_t kv_exp_offset(const KvGeom& ge, int64_t page,
 // How a layer's scores are shaped (mixattn_set_layer_scores; the formulas are in score_shape.cuh).
 // Kernels come in two instantiations: layers with plain scores carry none of this.
 constexpr int kMaxSlopeHeads = MIXATTN_MAX_SLOPE_HEADS;
+__host__ __device__ constexpr float tanh_coefficient(int i) {   // see score_shape.cuh
+  return i == 0 ? 0.9999994039535522f : i == 1 ? -0.3332904279232025f : i == 2 ? 0.13281433284282684f
+       : i == 3 ? -0.05160566791892052f : i == 4 ? 0.01674310676753521f : -0.0030670573469251394f;
+}
 struct ScoreShape {
   float pre;        // factor on q . k: scale / cap with a cap, scale * log2(e) without
   float post;       // cap * log2(e); 0 = no cap
+  float poly[6];    // post times the coefficients of score_shape.cuh's polynomial
   int32_t biased;   // 1: the slopes below apply
   float slope[kMaxSlopeHeads];   // per query head, times log2(e)
 };

@@ -42,6 +42,7 @@
 
 #include <type_traits>
 
+#include "f32x2.cuh"
 #include "internal.h"
 #include "score_shape.cuh"
 
@@ -296,7 +297,7 @@ __device__ __forceinline__ int tile_of(const WorkItem& w, int x) {
 // Entry that an item visits j-th: oldest keys first, or, with shaped scores, the newest first.  A
 // distance bias lifts the scores tile by tile towards the query, so from the oldest tile on a
 // steep head would have to move its exponent reference at every tile.
-template <bool kShape>
+template <int kShape>
 __device__ __forceinline__ int entry_at(const WorkItem& w, int j) { return kShape ? w.n_tiles - 1 - j : j; }
 
 // kRing: some sequences have cached keys in a ring (a separate instantiation, so that the
@@ -304,14 +305,16 @@ __device__ __forceinline__ int entry_at(const WorkItem& w, int j) { return kShap
 // kD: head_dim, 128 or 64.  With 64 channels an operand tile is one [128 x 64] block instead of
 // two (the buffers keep their size), the score product takes four steps of 16 channels, the
 // P V products write 64 accumulator columns, and the softmax warps do exactly the same work.
-// kShape: the layer's scores are capped and / or biased by distance (score_shape.cuh).  The softmax
-// warps turn each raw score into its shaped base-2 score in place right after the load, before the
-// masks; from there on nothing differs but the missing scale.
-template <bool kRing, int kD, bool kShape>
+// kShape: the layer's scores are capped (1), biased by distance (2) or both (3; score_shape.cuh).
+// The softmax warps turn each raw score into its shaped base-2 score less the row's reference in
+// place, right after the load and before the masks, with packed fp32 pairs: a capped score costs
+// four instructions (the cap's polynomial) and half a one for the largest argument, which tells
+// whether any lane's left the polynomial's range; a bias costs one.
+template <bool kRing, int kD, int kShape>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                   const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_ring,
-                  const __grid_constant__ std::conditional_t<kShape, ShapedTcParams, TcParams> p) {
+                  const __grid_constant__ std::conditional_t<kShape != 0, ShapedTcParams, TcParams> p) {
   static_assert(kD == 128 || kD == 64, "head_dim");
   constexpr uint32_t kOpBytes = kD == 128 ? kTileBytes : kHalfBytes;   // bytes of one Q / K / V tile
   constexpr int kSteps = kD / 16;                                        // 16-channel steps of the score product
@@ -590,11 +593,11 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       float m_ref = -INFINITY, l = 0.f;
       uint32_t sv[64];
       float slope = 0.f;                  // kShape: of this head, base-2 units per token
-      if constexpr (kShape) slope = p.shape.biased ? p.shape.slope[w.h] : 0.f;
+      if constexpr (kShape & 2) slope = p.shape.slope[w.h];
       const float scale = kShape ? 1.f : p.scale_log2e;
       // weight of a score: 2^(score - reference)
       auto weight = [&](uint32_t sc, float neg_m) {
-        if constexpr (kShape) return ex2_approx(__uint_as_float(sc) + neg_m);
+        if constexpr (kShape) return ex2_approx(__uint_as_float(sc));   // (shaped scores have it subtracted already)
         else return ex2_approx(fmaf(__uint_as_float(sc), p.scale_log2e, neg_m));
       };
       {
@@ -628,22 +631,53 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             for (int e = 0; e < 64; ++e)
               if (e > k_max || e < k_min) sv[e] = 0xff800000u;             // -inf
           };
-          auto shape_scores = [&]() {
-            if constexpr (kShape) {
-              const float base = -slope * (float)(i - j0);   // bias of column 0; column e is e tokens nearer
-              if (p.shape.post > 0.f) {
-  #pragma unroll
-                for (int e = 0; e < 64; ++e)
-                  sv[e] = __float_as_uint(fmaf(tanh_fast(__uint_as_float(sv[e]) * p.shape.pre), p.shape.post,
-                                               fmaf(slope, (float)e, base)));
-              } else {
-  #pragma unroll
-                for (int e = 0; e < 64; ++e)
-                  sv[e] = __float_as_uint(fmaf(__uint_as_float(sv[e]), p.shape.pre, fmaf(slope, (float)e, base)));
+          // raw scores in sv -> shaped base-2 scores plus `add`
+          auto shape_scores = [&](float add) {
+            if constexpr (kShape != 0) {
+              const f32x2 pre = pack2(p.shape.pre, p.shape.pre);
+              const float base = fmaf(-slope, (float)(i - j0), add);   // of column 0; column e is e tokens nearer
+              f32x2 off = pack2(base, (kShape & 2) ? base + slope : base);
+              float u_max = 0.f;
+#pragma unroll
+              for (int e = 0; e < 64; e += 2) {
+                if constexpr (kShape & 2) {   // (anchored every 16 columns, in between by addition)
+                  if (e % 16 == 0) off = pack2(fmaf(slope, (float)e, base), fmaf(slope, (float)(e + 1), base));
+                  else off = add2(off, pack2(2.f * slope, 2.f * slope));
+                }
+                const f32x2 raw = pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+                f32x2 s;
+                if constexpr (kShape & 1) {
+                  const f32x2 a = mul2(raw, pre), u = mul2(a, a);
+                  f32x2 q = fma2(pack2(p.shape.poly[5], p.shape.poly[5]), u, pack2(p.shape.poly[4], p.shape.poly[4]));
+                  q = fma2(q, u, pack2(p.shape.poly[3], p.shape.poly[3]));
+                  q = fma2(q, u, pack2(p.shape.poly[2], p.shape.poly[2]));
+                  q = fma2(q, u, pack2(p.shape.poly[1], p.shape.poly[1]));
+                  q = fma2(q, u, pack2(p.shape.poly[0], p.shape.poly[0]));
+                  s = fma2(q, a, off);
+                  const float2 uu = unpack2(u);
+                  u_max = fmax3(u_max, uu.x, uu.y);
+                } else {
+                  s = fma2(raw, pre, off);
+                }
+                const float2 ss = unpack2(s);
+                sv[e] = __float_as_uint(ss.x);
+                sv[e + 1] = __float_as_uint(ss.y);
+              }
+              if constexpr (kShape & 1) {
+                if (__any_sync(0xffffffffu, u_max > 1.f)) {   // beyond the polynomial: from the raw scores, which are still in the S buffer
+                  tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+                  tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+                  tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+#pragma unroll
+                  for (int e = 0; e < 64; ++e) {
+                    const float o = (kShape & 2) ? fmaf(slope, (float)e, base) : base;
+                    sv[e] = __float_as_uint(fmaf(tanh_fast(__uint_as_float(sv[e]) * p.shape.pre), p.shape.post, o));
+                  }
+                }
               }
             }
           };
-          shape_scores();
+          shape_scores(m_ref == -INFINITY ? 0.f : -m_ref);
           if (edge) mask_edges();
           // a row that has not seen a key yet takes its reference from this tile
           const bool fresh = m_ref == -INFINITY;
@@ -655,6 +689,11 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               mx1 = fmax3(mx1, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
             }
             if (fresh) m_ref = fmaxf(mx0, mx1) * scale;
+            if constexpr (kShape != 0) {   // fresh rows' scores stand without a reference so far
+              const float sub = fresh && m_ref > -INFINITY ? m_ref : 0.f;
+#pragma unroll
+              for (int e = 0; e < 64; ++e) sv[e] = __float_as_uint(__uint_as_float(sv[e]) - sub);
+            }
           }
           float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;   // no visible key yet: weights 0, no NaN
           // probe the next tile's scores now; the answer is read after the exponentials
@@ -696,7 +735,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
             tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
             tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
-            shape_scores();
+            shape_scores(0.f);
             if (edge) mask_edges();
             float mxa = -INFINITY, mxb = -INFINITY;
   #pragma unroll
@@ -725,6 +764,10 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             l *= alpha;
             if (far) m_ref = mt;
             neg_m = m_ref == -INFINITY ? 0.f : -m_ref;
+            if constexpr (kShape != 0) {
+#pragma unroll
+              for (int e = 0; e < 64; ++e) sv[e] = __float_as_uint(__uint_as_float(sv[e]) + neg_m);
+            }
             sum0 = 0.f;
             sum1 = 0.f;
   #pragma unroll
@@ -841,16 +884,40 @@ bool prefill_tc_supported(int dtype, int head_dim, const void* q, const void* k,
   return dtype == MIXATTN_BF16 && (head_dim == 128 || head_dim == 64) && aligned(q) && aligned(k) && aligned(v) && encode_fn() != nullptr;
 }
 
-cudaError_t prepare_prefill_tc() {
+namespace {
+
+template <int kShape>
+cudaError_t prepare_shape() {
   constexpr auto kAttr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(prefill_tc_kernel<false, 128, false>, kAttr, kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 128, false>, kAttr, kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<false, 64, false>, kAttr, kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 64, false>, kAttr, kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<false, 128, true>, kAttr, kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 128, true>, kAttr, kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<false, 64, true>, kAttr, kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 64, true>, kAttr, kSmemBytes);
+  cudaError_t e = cudaFuncSetAttribute(prefill_tc_kernel<false, 128, kShape>, kAttr, kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 128, kShape>, kAttr, kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<false, 64, kShape>, kAttr, kSmemBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill_tc_kernel<true, 64, kShape>, kAttr, kSmemBytes);
+  return e;
+}
+
+struct TcMaps {
+  CUtensorMap q, k, v, ring;
+};
+
+template <int kShape, typename Params>
+void launch_shape(int D, bool ring, int grid, const TcMaps& m, const Params& p, cudaStream_t st) {
+  if (D == 128) {
+    if (ring) prefill_tc_kernel<true, 128, kShape><<<grid, kThreads, kSmemBytes, st>>>(m.q, m.k, m.v, m.ring, p);
+    else prefill_tc_kernel<false, 128, kShape><<<grid, kThreads, kSmemBytes, st>>>(m.q, m.k, m.v, m.ring, p);
+  } else {
+    if (ring) prefill_tc_kernel<true, 64, kShape><<<grid, kThreads, kSmemBytes, st>>>(m.q, m.k, m.v, m.ring, p);
+    else prefill_tc_kernel<false, 64, kShape><<<grid, kThreads, kSmemBytes, st>>>(m.q, m.k, m.v, m.ring, p);
+  }
+}
+
+}  // namespace
+
+cudaError_t prepare_prefill_tc() {
+  cudaError_t e = prepare_shape<0>();
+  if (e == cudaSuccess) e = prepare_shape<1>();
+  if (e == cudaSuccess) e = prepare_shape<2>();
+  if (e == cudaSuccess) e = prepare_shape<3>();
   return e;
 }
 
@@ -864,18 +931,18 @@ cudaError_t launch_prefill_tc(const PrefillParams& pp, int max_len, int sm_count
     const int64_t end = (int64_t)pp.krow0[i] + pp.prefix[i] - cached + (pp.row0[i + 1] - pp.row0[i]);
     if (end > k_rows) k_rows = end;
   }
-  CUtensorMap tq, tk, tv, tring;
+  TcMaps m;
   const int D = pp.head_dim;
   if (D != 128 && D != 64) return cudaErrorInvalidValue;
-  if (!make_map(&tq, pp.q, rows, pp.n_q_heads, D) || !make_map(&tk, pp.k, k_rows, pp.n_kv_heads, D) ||
-      !make_map(&tv, pp.v, k_rows, pp.n_kv_heads, D))
+  if (!make_map(&m.q, pp.q, rows, pp.n_q_heads, D) || !make_map(&m.k, pp.k, k_rows, pp.n_kv_heads, D) ||
+      !make_map(&m.v, pp.v, k_rows, pp.n_kv_heads, D))
     return cudaErrorInvalidValue;
   if (pp.ring_pool != nullptr) {
     if (!prefill_tc_ring_direct_supported(pp.geom, pp.window) || pp.ring_pages * kPage != pp.window ||
-        !make_ring_map(&tring, pp.ring_pool, pp.geom, pp.ring_total_pages))
+        !make_ring_map(&m.ring, pp.ring_pool, pp.geom, pp.ring_total_pages))
       return cudaErrorInvalidValue;
   } else {
-    tring = tk;   // never read
+    m.ring = m.k;   // never read
   }
   ShapedTcParams p;   // (plain scores: the kernel is handed the TcParams part)
   if (pp.shape != nullptr) p.shape = *pp.shape;
@@ -898,19 +965,11 @@ cudaError_t launch_prefill_tc(const PrefillParams& pp, int max_len, int sm_count
   const int64_t n_ids = (int64_t)p.max_qt * pp.n_seqs * pp.n_q_heads;
   const int grid = (int)(n_ids < sm_count ? n_ids : sm_count);   // persistent: one CTA per SM
   const bool ring = pp.ring_pool != nullptr;
-  auto launch = [&](auto d_tag) {
-    constexpr int kD = decltype(d_tag)::value;
-    const TcParams& plain = p;
-    if (pp.shape != nullptr) {
-      if (ring) prefill_tc_kernel<true, kD, true><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, p);
-      else prefill_tc_kernel<false, kD, true><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, p);
-    } else {
-      if (ring) prefill_tc_kernel<true, kD, false><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, plain);
-      else prefill_tc_kernel<false, kD, false><<<grid, kThreads, kSmemBytes, st>>>(tq, tk, tv, tring, plain);
-    }
-  };
-  if (D == 128) launch(std::integral_constant<int, 128>{});
-  else launch(std::integral_constant<int, 64>{});
+  const int shape = pp.shape == nullptr ? 0 : (pp.shape->post > 0.f ? 1 : 0) | (pp.shape->biased ? 2 : 0);
+  if (shape == 0) launch_shape<0, TcParams>(D, ring, grid, m, p, st);
+  else if (shape == 1) launch_shape<1>(D, ring, grid, m, p, st);
+  else if (shape == 2) launch_shape<2>(D, ring, grid, m, p, st);
+  else launch_shape<3>(D, ring, grid, m, p, st);
   return cudaGetLastError();
 }
 

@@ -12,16 +12,14 @@ namespace mixattn {
 // tanh on |x| <= 1: x times a polynomial of degree 5 in x^2, fitted to tanh(x) / x by weighted
 // least squares until the relative error was level (5.9e-7; 6.9e-7 as evaluated in fp32, about six
 // fp32 roundings, and three orders below the bf16 rounding of the weights that follow).
-constexpr float kTanhC0 = 0.9999994039535522f, kTanhC1 = -0.3332904279232025f, kTanhC2 = 0.13281433284282684f,
-                kTanhC3 = -0.05160566791892052f, kTanhC4 = 0.01674310676753521f, kTanhC5 = -0.0030670573469251394f;
-
+// (tanh_coefficient is declared with ScoreShape.)
 __device__ __forceinline__ float tanh_poly(float x) {   // |x| <= 1
   const float u = x * x;
-  float p = fmaf(kTanhC5, u, kTanhC4);
-  p = fmaf(p, u, kTanhC3);
-  p = fmaf(p, u, kTanhC2);
-  p = fmaf(p, u, kTanhC1);
-  p = fmaf(p, u, kTanhC0);
+  float p = fmaf(tanh_coefficient(5), u, tanh_coefficient(4));
+  p = fmaf(p, u, tanh_coefficient(3));
+  p = fmaf(p, u, tanh_coefficient(2));
+  p = fmaf(p, u, tanh_coefficient(1));
+  p = fmaf(p, u, tanh_coefficient(0));
   return p * x;
 }
 // 1 - 2 / (1 + e^2|x|) with the sign of x: two special-function operations, an absolute error of
