@@ -29,7 +29,7 @@ struct ArenaPlan {
   std::vector<size_t> owner_off;  // per owner slot
   std::vector<size_t> owner_bytes;
   size_t table_off = 0, table_bytes = 0;
-  size_t part_o_off = 0, part_ml_off = 0, status_off = 0;
+  size_t part_o_off = 0, part_ml_off = 0, status_off = 0, ticket_off = 0;
   size_t chunk_k_off = 0, chunk_v_off = 0;   // [chunk_scratch_tokens, Hkv, D] each
   size_t cache_bytes = 0, total = 0;
 };
@@ -59,6 +59,8 @@ ArenaPlan plan_arena(const CacheManager& cm, const mixattn_config& cfg) {
   off += align_up((size_t)kWsChunks * cfg.n_q_heads * sizeof(float2));
   pl.status_off = off;
   off += kAlign;
+  pl.ticket_off = off;
+  off += align_up(kBeamTickets * sizeof(int32_t));
   if (cfg.chunk_scratch_tokens > 0) {
     const size_t bytes = align_up((size_t)cfg.chunk_scratch_tokens * ge.n_kv_heads * ge.row_bytes);
     pl.chunk_k_off = off;
@@ -313,7 +315,7 @@ int mixattn_create(const mixattn_config* cfg, mixattn_ctx** out) {
     c->sm_count = sms;
     c->l2_bytes = l2;
     if (prepare_decode_bf16() != cudaSuccess || prepare_prefill_tc() != cudaSuccess ||
-        prepare_beam_scan() != cudaSuccess) { delete c; return MIXATTN_ERR_CUDA; }
+        prepare_beam_select() != cudaSuccess) { delete c; return MIXATTN_ERR_CUDA; }
     if (cudaMemsetAsync(c->arena, 0, c->plan.total, 0) != cudaSuccess ||
         cudaStreamSynchronize(0) != cudaSuccess) {
       delete c;
@@ -503,6 +505,7 @@ int mixattn_beam_select(mixattn_ctx* c, int32_t n_groups, int32_t n_beams, int32
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   BeamParams p;
   p.status = c->dev_status();
+  p.tickets = reinterpret_cast<int32_t*>(c->arena + c->plan.ticket_off);
   p.row_stride = row_stride;
   p.n_beams = n_beams;
   p.vocab = vocab;
@@ -522,7 +525,7 @@ int mixattn_beam_select(mixattn_ctx* c, int32_t n_groups, int32_t n_beams, int32
   }
   const size_t per_group = (size_t)n_beams * p.n_chunks * per_chunk;
   int64_t batch = (int64_t)(room / per_group);
-  batch = std::min<int64_t>(batch, 65535 / n_beams);
+  batch = std::min<int64_t>(std::min<int64_t>(batch, 65535 / n_beams), kBeamTickets);
   char* ws = c->arena + c->plan.part_o_off;
   for (int64_t g0 = 0; g0 < n_groups; g0 += batch) {
     const int64_t r0 = g0 * n_beams;
@@ -535,9 +538,8 @@ int mixattn_beam_select(mixattn_ctx* c, int32_t n_groups, int32_t n_beams, int32
     p.out_tokens = out_tokens + g0 * n_out;
     p.part_keys = reinterpret_cast<uint64_t*>(ws);
     p.part_sums = reinterpret_cast<float2*>(ws + (size_t)p.n_groups * n_beams * p.n_chunks * n_out * sizeof(uint64_t));
-    cudaError_t e = launch_recorded(c, MIXATTN_K_SELECT, st, [&] { return launch_beam_scan(p, elem, st); });
-    if (e == cudaSuccess) e = launch_recorded(c, MIXATTN_K_SELECT, st, [&] { return launch_beam_merge(p, st); });
-    if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
+    if (launch_recorded(c, MIXATTN_K_SELECT, st, [&] { return launch_beam_select(p, elem, st); }) != cudaSuccess)
+      return MIXATTN_ERR_CUDA;
   }
   return MIXATTN_OK;
 }
@@ -607,6 +609,15 @@ static bool score_shape_of(const mixattn_ctx* c, int layer, ScoreShape* sh) {
   sh->pre = ls.softcap > 0.f ? c->scale / ls.softcap : c->scale * kLog2e;
   sh->post = ls.softcap * kLog2e;
   for (int i = 0; i < 6; ++i) sh->poly[i] = sh->post * tanh_coefficient(i);
+  const double pre = sh->pre;
+  bool normal = pre > 1e-18;   // (squares of products up to 1 / (2 pre) stay finite)
+  double power = pre;
+  for (int i = 0; i < 4; ++i, power *= pre * pre) {
+    const double f = tanh_near_coefficient(i) * power * ls.softcap * (double)kLog2e;
+    normal = normal && fabs(f) > 1e-36 && fabs(f) < 1e36;
+    sh->near[i] = (float)f;
+  }
+  sh->near_sq = normal ? (float)(0.25 / (pre * pre)) : -1.f;
   sh->biased = !ls.slopes.empty();
   for (size_t h = 0; h < ls.slopes.size(); ++h) sh->slope[h] = ls.slopes[h] * kLog2e;
   return true;

@@ -4,10 +4,11 @@
 // A candidate (beam, token) scores  score_beam + x - lse_beam,  lse = log sum exp(x) over the
 // beam's finite logits.  Within a beam the order is that of the logits, so one pass over the
 // logits gives both the sum and the beam's best n_out, and only those meet the other beams:
-//   * beam_scan_kernel: one CTA per (beam, chunk of the vocabulary) reads its logits once, keeps
-//     a running (maximum, sum) per thread and the chunk's best n_out in shared memory;
-//   * beam_merge_kernel: one CTA per group forms lse in double precision, scores the chunks'
-//     lists and picks the group's best.
+//   * one CTA per (beam, chunk of the vocabulary) reads its logits once, keeps a running (maximum,
+//     sum) per thread and the chunk's best n_out in shared memory;
+//   * the last CTA of a group to finish (a ticket counter) forms lse in double precision, scores the
+//     chunks' lists and picks the group's best.  (A second kernel for this cost 3 us of launch and
+//     set-up on the smallest calls.)
 // The scan is bound by HBM (the logits are read once): tiles of 16 KB stream into
 // shared memory with bulk async copies, two stages per CTA, four CTAs per SM.
 //
@@ -178,14 +179,131 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {   // 
   return true;
 }
 
+// A scored continuation; the score as an order-preserving integer, because ranking compares a lot.
+struct Scored {
+  uint64_t score;
+  int32_t flat;      // beam * vocab + token
+  int32_t pad;
+};
+__device__ __forceinline__ Scored scored(double x, int32_t flat) {
+  const uint64_t b = (uint64_t)__double_as_longlong(x + 0.0);
+  return Scored{b >> 63 ? ~b : b | 0x8000000000000000ull, flat, 0};
+}
+__device__ __forceinline__ double score_of(const Scored& s) {
+  return __longlong_as_double((long long)(s.score >> 63 ? s.score & 0x7fffffffffffffffull : ~s.score));
+}
+
+constexpr int kMergePool = 512;
+
+// The lists are sorted, so bounds come from one entry of each: with r such that the lists hold
+// n entries up to rank r, the k-th largest of their entries of rank r, k = ceil(n / (r + 1)), is
+// reached by at least k (r + 1) >= n candidates.  What reaches it is collected and ranked.
+__device__ __forceinline__ void merge_group(const BeamParams& p, int group, unsigned char* smem) {
+  const int n = p.n_out, nb = p.n_beams, nc = p.n_chunks;
+  Scored* list = reinterpret_cast<Scored*>(smem);                 // [n]
+  Scored* pool = list + n;                                         // [n + kMergePool]
+  double* offset = reinterpret_cast<double*>(pool + n + kMergePool);   // [nb] lse of a beam
+  float* start = reinterpret_cast<float*>(offset + nb);            // [nb] its score; NaN: no continuation
+  uint8_t* done = reinterpret_cast<uint8_t*>(start + nb);          // [nb]
+  __shared__ int s_count;
+  __shared__ Scored s_floor;
+  auto greater = [](const Scored& a, const Scored& b) { return a.score > b.score || (a.score == b.score && a.flat < b.flat); };
+  const int lists = nb * nc;
+
+  for (int b = threadIdx.x; b < nb; b += kThreads) {
+    const float s = p.scores[group * nb + b];
+    start[b] = fabsf(s) < INFINITY ? s : __int_as_float(0x7fc00000);
+    done[b] = p.finished != nullptr && p.finished[group * nb + b] != 0;
+  }
+  if (threadIdx.x == 0) { s_count = 0; s_floor = Scored{0, 0x7fffffff, 0}; }
+  __syncthreads();
+  // lse in double from the chunks' fp32 sums, one warp per beam
+  for (int b = threadIdx.x >> 5; b < nb; b += kThreads / 32) {
+    if (done[b]) continue;
+    const float2* ps = p.part_sums + (int64_t)(group * nb + b) * nc;
+    const int lane = threadIdx.x & 31;
+    float m = -INFINITY;
+    for (int c = lane; c < nc; c += 32) m = fmaxf(m, __ldcg(&ps[c]).x);
+#pragma unroll
+    for (int sh = 16; sh > 0; sh >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, sh));
+    double s = 0.0;
+    for (int c = lane; c < nc; c += 32) {
+      const float2 x = __ldcg(&ps[c]);
+      if (x.x > -INFINITY) s += (double)x.y * exp((double)x.x - (double)m);
+    }
+#pragma unroll
+    for (int sh = 16; sh > 0; sh >>= 1) s += __shfl_xor_sync(0xffffffffu, s, sh);
+    if (lane == 0) offset[b] = (double)m + log(s);
+  }
+  __syncthreads();
+
+  // entry r of list l
+  auto candidate = [&](int l, int r, Scored* out) {
+    const int b = l / nc, c = l - b * nc;
+    const float s = start[b];
+    if (!(fabsf(s) < INFINITY)) return false;
+    if (done[b]) {   // one continuation
+      *out = scored((double)s, b * p.vocab + p.eos);
+      return r == 0 && c == 0;
+    }
+    const uint64_t key = __ldcg(p.part_keys + ((int64_t)(group * nb + b) * nc + c) * n + r);
+    *out = scored((double)unordered((uint32_t)(key >> 32)) - offset[b] + (double)s,
+                  b * p.vocab + (int32_t)(uint32_t)~(uint32_t)key);
+    return key != 0;
+  };
+  // the bound (skipped where the entries would not fit the pool: everything is looked at then)
+  const int r0 = (n + lists - 1) / lists - 1, k = (n + r0) / (r0 + 1);
+  int have = 0;
+  if (lists <= kMergePool) {
+    for (int l0 = 0; l0 < lists; l0 += kThreads) {
+      Scored x;
+      const int l = l0 + (int)threadIdx.x;
+      const bool in = l < lists && candidate(l, r0, &x);
+      if (in) pool[atomicAdd(&s_count, 1)] = x;
+      have += __syncthreads_count(in);
+    }
+    if (have >= k) {
+      keep_best(pool, have, list, k, greater);
+      if (threadIdx.x == 0) s_floor = list[k - 1];
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) s_count = 0;
+    have = 0;
+  }
+  __syncthreads();
+  Scored floor = s_floor;
+  for (int64_t at = threadIdx.x; at - threadIdx.x < (int64_t)lists * n; at += kThreads) {
+    Scored x;
+    const bool in = at < (int64_t)lists * n && candidate((int)(at / n), (int)(at % n), &x) && !greater(floor, x);
+    const int n_in = __syncthreads_count(in);
+    if (n_in == 0) continue;
+    if (have + n_in > n + kMergePool) {   // (uniform) a full pool shrinks to its best n, which raise the bound
+      have = keep_best(pool, have, list, n, greater);
+      for (int i = threadIdx.x; i < have; i += kThreads) pool[i] = list[i];
+      if (threadIdx.x == 0) s_count = have;
+      if (have == n) floor = list[n - 1];
+      __syncthreads();
+    }
+    if (in) pool[atomicAdd(&s_count, 1)] = x;
+    have += n_in;
+  }
+  __syncthreads();
+  have = keep_best(pool, have, list, n, greater);
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const int64_t o = (int64_t)group * n + i;
+    p.out_scores[o] = i < have ? (float)score_of(list[i]) : -INFINITY;
+    p.out_beams[o] = i < have ? list[i].flat / p.vocab : -1;
+    p.out_tokens[o] = i < have ? list[i].flat % p.vocab : -1;
+  }
+}
+
 // T: float or __nv_bfloat16
 template <typename T>
-__global__ void __launch_bounds__(kThreads, kScanCtas) beam_scan_kernel(const __grid_constant__ BeamParams p) {
+__global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const __grid_constant__ BeamParams p) {
   constexpr int kVec = 16 / (int)sizeof(T);          // logits per 16-byte granule
   constexpr int kTileGranules = kThreads * kVecs;
   const int row = blockIdx.y, n = p.n_out;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the merge may get ready (it waits for all of this grid)
-  if (p.finished != nullptr && p.finished[row]) return;   // its logits are not read
+  const bool finished = p.finished != nullptr && p.finished[row] != 0;   // its logits are not read
   extern __shared__ __align__(128) unsigned char smem[];       // [kStages] tiles, then:
   uint64_t* list = reinterpret_cast<uint64_t*>(smem + kStages * kTileBytes);   // [n] the best so far, descending
   uint64_t* scratch = list + n;                                 // [n + max(kPending, n * logits of a thread)]: see below
@@ -205,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_scan_kernel(const __
   const int g1 = min(granules, g0 + p.chunk_granules);
   // Whole granules [gw0, gw1) are copied; the row's first and last one may be partial and are read one by one.
   const int gw0 = max(g0, lead > 0 ? 1 : 0), gw1 = min(g1, (int)(((int64_t)lead + p.vocab) / kVec));
-  const int n_tiles = (g1 - g0 + kTileGranules - 1) / kTileGranules;   // (not positive: nothing of the row in this chunk)
+  const int n_tiles = finished ? 0 : (g1 - g0 + kTileGranules - 1) / kTileGranules;   // (not positive: nothing of the row in this chunk)
   auto issue = [&](int k) {   // thread 0: tile k into its stage
     const int a = max(gw0, g0 + k * kTileGranules), b = min(gw1, g0 + (k + 1) * kTileGranules);
     const uint32_t bar = smem_u32(&s_bar[k % kStages]);
@@ -429,124 +547,19 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_scan_kernel(const __
     for (int w = 0; w < kThreads / 32; ++w) s += s_red[1][w];
     p.part_sums[part] = make_float2(m, s);
   }
-}
-
-// A scored continuation; the score as an order-preserving integer, because ranking compares a lot.
-struct Scored {
-  uint64_t score;
-  int32_t flat;      // beam * vocab + token
-  int32_t pad;
-};
-__device__ __forceinline__ Scored scored(double x, int32_t flat) {
-  const uint64_t b = (uint64_t)__double_as_longlong(x + 0.0);
-  return Scored{b >> 63 ? ~b : b | 0x8000000000000000ull, flat, 0};
-}
-__device__ __forceinline__ double score_of(const Scored& s) {
-  return __longlong_as_double((long long)(s.score >> 63 ? s.score & 0x7fffffffffffffffull : ~s.score));
-}
-
-constexpr int kMergePool = 512;
-
-// The lists are sorted, so bounds come from one entry of each: with r such that the lists hold
-// n entries up to rank r, the k-th largest of their entries of rank r, k = ceil(n / (r + 1)), is
-// reached by at least k (r + 1) >= n candidates.  What reaches it is collected and ranked.
-__global__ void __launch_bounds__(kThreads) beam_merge_kernel(const __grid_constant__ BeamParams p) {
-  const int group = blockIdx.x, n = p.n_out, nb = p.n_beams, nc = p.n_chunks;
-  extern __shared__ __align__(128) unsigned char smem[];
-  Scored* list = reinterpret_cast<Scored*>(smem);                 // [n]
-  Scored* pool = list + n;                                         // [n + kMergePool]
-  double* offset = reinterpret_cast<double*>(pool + n + kMergePool);   // [nb] lse of a beam
-  float* start = reinterpret_cast<float*>(offset + nb);            // [nb] its score; NaN: no continuation
-  uint8_t* done = reinterpret_cast<uint8_t*>(start + nb);          // [nb]
-  __shared__ int s_count;
-  __shared__ Scored s_floor;
-  auto greater = [](const Scored& a, const Scored& b) { return a.score > b.score || (a.score == b.score && a.flat < b.flat); };
-  const int lists = nb * nc;
-
-  for (int b = threadIdx.x; b < nb; b += kThreads) {   // (inputs of the call, not of the scan)
-    const float s = p.scores[group * nb + b];
-    start[b] = fabsf(s) < INFINITY ? s : __int_as_float(0x7fc00000);
-    done[b] = p.finished != nullptr && p.finished[group * nb + b] != 0;
-  }
-  if (threadIdx.x == 0) { s_count = 0; s_floor = Scored{0, 0x7fffffff, 0}; }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // ---- the last CTA of the group merges its lists ----
+  __threadfence();
   __syncthreads();
-  // lse in double from the chunks' fp32 sums, one warp per beam
-  for (int b = threadIdx.x >> 5; b < nb; b += kThreads / 32) {
-    if (done[b]) continue;
-    const float2* ps = p.part_sums + (int64_t)(group * nb + b) * nc;
-    const int lane = threadIdx.x & 31;
-    float m = -INFINITY;
-    for (int c = lane; c < nc; c += 32) m = fmaxf(m, ps[c].x);
-#pragma unroll
-    for (int sh = 16; sh > 0; sh >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, sh));
-    double s = 0.0;
-    for (int c = lane; c < nc; c += 32)
-      if (ps[c].x > -INFINITY) s += (double)ps[c].y * exp((double)ps[c].x - (double)m);
-#pragma unroll
-    for (int sh = 16; sh > 0; sh >>= 1) s += __shfl_xor_sync(0xffffffffu, s, sh);
-    if (lane == 0) offset[b] = (double)m + log(s);
+  const int group = row / p.n_beams;
+  if (threadIdx.x == 0) {
+    const int32_t before = atomicAdd(&p.tickets[group], 1);
+    s_count = before == p.n_beams * (int)gridDim.x - 1;
+    if (s_count) p.tickets[group] = 0;   // (as the next call wants it)
   }
   __syncthreads();
-
-  // entry r of list l
-  auto candidate = [&](int l, int r, Scored* out) {
-    const int b = l / nc, c = l - b * nc;
-    const float s = start[b];
-    if (!(fabsf(s) < INFINITY)) return false;
-    if (done[b]) {   // one continuation
-      *out = scored((double)s, b * p.vocab + p.eos);
-      return r == 0 && c == 0;
-    }
-    const uint64_t key = p.part_keys[((int64_t)(group * nb + b) * nc + c) * n + r];
-    *out = scored((double)unordered((uint32_t)(key >> 32)) - offset[b] + (double)s,
-                  b * p.vocab + (int32_t)(uint32_t)~(uint32_t)key);
-    return key != 0;
-  };
-  // the bound (skipped where the entries would not fit the pool: everything is looked at then)
-  const int r0 = (n + lists - 1) / lists - 1, k = (n + r0) / (r0 + 1);
-  int have = 0;
-  if (lists <= kMergePool) {
-    for (int l0 = 0; l0 < lists; l0 += kThreads) {
-      Scored x;
-      const int l = l0 + (int)threadIdx.x;
-      const bool in = l < lists && candidate(l, r0, &x);
-      if (in) pool[atomicAdd(&s_count, 1)] = x;
-      have += __syncthreads_count(in);
-    }
-    if (have >= k) {
-      keep_best(pool, have, list, k, greater);
-      if (threadIdx.x == 0) s_floor = list[k - 1];
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) s_count = 0;
-    have = 0;
-  }
-  __syncthreads();
-  Scored floor = s_floor;
-  for (int64_t at = threadIdx.x; at - threadIdx.x < (int64_t)lists * n; at += kThreads) {
-    Scored x;
-    const bool in = at < (int64_t)lists * n && candidate((int)(at / n), (int)(at % n), &x) && !greater(floor, x);
-    const int n_in = __syncthreads_count(in);
-    if (n_in == 0) continue;
-    if (have + n_in > n + kMergePool) {   // (uniform) a full pool shrinks to its best n, which raise the bound
-      have = keep_best(pool, have, list, n, greater);
-      for (int i = threadIdx.x; i < have; i += kThreads) pool[i] = list[i];
-      if (threadIdx.x == 0) s_count = have;
-      if (have == n) floor = list[n - 1];
-      __syncthreads();
-    }
-    if (in) pool[atomicAdd(&s_count, 1)] = x;
-    have += n_in;
-  }
-  __syncthreads();
-  have = keep_best(pool, have, list, n, greater);
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int64_t o = (int64_t)group * n + i;
-    p.out_scores[o] = i < have ? (float)score_of(list[i]) : -INFINITY;
-    p.out_beams[o] = i < have ? list[i].flat / p.vocab : -1;
-    p.out_tokens[o] = i < have ? list[i].flat % p.vocab : -1;
-  }
+  if (!s_count) return;
+  __threadfence();
+  merge_group(p, group, smem);
 }
 
 }  // namespace
@@ -578,33 +591,21 @@ int beam_chunks(int rows, int vocab, int elem_bytes, int sm_count, int* chunk_gr
   return (int)((granules + best_len - 1) / best_len);
 }
 
-cudaError_t prepare_beam_scan() {
+cudaError_t prepare_beam_select() {
   constexpr auto kAttr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(beam_scan_kernel<__nv_bfloat16>, kAttr, 56 * 1024);
-  return e == cudaSuccess ? cudaFuncSetAttribute(beam_scan_kernel<float>, kAttr, 56 * 1024) : e;
+  cudaError_t e = cudaFuncSetAttribute(beam_select_kernel<__nv_bfloat16>, kAttr, 56 * 1024);
+  return e == cudaSuccess ? cudaFuncSetAttribute(beam_select_kernel<float>, kAttr, 56 * 1024) : e;
 }
 
-cudaError_t launch_beam_scan(const BeamParams& p, int elem_bytes, cudaStream_t st) {
+cudaError_t launch_beam_select(const BeamParams& p, int elem_bytes, cudaStream_t st) {
   const int keys = 2 * p.n_out + std::max(kPending, p.n_out * kVecs * 16 / elem_bytes);
   const size_t smem = (size_t)kStages * kTileBytes + (size_t)keys * sizeof(uint64_t);
+  static_assert((2 * MIXATTN_MAX_BEAM_OUT + kMergePool) * sizeof(Scored) + MIXATTN_MAX_BEAMS * 13 <= kStages * kTileBytes,
+                "the merge works where the tiles were");
   const dim3 grid(p.n_chunks, p.n_groups * p.n_beams);
-  if (elem_bytes == 2) beam_scan_kernel<__nv_bfloat16><<<grid, kThreads, smem, st>>>(p);
-  else beam_scan_kernel<float><<<grid, kThreads, smem, st>>>(p);
+  if (elem_bytes == 2) beam_select_kernel<__nv_bfloat16><<<grid, kThreads, smem, st>>>(p);
+  else beam_select_kernel<float><<<grid, kThreads, smem, st>>>(p);
   return cudaGetLastError();
-}
-
-cudaError_t launch_beam_merge(const BeamParams& p, cudaStream_t st) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.n_groups);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = (size_t)(2 * p.n_out + kMergePool) * sizeof(Scored) + (size_t)p.n_beams * (sizeof(double) + sizeof(float) + 1);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // set-up overlaps the scan's tail
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, beam_merge_kernel, p);
 }
 
 }  // namespace mixattn

@@ -489,19 +489,23 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
           st[2] = (st[2] + st2[2]) * ks1; st[3] = (st[3] + st2[3]) * ks1;
         }
         if constexpr (SH) {   // this thread's two keys and two heads
-          float d0 = 0.f, d1 = 0.f;
-          if (p.shape.biased) {
-            int b0 = p.newest[x.i] - tok_base - (KV8 ? key0 : frow);
-            int b1 = b0 - (KV8 ? 2 : 8);
-            if (b0 < 0) b0 += p.wrap;
-            if (b1 < 0) b1 += p.wrap;
-            d0 = -(float)b0;
-            d1 = -(float)b1;
+          if (p.shape.post > 0.f) cap_scores(st, p.shape);
+          else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st[e] *= p.shape.pre;
           }
-          st[0] = shaped_score(st[0], p.shape, slope[0] * d0);
-          st[1] = shaped_score(st[1], p.shape, slope[1] * d0);
-          st[2] = shaped_score(st[2], p.shape, slope[0] * d1);
-          st[3] = shaped_score(st[3], p.shape, slope[1] * d1);
+          if (p.shape.biased) {
+            int back = p.newest[x.i] - tok_base - (KV8 ? key0 : frow);
+            float d0 = -(float)back, d1 = d0 + (KV8 ? 2.f : 8.f);
+            if (p.wrap > 0) {   // a ring: slots behind the newest one are a turn older
+              if (back < 0) d0 -= (float)p.wrap;
+              if (back < (KV8 ? 2 : 8)) d1 -= (float)p.wrap;
+            }
+            st[0] = fmaf(slope[0], d0, st[0]);
+            st[1] = fmaf(slope[1], d0, st[1]);
+            st[2] = fmaf(slope[0], d1, st[2]);
+            st[3] = fmaf(slope[1], d1, st[3]);
+          }
         }
         if (tok_base + kPage > x.t1) {  // ragged end of the split: this thread's two keys (tile rows frow, frow + 8)
           const int lim = x.t1 - tok_base;
@@ -581,18 +585,14 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
           // V^T rows are channels, 16 key bytes each: one ldmatrix.x4 = 32 channels; a register
           // holds keys 4t .. 4t+3 of a channel, which are the contraction indices 2t, 2t+1 and
           // 2t+8, 2t+9 in the key order of the tile rows above
-          uint32_t keep = 0xffffffffu;   // (SH: as above; a register holds four keys of a channel)
-          if constexpr (SH) {
-            if (tok_base + kPage > x.t1) {
-              const int left = x.t1 - tok_base - 2 * fcol;   // keys 4t .. 4t + 3 that belong to the sequence
-              keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-            }
-          }
+          const bool ragged = SH && tok_base + kPage > x.t1;   // (SH: cleared as above; a register holds four keys of a channel)
+          const int left = x.t1 - tok_base - 2 * fcol;          // keys 4t .. 4t + 3 that belong to the sequence
+          const uint32_t keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) {
             uint32_t r[4], a[4], b[4];
             ldsm_x4(vb + (32 * j + lane) * kPage, r[0], r[1], r[2], r[3]);
-            if constexpr (SH) { r[0] &= keep; r[1] &= keep; r[2] &= keep; r[3] &= keep; }
+            if (ragged) { r[0] &= keep; r[1] &= keep; r[2] &= keep; r[3] &= keep; }
             e4m3x4_to_f16x2x2(r[0], a[0], a[2]);
             e4m3x4_to_f16x2x2(r[1], a[1], a[3]);
             e4m3x4_to_f16x2x2(r[2], b[0], b[2]);

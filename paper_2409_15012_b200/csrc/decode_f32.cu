@@ -64,7 +64,76 @@ decode_split_f32_kernel(const __grid_constant__ std::conditional_t<SH != 0, Shap
                          : 0.f;
       }
     }
-    for (int t = t0 + warp; t < t1; t += kWarps) {
+    if constexpr (SH) {
+      // Four keys of four heads at a time: their 16 products are summed over the warp in 16 shuffles
+      // (each step hands half of the values over), which leaves value v = 4 key + head with lanes
+      // 2 v and 2 v + 1, so that each lane shapes one score; the keys' loads overlap.
+      constexpr int kKeys = 4;
+      static_assert(kKeys * kRowsPerPass == 16, "one value per pair of lanes");
+      const int my_key = lane >> 3, my_row = (lane >> 1) & 3;
+      const float my_slope = p.shape.biased && my_row < nr ? p.shape.slope[h0 + r0 + my_row] : 0.f;
+      for (int t = t0 + warp * kKeys; t < t1; t += kWarps * kKeys) {
+        float kv[kKeys][V], vv[kKeys][V];
+#pragma unroll
+        for (int j = 0; j < kKeys; ++j) {
+          const int tj = min(t + j, t1 - 1);   // (past the end: read again, masked below)
+          const int64_t page = tbl ? (int64_t)tbl[tj / kPage] : (int64_t)seq * p.ring_pages + tj / kPage;
+          const char* blk = p.pool + page * ge.page_bytes + (int64_t)g * ge.blk_bytes;
+          const float* kr = reinterpret_cast<const float*>(blk + (int64_t)(tj % kPage) * ge.row_bytes) + lane * V;
+          const float* vr = kr + kPage * D;
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            kv[j][e] = kr[e];
+            vv[j][e] = vr[e];
+          }
+        }
+        float s[16];
+#pragma unroll
+        for (int j = 0; j < kKeys; ++j)
+#pragma unroll
+          for (int r = 0; r < kRowsPerPass; ++r) {
+            float acc = 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc = fmaf(q[r][e], kv[j][e], acc);
+            s[4 * j + r] = acc;
+          }
+#pragma unroll
+        for (int half = 8; half > 0; half >>= 1) {
+          const bool up = lane & (2 * half);
+#pragma unroll
+          for (int v = 0; v < half; ++v) {
+            const float keep = up ? s[v + half] : s[v], give = up ? s[v] : s[v + half];
+            s[v] = keep + __shfl_xor_sync(0xffffffffu, give, 2 * half);
+          }
+        }
+        float mine = s[0] + __shfl_xor_sync(0xffffffffu, s[0], 1);
+        int back = p.newest[i] - (t + my_key);
+        if (back < 0) back += p.wrap;
+        mine = t + my_key < t1 ? shaped_score_exact(mine, p.shape, -my_slope * (float)back) : -INFINITY;
+#pragma unroll
+        for (int r = 0; r < kRowsPerPass; ++r) {
+          float sc[kKeys], mn = m[r];
+#pragma unroll
+          for (int j = 0; j < kKeys; ++j) {
+            sc[j] = __shfl_sync(0xffffffffu, mine, 2 * (4 * j + r));
+            mn = fmaxf(mn, sc[j]);
+          }
+          const float a = exp2f(m[r] - mn);   // (the first key of the four is there, so mn is finite)
+          m[r] = mn;
+          l[r] *= a;
+#pragma unroll
+          for (int e = 0; e < V; ++e) o[r][e] *= a;
+#pragma unroll
+          for (int j = 0; j < kKeys; ++j) {
+            const float pe = exp2f(sc[j] - mn);
+            l[r] += pe;
+#pragma unroll
+            for (int e = 0; e < V; ++e) o[r][e] = fmaf(pe, vv[j][e], o[r][e]);
+          }
+        }
+      }
+    } else {
+        for (int t = t0 + warp; t < t1; t += kWarps) {
       const int64_t page = tbl ? (int64_t)tbl[t / kPage] : (int64_t)seq * p.ring_pages + t / kPage;
       const char* blk = p.pool + page * ge.page_bytes + (int64_t)g * ge.blk_bytes;
       const float* kr = reinterpret_cast<const float*>(blk + (int64_t)(t % kPage) * ge.row_bytes) + lane * V;
@@ -82,17 +151,7 @@ decode_split_f32_kernel(const __grid_constant__ std::conditional_t<SH != 0, Shap
         for (int e = 0; e < V; ++e) s = fmaf(q[r][e], kv[e], s);
 #pragma unroll
         for (int sh = 16; sh > 0; sh >>= 1) s += __shfl_xor_sync(0xffffffffu, s, sh);
-        if constexpr (SH) {
-          float bias = 0.f;
-          if (p.shape.biased) {
-            int back = p.newest[i] - t;
-            if (back < 0) back += p.wrap;
-            bias = r < nr ? -p.shape.slope[h0 + r0 + r] * (float)back : 0.f;
-          }
-          s = shaped_score_exact(s, p.shape, bias);
-        } else {
-          s *= p.scale_log2e;
-        }
+        s *= p.scale_log2e;
         const float mn = fmaxf(m[r], s);
         const float a = exp2f(m[r] - mn);
         const float pe = exp2f(s - mn);
@@ -101,6 +160,7 @@ decode_split_f32_kernel(const __grid_constant__ std::conditional_t<SH != 0, Shap
 #pragma unroll
         for (int e = 0; e < V; ++e) o[r][e] = fmaf(pe, vv[e], o[r][e] * a);
       }
+    }
     }
 #pragma unroll
     for (int r = 0; r < kRowsPerPass; ++r) {

@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kThreads) fork_copy_kernel(const __grid_consta
 // One block: kThreads / chunks tokens; a thread owns one 16-byte chunk of a token's rows and
 // walks the KV heads, so the page lookup is made once per thread and every warp reads and
 // writes whole rows.
-__global__ void __launch_bounds__(kThreads) read_kv_kernel(const __grid_constant__ GatherParams p) {
+__global__ void __launch_bounds__(kThreads, MINB) read_kv_kernel(const __grid_constant__ GatherParams p) {
   const GatherEntry& e = p.e[blockIdx.y];
   const KvGeom& ge = p.geom;
   const int chunks = ge.row_bytes / 16;                // 8, 16 or 32
@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(kThreads) read_kv_kernel(const __grid_constant
   const int64_t out = (int64_t)(e.dst_row0 + t) * ge.n_kv_heads * ge.row_bytes + chunk * 16;
   char* ko = static_cast<char*>(p.k_out) + out;
   char* vo = static_cast<char*>(p.v_out) + out;
-#pragma unroll 4
+#pragma unroll UNR
   for (int g = 0; g < ge.n_kv_heads; ++g) {
     const int4 a = *reinterpret_cast<const int4*>(k + (int64_t)g * ge.blk_bytes);
     const int4 b = *reinterpret_cast<const int4*>(v + (int64_t)g * ge.blk_bytes);

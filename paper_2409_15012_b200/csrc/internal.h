@@ -92,10 +92,16 @@ __host__ __device__ constexpr float tanh_coefficient(int i) {   // see score_sha
   return i == 0 ? 0.9999994039535522f : i == 1 ? -0.3332904279232025f : i == 2 ? 0.13281433284282684f
        : i == 3 ? -0.05160566791892052f : i == 4 ? 0.01674310676753521f : -0.0030670573469251394f;
 }
+// the same on half the range: |x| <= 1/2, cubic in x^2, relative error 5.4e-7
+__host__ __device__ constexpr float tanh_near_coefficient(int i) {
+  return i == 0 ? 0.999999463558197f : i == 1 ? -0.33326318860054016f : i == 2 ? 0.13190296292304993f : -0.04440222308039665f;
+}
 struct ScoreShape {
   float pre;        // factor on q . k: scale / cap with a cap, scale * log2(e) without
   float post;       // cap * log2(e); 0 = no cap
   float poly[6];    // post times the coefficients of score_shape.cuh's polynomial
+  float near[4];    // the cubic's for raw products: score = raw * (near[0] + near[1] raw^2 + ...) while raw^2 <= near_sq
+  float near_sq;    // (negative: not used, a coefficient would leave fp32's normal range)
   int32_t biased;   // 1: the slopes below apply
   float slope[kMaxSlopeHeads];   // per query head, times log2(e)
 };
@@ -244,7 +250,8 @@ struct ForkParams {
   TableRow row[kForkRows];
 };
 
-// Beam selection.  part_sums and part_keys are the scan's results per (beam, chunk).
+// Beam selection.  Groups of one launch have a ticket counter each.  part_sums and part_keys are the scan's results per (beam, chunk).
+constexpr int kBeamTickets = 1024;
 struct BeamParams {
   const void* logits;        // [n_groups * n_beams] rows of `vocab`, row_stride elements apart
   int64_t row_stride;
@@ -258,6 +265,7 @@ struct BeamParams {
   int32_t n_groups, n_beams, vocab, n_out, eos;
   int32_t n_chunks, chunk_granules;
   int32_t* status;           // device error word
+  int32_t* tickets;          // [n_groups] CTAs that have finished; 0 before and after a call
 };
 
 // device status codes written to the status word
@@ -270,9 +278,8 @@ cudaError_t launch_gather(const GatherParams& p, int max_rows, cudaStream_t st);
 cudaError_t launch_fork_copy(const ForkParams& p, cudaStream_t st);
 cudaError_t launch_read_kv(const GatherParams& p, int max_rows, cudaStream_t st);   // entries without chunk rows
 int beam_chunks(int rows, int vocab, int elem_bytes, int sm_count, int* chunk_granules);
-cudaError_t prepare_beam_scan();
-cudaError_t launch_beam_scan(const BeamParams& p, int elem_bytes, cudaStream_t st);
-cudaError_t launch_beam_merge(const BeamParams& p, cudaStream_t st);
+cudaError_t prepare_beam_select();
+cudaError_t launch_beam_select(const BeamParams& p, int elem_bytes, cudaStream_t st);
 cudaError_t prepare_decode_bf16();
 // (a launch whose layer has shaped scores passes its block as both p and shaped; else shaped = nullptr)
 cudaError_t launch_decode_split_bf16(const DecodeParams& p, const ShapedDecodeParams* shaped, int sm_count,

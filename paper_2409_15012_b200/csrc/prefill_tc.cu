@@ -308,8 +308,9 @@ __device__ __forceinline__ int entry_at(const WorkItem& w, int j) { return kShap
 // kShape: the layer's scores are capped (1), biased by distance (2) or both (3; score_shape.cuh).
 // The softmax warps turn each raw score into its shaped base-2 score less the row's reference in
 // place, right after the load and before the masks, with packed fp32 pairs: a capped score costs
-// four instructions (the cap's polynomial) and half a one for the largest argument, which tells
-// whether any lane's left the polynomial's range; a bias costs one.
+// two and a half instructions (a cubic in the product's square) and half a one for the largest
+// square, which tells whether any of the warp's left half the cap, where a longer polynomial takes
+// over; a bias costs half a one (one without a cap).
 template <bool kRing, int kD, int kShape>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -634,49 +635,110 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           // raw scores in sv -> shaped base-2 scores plus `add`
           auto shape_scores = [&](float add) {
             if constexpr (kShape != 0) {
-              const f32x2 pre = pack2(p.shape.pre, p.shape.pre);
               const float base = fmaf(-slope, (float)(i - j0), add);   // of column 0; column e is e tokens nearer
-              f32x2 off = pack2(base, (kShape & 2) ? base + slope : base);
-              float u_max = 0.f;
-#pragma unroll
-              for (int e = 0; e < 64; e += 2) {
-                if constexpr (kShape & 2) {   // (anchored every 16 columns, in between by addition)
+              f32x2 off = pack2(base, base);
+              auto next_off = [&](int e) {   // of columns e, e + 1: anchored every 16 columns, in between by addition
+                if constexpr (kShape & 2) {
                   if (e % 16 == 0) off = pack2(fmaf(slope, (float)e, base), fmaf(slope, (float)(e + 1), base));
                   else off = add2(off, pack2(2.f * slope, 2.f * slope));
                 }
-                const f32x2 raw = pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
-                f32x2 s;
-                if constexpr (kShape & 1) {
-                  const f32x2 a = mul2(raw, pre), u = mul2(a, a);
-                  f32x2 q = fma2(pack2(p.shape.poly[5], p.shape.poly[5]), u, pack2(p.shape.poly[4], p.shape.poly[4]));
-                  q = fma2(q, u, pack2(p.shape.poly[3], p.shape.poly[3]));
-                  q = fma2(q, u, pack2(p.shape.poly[2], p.shape.poly[2]));
-                  q = fma2(q, u, pack2(p.shape.poly[1], p.shape.poly[1]));
-                  q = fma2(q, u, pack2(p.shape.poly[0], p.shape.poly[0]));
-                  s = fma2(q, a, off);
-                  const float2 uu = unpack2(u);
-                  u_max = fmax3(u_max, uu.x, uu.y);
-                } else {
-                  s = fma2(raw, pre, off);
-                }
+              };
+              auto raw_of = [&](int e) { return pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])); };
+              auto put = [&](int e, f32x2 s) {
                 const float2 ss = unpack2(s);
                 sv[e] = __float_as_uint(ss.x);
                 sv[e + 1] = __float_as_uint(ss.y);
-              }
-              if constexpr (kShape & 1) {
-                if (__any_sync(0xffffffffu, u_max > 1.f)) {   // beyond the polynomial: from the raw scores, which are still in the S buffer
+              };
+              auto both = [](float x) { return pack2(x, x); };
+              if constexpr (kShape == 2) {
+#pragma unroll
+                for (int e = 0; e < 64; e += 2) {
+                  next_off(e);
+                  put(e, fma2(raw_of(e), both(p.shape.pre), off));
+                }
+              } else {
+                float top = 0.f;   // largest square of a product
+#pragma unroll
+                for (int e = 0; e < 64; e += 2) {
+                  next_off(e);
+                  const f32x2 raw = raw_of(e), u = mul2(raw, raw);
+                  f32x2 q = fma2(both(p.shape.near[3]), u, both(p.shape.near[2]));
+                  q = fma2(q, u, both(p.shape.near[1]));
+                  q = fma2(q, u, both(p.shape.near[0]));
+                  put(e, fma2(q, raw, off));
+                  const float2 uu = unpack2(u);
+                  top = fmax3(top, uu.x, uu.y);
+                }
+                if (__any_sync(0xffffffffu, top > p.shape.near_sq)) {
+                  // some score is above half the cap: again from the raw products, which are still in
+                  // the S buffer, with the polynomial of the whole range, and one by one beyond it
                   tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
                   tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
                   tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
 #pragma unroll
-                  for (int e = 0; e < 64; ++e) {
-                    const float o = (kShape & 2) ? fmaf(slope, (float)e, base) : base;
-                    sv[e] = __float_as_uint(fmaf(tanh_fast(__uint_as_float(sv[e]) * p.shape.pre), p.shape.post, o));
+                  for (int e = 0; e < 64; e += 2) {
+                    next_off(e);
+                    const f32x2 x = mul2(raw_of(e), both(p.shape.pre)), u = mul2(x, x);
+                    f32x2 q = fma2(both(p.shape.poly[5]), u, both(p.shape.poly[4]));
+                    q = fma2(q, u, both(p.shape.poly[3]));
+                    q = fma2(q, u, both(p.shape.poly[2]));
+                    q = fma2(q, u, both(p.shape.poly[1]));
+                    q = fma2(q, u, both(p.shape.poly[0]));
+                    float2 s = unpack2(fma2(q, x, off));
+                    const float2 xx = unpack2(x), oo = unpack2(off);
+                    if (fabsf(xx.x) > 1.f) s.x = fmaf(tanh_exp(xx.x), p.shape.post, oo.x);
+                    if (fabsf(xx.y) > 1.f) s.y = fmaf(tanh_exp(xx.y), p.shape.post, oo.y);
+                    sv[e] = __float_as_uint(s.x);
+                    sv[e + 1] = __float_as_uint(s.y);
                   }
                 }
               }
             }
           };
+          // probe the next tile's scores now; the answer is read after the exponentials
+          const bool more = j + 1 < w.n_tiles;
+          const bool next_ready = more && mbar_test_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1);
+          float sum0 = 0.f, sum1 = 0.f;
+          uint32_t pk[32], pl[32];   // P as bf16 pairs; pl = rounding residuals (only on w.lo items)
+          // Capped scores of a tile that no band edge crosses, for rows that all have their reference:
+          // straight from the raw products to the weights, so that the packed arithmetic of one column
+          // runs under the exponentials of others (8k causal prompt: 710 -> 650 us).  Whether that was
+          // right (every square within the cubic's range, no far lead) is only looked at afterwards;
+          // if not, the raw products are fetched again and the tile takes the general way below.
+          // (With a distance bias as well, or alone, the general way was as fast or faster: 34.9
+          // against 36.9 us on ragged windows, 99 against 108 on chunks.)
+          bool done = false;
+          if constexpr (kShape == 1) {
+            if (!kLo && !edge && p.shape.near_sq >= 0.f && !__any_sync(0xffffffffu, m_ref == -INFINITY)) {
+              const f32x2 off = pack2(-m_ref, -m_ref);
+              f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
+              float top = 0.f;
+#pragma unroll
+              for (int e = 0; e < 64; e += 2) {
+                const f32x2 raw = pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), u = mul2(raw, raw);
+                f32x2 q = fma2(pack2(p.shape.near[3], p.shape.near[3]), u, pack2(p.shape.near[2], p.shape.near[2]));
+                q = fma2(q, u, pack2(p.shape.near[1], p.shape.near[1]));
+                q = fma2(q, u, pack2(p.shape.near[0], p.shape.near[0]));
+                const float2 uu = unpack2(u), ss = unpack2(fma2(q, raw, off));
+                top = fmax3(top, uu.x, uu.y);
+                const float p0 = ex2_approx(ss.x), p1 = ex2_approx(ss.y);
+                if (e & 2) sum3 = add2(sum3, pack2(p0, p1));
+                else sum2 = add2(sum2, pack2(p0, p1));
+                pk[e >> 1] = pack_bf16(p0, p1);
+              }
+              const float2 s01 = unpack2(add2(sum2, sum3));
+              sum0 = s01.x;
+              sum1 = s01.y;
+              done = __all_sync(0xffffffffu, sum0 + sum1 <= 0x1p70f && top <= p.shape.near_sq);
+              if (!done) {
+                tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+                tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+                tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+              }
+            }
+          }
+          if (!done) {
+          sum0 = sum1 = 0.f;
           shape_scores(m_ref == -INFINITY ? 0.f : -m_ref);
           if (edge) mask_edges();
           // a row that has not seen a key yet takes its reference from this tile
@@ -696,12 +758,21 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
           }
           float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;   // no visible key yet: weights 0, no NaN
-          // probe the next tile's scores now; the answer is read after the exponentials
-          const bool more = j + 1 < w.n_tiles;
-          const bool next_ready = more && mbar_test_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1);
-          float sum0 = 0.f, sum1 = 0.f;
-          uint32_t pk[32], pl[32];   // P as bf16 pairs; pl = rounding residuals (only on w.lo items)
-          if constexpr (!kLo) {
+          if constexpr (!kLo && kShape != 0) {
+            f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
+  #pragma unroll
+            for (int e = 0; e < 64; e += 4) {
+              const float p0 = ex2_approx(__uint_as_float(sv[e])), p1 = ex2_approx(__uint_as_float(sv[e + 1]));
+              const float p2 = ex2_approx(__uint_as_float(sv[e + 2])), p3 = ex2_approx(__uint_as_float(sv[e + 3]));
+              sum2 = add2(sum2, pack2(p0, p1));
+              sum3 = add2(sum3, pack2(p2, p3));
+              pk[e >> 1] = pack_bf16(p0, p1);
+              pk[(e >> 1) + 1] = pack_bf16(p2, p3);
+            }
+            const float2 s01 = unpack2(add2(sum2, sum3));
+            sum0 = s01.x;
+            sum1 = s01.y;
+          } else if constexpr (!kLo) {
   #pragma unroll
             for (int e = 0; e < 64; e += 4) {
               const float p0 = weight(sv[e], neg_m);
@@ -780,6 +851,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               else pk[e >> 1] = pack_bf16(p0, p1);
             }
           }
+          }   // !done
           l += sum0 + sum1;
           // P (bf16 pairs) over the first 32 of this stream's 64 score columns, the residual
           // term, where the item carries one, over the other 32

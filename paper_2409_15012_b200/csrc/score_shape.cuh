@@ -30,13 +30,20 @@ __device__ __forceinline__ float tanh_exp(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e + 1.f));
   return copysignf(fmaf(-2.f, r, 1.f), x);
 }
-__device__ __forceinline__ float tanh_fast(float x) { return fabsf(x) <= 1.f ? tanh_poly(x) : tanh_exp(x); }
-
-// base-2 score of a raw product q . k; `bias` = -slope * log2(e) * distance (0 without a bias)
-__device__ __forceinline__ float shaped_score(float raw, const ScoreShape& sh, float bias) {
-  float y = raw * sh.pre;
-  if (sh.post > 0.f) y = tanh_fast(y) * sh.post;
-  return y + bias;
+// raw products -> capped base-2 scores
+__device__ __forceinline__ void cap_scores(float (&s)[4], const ScoreShape& sh) {
+  float x[4], top = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] = s[e] * sh.pre;
+    s[e] = tanh_poly(x[e]) * sh.post;
+    top = fmaxf(top, fabsf(x[e]));
+  }
+  if (top > 1.f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (fabsf(x[e]) > 1.f) s[e] = tanh_exp(x[e]) * sh.post;
+  }
 }
 __device__ __forceinline__ float shaped_score_exact(float raw, const ScoreShape& sh, float bias) {   // fp32 mode
   float y = raw * sh.pre;
