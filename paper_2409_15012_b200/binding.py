@@ -350,23 +350,27 @@ class Context:
         """Returns (K, V), the cached tokens [sum n_tokens, Hkv, D] of the sequences, oldest first
         (default: everything stored).  The tensors are allocated on torch's current stream."""
         import torch
-        (s, m), (p, mp), (n, mn) = _ints(seq_ids), _ints(first_pos), _ints(n_tokens)
-        if (p is not None and mp != m) or (n is not None and mn != m):
-            raise MixAttnError(ERR_INVALID_ARG, "mixattn_read_kv")
-        if n is None:
-            stored = (C.c_int32 * max(m, 1))()
+        s, m = _ints(seq_ids)
+        p = n = None
+        if first_pos is not None or n_tokens is not None:
+            (p, mp), (n, mn) = _ints(first_pos), _ints(n_tokens)
+            if (p is not None and mp != m) or (n is not None and mn != m):
+                raise MixAttnError(ERR_INVALID_ARG, "mixattn_read_kv")
+        if n is not None:
+            rows = sum([max(0, x) for x in n[:m]])
+        elif p is not None:
+            rows = sum([max(0, self.get_len(layer, seq) - first) for seq, first in zip(s[:m], p[:m])])
+        else:
+            stored = (C.c_int32 * (m or 1))()
             rc = lib.mixattn_get_stored(self.h, layer, m, s, stored)
             if rc:
                 raise MixAttnError(rc, "mixattn_read_kv")
-            rows = sum(stored[:m])
-            if p is not None:
-                rows = sum(max(0, self.get_len(layer, seq) - first) for seq, first in zip(s[:m], p[:m]))
-        else:
-            rows = sum(max(0, x) for x in n[:m])
+            rows = sum(stored) if m else 0
         kv = torch.empty((2, rows, self.n_kv_heads, self.head_dim),
                          dtype=torch.bfloat16 if self.dtype == BF16 else torch.float32, device=self._device())
         k, v = kv.unbind(0)
-        rc = lib.mixattn_read_kv(self.h, layer, m, s, p, n, _dev(k), _dev(v), _stream(stream))
+        at = kv.data_ptr()
+        rc = lib.mixattn_read_kv(self.h, layer, m, s, p, n, at, at + kv.nbytes // 2, _stream(stream))
         if rc:
             raise MixAttnError(rc, "mixattn_read_kv")
         return k, v

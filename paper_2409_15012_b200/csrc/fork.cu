@@ -13,6 +13,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnroll = 8;                            // 16-byte loads in flight per thread
+constexpr int kReadVecs = 2;                          // (32 copies of 4103 tokens, 32 query / 8 KV heads of 128 bf16: 1: 172 us, 2: 161, 4: 162, 8: 197)
 constexpr int kBlock16 = kThreads * kUnroll;          // 16-byte units per block: 32 KB
 
 __global__ void __launch_bounds__(kThreads) fork_copy_kernel(const __grid_constant__ ForkParams p) {
@@ -40,39 +41,46 @@ __global__ void __launch_bounds__(kThreads) fork_copy_kernel(const __grid_consta
   if ((int)threadIdx.x < r.n_set) dst[r.set0 + threadIdx.x] = r.page[threadIdx.x];
 }
 
-// One block: kThreads / chunks tokens; a thread owns one 16-byte chunk of a token's rows and
-// walks the KV heads, so the page lookup is made once per thread and every warp reads and
-// writes whole rows.
-__global__ void __launch_bounds__(kThreads, MINB) read_kv_kernel(const __grid_constant__ GatherParams p) {
+// The head vectors of the rows in the order they are written are dealt out to the blocks, kReadVecs
+// per group of threads that copies one (a thread per 16 bytes): a block writes one contiguous
+// stretch of K and one of V, with all its loads in flight at once.  (Reading a page that several
+// copies share once for all of them, in one block, was slower, 195 us against 184 for the fork and
+// the read back of the case below: the rows written bound it, not the pages read.)
+__global__ void __launch_bounds__(kThreads, 8) read_kv_kernel(const __grid_constant__ GatherParams p) {
   const GatherEntry& e = p.e[blockIdx.y];
   const KvGeom& ge = p.geom;
   const int chunks = ge.row_bytes / 16;                // 8, 16 or 32
-  const int tokens = kThreads / chunks;
-  const int t = blockIdx.x * tokens + (int)threadIdx.x / chunks;
-  const int chunk = (int)threadIdx.x % chunks;
-  if (t >= e.n_prefix) return;
-  const int pos = e.pos0 + t;
-  int64_t page;
-  int slot;
-  if (p.is_ring) {
-    const int rs = pos % p.window;
-    page = (int64_t)e.seq * p.ring_pages + rs / kPage;
-    slot = rs % kPage;
-  } else {
-    page = p.table[(int64_t)e.seq * p.table_stride + pos / kPage];
-    slot = pos % kPage;
+  const int chunk = (int)threadIdx.x % chunks, groups = kThreads / chunks;
+  const int64_t vecs = (int64_t)e.n_prefix * ge.n_kv_heads;
+  const int64_t v0 = (int64_t)blockIdx.x * groups * kReadVecs + (int)threadIdx.x / chunks;
+  const int32_t* tbl = p.table + (int64_t)e.seq * p.table_stride;
+  int4 a[kReadVecs], b[kReadVecs];
+#pragma unroll
+  for (int i = 0; i < kReadVecs; ++i) {
+    const int64_t x = v0 + i * groups;
+    if (x >= vecs) break;
+    const int t = (int)(x / ge.n_kv_heads), g = (int)(x - (int64_t)t * ge.n_kv_heads), pos = e.pos0 + t;
+    int64_t page;
+    int slot;
+    if (p.is_ring) {
+      const int rs = pos % p.window;
+      page = (int64_t)e.seq * p.ring_pages + rs / kPage;
+      slot = rs % kPage;
+    } else {
+      page = tbl[pos / kPage];
+      slot = pos % kPage;
+    }
+    const char* k = p.pool + kv_chunk_offset(ge, page, g, 0, slot, chunk);
+    a[i] = *reinterpret_cast<const int4*>(k);
+    b[i] = *reinterpret_cast<const int4*>(k + (int64_t)kPage * ge.st_row_bytes);
   }
-  const char* k = p.pool + kv_chunk_offset(ge, page, 0, 0, slot, chunk);
-  const char* v = k + (int64_t)kPage * ge.st_row_bytes;
-  const int64_t out = (int64_t)(e.dst_row0 + t) * ge.n_kv_heads * ge.row_bytes + chunk * 16;
-  char* ko = static_cast<char*>(p.k_out) + out;
-  char* vo = static_cast<char*>(p.v_out) + out;
-#pragma unroll UNR
-  for (int g = 0; g < ge.n_kv_heads; ++g) {
-    const int4 a = *reinterpret_cast<const int4*>(k + (int64_t)g * ge.blk_bytes);
-    const int4 b = *reinterpret_cast<const int4*>(v + (int64_t)g * ge.blk_bytes);
-    __stcs(reinterpret_cast<int4*>(ko + (int64_t)g * ge.row_bytes), a);   // (not read again here: shared pages and rings are)
-    __stcs(reinterpret_cast<int4*>(vo + (int64_t)g * ge.row_bytes), b);
+#pragma unroll
+  for (int i = 0; i < kReadVecs; ++i) {
+    const int64_t x = v0 + i * groups;
+    if (x >= vecs) break;
+    const int64_t out = ((int64_t)e.dst_row0 * ge.n_kv_heads + x) * ge.row_bytes + chunk * 16;
+    __stcs(reinterpret_cast<int4*>(static_cast<char*>(p.k_out) + out), a[i]);   // (not read again here: shared pages and rings are)
+    __stcs(reinterpret_cast<int4*>(static_cast<char*>(p.v_out) + out), b[i]);
   }
 }
 
@@ -91,8 +99,10 @@ cudaError_t launch_fork_copy(const ForkParams& p, cudaStream_t st) {
 cudaError_t launch_read_kv(const GatherParams& p, int max_rows, cudaStream_t st) {
   if (p.geom.fp8) return launch_gather(p, max_rows, st);   // dequantises
   if (p.n_entries <= 0 || max_rows <= 0) return cudaSuccess;
-  const int tokens = kThreads / (p.geom.row_bytes / 16);
-  read_kv_kernel<<<dim3((max_rows + tokens - 1) / tokens, p.n_entries), kThreads, 0, st>>>(p);
+  const int64_t per_block = (int64_t)kThreads / (p.geom.row_bytes / 16) * kReadVecs;
+  const int64_t blocks = ((int64_t)max_rows * p.geom.n_kv_heads + per_block - 1) / per_block;
+  if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
+  read_kv_kernel<<<dim3((unsigned)blocks, p.n_entries), kThreads, 0, st>>>(p);
   return cudaGetLastError();
 }
 
