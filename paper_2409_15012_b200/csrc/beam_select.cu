@@ -79,8 +79,15 @@ __device__ __forceinline__ int keep_best(const Key* keys, int m, Key* best, int 
     Key k{};
     if (i < m) {
       k = keys[i];
-#pragma unroll 4
-      for (int j = part; j < m; j += share) rank += greater(keys[j], k);
+      int j = part;
+      for (; j + 7 * share < m; j += 8 * share) {   // (eight loads in flight)
+        Key o[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) o[u] = keys[j + u * share];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) rank += greater(o[u], k);
+      }
+      for (; j < m; j += share) rank += greater(keys[j], k);
     }
     for (int sh = 1; sh < share; sh <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, sh);
     if (i < m && part == 0 && rank < n) best[rank] = k;
@@ -207,9 +214,27 @@ __device__ __forceinline__ void merge_group(const BeamParams& p, int group, unsi
   uint8_t* done = reinterpret_cast<uint8_t*>(start + nb);          // [nb]
   __shared__ int s_count;
   __shared__ Scored s_floor;
-  auto greater = [](const Scored& a, const Scored& b) { return a.score > b.score || (a.score == b.score && a.flat < b.flat); };
-  const int lists = nb * nc;
+  auto greater = [](const Scored& a, const Scored& b) { return (bool)((a.score > b.score) | ((a.score == b.score) & (a.flat < b.flat))); };   // (no branches)
+  const int lists = nb * nc, lane = (int)threadIdx.x & 31;
+  const int64_t total = (int64_t)lists * n;
+  const uint64_t* keys = p.part_keys + (int64_t)group * total;
+  const float2* sums = p.part_sums + (int64_t)group * lists;
+  // bounds from rank r0 of the k best lists (see above)
+  const int r0 = (n + lists - 1) / lists - 1, k = (n + r0) / (r0 + 1);
 
+  // What the other CTAs left is a trip to L2 away: everything most groups need is asked for at once.
+  // (Entries of finished beams were never written; they are not looked at.)
+  constexpr int kEarly = 4;
+  uint64_t early[kEarly], head = 0;
+  float2 part = make_float2(-INFINITY, 0.f);
+#pragma unroll
+  for (int i = 0; i < kEarly; ++i) {
+    const int64_t at = (int)threadIdx.x + i * kThreads;
+    early[i] = at < total ? __ldcg(keys + at) : 0;
+  }
+  if ((int)threadIdx.x < lists) head = __ldcg(keys + (int64_t)threadIdx.x * n + r0);
+  const int b0 = (int)threadIdx.x >> 5;   // a warp per beam
+  if (b0 < nb && lane < nc) part = __ldcg(sums + b0 * nc + lane);
   for (int b = threadIdx.x; b < nb; b += kThreads) {
     const float s = p.scores[group * nb + b];
     start[b] = fabsf(s) < INFINITY ? s : __int_as_float(0x7fc00000);
@@ -217,28 +242,27 @@ __device__ __forceinline__ void merge_group(const BeamParams& p, int group, unsi
   }
   if (threadIdx.x == 0) { s_count = 0; s_floor = Scored{0, 0x7fffffff, 0}; }
   __syncthreads();
-  // lse in double from the chunks' fp32 sums, one warp per beam
-  for (int b = threadIdx.x >> 5; b < nb; b += kThreads / 32) {
+  // lse in double from the chunks' fp32 sums
+  for (int b = b0; b < nb; b += kThreads / 32) {
     if (done[b]) continue;
-    const float2* ps = p.part_sums + (int64_t)(group * nb + b) * nc;
-    const int lane = threadIdx.x & 31;
-    float m = -INFINITY;
-    for (int c = lane; c < nc; c += 32) m = fmaxf(m, __ldcg(&ps[c]).x);
+    if (b != b0) part = lane < nc ? __ldcg(sums + b * nc + lane) : make_float2(-INFINITY, 0.f);
+    float m = part.x;
+    for (int c = lane + 32; c < nc; c += 32) m = fmaxf(m, __ldcg(sums + b * nc + c).x);
 #pragma unroll
     for (int sh = 16; sh > 0; sh >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, sh));
-    double s = 0.0;
-    for (int c = lane; c < nc; c += 32) {
-      const float2 x = __ldcg(&ps[c]);
-      if (x.x > -INFINITY) s += (double)x.y * exp((double)x.x - (double)m);
-    }
+    auto share = [&](const float2& x) {   // (most beams have their maximum in one chunk or are one)
+      return x.x == m ? (double)x.y : x.x > -INFINITY ? (double)x.y * exp((double)x.x - (double)m) : 0.0;
+    };
+    double s = share(part);
+    for (int c = lane + 32; c < nc; c += 32) s += share(__ldcg(sums + b * nc + c));
 #pragma unroll
     for (int sh = 16; sh > 0; sh >>= 1) s += __shfl_xor_sync(0xffffffffu, s, sh);
     if (lane == 0) offset[b] = (double)m + log(s);
   }
   __syncthreads();
 
-  // entry r of list l
-  auto candidate = [&](int l, int r, Scored* out) {
+  // entry r of list l, whose key is `key`
+  auto candidate = [&](int l, int r, uint64_t key, Scored* out) {
     const int b = l / nc, c = l - b * nc;
     const float s = start[b];
     if (!(fabsf(s) < INFINITY)) return false;
@@ -246,40 +270,42 @@ __device__ __forceinline__ void merge_group(const BeamParams& p, int group, unsi
       *out = scored((double)s, b * p.vocab + p.eos);
       return r == 0 && c == 0;
     }
-    const uint64_t key = __ldcg(p.part_keys + ((int64_t)(group * nb + b) * nc + c) * n + r);
     *out = scored((double)unordered((uint32_t)(key >> 32)) - offset[b] + (double)s,
                   b * p.vocab + (int32_t)(uint32_t)~(uint32_t)key);
     return key != 0;
   };
-  // the bound (skipped where the entries would not fit the pool: everything is looked at then)
-  const int r0 = (n + lists - 1) / lists - 1, k = (n + r0) / (r0 + 1);
   int have = 0;
-  if (lists <= kMergePool) {
-    for (int l0 = 0; l0 < lists; l0 += kThreads) {
-      Scored x;
-      const int l = l0 + (int)threadIdx.x;
-      const bool in = l < lists && candidate(l, r0, &x);
-      if (in) pool[atomicAdd(&s_count, 1)] = x;
-      have += __syncthreads_count(in);
-    }
+  if (lists <= kThreads) {   // (more lists: everything is looked at)
+    Scored x;
+    const bool in = (int)threadIdx.x < lists && candidate((int)threadIdx.x, r0, head, &x);
+    if (in) pool[atomicAdd(&s_count, 1)] = x;
+    have = __syncthreads_count(in);
     if (have >= k) {
       keep_best(pool, have, list, k, greater);
       if (threadIdx.x == 0) s_floor = list[k - 1];
     }
-    __syncthreads();
     if (threadIdx.x == 0) s_count = 0;
     have = 0;
+    __syncthreads();
   }
-  __syncthreads();
   Scored floor = s_floor;
-  for (int64_t at = threadIdx.x; at - threadIdx.x < (int64_t)lists * n; at += kThreads) {
+  for (int i = 0; (int64_t)i * kThreads < total; ++i) {
+    const int64_t at = (int)threadIdx.x + (int64_t)i * kThreads;
     Scored x;
-    const bool in = at < (int64_t)lists * n && candidate((int)(at / n), (int)(at % n), &x) && !greater(floor, x);
+    bool in = false;
+    if (at < total) {
+      uint64_t key = 0;
+#pragma unroll
+      for (int j = 0; j < kEarly; ++j)
+        if (i == j) key = early[j];
+      if (i >= kEarly) key = __ldcg(keys + at);
+      in = candidate((int)(at / n), (int)(at % n), key, &x) && !greater(floor, x);
+    }
     const int n_in = __syncthreads_count(in);
     if (n_in == 0) continue;
     if (have + n_in > n + kMergePool) {   // (uniform) a full pool shrinks to its best n, which raise the bound
       have = keep_best(pool, have, list, n, greater);
-      for (int i = threadIdx.x; i < have; i += kThreads) pool[i] = list[i];
+      for (int j = threadIdx.x; j < have; j += kThreads) pool[j] = list[j];
       if (threadIdx.x == 0) s_count = have;
       if (have == n) floor = list[n - 1];
       __syncthreads();
@@ -464,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
       const int c = __popc(mask);
       int at = atomicAdd(&s_count, c);
       if (at + c <= kPending) {
-        crowded = at + c > 2 * n + 32;               // rank now and then: the higher `last`, the fewer candidates
+        crowded = at + c > 2 * n + 16;               // rank now and then: the higher `last`, the fewer candidates
         for (; mask != 0; mask &= mask - 1) pending[at++] = key_of(__ffs(mask) - 1);
       } else {
         failed = true;
