@@ -428,9 +428,17 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
         qb[ks][1] = pack_f16(__low2float(b), __high2float(b));
       }
     }
-    float slope[2] = {0.f, 0.f};   // of this thread's two heads (SH)
+    // SH: slopes of this thread's two heads; distance of its first key in page 0; factor on a raw product
+    float slope[2] = {0.f, 0.f}, factor = 1.f;
+    int newest = 0;
+    bool capped = false, biased = false, ring = false;
     if constexpr (SH) {
-      if (p.shape.biased) {
+      capped = p.shape.post > 0.f;
+      biased = p.shape.biased;
+      ring = p.wrap > 0;
+      if (!capped) factor = p.shape.pre;   // (the cap applies it itself)
+      newest = p.newest[x.i] - (KV8 ? key0 : frow);
+      if (biased) {
         slope[0] = fcol < rows ? p.shape.slope[h0 + fcol] : 0.f;
         slope[1] = fcol + 1 < rows ? p.shape.slope[h0 + fcol + 1] : 0.f;
       }
@@ -465,7 +473,7 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
             mma_bf16(st2, b, qb[ks + 1][0], qb[ks + 1][1]);
           }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) st[e] = SH ? st[e] + st2[e] : (st[e] + st2[e]) * p.scale_log2e;
+          for (int e = 0; e < 4; ++e) st[e] = (st[e] + st2[e]) * (SH ? factor : p.scale_log2e);
         } else {
           // one ldmatrix.x4 = (tile rows 0-7 | 8-15) x (16-byte chunk 2j | 2j+1) = two 16-channel steps
 #pragma unroll
@@ -481,23 +489,19 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
           }
           // the shared exponents of the page's rows sit behind its K and V elements
           const unsigned char* xs = stages + (size_t)s * kStageBytes + wig * kBlkBytes + 2 * kPage * kRowBytes;
-          const float ks0 = SH ? exp_byte_to_float(xs[key0]) : exp_byte_to_float(xs[key0]) * p.scale_log2e;
-          const float ks1 = SH ? exp_byte_to_float(xs[key0 + 2]) : exp_byte_to_float(xs[key0 + 2]) * p.scale_log2e;
+          const float ks0 = exp_byte_to_float(xs[key0]) * (SH ? factor : p.scale_log2e);
+          const float ks1 = exp_byte_to_float(xs[key0 + 2]) * (SH ? factor : p.scale_log2e);
           vscale0 = exp_byte_to_float(xs[kPage + key0]);
           vscale1 = exp_byte_to_float(xs[kPage + key0 + 2]);
           st[0] = (st[0] + st2[0]) * ks0; st[1] = (st[1] + st2[1]) * ks0;
           st[2] = (st[2] + st2[2]) * ks1; st[3] = (st[3] + st2[3]) * ks1;
         }
         if constexpr (SH) {   // this thread's two keys and two heads
-          if (p.shape.post > 0.f) cap_scores(st, p.shape);
-          else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) st[e] *= p.shape.pre;
-          }
-          if (p.shape.biased) {
-            int back = p.newest[x.i] - tok_base - (KV8 ? key0 : frow);
+          if (capped) cap_scores(st, p.shape);
+          if (biased) {
+            const int back = newest - tok_base;
             float d0 = -(float)back, d1 = d0 + (KV8 ? 2.f : 8.f);
-            if (p.wrap > 0) {   // a ring: slots behind the newest one are a turn older
+            if (ring) {   // slots behind the newest one are a turn older
               if (back < 0) d0 -= (float)p.wrap;
               if (back < (KV8 ? 2 : 8)) d1 -= (float)p.wrap;
             }
@@ -585,20 +589,25 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
           // V^T rows are channels, 16 key bytes each: one ldmatrix.x4 = 32 channels; a register
           // holds keys 4t .. 4t+3 of a channel, which are the contraction indices 2t, 2t+1 and
           // 2t+8, 2t+9 in the key order of the tile rows above
-          const bool ragged = SH && tok_base + kPage > x.t1;   // (SH: cleared as above; a register holds four keys of a channel)
-          const int left = x.t1 - tok_base - 2 * fcol;          // keys 4t .. 4t + 3 that belong to the sequence
-          const uint32_t keep = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+          auto add_values = [&](uint32_t keep) {
 #pragma unroll
-          for (int j = 0; j < D / 32; ++j) {
-            uint32_t r[4], a[4], b[4];
-            ldsm_x4(vb + (32 * j + lane) * kPage, r[0], r[1], r[2], r[3]);
-            if (ragged) { r[0] &= keep; r[1] &= keep; r[2] &= keep; r[3] &= keep; }
-            e4m3x4_to_f16x2x2(r[0], a[0], a[2]);
-            e4m3x4_to_f16x2x2(r[1], a[1], a[3]);
-            e4m3x4_to_f16x2x2(r[2], b[0], b[2]);
-            e4m3x4_to_f16x2x2(r[3], b[1], b[3]);
-            mma_f16(o[2 * j], a, ph0, ph1);
-            mma_f16(o[2 * j + 1], b, ph0, ph1);
+            for (int j = 0; j < D / 32; ++j) {
+              uint32_t r[4], a[4], b[4];
+              ldsm_x4(vb + (32 * j + lane) * kPage, r[0], r[1], r[2], r[3]);
+              if (SH && keep != 0xffffffffu) { r[0] &= keep; r[1] &= keep; r[2] &= keep; r[3] &= keep; }
+              e4m3x4_to_f16x2x2(r[0], a[0], a[2]);
+              e4m3x4_to_f16x2x2(r[1], a[1], a[3]);
+              e4m3x4_to_f16x2x2(r[2], b[0], b[2]);
+              e4m3x4_to_f16x2x2(r[3], b[1], b[3]);
+              mma_f16(o[2 * j], a, ph0, ph1);
+              mma_f16(o[2 * j + 1], b, ph0, ph1);
+            }
+          };
+          if (SH && tok_base + kPage > x.t1) {   // cleared as above; a register holds four keys of a channel, 4t .. 4t + 3
+            const int left = x.t1 - tok_base - 2 * fcol;
+            add_values(left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u);
+          } else {
+            add_values(0xffffffffu);
           }
         }
       }
