@@ -188,7 +188,7 @@ int mixattn_append_kv_rope(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, cons
  * The cap is evaluated to about six fp32 roundings (the fp32 mode: tanhf).  Keys and values of the
  * attended tokens must be finite; what lies behind a sequence's last token does not matter.
  * Errors: INVALID_ARG (layer, a softcap that is neither 0 nor in [MIXATTN_SOFTCAP_MIN,
- * MIXATTN_SOFTCAP_MAX], a slope out of range or NaN), UNSUPPORTED (slopes with more than
+ * MIXATTN_SOFTCAP_MAX] or whose quotient with softmax_scale leaves fp32, a slope out of range or NaN), UNSUPPORTED (slopes with more than
  * MIXATTN_MAX_SLOPE_HEADS query heads).  A call that fails changes nothing. */
 #define MIXATTN_SOFTCAP_MIN 1e-3f
 #define MIXATTN_SOFTCAP_MAX 1e6f
@@ -313,7 +313,9 @@ int mixattn_set_chunk_ring_direct(mixattn_ctx* ctx, int32_t enable);
  * owners (a page is free again when the last sequence that holds it lets go), and gets its own
  * copy of the pages that are not and of the rings.  The overwritten sequences' pages return to
  * the FIFO tail first (in call order, blocks in order); the copies then take theirs from its
- * head, in call order.
+ * head, in call order.  A sequence may thereby move to other storage: work captured into a graph
+ * earlier still refers to the old one, and the bookkeeping of a fork that is itself captured moves
+ * once, at the capture.
  * Errors: BAD_SEQ, INVALID_ARG (null, n < 0, dst not distinct), OUT_OF_PAGES (nothing changed),
  * CUDA. */
 int mixattn_fork_seqs(mixattn_ctx* ctx, int32_t n, const int32_t* src, const int32_t* dst, void* stream);
@@ -349,8 +351,10 @@ int mixattn_read_kv(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32
  * precision; the outputs are rounded to fp32 once.  Uses the context's workspace (one stream at a
  * time, like every call).
  * Errors: INVALID_ARG (null, n_beams outside 1 .. MIXATTN_MAX_BEAMS, n_out outside 1 ..
- * MIXATTN_MAX_BEAM_OUT, vocab < 1 or n_beams * vocab beyond 2^31 - 1, row_stride < vocab, eos_token
- * outside the vocabulary while `finished` is given), CUDA. */
+ * MIXATTN_MAX_BEAM_OUT, vocab outside 1 .. MIXATTN_MAX_VOCAB or n_beams * vocab beyond 2^31 - 1,
+ * row_stride < vocab or so large that 64-bit byte offsets overflow, eos_token outside the vocabulary
+ * while `finished` is given), CUDA. */
+#define MIXATTN_MAX_VOCAB (1 << 30)
 #define MIXATTN_MAX_BEAMS 64
 #define MIXATTN_MAX_BEAM_OUT 64
 int mixattn_beam_select(mixattn_ctx* ctx, int32_t n_groups, int32_t n_beams, int32_t vocab,
@@ -380,7 +384,8 @@ int mixattn_beam_select(mixattn_ctx* ctx, int32_t n_groups, int32_t n_beams, int
  * Arguments, results and errors are those of mixattn_decode, plus:
  *   - n_seqs > 128, or more scratch needed than the array holds
  *     (splits * n_q_heads * (head_dim + 2) * 4 bytes, where a sequence of n
- *     attended keys makes about n / 4096 splits) -> MIXATTN_ERR_TOO_LARGE,
+ *     attended keys makes about n / 4096 splits, up to n / 2048 on a layer with
+ *     shaped scores) -> MIXATTN_ERR_TOO_LARGE,
  *     nothing launched;
  *   - the first call on a device looks up the array's device address (a CUDA
  *     runtime query with that device current); make that first call outside

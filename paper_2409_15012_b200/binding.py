@@ -394,7 +394,7 @@ class Context:
         g, b, v = logits.shape
         o = g * n_out
         for t, dt in ((out_scores, torch.float32), (out_beams, torch.int32), (out_tokens, torch.int32)):
-            if t.dtype is not dt or t.numel() != o or not t.is_contiguous():
+            if t.dtype is not dt or t.numel() != o or not t.is_contiguous() or t.get_device() != self.cfg.device:
                 return ERR_INVALID_ARG
         return self._beam_select(logits, scores, n_out, out_scores.data_ptr(), out_beams.data_ptr(), out_tokens.data_ptr(),
                                  finished, eos_token, stream)
@@ -416,6 +416,9 @@ class Context:
             sb = v
         if (v > 1 and sv != 1) or (g > 1 and sg != b * sb):
             return ERR_INVALID_ARG
+        dev = self.cfg.device
+        if logits.get_device() != dev or scores.get_device() != dev or (finished is not None and finished.get_device() != dev):
+            return ERR_INVALID_ARG               # a tensor of the host or of another device
         if scores.dtype is not torch.float32 or scores.numel() != g * b or not scores.is_contiguous():
             return ERR_INVALID_ARG
         if finished is not None and (finished.dtype is not torch.uint8 or finished.numel() != g * b or

@@ -493,7 +493,9 @@ int mixattn_beam_select(mixattn_ctx* c, int32_t n_groups, int32_t n_beams, int32
       n_out > MIXATTN_MAX_BEAM_OUT || (logits_dtype != MIXATTN_F32 && logits_dtype != MIXATTN_BF16) ||
       row_stride < vocab)
     return MIXATTN_ERR_INVALID_ARG;
-  if ((int64_t)n_beams * vocab > INT32_MAX || (int64_t)n_groups * n_beams > INT32_MAX) return MIXATTN_ERR_INVALID_ARG;
+  if (vocab > MIXATTN_MAX_VOCAB || (int64_t)n_beams * vocab > INT32_MAX || (int64_t)n_groups * n_beams > INT32_MAX)
+    return MIXATTN_ERR_INVALID_ARG;
+  if (row_stride > INT64_MAX / 8 / std::max<int64_t>((int64_t)n_groups * n_beams, 1)) return MIXATTN_ERR_INVALID_ARG;   // byte offsets in 64 bits
   if (finished != nullptr && (eos_token < 0 || eos_token >= vocab)) return MIXATTN_ERR_INVALID_ARG;
   if (c->host_only || c->sticky_cuda_error) return MIXATTN_ERR_CUDA;
   if (n_groups == 0) return MIXATTN_OK;
@@ -1196,6 +1198,7 @@ int mixattn_get_device_status(mixattn_ctx* c, int32_t* status) {
 int mixattn_set_layer_scores(mixattn_ctx* c, int32_t layer, float softcap, const float* slopes) {
   if (c == nullptr || !c->cm.valid_layer(layer)) return MIXATTN_ERR_INVALID_ARG;
   if (!(softcap == 0.f || (softcap >= MIXATTN_SOFTCAP_MIN && softcap <= MIXATTN_SOFTCAP_MAX))) return MIXATTN_ERR_INVALID_ARG;
+  if (softcap > 0.f && !isnormal(c->scale / softcap)) return MIXATTN_ERR_INVALID_ARG;
   const int Hq = c->cfg.n_q_heads;
   if (slopes != nullptr) {
     for (int h = 0; h < Hq; ++h)

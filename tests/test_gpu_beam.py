@@ -141,7 +141,8 @@ def test_refusals_of_the_binding():
     ctx = context(mx)
     x, s = torch.zeros(2, 3, 100, device="cuda"), torch.zeros(2, 3, device="cuda")
     for bad in (dict(logits=x.half()), dict(logits=x.transpose(1, 2)), dict(scores=s.double()), dict(scores=s[:1]),
-                dict(finished=s), dict(logits=x.transpose(0, 1))):
+                dict(finished=s), dict(logits=x.transpose(0, 1)), dict(logits=x.cpu()), dict(scores=s.cpu()),
+                dict(finished=torch.zeros(2, 3, dtype=torch.uint8)), dict(n_out=65), dict(n_out=0)):
         with pytest.raises(mx.MixAttnError):
             ctx.beam_select(**{"logits": x, "scores": s, "n_out": 4, **bad})
     ctx.close()

@@ -118,11 +118,16 @@ def test_decode(shape, dtype, heads, window):
                                  slopes, window)
         kind = {"bf16": "decode", "fp8": "fp8", "f32": "f32"}[dtype]
         check(out[i:i + 1], want, A, top, dtype, d, kind, min(n, window or n), f"len {n}")
+    # plain scores again
+    ctx.set_layer_scores(1)
+    again = torch.empty_like(q)
+    ctx.decode(1, list(range(len(lens))), q, again)
     # layer 0 keeps its plain scores
     ctx.decode(0, list(range(len(lens))), q, out)
     want, A, top = reference(q[9:10].double(), K[9].double(), V[9].double(), torch.tensor([lens[9] - 1], device="cuda"), 0.0,
                              None, window)
     check(out[9:10], want, A, top, dtype, d, {"bf16": "decode", "fp8": "fp8", "f32": "f32"}[dtype], lens[9], "plain layer")
+    assert torch.equal(out, again)
     ctx.close()
 
 
@@ -203,6 +208,25 @@ def test_prompt(shape, dtype, heads, window):
         want, A, top = reference(q[r].double(), k[r].double(), v[r].double(), torch.arange(n, device="cuda"), cap, slopes, window)
         check(out[r], want, A, top, dtype, d, "f32" if dtype == "f32" else "prompt", n, f"len {n}")
         row += n
+    ctx.close()
+
+
+@pytest.mark.parametrize("shape", ["cap", "bias", "both"])
+def test_unaligned_tensors_take_the_exact_kernel(shape):
+    mx, _ = load_lib()
+    cap, biased = SHAPES[shape]
+    hq, hkv, d, n = 4, 2, 64, 90
+    gen = torch.Generator("cuda").manual_seed(8)
+    flat = torch.randn(3, n * hq * d + 8, generator=gen, device="cuda").bfloat16()
+    q, k, v = flat[0, 1:1 + n * hq * d].view(n, hq, d), flat[1, 3:3 + n * hkv * d].view(n, hkv, d), flat[2, 5:5 + n * hkv * d].view(n, hkv, d)
+    ctx = make(mx, "prompt", 33, (hq, hkv, d), "bf16", 1, n)
+    ctx.set_layer_scores(1, cap, slopes_of(hq) if biased else None)
+    out = torch.full((n, hq, d), float("nan"), device="cuda", dtype=torch.bfloat16)
+    ctx.prefill(1, [0], [n], q, k, v, out)      # (a layer that reads a cache: nothing is stored)
+    torch.cuda.synchronize()
+    want, A, top = reference(q.double(), k.double(), v.double(), torch.arange(n, device="cuda"), cap,
+                             slopes_of(hq) if biased else None, 33)
+    check(out, want, A, top, "bf16", d, "f32", n, "unaligned")
     ctx.close()
 
 

@@ -202,6 +202,11 @@ def test_read_kv_refusals():
     assert rc(0, [0], [3], [-1]) == mx.ERR_INVALID_ARG
     assert rc(0, [0], [2147483647], [2147483647]) == mx.ERR_INVALID_ARG
     assert rc(1, [0], [27], [1]) == mx.ERR_INVALID_ARG             # fell out of the window
+    with pytest.raises(mx.MixAttnError):
+        ctx.read_kv(0, [0, 1], [0])
+    assert list(ctx.get_stored(0, [0, 1])) == [33, 0] and list(ctx.get_stored(1, [0, 1])) == [5, 0]
+    with pytest.raises(mx.MixAttnError):
+        ctx.get_stored(0, [2])
     assert rc(1, [0], [28], [5]) == mx.ERR_CUDA                    # in order, but there is no device
     assert rc(0, [0], None, None) == mx.ERR_CUDA
     ctx.close()
@@ -220,6 +225,9 @@ def test_layer_scores_refusals():
     assert ctx.rc_set_layer_scores(1, 30.0, [0.0, 0.5, 1.0, 1024.0]) == 0
     assert ctx.rc_set_layer_scores(1) == 0
     ctx.close()
+    steep = mx.Context([(0, 0, 0)], 4, 2, 64, mx.F32, 1, 10, device=-1, softmax_scale=3e38)
+    assert steep.rc_set_layer_scores(0, 1e-3) == mx.ERR_INVALID_ARG
+    steep.close()
     wide = mx.Context([(0, 0, 0)], 130, 2, 64, mx.F32, 1, 10, device=-1)
     assert wide.rc_set_layer_scores(0, 0.0, [0.5] * 130) == mx.ERR_UNSUPPORTED
     assert wide.rc_set_layer_scores(0, 50.0) == 0                   # a cap alone has no such limit
@@ -236,7 +244,7 @@ def test_beam_select_refusals():
 
     for kw in (dict(groups=-1), dict(beams=0), dict(beams=65), dict(vocab=0), dict(n_out=0), dict(n_out=65), dict(dtype=2),
                dict(stride=99), dict(vocab=2 ** 31 - 1, stride=2 ** 31), dict(finished=p, eos=100), dict(finished=p, eos=-1),
-               dict(groups=2 ** 31 - 1, beams=2)):
+               dict(groups=2 ** 31 - 1, beams=2), dict(stride=2 ** 62), dict(vocab=2 ** 30 + 1, stride=2 ** 31, beams=1)):
         assert rc(**kw) == mx.ERR_INVALID_ARG, kw
     assert rc() == mx.ERR_CUDA                # in order, but there is no device
     assert rc(finished=p, eos=99) == mx.ERR_CUDA
