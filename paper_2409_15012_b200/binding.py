@@ -342,7 +342,8 @@ class Context:
 
     def fork_seqs(self, src, dst, stream=None):
         """Every sequence dst[i] becomes a copy of what src[i] was before the call (all at once)."""
-        rc = self.rc_fork_seqs(src, dst, stream)
+        (s, n), (d, m) = _ints(src), _ints(dst)
+        rc = lib.mixattn_fork_seqs(self.h, n, s, d, _stream(stream)) if n == m else ERR_INVALID_ARG
         if rc:
             raise MixAttnError(rc, "mixattn_fork_seqs")
 
@@ -367,7 +368,8 @@ class Context:
                 raise MixAttnError(rc, "mixattn_read_kv")
             rows = sum(stored) if m else 0
         kv = torch.empty((2, rows, self.n_kv_heads, self.head_dim),
-                         dtype=torch.bfloat16 if self.dtype == BF16 else torch.float32, device=self._device())
+                         dtype=torch.bfloat16 if self.dtype == BF16 else torch.float32,
+                         device="cpu" if self.arena is None else self.arena.device)
         k, v = kv.unbind(0)
         at = kv.data_ptr()
         rc = lib.mixattn_read_kv(self.h, layer, m, s, p, n, at, at + kv.nbytes // 2, _stream(stream))
@@ -383,9 +385,6 @@ class Context:
         if rc:
             raise MixAttnError(rc, "mixattn_get_stored")
         return out[:n]
-
-    def _device(self):
-        return "cpu" if self.arena is None else self.arena.device
 
     def rc_beam_select(self, logits, scores, n_out, out_scores, out_beams, out_tokens, finished=None, eos_token=0,
                        stream=None) -> int:
