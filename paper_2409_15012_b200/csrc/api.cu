@@ -413,14 +413,18 @@ int mixattn_fork_seqs(mixattn_ctx* c, int32_t n, const int32_t* src, const int32
     int rc = c->cm.check_fork(n, src, dst);
     if (rc != MIXATTN_OK) return rc;
     if (!c->host_only && c->sticky_cuda_error) return MIXATTN_ERR_CUDA;
-    DeviceGuard g(c->host_only ? -1 : c->device);
-    if (!c->host_only && !g.ok) return MIXATTN_ERR_CUDA;
     std::vector<ForkCopy> copies;
     moved = true;
     rc = c->cm.apply_fork(n, src, dst, &copies);
     if (rc != MIXATTN_OK) return rc;
     ++c->cache_epoch;
-    return c->host_only ? MIXATTN_OK : enqueue_fork(c, copies, static_cast<cudaStream_t>(stream));
+    if (c->host_only || copies.empty()) return MIXATTN_OK;
+    DeviceGuard g(c->device);
+    if (!g.ok) {
+      c->sticky_cuda_error = true;   // the bookkeeping has moved
+      return MIXATTN_ERR_CUDA;
+    }
+    return enqueue_fork(c, copies, static_cast<cudaStream_t>(stream));
   } catch (const std::bad_alloc&) {   // no host memory: the bookkeeping may have moved, so the context is done
     if (moved) c->sticky_cuda_error = true;
     return MIXATTN_ERR_CUDA;
@@ -1205,10 +1209,14 @@ int mixattn_set_layer_scores(mixattn_ctx* c, int32_t layer, float softcap, const
       if (!(slopes[h] >= 0.f && slopes[h] <= MIXATTN_SLOPE_MAX)) return MIXATTN_ERR_INVALID_ARG;
     if (Hq > kMaxSlopeHeads) return MIXATTN_ERR_UNSUPPORTED;
   }
-  LayerScores ls;
-  ls.softcap = softcap;
-  if (slopes != nullptr) ls.slopes.assign(slopes, slopes + Hq);
-  c->scores[layer] = std::move(ls);
+  try {
+    LayerScores ls;
+    ls.softcap = softcap;
+    if (slopes != nullptr) ls.slopes.assign(slopes, slopes + Hq);
+    c->scores[layer] = std::move(ls);
+  } catch (const std::bad_alloc&) {
+    return MIXATTN_ERR_INVALID_ARG;   // (as mixattn_create without host memory)
+  }
   return MIXATTN_OK;
 }
 

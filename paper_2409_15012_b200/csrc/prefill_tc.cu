@@ -595,7 +595,6 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       uint32_t sv[64];
       float slope = 0.f;                  // kShape: of this head, base-2 units per token
       if constexpr (kShape & 2) slope = p.shape.slope[w.h];
-      const float scale = kShape ? 1.f : p.scale_log2e;
       // weight of a score: 2^(score - reference)
       auto weight = [&](uint32_t sc, float neg_m) {
         if constexpr (kShape) return ex2_approx(__uint_as_float(sc));   // (shaped scores have it subtracted already)
@@ -695,9 +694,11 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               }
             }
           };
-          // probe the next tile's scores now; the answer is read after the exponentials
+          // the next tile's scores are probed before the exponentials, the answer is read after them
+          // (early or right before them as measured: 8k causal prompts, plain scores 502 / 545 us, biased 581 / 568)
           const bool more = j + 1 < w.n_tiles;
-          const bool next_ready = more && mbar_test_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1);
+          bool next_ready = false;
+          if constexpr (kShape != 2) next_ready = more && mbar_test_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1);
           float sum0 = 0.f, sum1 = 0.f;
           uint32_t pk[32], pl[32];   // P as bf16 pairs; pl = rounding residuals (only on w.lo items)
           // Capped scores of a tile that no band edge crosses, for rows that all have their reference:
@@ -750,7 +751,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               mx0 = fmax3(mx0, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
               mx1 = fmax3(mx1, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
             }
-            if (fresh) m_ref = fmaxf(mx0, mx1) * scale;
+            if (fresh) m_ref = kShape ? fmaxf(mx0, mx1) : fmaxf(mx0, mx1) * p.scale_log2e;
             if constexpr (kShape != 0) {   // fresh rows' scores stand without a reference so far
               const float sub = fresh && m_ref > -INFINITY ? m_ref : 0.f;
 #pragma unroll
@@ -758,6 +759,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
           }
           float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;   // no visible key yet: weights 0, no NaN
+          if constexpr (kShape == 2) next_ready = more && mbar_test_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1);
           if constexpr (!kLo && kShape != 0) {
             f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
   #pragma unroll
@@ -814,7 +816,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               mxa = fmax3(mxa, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
               mxb = fmax3(mxb, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
             }
-            const float mt = fmaxf(mxa, mxb) * scale;
+            const float mt = kShape ? fmaxf(mxa, mxb) : fmaxf(mxa, mxb) * p.scale_log2e;
             const bool far = mt > m_ref + kMaxLead;
             const float alpha = far ? ex2_approx(m_ref - mt) : 1.f;
             if (j > 0) {   // the O row holds earlier tiles: rescale it once this stream's previous P V has landed
