@@ -125,6 +125,18 @@ EXPORTS = [
 ]
 
 
+_torch = None
+
+
+def _get_torch():
+    """torch, imported on first use (host-only contexts never need it)."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 class MixAttnError(RuntimeError):
     def __init__(self, code: int, where: str):
         super().__init__(f"{where}: {lib.mixattn_strerror(code).decode()} ({code})")
@@ -214,8 +226,10 @@ class Context:
                                            n_pages, max_seq_len, free_order, softmax_scale, device,
                                            chunk_scratch_tokens=chunk_scratch_tokens, kv_format=kv_format)
         self.arena = None
+        self._like = None      # what tensors of cached rows are allocated with
         if device >= 0:
-            import torch
+            torch = _get_torch()
+            self._like = {"dtype": torch.bfloat16 if dtype == BF16 else torch.float32, "device": torch.device("cuda", device)}
             nbytes = arena_bytes(self.cfg)
             self.arena = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{device}")
             self.cfg.arena = self.arena.data_ptr()
@@ -350,7 +364,6 @@ class Context:
     def read_kv(self, layer, seq_ids, first_pos=None, n_tokens=None, stream=None):
         """Returns (K, V), the cached tokens [sum n_tokens, Hkv, D] of the sequences, oldest first
         (default: everything stored).  The tensors are allocated on torch's current stream."""
-        import torch
         s, m = _ints(seq_ids)
         p = n = None
         if first_pos is not None or n_tokens is not None:
@@ -367,15 +380,16 @@ class Context:
             if rc:
                 raise MixAttnError(rc, "mixattn_read_kv")
             rows = sum(stored) if m else 0
-        kv = torch.empty((2, rows, self.n_kv_heads, self.head_dim),
-                         dtype=torch.bfloat16 if self.dtype == BF16 else torch.float32,
-                         device="cpu" if self.arena is None else self.arena.device)
-        k, v = kv.unbind(0)
+        if self._like is None:
+            raise MixAttnError(ERR_CUDA, "mixattn_read_kv")
+        hkv, d = self.n_kv_heads, self.head_dim
+        kv = _torch.empty((2, rows, hkv, d), **self._like)
         at = kv.data_ptr()
-        rc = lib.mixattn_read_kv(self.h, layer, m, s, p, n, at, at + kv.nbytes // 2, _stream(stream))
+        rc = lib.mixattn_read_kv(self.h, layer, m, s, p, n, at, at + rows * hkv * d * (2 if self.dtype == BF16 else 4),
+                                 _stream(stream))
         if rc:
             raise MixAttnError(rc, "mixattn_read_kv")
-        return k, v
+        return kv.unbind(0)
 
     def get_stored(self, layer, seq_ids):
         """Tokens the layer's cache holds of each sequence: its length, or at most the window."""
@@ -389,9 +403,8 @@ class Context:
     def rc_beam_select(self, logits, scores, n_out, out_scores, out_beams, out_tokens, finished=None, eos_token=0,
                        stream=None) -> int:
         """logits [groups, beams, vocab] (fp32 or bf16, last dimension dense, rows evenly spaced)."""
-        import torch
-        g, b, v = logits.shape
-        o = g * n_out
+        torch = _get_torch()
+        o = logits.shape[0] * n_out
         for t, dt in ((out_scores, torch.float32), (out_beams, torch.int32), (out_tokens, torch.int32)):
             if t.dtype is not dt or t.numel() != o or not t.is_contiguous() or t.get_device() != self.cfg.device:
                 return ERR_INVALID_ARG
@@ -399,7 +412,7 @@ class Context:
                                  finished, eos_token, stream)
 
     def _beam_select(self, logits, scores, n_out, out_scores, out_beams, out_tokens, finished, eos_token, stream) -> int:
-        import torch
+        torch = _get_torch()
         g, b, v = logits.shape
         sg, sb, sv = logits.stride()
         dt = logits.dtype
@@ -429,14 +442,14 @@ class Context:
     def beam_select(self, logits, scores, n_out, finished=None, eos_token=0, stream=None):
         """The n_out best continuations of every group: (scores fp32, beams int32, tokens int32),
         [groups, n_out] each, allocated on torch's current stream."""
-        import torch
+        torch = _get_torch()
         g = logits.shape[0]
         out = torch.empty((3, g, n_out), dtype=torch.int32, device=logits.device)
-        s, b, t = out.unbind(0)
         at, step = out.data_ptr(), 4 * g * n_out
         rc = self._beam_select(logits, scores, n_out, at, at + step, at + 2 * step, finished, eos_token, stream)
         if rc:
             raise MixAttnError(rc, "mixattn_beam_select")
+        s, b, t = out.unbind(0)      # (while the kernel runs)
         return s.view(torch.float32), b, t
 
     def seq_reset(self, seq):

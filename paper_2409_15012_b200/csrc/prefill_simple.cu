@@ -31,11 +31,12 @@ struct Plain {};   // plain scores: no further parameters
 template <typename T, int D, typename SH>
 __global__ void __launch_bounds__(kThreads)
 prefill_simple_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ SH shape) {
-  extern __shared__ float sm[];
-  float* Qs = sm;                      // [kBM][D + 1]
-  float* Ks = Qs + kBM * (D + 1);      // [kBN][D + 1]
-  float* Vs = Ks + kBN * (D + 1);      // [kBN][D]
-  float* Ps = Vs + kBN * D;            // [kBM][kBN + 1]
+  constexpr int kRow = D + 4;          // row pitch: 16-byte aligned, and eight rows apart fall on different banks
+  extern __shared__ __align__(16) float sm[];
+  float* Qs = sm;                      // [kBM][kRow]
+  float* Ks = Qs + kBM * kRow;         // [kBN][kRow]
+  float* Vs = Ks + kBN * kRow;         // [kBN][D]
+  float* Ps = Vs + kBN * D;            // [kBM][kBN + 4]
 
   const int b = blockIdx.z, h = blockIdx.y;
   const int S = p.row0[b + 1] - p.row0[b];
@@ -51,7 +52,7 @@ prefill_simple_kernel(const __grid_constant__ PrefillParams p, const __grid_cons
 
   for (int e = tid; e < kBM * D; e += kThreads) {
     const int rr = e / D, d = e - rr * D;
-    Qs[rr * (D + 1) + d] = i0 + rr < S ? to_f32(q[((base + i0 + rr) * p.n_q_heads + h) * D + d]) : 0.f;
+    Qs[rr * kRow + d] = i0 + rr < S ? to_f32(q[((base + i0 + rr) * p.n_q_heads + h) * D + d]) : 0.f;
   }
   float o[D / 4];
 #pragma unroll
@@ -64,22 +65,41 @@ prefill_simple_kernel(const __grid_constant__ PrefillParams p, const __grid_cons
   const int i_last = P + min(S, i0 + kBM) - 1;
   int j_lo = 0;
   if (p.window > 0) j_lo = max(0, P + i0 - p.window + 1) / kBN * kBN;
+  // this thread loads channel ld of every kThreads / D-th row of a tile
+  constexpr int kStep = kThreads / D, kPer = kBN / kStep;
+  const int ld = tid % D, lj = tid / D;
+  const int64_t pitch = (int64_t)p.n_kv_heads * D;
+  const T* kp = k + (kbase + lj) * pitch + g * D + ld;
+  const T* vp = v + (kbase + lj) * pitch + g * D + ld;
   for (int j0 = j_lo; j0 <= i_last; j0 += kBN) {
     __syncthreads();
-    for (int e = tid; e < kBN * D; e += kThreads) {
-      const int jj = e / D, d = e - jj * D;
+#pragma unroll 8
+    for (int e = 0; e < kPer; ++e) {
+      const int jj = lj + e * kStep;
       const bool in = j0 + jj < n_keys;
-      Ks[jj * (D + 1) + d] = in ? to_f32(k[((kbase + j0 + jj) * p.n_kv_heads + g) * D + d]) : 0.f;
-      Vs[jj * D + d] = in ? to_f32(v[((kbase + j0 + jj) * p.n_kv_heads + g) * D + d]) : 0.f;
+      const int64_t at = (int64_t)(j0 + e * kStep) * pitch;
+      Ks[jj * kRow + ld] = in ? to_f32(kp[at]) : 0.f;
+      Vs[jj * D + ld] = in ? to_f32(vp[at]) : 0.f;
     }
     __syncthreads();
+    // (the eight sums of a thread advance together, four channels per load; each adds its channels in order)
     float s[kBN / 4];
     float mx = -INFINITY;
 #pragma unroll
+    for (int jj = 0; jj < kBN / 4; ++jj) s[jj] = 0.f;
+#pragma unroll 4
+    for (int d = 0; d < D; d += 4) {
+      const float4 a = *reinterpret_cast<const float4*>(Qs + r * kRow + d);
+#pragma unroll
+      for (int jj = 0; jj < kBN / 4; ++jj) {
+        const float4 b = *reinterpret_cast<const float4*>(Ks + (c + 4 * jj) * kRow + d);
+        s[jj] = fmaf(a.w, b.w, fmaf(a.z, b.z, fmaf(a.y, b.y, fmaf(a.x, b.x, s[jj]))));
+      }
+    }
+#pragma unroll
     for (int jj = 0; jj < kBN / 4; ++jj) {
       const int j = j0 + c + 4 * jj;
-      float acc = 0.f;
-      for (int d = 0; d < D; ++d) acc = fmaf(Qs[r * (D + 1) + d], Ks[(c + 4 * jj) * (D + 1) + d], acc);
+      const float acc = s[jj];
       const bool seen = j <= i && row_ok && (p.window == 0 || i - j < p.window);
       if constexpr (std::is_same_v<SH, ScoreShape>)
         s[jj] = seen ? shaped_score_exact(acc, shape, shape.biased ? -shape.slope[h] * (float)(i - j) : 0.f) : -INFINITY;
@@ -96,7 +116,7 @@ prefill_simple_kernel(const __grid_constant__ PrefillParams p, const __grid_cons
 #pragma unroll
     for (int jj = 0; jj < kBN / 4; ++jj) {
       const float pe = mn == -INFINITY ? 0.f : exp2f(s[jj] - mn);
-      Ps[r * (kBN + 1) + c + 4 * jj] = pe;
+      Ps[r * (kBN + 4) + c + 4 * jj] = pe;
       sum += pe;
     }
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
@@ -106,23 +126,30 @@ prefill_simple_kernel(const __grid_constant__ PrefillParams p, const __grid_cons
     __syncwarp();
 #pragma unroll
     for (int e = 0; e < D / 4; ++e) o[e] *= a;
+    // this thread's channels: groups of four, c, c + 4, c + 8, ...
     for (int jj = 0; jj < kBN; ++jj) {
-      const float pe = Ps[r * (kBN + 1) + jj];
+      const float pe = Ps[r * (kBN + 4) + jj];
 #pragma unroll
-      for (int e = 0; e < D / 4; ++e) o[e] = fmaf(pe, Vs[jj * D + c + 4 * e], o[e]);
+      for (int e = 0; e < D / 4; e += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(Vs + jj * D + 4 * c + 4 * e);
+        o[e] = fmaf(pe, x.x, o[e]);
+        o[e + 1] = fmaf(pe, x.y, o[e + 1]);
+        o[e + 2] = fmaf(pe, x.z, o[e + 2]);
+        o[e + 3] = fmaf(pe, x.w, o[e + 3]);
+      }
     }
   }
   if (row_ok) {
     T* out = reinterpret_cast<T*>(p.out) + ((base + i0 + r) * p.n_q_heads + h) * D;
     const float inv = 1.f / l;
 #pragma unroll
-    for (int e = 0; e < D / 4; ++e) store_out(out + c + 4 * e, o[e] * inv);
+    for (int e = 0; e < D / 4; ++e) store_out(out + 4 * c + 16 * (e / 4) + e % 4, o[e] * inv);
   }
 }
 
 template <typename T, int D, typename SH>
 cudaError_t launch(const PrefillParams& p, const SH& shape, int max_len, cudaStream_t st) {
-  const size_t smem = (size_t)(kBM * (D + 1) + kBN * (D + 1) + kBN * D + kBM * (kBN + 1)) * 4;
+  const size_t smem = (size_t)((kBM + kBN) * (D + 4) + kBN * D + kBM * (kBN + 4)) * 4;
   cudaError_t e = cudaFuncSetAttribute(prefill_simple_kernel<T, D, SH>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
