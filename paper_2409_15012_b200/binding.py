@@ -226,12 +226,12 @@ class Context:
                                            n_pages, max_seq_len, free_order, softmax_scale, device,
                                            chunk_scratch_tokens=chunk_scratch_tokens, kv_format=kv_format)
         self.arena = None
-        self._like = None      # what tensors of cached rows are allocated with
+        self._like = None      # an empty tensor that tensors of cached rows are allocated like
         if device >= 0:
             torch = _get_torch()
-            self._like = {"dtype": torch.bfloat16 if dtype == BF16 else torch.float32, "device": torch.device("cuda", device)}
             nbytes = arena_bytes(self.cfg)
             self.arena = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{device}")
+            self._like = torch.empty(0, dtype=torch.bfloat16 if dtype == BF16 else torch.float32, device=self.arena.device)
             self.cfg.arena = self.arena.data_ptr()
             self.cfg.arena_bytes = nbytes
         h = C.c_void_p()
@@ -383,7 +383,7 @@ class Context:
         if self._like is None:
             raise MixAttnError(ERR_CUDA, "mixattn_read_kv")
         hkv, d = self.n_kv_heads, self.head_dim
-        kv = _torch.empty((2, rows, hkv, d), **self._like)
+        kv = self._like.new_empty((2, rows, hkv, d))
         at = kv.data_ptr()
         rc = lib.mixattn_read_kv(self.h, layer, m, s, p, n, at, at + rows * hkv * d * (2 if self.dtype == BF16 else 4),
                                  _stream(stream))

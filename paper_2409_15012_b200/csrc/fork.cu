@@ -17,6 +17,7 @@ constexpr int kReadVecs = 2;                          // (32 copies of 4103 toke
 constexpr int kBlock16 = kThreads * kUnroll;          // 16-byte units per block: 32 KB
 
 __global__ void __launch_bounds__(kThreads) fork_copy_kernel(const __grid_constant__ ForkParams p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // a read that follows may get ready
   const int y = blockIdx.y;
   if (y < p.n_segs) {
     const CopySeg& s = p.seg[y];
@@ -47,6 +48,9 @@ __global__ void __launch_bounds__(kThreads) fork_copy_kernel(const __grid_consta
 // copies share once for all of them, in one block, was slower, 195 us against 184 for the fork and
 // the read back of the case below: the rows written bound it, not the pages read.)
 __global__ void __launch_bounds__(kThreads, 8) read_kv_kernel(const __grid_constant__ GatherParams p) {
+  // (launched while the kernel ahead in the stream still runs; nothing is read before that one is done)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const GatherEntry& e = p.e[blockIdx.y];
   const KvGeom& ge = p.geom;
   const int chunks = ge.row_bytes / 16;                // 8, 16 or 32
@@ -102,8 +106,16 @@ cudaError_t launch_read_kv(const GatherParams& p, int max_rows, cudaStream_t st)
   const int64_t per_block = (int64_t)kThreads / (p.geom.row_bytes / 16) * kReadVecs;
   const int64_t blocks = ((int64_t)max_rows * p.geom.n_kv_heads + per_block - 1) / per_block;
   if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
-  read_kv_kernel<<<dim3((unsigned)blocks, p.n_entries), kThreads, 0, st>>>(p);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks, p.n_entries);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, read_kv_kernel, p);
 }
 
 }  // namespace mixattn
