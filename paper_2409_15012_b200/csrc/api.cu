@@ -350,7 +350,7 @@ int mixattn_seq_reset(mixattn_ctx* c, int32_t seq) {
 }
 
 // Device side of the copies a fork made (see CacheManager::apply_fork).
-static int enqueue_fork(mixattn_ctx* c, const std::vector<ForkCopy>& copies, cudaStream_t st) {
+static int enqueue_fork(mixattn_ctx* c, const ForkPlan& plan, cudaStream_t st) {
   ForkParams p;
   p.arena = c->arena;
   p.table = c->dev_table();
@@ -363,20 +363,22 @@ static int enqueue_fork(mixattn_ctx* c, const std::vector<ForkCopy>& copies, cud
     return e;
   };
   auto add_seg = [&](size_t src, size_t dst, int64_t bytes) {
-    cudaError_t e = p.n_segs == kForkSegs ? flush() : cudaSuccess;
+    cudaError_t e = p.n_segs == ForkParams::kMaxSegs ? flush() : cudaSuccess;
     p.seg[p.n_segs++] = CopySeg{(int64_t)src, (int64_t)dst, (uint32_t)(bytes / 16)};
     return e;
   };
   const int64_t page_bytes = c->geom.page_bytes;
   // a segment's length is counted in 32 bits of 16-byte units; rings longer than that are cut
   const int64_t max_bytes = (int64_t)1 << 34;
-  for (const ForkCopy& f : copies) {
+  for (const ForkCopy& f : plan.copies) {
+    const int32_t* src_pages = plan.src_pages.data() + f.tail0;
+    const int32_t* dst_pages = plan.dst_pages.data() + f.tail0;
     for (size_t o = 0; o < c->cm.owners().size(); ++o) {
       const LayerInfo& li = c->cm.layer(c->cm.owners()[o]);
       const size_t pool = c->plan.owner_off[o];
       if (li.kind == MIXATTN_FULL) {
-        for (size_t b = 0; b < f.src_pages.size(); ++b)
-          if (add_seg(pool + (size_t)f.src_pages[b] * page_bytes, pool + (size_t)f.dst_pages[b] * page_bytes, page_bytes) != cudaSuccess)
+        for (int b = 0; b < f.n_tail; ++b)
+          if (add_seg(pool + (size_t)src_pages[b] * page_bytes, pool + (size_t)dst_pages[b] * page_bytes, page_bytes) != cudaSuccess)
             return MIXATTN_ERR_CUDA;
         continue;
       }
@@ -387,19 +389,19 @@ static int enqueue_fork(mixattn_ctx* c, const std::vector<ForkCopy>& copies, cud
         if (add_seg(pool + f.src_slot * ring + a, pool + f.dst_slot * ring + a, std::min(max_bytes, bytes - a)) != cudaSuccess)
           return MIXATTN_ERR_CUDA;
     }
-    int32_t set0 = f.n_shared, left = (int32_t)f.dst_pages.size();
-    bool first = true;
-    while ((first && f.n_shared > 0) || left > 0) {
-      if (p.n_rows == kForkRows && flush() != cudaSuccess) return MIXATTN_ERR_CUDA;
+    int32_t done = 0;
+    bool first = f.n_shared > f.same;
+    while (first || done < f.n_tail) {
+      if (p.n_rows == ForkParams::kMaxRows && flush() != cudaSuccess) return MIXATTN_ERR_CUDA;
       TableRow& r = p.row[p.n_rows++];
       r.src_slot = f.src_slot;
       r.dst_slot = f.dst_slot;
-      r.n_copy = first ? f.n_shared : 0;
-      r.set0 = set0;
-      r.n_set = left < kRowPages ? left : kRowPages;
-      for (int i = 0; i < r.n_set; ++i) r.page[i] = f.dst_pages[f.dst_pages.size() - left + i];
-      set0 += r.n_set;
-      left -= r.n_set;
+      r.copy0 = f.same;
+      r.n_copy = first ? f.n_shared - f.same : 0;
+      r.set0 = f.n_shared + done;
+      r.n_set = std::min(f.n_tail - done, kRowPages);
+      for (int i = 0; i < r.n_set; ++i) r.page[i] = dst_pages[done + i];
+      done += r.n_set;
       first = false;
     }
   }
@@ -413,18 +415,18 @@ int mixattn_fork_seqs(mixattn_ctx* c, int32_t n, const int32_t* src, const int32
     int rc = c->cm.check_fork(n, src, dst);
     if (rc != MIXATTN_OK) return rc;
     if (!c->host_only && c->sticky_cuda_error) return MIXATTN_ERR_CUDA;
-    std::vector<ForkCopy> copies;
+    ForkPlan plan;
     moved = true;
-    rc = c->cm.apply_fork(n, src, dst, &copies);
+    rc = c->cm.apply_fork(n, src, dst, &plan);
     if (rc != MIXATTN_OK) return rc;
     ++c->cache_epoch;
-    if (c->host_only || copies.empty()) return MIXATTN_OK;
+    if (c->host_only || plan.copies.empty()) return MIXATTN_OK;
     DeviceGuard g(c->device);
     if (!g.ok) {
       c->sticky_cuda_error = true;   // the bookkeeping has moved
       return MIXATTN_ERR_CUDA;
     }
-    return enqueue_fork(c, copies, static_cast<cudaStream_t>(stream));
+    return enqueue_fork(c, plan, static_cast<cudaStream_t>(stream));
   } catch (const std::bad_alloc&) {   // no host memory: the bookkeeping may have moved, so the context is done
     if (moved) c->sticky_cuda_error = true;
     return MIXATTN_ERR_CUDA;

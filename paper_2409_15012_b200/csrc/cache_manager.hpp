@@ -8,8 +8,8 @@
 
 #include <stdint.h>
 
+#include <algorithm>
 #include <deque>
-#include <utility>
 #include <vector>
 
 #include "mixattn.h"
@@ -31,11 +31,17 @@ struct PageGrant {     // a block-table entry set during an append
 
 // What a fork has to move on the device for one copy that could not simply take over its
 // source's slot.  Blocks [0, n_shared) of the source's block table are shared (their pages gain
-// a reference); the blocks from n_shared on, which an append may still write to, are copied.
+// a reference); of those, the first `same` were in the slot's row already (copies of one prompt
+// mostly differ in their last pages).  The blocks from n_shared on, which an append may still
+// write to, are copied: pages tail0 .. tail0 + n_tail - 1 of the plan.
 struct ForkCopy {
   int32_t src_slot, dst_slot;
-  int32_t n_shared;
-  std::vector<int32_t> src_pages, dst_pages;   // blocks n_shared .. of the source and of the copy
+  int32_t same, n_shared;
+  int32_t tail0, n_tail;
+};
+struct ForkPlan {
+  std::vector<ForkCopy> copies;
+  std::vector<int32_t> src_pages, dst_pages;
 };
 
 class CacheManager {
@@ -207,7 +213,7 @@ class CacheManager {
   // rest.  Order of the page movements: the overwritten sequences' pages return to the FIFO
   // tail in call order, then the copies take theirs from its head in call order.
   // Returns MIXATTN_OK, or OUT_OF_PAGES with nothing changed.
-  int apply_fork(int n, const int32_t* src, const int32_t* dst, std::vector<ForkCopy>* copies) {
+  int apply_fork(int n, const int32_t* src, const int32_t* dst, ForkPlan* plan) {
     std::vector<int32_t> from(n), to(n, -1);              // slots before and after, per entry
     std::vector<char> held(max_seqs_, 0);                 // slots that keep their contents
     std::vector<char> overwritten(max_seqs_, 0);          // sequences the call replaces
@@ -225,8 +231,8 @@ class CacheManager {
         held[from[i]] = 1;
         to[i] = from[i];
       }
-    // slots whose contents die, in call order, and the copies that move in: a copy stays in the
-    // slot its sequence had where it can
+    // slots whose contents die, in call order, and the copies that move in (one each): a copy stays
+    // in the slot its sequence had where it can
     std::vector<int32_t> dead;
     for (int i = 0; i < n; ++i)
       if (!held[slot_[dst[i]]]) dead.push_back(slot_[dst[i]]);
@@ -242,45 +248,57 @@ class CacheManager {
         while (taken[dead[at]]) ++at;
         to[i] = dead[at++];
       }
-    // shared pages gain their references before the dead slots lose theirs; the pages needed are
-    // counted first, so that a call that cannot be served changes nothing
     auto row = [&](int slot) { return &table_[(size_t)slot * max_blocks_]; };
-    int64_t need = 0, freed = 0;
-    for (int i = 0; i < n; ++i)
-      if (to[i] != from[i]) {
-        const int shared = n_shared(from[i]);
-        need += n_blocks_[from[i]] - shared;
-        for (int b = 0; b < shared; ++b) ++refs_[row(from[i])[b]];
-      }
-    for (int s : dead)
-      for (int b = 0; b < n_blocks_[s]; ++b) freed += --refs_[row(s)[b]] == 0;
-    for (int s : dead)                                    // (back as they were: release_slot does it for good)
-      for (int b = 0; b < n_blocks_[s]; ++b) ++refs_[row(s)[b]];
-    if (need > (int64_t)free_.size() + freed) {
-      for (int i = 0; i < n; ++i)
-        if (to[i] != from[i])
-          for (int b = 0; b < n_shared(from[i]); ++b) --refs_[row(from[i])[b]];
-      return MIXATTN_ERR_OUT_OF_PAGES;
-    }
-    for (int s : dead) release_slot(s);
+    std::vector<int32_t> same(dead.empty() ? 0 : max_seqs_, 0);   // per dead slot
+    size_t n_tails = 0;
+    plan->copies.reserve(dead.size());
     for (int i = 0; i < n; ++i) {
       if (to[i] == from[i]) continue;
       ForkCopy c;
       c.src_slot = from[i];
       c.dst_slot = to[i];
       c.n_shared = n_shared(from[i]);
-      for (int b = 0; b < n_blocks_[from[i]]; ++b) {
-        int32_t pg = row(from[i])[b];
-        if (b >= c.n_shared) {
-          c.src_pages.push_back(pg);
-          pg = take_page();
-          c.dst_pages.push_back(pg);
-        }
-        row(to[i])[b] = pg;
+      const int most = c.n_shared < n_blocks_[to[i]] ? c.n_shared : n_blocks_[to[i]];
+      c.same = (int32_t)(std::mismatch(row(from[i]), row(from[i]) + most, row(to[i])).first - row(from[i]));
+      c.n_tail = n_blocks_[from[i]] - c.n_shared;
+      c.tail0 = (int32_t)n_tails;
+      n_tails += c.n_tail;
+      same[to[i]] = c.same;
+      plan->copies.push_back(c);
+    }
+    plan->src_pages.reserve(n_tails);
+    plan->dst_pages.reserve(n_tails);
+    // Shared pages gain their references before the dead slots lose theirs (a page both hold keeps
+    // its count).  Only where the FIFO is short are the pages the dead slots free counted first, so
+    // that a call that cannot be served changes nothing.
+    auto share = [&](int by) {
+      for (const ForkCopy& c : plan->copies)
+        for (int b = c.same; b < c.n_shared; ++b) refs_[row(c.src_slot)[b]] += by;
+    };
+    share(1);
+    if (n_tails > free_.size()) {
+      size_t freed = 0;
+      for (int s : dead)
+        for (int b = same[s]; b < n_blocks_[s]; ++b) freed += --refs_[row(s)[b]] == 0;
+      for (int s : dead)
+        for (int b = same[s]; b < n_blocks_[s]; ++b) ++refs_[row(s)[b]];
+      if (n_tails > free_.size() + freed) {
+        share(-1);
+        plan->copies.clear();
+        return MIXATTN_ERR_OUT_OF_PAGES;
       }
-      n_blocks_[to[i]] = n_blocks_[from[i]];
-      for (size_t o = 0; o < owners_.size(); ++o) len_[o * max_seqs_ + to[i]] = len_[o * max_seqs_ + from[i]];
-      copies->push_back(std::move(c));
+    }
+    for (int s : dead) release_slot(s, same[s]);
+    for (const ForkCopy& c : plan->copies) {
+      int32_t* to_row = row(c.dst_slot);
+      const int32_t* from_row = row(c.src_slot);
+      std::copy(from_row + c.same, from_row + c.n_shared, to_row + c.same);
+      for (int b = c.n_shared; b < c.n_shared + c.n_tail; ++b) {
+        plan->src_pages.push_back(from_row[b]);
+        plan->dst_pages.push_back(to_row[b] = take_page());
+      }
+      n_blocks_[c.dst_slot] = c.n_shared + c.n_tail;
+      for (size_t o = 0; o < owners_.size(); ++o) len_[o * max_seqs_ + c.dst_slot] = len_[o * max_seqs_ + c.src_slot];
     }
     for (int i = 0; i < n; ++i) slot_[dst[i]] = to[i];
     return MIXATTN_OK;
@@ -319,15 +337,15 @@ class CacheManager {
     refs_[pg] = 1;
     return pg;
   }
-  // Empties a slot; a page returns to the FIFO tail when its last reference goes.
-  void release_slot(int slot) {
+  // Empties a slot from block `first` on; a page returns to the FIFO tail when its last reference goes.
+  void release_slot(int slot, int first = 0) {
     for (size_t o = 0; o < owners_.size(); ++o) len_[o * max_seqs_ + slot] = 0;
     int32_t* row = &table_[(size_t)slot * max_blocks_];
-    for (int b = 0; b < n_blocks_[slot]; ++b) {
+    for (int b = first; b < n_blocks_[slot]; ++b) {
       if (--refs_[row[b]] == 0) free_.push_back(row[b]);
       row[b] = -1;
     }
-    n_blocks_[slot] = 0;
+    n_blocks_[slot] = first < n_blocks_[slot] ? first : n_blocks_[slot];
   }
 
   std::vector<LayerInfo> layers_;

@@ -16,7 +16,8 @@ constexpr int kUnroll = 8;                            // 16-byte loads in flight
 constexpr int kReadVecs = 2;                          // (32 copies of 4103 tokens, 32 query / 8 KV heads of 128 bf16: 1: 172 us, 2: 161, 4: 162, 8: 197)
 constexpr int kBlock16 = kThreads * kUnroll;          // 16-byte units per block: 32 KB
 
-__global__ void __launch_bounds__(kThreads) fork_copy_kernel(const __grid_constant__ ForkParams p) {
+template <typename Params>
+__global__ void __launch_bounds__(kThreads) fork_copy_kernel(const __grid_constant__ Params p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // a read that follows may get ready
   const int y = blockIdx.y;
   if (y < p.n_segs) {
@@ -38,7 +39,7 @@ __global__ void __launch_bounds__(kThreads) fork_copy_kernel(const __grid_consta
   const TableRow& r = p.row[y - p.n_segs];
   const int32_t* src = p.table + (int64_t)r.src_slot * p.table_stride;
   int32_t* dst = p.table + (int64_t)r.dst_slot * p.table_stride;
-  for (int b = threadIdx.x; b < r.n_copy; b += kThreads) dst[b] = src[b];
+  for (int b = r.copy0 + (int)threadIdx.x; b < r.copy0 + r.n_copy; b += kThreads) dst[b] = src[b];
   if ((int)threadIdx.x < r.n_set) dst[r.set0 + threadIdx.x] = r.page[threadIdx.x];
 }
 
@@ -96,7 +97,20 @@ cudaError_t launch_fork_copy(const ForkParams& p, cudaStream_t st) {
   for (int i = 0; i < p.n_segs; ++i) longest = p.seg[i].n16 > longest ? p.seg[i].n16 : longest;
   unsigned bx = (longest + kBlock16 - 1) / kBlock16;
   if (bx < 1) bx = 1;
-  fork_copy_kernel<<<dim3(bx, p.n_segs + p.n_rows), kThreads, 0, st>>>(p);
+  const dim3 grid(bx, p.n_segs + p.n_rows);
+  if (p.n_segs > SmallForkParams::kMaxSegs || p.n_rows > SmallForkParams::kMaxRows) {
+    fork_copy_kernel<<<grid, kThreads, 0, st>>>(p);
+    return cudaGetLastError();
+  }
+  SmallForkParams s;
+  s.arena = p.arena;
+  s.table = p.table;
+  s.table_stride = p.table_stride;
+  s.n_segs = p.n_segs;
+  s.n_rows = p.n_rows;
+  for (int i = 0; i < p.n_segs; ++i) s.seg[i] = p.seg[i];
+  for (int i = 0; i < p.n_rows; ++i) s.row[i] = p.row[i];
+  fork_copy_kernel<<<grid, kThreads, 0, st>>>(s);
   return cudaGetLastError();
 }
 

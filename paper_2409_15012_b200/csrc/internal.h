@@ -235,20 +235,24 @@ struct CopySeg {
 constexpr int kRowPages = 4;
 struct TableRow {
   int32_t src_slot, dst_slot;
-  int32_t n_copy;     // entries [0, n_copy) are copied from the source's row
-  int32_t set0;       // entries set0 .. set0 + n_set - 1 become page[]
+  int32_t copy0, n_copy;   // entries [copy0, copy0 + n_copy) are copied from the source's row
+  int32_t set0;            // entries set0 .. set0 + n_set - 1 become page[]
   int32_t n_set;
   int32_t page[kRowPages];
 };
-constexpr int kForkSegs = 96, kForkRows = 48;   // (both lists of a launch stay below 4 KB of parameters)
-struct ForkParams {
+// Two sizes of launch: parameter blocks cost time to hand over, and so do launches.
+template <int kSegs, int kRows>
+struct ForkParamsOf {
+  static constexpr int kMaxSegs = kSegs, kMaxRows = kRows;
   char* arena;
   int32_t* table;
   int32_t table_stride;
   int32_t n_segs, n_rows;
-  CopySeg seg[kForkSegs];
-  TableRow row[kForkRows];
+  CopySeg seg[kSegs];
+  TableRow row[kRows];
 };
+using ForkParams = ForkParamsOf<512, 256>;
+using SmallForkParams = ForkParamsOf<90, 45>;   // below 4 KB
 
 // Beam selection.  Groups of one launch have a ticket counter each.  part_sums and part_keys are the scan's results per (beam, chunk).
 constexpr int kBeamTickets = 1024;
@@ -275,7 +279,7 @@ enum { kDevOk = 0, kDevWaitTimeout = 1 };
 cudaError_t launch_append(const AppendParams& p, int max_n_new, cudaStream_t st);
 cudaError_t launch_table_set(const TableSetParams& p, cudaStream_t st);
 cudaError_t launch_gather(const GatherParams& p, int max_rows, cudaStream_t st);
-cudaError_t launch_fork_copy(const ForkParams& p, cudaStream_t st);
+cudaError_t launch_fork_copy(const ForkParams& p, cudaStream_t st);   // (as a SmallForkParams where it fits)
 cudaError_t launch_read_kv(const GatherParams& p, int max_rows, cudaStream_t st);   // entries without chunk rows
 int beam_chunks(int rows, int vocab, int elem_bytes, int sm_count, int* chunk_granules);
 cudaError_t prepare_beam_select();
