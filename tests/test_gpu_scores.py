@@ -268,6 +268,27 @@ def test_chunks_behind_a_cache(direct, shape, window, d):
     ctx.close()
 
 
+@pytest.mark.parametrize("window", [0, 128])
+def test_chunks_behind_a_quantised_cache(window):
+    mx, _ = load_lib()
+    hq, hkv, d = heads = 6, 2, 128
+    prefix, n = 210, 150
+    gen = torch.Generator("cuda").manual_seed(10)
+    ctx = make(mx, "chunk", window, heads, "fp8", 1, 500, chunk=1000)
+    k, v = (torch.randn(prefix + n, hkv, d, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    k[:prefix], v[:prefix] = on_e4m3(k[:prefix]), on_e4m3(v[:prefix])
+    ctx.append_kv(0, [0], [prefix], k[:prefix].contiguous(), v[:prefix].contiguous())
+    q = (3 * torch.randn(n, hq, d, generator=gen, device="cuda")).bfloat16()
+    ctx.set_layer_scores(1, 25.0, slopes_of(hq))
+    out = torch.full_like(q, float("nan"))
+    ctx.attend_chunk(1, [0], [n], q, k[prefix:].contiguous(), v[prefix:].contiguous(), out)
+    torch.cuda.synchronize()
+    want, A, top = reference(q.double(), k.double(), v.double(), torch.arange(prefix, prefix + n, device="cuda"), 25.0,
+                             slopes_of(hq), window)
+    check(out, want, A, top, "bf16", d, "prompt", prefix + n, "quantised prefix")
+    ctx.close()
+
+
 @pytest.mark.parametrize("window", [0, 256])
 def test_scores_far_above_the_first_tile(window):
     # scores of several hundred, which make the prompt kernel move its exponent reference; capped
