@@ -94,6 +94,7 @@ struct TcParams {
 };
 struct ShapedTcParams : TcParams {
   ScoreShape shape;
+  int32_t item0[kMaxCallSeqs + 1];  // first work item of each sequence
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -253,12 +254,23 @@ struct WorkItem {
   bool valid;
   bool lo;   // rows of this tile may see fewer than a tile of keys: P enters P V as two bf16 terms
 };
-template <bool kRing>
-__device__ __forceinline__ WorkItem get_item(const TcParams& p, int id) {
+// (Launches with shaped scores number the items that exist through, so that ragged batches spread
+// evenly over the CTAs: prompts of 1 to 2500 tokens in one call 37 -> 32 us; `seq` is the caller's
+// place in the sequences, as its ids only grow.  The others also count the tiles that shorter
+// sequences do not have.)
+template <bool kRing, typename Params>
+__device__ __forceinline__ WorkItem get_item(const Params& p, int id, int& seq) {
   WorkItem w;
-  const int per_seq = p.max_qt * p.n_q_heads;
-  const int b = id / per_seq;
-  const int rem = id - b * per_seq;
+  int b, rem;
+  if constexpr (std::is_same_v<Params, ShapedTcParams>) {
+    while (p.item0[seq + 1] <= id) ++seq;
+    b = seq;
+    rem = id - p.item0[b];
+  } else {
+    const int per_seq = p.max_qt * p.n_q_heads;
+    b = id / per_seq;
+    rem = id - b * per_seq;
+  }
   const int qt_rev = rem / p.n_q_heads;
   w.h = rem - qt_rev * p.n_q_heads;
   w.g = w.h / p.group;
@@ -328,7 +340,9 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 #define BAR(i) (bar0 + 8u * (i))
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n_ids = p.max_qt * p.n_seqs * p.n_q_heads;
+  int n_ids, seq = 0;
+  if constexpr (kShape != 0) n_ids = p.item0[p.n_seqs];
+  else n_ids = p.max_qt * p.n_seqs * p.n_q_heads;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < 2; ++s) {
@@ -377,7 +391,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         bool ok = true;
         int G = 0, it = 0, q_issued = 0, k_issued = 0, v_issued = 0;
         for (int id = blockIdx.x; id < n_ids && ok; id += gridDim.x) {
-          const WorkItem w = get_item<kRing>(p, id);
+          const WorkItem w = get_item<kRing>(p, id, seq);
           if (!w.valid) continue;
           const int qb = it & 1;
           if (it >= 2) ok = mbar_wait(BAR(B_QE + qb), ((it >> 1) - 1) & 1, abort_flag);
@@ -445,7 +459,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         bool ok = true;
         int G = 0, it = 0;
         for (int id = blockIdx.x; id < n_ids && ok; id += gridDim.x) {
-          const WorkItem w = get_item<kRing>(p, id);
+          const WorkItem w = get_item<kRing>(p, id, seq);
           if (!w.valid) continue;
           const int qb = it & 1;
           ok = mbar_wait(BAR(B_QF + qb), (it >> 1) & 1, abort_flag);
@@ -483,7 +497,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         bool ok = true;
         int G = 0, it = 0;
         for (int id = blockIdx.x; id < n_ids && ok; id += gridDim.x) {
-          const WorkItem w = get_item<kRing>(p, id);
+          const WorkItem w = get_item<kRing>(p, id, seq);
           if (!w.valid) continue;
           // the first P V of an item overwrites the O accumulator: the streams must have
           // read the previous item's result
@@ -528,7 +542,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     bool ok = true;
     int it = 0;
     for (int id = blockIdx.x; id < n_ids && ok; id += gridDim.x) {
-      const WorkItem w = get_item<kRing>(p, id);
+      const WorkItem w = get_item<kRing>(p, id, seq);
       if (!w.valid) continue;
       ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_XC), it & 1, abort_flag));
       if (!ok) break;
@@ -588,7 +602,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     bool ok = true;
     int G = 0, it = 0;
     for (int id = blockIdx.x; id < n_ids && ok; id += gridDim.x) {
-      const WorkItem w = get_item<kRing>(p, id);
+      const WorkItem w = get_item<kRing>(p, id, seq);
       if (!w.valid) continue;
       const int i = w.pos0 + r;           // query position among the sequence's keys
       float m_ref = -INFINITY, l = 0.f;
@@ -1036,7 +1050,16 @@ cudaError_t launch_prefill_tc(const PrefillParams& pp, int max_len, int sm_count
   }
   p.ring_pages = pp.ring_pool != nullptr ? pp.ring_pages : kBN / kPage;
   p.max_qt = (max_len + kBM - 1) / kBM;
-  const int64_t n_ids = (int64_t)p.max_qt * pp.n_seqs * pp.n_q_heads;
+  int64_t n_ids = (int64_t)p.max_qt * pp.n_seqs * pp.n_q_heads;
+  if (pp.shape != nullptr) {
+    n_ids = 0;
+    for (int i = 0; i < pp.n_seqs; ++i) {
+      p.item0[i] = (int32_t)n_ids;
+      n_ids += (int64_t)((pp.row0[i + 1] - pp.row0[i] + kBM - 1) / kBM) * pp.n_q_heads;
+      if (n_ids > INT32_MAX) return cudaErrorInvalidValue;
+    }
+    p.item0[pp.n_seqs] = (int32_t)n_ids;
+  }
   const int grid = (int)(n_ids < sm_count ? n_ids : sm_count);   // persistent: one CTA per SM
   const bool ring = pp.ring_pool != nullptr;
   const int shape = pp.shape == nullptr ? 0 : (pp.shape->post > 0.f ? 1 : 0) | (pp.shape->biased ? 2 : 0);
