@@ -617,7 +617,6 @@ static bool score_shape_of(const mixattn_ctx* c, int layer, ScoreShape* sh) {
   if (ls.plain()) return false;
   sh->pre = ls.softcap > 0.f ? c->scale / ls.softcap : c->scale * kLog2e;
   sh->post = ls.softcap * kLog2e;
-  for (int i = 0; i < 6; ++i) sh->poly[i] = sh->post * tanh_coefficient(i);
   const double pre = sh->pre;
   bool normal = pre > 1e-18;   // (squares of products up to 1 / (2 pre) stay finite)
   double power = pre;

@@ -99,7 +99,6 @@ __host__ __device__ constexpr float tanh_near_coefficient(int i) {
 struct ScoreShape {
   float pre;        // factor on q . k: scale / cap with a cap, scale * log2(e) without
   float post;       // cap * log2(e); 0 = no cap
-  float poly[6];    // post times the coefficients of score_shape.cuh's polynomial
   float near[4];    // the cubic's for raw products: score = raw * (near[0] + near[1] raw^2 + ...) while raw^2 <= near_sq
   float near_sq;    // (negative: not used, a coefficient would leave fp32's normal range)
   int32_t biased;   // 1: the slopes below apply

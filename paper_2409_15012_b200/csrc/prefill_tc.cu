@@ -684,25 +684,17 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 }
                 if (__any_sync(0xffffffffu, top > p.shape.near_sq)) {
                   // some score is above half the cap: again from the raw products, which are still in
-                  // the S buffer, with the polynomial of the whole range, and one by one beyond it
+                  // the S buffer, as the decode kernels cap them, but with both forms computed and one
+                  // taken: a branch at each column went either way in nearly every warp (8k causal
+                  // prompt with every tile here, cap 4: 2080 -> 1880 us; cap 2: 3020 -> 1880)
                   tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
                   tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
                   tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
 #pragma unroll
-                  for (int e = 0; e < 64; e += 2) {
-                    next_off(e);
-                    const f32x2 x = mul2(raw_of(e), both(p.shape.pre)), u = mul2(x, x);
-                    f32x2 q = fma2(both(p.shape.poly[5]), u, both(p.shape.poly[4]));
-                    q = fma2(q, u, both(p.shape.poly[3]));
-                    q = fma2(q, u, both(p.shape.poly[2]));
-                    q = fma2(q, u, both(p.shape.poly[1]));
-                    q = fma2(q, u, both(p.shape.poly[0]));
-                    float2 s = unpack2(fma2(q, x, off));
-                    const float2 xx = unpack2(x), oo = unpack2(off);
-                    if (fabsf(xx.x) > 1.f) s.x = fmaf(tanh_exp(xx.x), p.shape.post, oo.x);
-                    if (fabsf(xx.y) > 1.f) s.y = fmaf(tanh_exp(xx.y), p.shape.post, oo.y);
-                    sv[e] = __float_as_uint(s.x);
-                    sv[e + 1] = __float_as_uint(s.y);
+                  for (int e = 0; e < 64; ++e) {
+                    const float x = __uint_as_float(sv[e]) * p.shape.pre, o = (kShape & 2) ? fmaf(slope, (float)e, base) : base;
+                    const float t = tanh_poly(x), w = tanh_exp(x);
+                    sv[e] = __float_as_uint(fmaf(fabsf(x) <= 1.f ? t : w, p.shape.post, o));
                   }
                 }
               }
