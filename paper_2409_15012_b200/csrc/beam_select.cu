@@ -375,12 +375,12 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
   float last = -INFINITY;             // logits up to this one are out
   bool full = false;                  // `last` is the n-th best so far (else the first tile is still to come)
   int have = 0;                       // entries in the list
-  bool gave_up = false;
+  int waited = n_tiles;               // the tile whose wait ran out
   for (int k = 0; k < n_tiles; ++k) {
     const int gt = g0 + k * kTileGranules;
     unsigned char* tile_at = smem + (k % kStages) * kTileBytes;
-    if (!gave_up && !mbar_wait(smem_u32(&s_bar[k % kStages]), (k / kStages) & 1)) {
-      gave_up = true;   // the status word tells that the results are invalid; no further wait
+    if (k < waited && !mbar_wait(smem_u32(&s_bar[k % kStages]), (k / kStages) & 1)) {
+      waited = k;   // the status word tells that the results are invalid; no further copy or wait in this loop
       atomicExch(p.status, kDevWaitTimeout);
     }
     int4 raw[kVecs];
@@ -551,8 +551,11 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
       if (threadIdx.x == 0) { s_count = 0; s_valid = kPending; }
       __syncthreads();
     }
-    if (threadIdx.x == 0 && k + kStages < n_tiles) issue(k + kStages);   // (every thread is done with the stage)
+    if (threadIdx.x == 0 && k + kStages < waited) issue(k + kStages);   // (every thread is done with the stage)
   }
+  if (threadIdx.x == 0)   // after a wait that ran out: copies may still be on their way into this block's memory
+    for (int k = waited; k < min(n_tiles, waited + kStages); ++k)
+      mbar_wait(smem_u32(&s_bar[k % kStages]), (k / kStages) & 1);
   // ---- results of the chunk ----
   const int64_t part = (int64_t)row * gridDim.x + blockIdx.x;
   for (int i = threadIdx.x; i < n; i += kThreads) p.part_keys[part * n + i] = i < have ? list[i] : 0;
