@@ -156,17 +156,22 @@ def _p32(a: Optional[np.ndarray]):
 
 
 def _ints(a):
-    """(ctypes int32 array or None, length) of a host sequence; short lists are a step of a
-    generation loop's cost, and this is several times faster than going through numpy."""
-    if a is None:
-        return None, 0
+    """(ctypes int32 array, length) of a host sequence of whole numbers; short lists are a step of a
+    generation loop's cost, and this is several times faster than going through numpy.  What is not
+    one whole number per entry (a nested sequence, say) is refused."""
+    b = None
     if type(a) is list:
         try:
             b = array("i", a)
         except TypeError:
-            b = np.array(a, dtype=np.int32)
-    else:
-        b = np.array(a, dtype=np.int32)
+            pass
+    if b is None:
+        x = np.asarray(a)
+        if x.ndim != 1 or x.dtype.kind not in "iufb":
+            raise MixAttnError(ERR_INVALID_ARG, "sequence of integers")
+        b = x.astype(np.int32)
+        if not np.array_equal(b, x):
+            raise MixAttnError(ERR_INVALID_ARG, "sequence of integers")
     n = len(b)
     return ((C.c_int32 * n).from_buffer(b) if n else (C.c_int32 * 1)()), n
 
@@ -257,6 +262,8 @@ class Context:
     def rc_append_kv(self, layer, seq_ids, n_new=None, k=None, v=None, stream=None) -> int:
         s = _i32(seq_ids)
         n = None if n_new is None else _i32(n_new)
+        if n is not None and len(n) != len(s):
+            return ERR_INVALID_ARG
         return lib.mixattn_append_kv(self.h, layer, len(s), _p32(s), _p32(n), _dev(k), _dev(v), _stream(stream))
 
     def append_kv(self, layer, seq_ids, n_new=None, k=None, v=None, stream=None):
@@ -267,6 +274,8 @@ class Context:
     def rc_append_kv_rope(self, layer, seq_ids, n_new, k, v, rope_theta, stream=None) -> int:
         s = _i32(seq_ids)
         n = None if n_new is None else _i32(n_new)
+        if n is not None and len(n) != len(s):
+            return ERR_INVALID_ARG
         return lib.mixattn_append_kv_rope(self.h, layer, len(s), _p32(s), _p32(n), _dev(k), _dev(v),
                                           float(rope_theta), _stream(stream))
 
@@ -315,7 +324,9 @@ class Context:
             raise MixAttnError(rc, "mixattn_decode_layers")
 
     def rc_prefill(self, layer, seq_ids, seq_lens, q, k, v, out, stream=None) -> int:
-        (s, n), (lens, _) = _ints(seq_ids), _ints(seq_lens)
+        (s, n), (lens, m) = _ints(seq_ids), _ints(seq_lens)
+        if n != m:
+            return ERR_INVALID_ARG
         return lib.mixattn_prefill(self.h, layer, n, s, lens, _dev(q), _dev(k), _dev(v), _dev(out), _stream(stream))
 
     def prefill(self, layer, seq_ids, seq_lens, q, k, v, out, stream=None):
@@ -324,7 +335,9 @@ class Context:
             raise MixAttnError(rc, "mixattn_prefill")
 
     def rc_attend_chunk(self, layer, seq_ids, seq_lens, q, k, v, out, stream=None) -> int:
-        (s, n), (lens, _) = _ints(seq_ids), _ints(seq_lens)
+        (s, n), (lens, m) = _ints(seq_ids), _ints(seq_lens)
+        if n != m:
+            return ERR_INVALID_ARG
         return lib.mixattn_attend_chunk(self.h, layer, n, s, lens, _dev(q), _dev(k), _dev(v), _dev(out), _stream(stream))
 
     def attend_chunk(self, layer, seq_ids, seq_lens, q, k, v, out, stream=None):
@@ -366,9 +379,13 @@ class Context:
         (default: everything stored).  The tensors are allocated on torch's current stream."""
         s, m = _ints(seq_ids)
         p = n = None
-        if first_pos is not None or n_tokens is not None:
-            (p, mp), (n, mn) = _ints(first_pos), _ints(n_tokens)
-            if (p is not None and mp != m) or (n is not None and mn != m):
+        if first_pos is not None:
+            p, mp = _ints(first_pos)
+            if mp != m:
+                raise MixAttnError(ERR_INVALID_ARG, "mixattn_read_kv")
+        if n_tokens is not None:
+            n, mn = _ints(n_tokens)
+            if mn != m:
                 raise MixAttnError(ERR_INVALID_ARG, "mixattn_read_kv")
         if n is not None:
             rows = sum([max(0, x) for x in n[:m]])
