@@ -176,6 +176,18 @@ def _ints(a):
     return ((C.c_int32 * n).from_buffer(b) if n else (C.c_int32 * 1)()), n
 
 
+def _empty(like, shape, stream):
+    """like.new_empty(shape), its memory taken from the stream that the call's kernels run on: a block
+    that was let go on another stream may still be written to there."""
+    torch = _get_torch()
+    handle, dev = _stream(stream) or 0, like.get_device()
+    if handle == torch._C._cuda_getCurrentRawStream(dev):
+        return like.new_empty(shape)
+    on = torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)
+    with torch.cuda.stream(on):
+        return like.new_empty(shape)
+
+
 def _dev(t) -> Optional[int]:
     return None if t is None else int(t.data_ptr())
 
@@ -231,12 +243,13 @@ class Context:
                                            n_pages, max_seq_len, free_order, softmax_scale, device,
                                            chunk_scratch_tokens=chunk_scratch_tokens, kv_format=kv_format)
         self.arena = None
-        self._like = None      # an empty tensor that tensors of cached rows are allocated like
+        self._like = self._ints_like = None      # empty tensors that results are allocated like
         if device >= 0:
             torch = _get_torch()
             nbytes = arena_bytes(self.cfg)
             self.arena = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{device}")
             self._like = torch.empty(0, dtype=torch.bfloat16 if dtype == BF16 else torch.float32, device=self.arena.device)
+            self._ints_like = torch.empty(0, dtype=torch.int32, device=self.arena.device)
             self.cfg.arena = self.arena.data_ptr()
             self.cfg.arena_bytes = nbytes
         h = C.c_void_p()
@@ -376,7 +389,7 @@ class Context:
 
     def read_kv(self, layer, seq_ids, first_pos=None, n_tokens=None, stream=None):
         """Returns (K, V), the cached tokens [sum n_tokens, Hkv, D] of the sequences, oldest first
-        (default: everything stored).  The tensors are allocated on torch's current stream."""
+        (default: everything stored).  The tensors belong to `stream` (default: the default stream)."""
         s, m = _ints(seq_ids)
         p = n = None
         if first_pos is not None:
@@ -400,7 +413,7 @@ class Context:
         if self._like is None:
             raise MixAttnError(ERR_CUDA, "mixattn_read_kv")
         hkv, d = self.n_kv_heads, self.head_dim
-        kv = self._like.new_empty((2, rows, hkv, d))
+        kv = _empty(self._like, (2, rows, hkv, d), stream)
         at = kv.data_ptr()
         rc = lib.mixattn_read_kv(self.h, layer, m, s, p, n, at, at + rows * hkv * d * (2 if self.dtype == BF16 else 4),
                                  _stream(stream))
@@ -458,16 +471,17 @@ class Context:
 
     def beam_select(self, logits, scores, n_out, finished=None, eos_token=0, stream=None):
         """The n_out best continuations of every group: (scores fp32, beams int32, tokens int32),
-        [groups, n_out] each, allocated on torch's current stream."""
-        torch = _get_torch()
+        [groups, n_out] each.  The tensors belong to `stream` (default: the default stream)."""
+        if self._ints_like is None or n_out < 1:
+            raise MixAttnError(ERR_INVALID_ARG if n_out < 1 else ERR_CUDA, "mixattn_beam_select")
         g = logits.shape[0]
-        out = torch.empty((3, g, n_out), dtype=torch.int32, device=logits.device)
+        out = _empty(self._ints_like, (3, g, n_out), stream)
         at, step = out.data_ptr(), 4 * g * n_out
         rc = self._beam_select(logits, scores, n_out, at, at + step, at + 2 * step, finished, eos_token, stream)
         if rc:
             raise MixAttnError(rc, "mixattn_beam_select")
         s, b, t = out.unbind(0)      # (while the kernel runs)
-        return s.view(torch.float32), b, t
+        return s.view(_get_torch().float32), b, t
 
     def seq_reset(self, seq):
         rc = lib.mixattn_seq_reset(self.h, seq)
