@@ -14,9 +14,12 @@
 //
 // The scan is one pass with packed fp32 pairs: per logit about half an instruction each for the
 // subtraction of the reference, the factor log2(e), the sum and the maximum, one for unpacking
-// bf16 and one exponential.  The reference a thread subtracts is the largest logit it had seen
-// before the tile; a tile that leads it by more than 60 (or holds an infinity or a NaN, which the
-// plain code below would let into the sum) is noticed from its maximum and sum and is done over.
+// bf16 and one exponential.  The reference a thread subtracts is within 2 of the largest logit it
+// has seen, so that the terms that matter have small exponents: the subtraction and the product
+// round in proportion to them (a reference that may lag by 60 costs 2^-18 of the sum; by 2, and with
+// the moves' factors kept to full precision, the logarithm of the sum is right to 2^-20).  A tile
+// that holds an infinity or a NaN, which the plain code below would let into the sum, is noticed
+// from its maximum and sum and is done over.
 //
 // Selection without sorting: a thread's logits matter only if they are above the list's n-th
 // entry `last`.  The few that are wait in shared memory, and now and then the list
@@ -45,13 +48,24 @@ constexpr int kStages = 2;                           // tiles in shared memory
 constexpr int kTileBytes = kThreads * kVecs * 16;
 constexpr int kPending = 512;                        // candidates of a chunk waiting to be ranked
 constexpr long long kWaitLimitCycles = 4000000000ll; // about two seconds of SM clock
-constexpr float kMaxLead = 60.f;                     // e^60 times 32 logits is far from fp32's end
+constexpr float kMaxLead = 2.f;                      // of a logit over the reference: see below
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2eRest = 1.9259629911e-8f;       // log2(e) - kLog2e
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// e^(a - b) for a <= b, with what the difference and the factor log2(e) round off kept in the exponent.
+__device__ __forceinline__ float exp_of_lag(float a, float b) {
+  const float d = a - b;
+  if (!(d > -100.f)) return 0.f;                     // (below fp32's normal numbers; a = -inf among them)
+  const float b2 = a - d, a2 = d + b2, rest = (a - a2) + (b2 - b);
+  const float p = d * kLog2e;
+  const float r = fmaf(d, kLog2e, -p) + fmaf(d, kLog2eRest, rest * kLog2e);
+  const float t = ex2(p);
+  return fmaf(t, r * 0.6931472f, t);
 }
 // Order-preserving image of a finite float; both zeros give the same one.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -337,7 +351,8 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
   __shared__ uint64_t s_bar[kStages];
   __shared__ uint64_t s_floor;
   __shared__ int s_count, s_valid;   // pending candidates; of those, the first that found no room
-  __shared__ float s_red[2][kThreads / 32];
+  __shared__ float s_refs[kThreads / 32];
+  __shared__ double s_sums[kThreads / 32];
   uint64_t* pending = scratch + n;                              // candidates wait behind n places for the list
 
   // granules of 16 aligned bytes; the row starts `lead` logits into granule 0
@@ -371,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
   }
   __syncthreads();
 
-  float ref = -INFINITY, sum = 0.f;   // sum of e^(x - ref) over this thread's logits
+  float ref = -INFINITY, sum = 0.f, rest = 0.f;   // sum + rest = sum of e^(x - ref) over this thread's logits
   float last = -INFINITY;             // logits up to this one are out
   bool full = false;                  // `last` is the n-th best so far (else the first tile is still to come)
   int have = 0;                       // entries in the list
@@ -422,15 +437,23 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
       const float2 s = unpack2(add2(s0, s1));
       return s.x + s.y;
     };
-    if (ref == -INFINITY && top > -INFINITY && top < 0x1p126f) ref = top;
+    auto follow = [&]() {   // the reference moves up to the tile's maximum
+      if (top > ref + kMaxLead) {
+        const float f = exp_of_lag(ref, top);
+        sum *= f;
+        rest *= f;
+        ref = top;
+      }
+    };
     float tile = 0.f;
-    bool over = !(top <= ref + kMaxLead);            // (a row of nothing but -inf so far: -inf <= -inf)
-    if (ref > -INFINITY) {
-      tile = add_tile();
-      over = over || !(tile < INFINITY);             // a NaN
+    bool over = !(top < 0x1p126f);                   // an infinity
+    if (!over) {
+      follow();
+      if (ref > -INFINITY) tile = add_tile();        // (else: nothing but -inf and NaN so far)
+      over = !(tile < INFINITY);                     // a NaN
     }
     if (over) {
-      // only finite logits count: the others become -inf; then the reference moves up to the tile's maximum
+      // only finite logits count: the others become -inf
       top = -INFINITY;
 #pragma unroll
       for (int v = 0; v < kVecs; ++v)
@@ -440,13 +463,14 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
           if (fabsf(x) < 0x1p126f) top = fmaxf(top, x);
           else drop_logit<T>(raw[v], e);
         }
-      if (top > ref) {
-        sum *= ex2((ref - top) * kLog2e);            // (2^-inf = 0 where nothing had been summed)
-        ref = top;
-      }
+      follow();
       tile = ref > -INFINITY ? add_tile() : 0.f;
     }
-    sum += tile;
+    {   // sum + rest += tile; what the addition rounds off goes to rest
+      const float s = sum + tile, t2 = s - sum, s2 = s - t2;
+      rest += (sum - s2) + (tile - t2);
+      sum = s;
+    }
 
     // ---- the chunk's best ----
     float floor_x = fmaxf(last, -0x1p126f);          // logits above it are candidates
@@ -562,19 +586,19 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
   float m = ref;
 #pragma unroll
   for (int sh = 16; sh > 0; sh >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, sh));
-  if ((threadIdx.x & 31) == 0) s_red[0][threadIdx.x >> 5] = m;
+  if ((threadIdx.x & 31) == 0) s_refs[threadIdx.x >> 5] = m;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, s_red[0][w]);
-  float s = ref > -INFINITY ? sum * ex2((ref - m) * kLog2e) : 0.f;
+  for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, s_refs[w]);
+  double s = ref > -INFINITY ? (double)exp_of_lag(ref, m) * ((double)sum + (double)rest) : 0.0;
 #pragma unroll
   for (int sh = 16; sh > 0; sh >>= 1) s += __shfl_xor_sync(0xffffffffu, s, sh);
-  if ((threadIdx.x & 31) == 0) s_red[1][threadIdx.x >> 5] = s;
+  if ((threadIdx.x & 31) == 0) s_sums[threadIdx.x >> 5] = s;
   __syncthreads();
   if (threadIdx.x == 0) {
-    s = 0.f;
-    for (int w = 0; w < kThreads / 32; ++w) s += s_red[1][w];
-    p.part_sums[part] = make_float2(m, s);
+    s = 0.0;
+    for (int w = 0; w < kThreads / 32; ++w) s += s_sums[w];
+    p.part_sums[part] = make_float2(m, (float)s);
   }
   // ---- the last CTA of the group merges its lists ----
   __threadfence();
