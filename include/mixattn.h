@@ -347,11 +347,12 @@ int mixattn_read_kv(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32
  *   out_scores, out_beams, out_tokens
  *               device, [n_groups, n_out]; must not overlap the inputs.  Places without a
  *               continuation hold -infinity, -1 and -1
- * Only finite logits count (|x| < 2^126): a token with an infinite or NaN logit is no continuation
- * and adds nothing to the sum.  A beam whose score is not finite has no continuation, so the first
- * step of a group is scores = 0, -inf, -inf, ...  Sums and scores are formed in fp32 and double
- * precision; the outputs are rounded to fp32 once.  Uses the context's workspace (one stream at a
- * time, like every call).
+ * Only finite logits count: a token with an infinite or NaN logit is no continuation and adds
+ * nothing to the sum (one masked with the type's lowest finite value is one, behind all others).
+ * A beam whose score is not finite has no continuation, so the first step of a group is
+ * scores = 0, -inf, -inf, ...  Sums and scores are formed in fp32 and double precision, an error of
+ * at most 2^-20; the outputs are rounded to fp32 once.  Uses the context's workspace (one stream at
+ * a time, like every call).
  * Errors: INVALID_ARG (null, n_beams outside 1 .. MIXATTN_MAX_BEAMS, n_out outside 1 ..
  * MIXATTN_MAX_BEAM_OUT, vocab outside 1 .. MIXATTN_MAX_VOCAB or n_beams * vocab beyond 2^31 - 1,
  * row_stride < vocab or so large that 64-bit byte offsets overflow, eos_token outside the vocabulary

@@ -223,8 +223,9 @@ __device__ __forceinline__ void merge_group(const BeamParams& p, int group, unsi
   const int n = p.n_out, nb = p.n_beams, nc = p.n_chunks;
   Scored* list = reinterpret_cast<Scored*>(smem);                 // [n]
   Scored* pool = list + n;                                         // [n + kMergePool]
-  double* offset = reinterpret_cast<double*>(pool + n + kMergePool);   // [nb] lse of a beam
-  float* start = reinterpret_cast<float*>(offset + nb);            // [nb] its score; NaN: no continuation
+  double* offset = reinterpret_cast<double*>(pool + n + kMergePool);   // [nb] log of a beam's sum of e^(x - most)
+  float* most = reinterpret_cast<float*>(offset + nb);             // [nb] its reference
+  float* start = most + nb;                                        // [nb] its score; NaN: no continuation
   uint8_t* done = reinterpret_cast<uint8_t*>(start + nb);          // [nb]
   __shared__ int s_count;
   __shared__ Scored s_floor;
@@ -271,7 +272,7 @@ __device__ __forceinline__ void merge_group(const BeamParams& p, int group, unsi
     for (int c = lane + 32; c < nc; c += 32) s += share(__ldcg(sums + b * nc + c));
 #pragma unroll
     for (int sh = 16; sh > 0; sh >>= 1) s += __shfl_xor_sync(0xffffffffu, s, sh);
-    if (lane == 0) offset[b] = (double)m + log(s);
+    if (lane == 0) { offset[b] = log(s); most[b] = m; }
   }
   __syncthreads();
 
@@ -284,7 +285,8 @@ __device__ __forceinline__ void merge_group(const BeamParams& p, int group, unsi
       *out = scored((double)s, b * p.vocab + p.eos);
       return r == 0 && c == 0;
     }
-    *out = scored((double)unordered((uint32_t)(key >> 32)) - offset[b] + (double)s,
+    // (in this order: next to a reference of 1e38 the logarithm would be lost)
+    *out = scored((double)unordered((uint32_t)(key >> 32)) - (double)most[b] - offset[b] + (double)s,
                   b * p.vocab + (int32_t)(uint32_t)~(uint32_t)key);
     return key != 0;
   };
@@ -446,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
       }
     };
     float tile = 0.f;
-    bool over = !(top < 0x1p126f);                   // an infinity
+    bool over = !(top < INFINITY);                   // an infinity
     if (!over) {
       follow();
       if (ref > -INFINITY) tile = add_tile();        // (else: nothing but -inf and NaN so far)
@@ -460,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
           const float x = logit_of<T>(raw[v], e);
-          if (fabsf(x) < 0x1p126f) top = fmaxf(top, x);
+          if (fabsf(x) < INFINITY) top = fmaxf(top, x);
           else drop_logit<T>(raw[v], e);
         }
       follow();
@@ -473,7 +475,7 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
     }
 
     // ---- the chunk's best ----
-    float floor_x = fmaxf(last, -0x1p126f);          // logits above it are candidates
+    float floor_x = last;                            // logits above it are candidates
     if (!full) {
       // first tile: maxima of at least n groups of threads.  A group takes its threads from all
       // warps (every other one if n > 32), so that a short tile leaves none empty.
@@ -492,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, kScanCtas) beam_select_kernel(const 
       if (n <= 8) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));    // ... or 8
 #pragma unroll
       for (int sh = 1; sh < 32; sh <<= 1) m = fminf(m, __shfl_xor_sync(0xffffffffu, m, sh));
-      if (m > -0x1p126f) floor_x = below<T>(m);      // (a group without a logit: all are in)
+      if (m > -INFINITY) floor_x = below<T>(m);      // (a group without a logit: all are in)
     }
     auto above = [&]() {   // the logits of this thread's tile above floor_x
       uint32_t mask = 0;
@@ -653,7 +655,7 @@ cudaError_t prepare_beam_select() {
 cudaError_t launch_beam_select(const BeamParams& p, int elem_bytes, cudaStream_t st) {
   const int keys = 2 * p.n_out + std::max(kPending, p.n_out * kVecs * 16 / elem_bytes);
   const size_t smem = (size_t)kStages * kTileBytes + (size_t)keys * sizeof(uint64_t);
-  static_assert((2 * MIXATTN_MAX_BEAM_OUT + kMergePool) * sizeof(Scored) + MIXATTN_MAX_BEAMS * 13 <= kStages * kTileBytes,
+  static_assert((2 * MIXATTN_MAX_BEAM_OUT + kMergePool) * sizeof(Scored) + MIXATTN_MAX_BEAMS * 17 <= kStages * kTileBytes,
                 "the merge works where the tiles were");
   const dim3 grid(p.n_chunks, p.n_groups * p.n_beams);
   if (elem_bytes == 2) beam_select_kernel<__nv_bfloat16><<<grid, kThreads, smem, st>>>(p);
