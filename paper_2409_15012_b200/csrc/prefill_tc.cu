@@ -609,11 +609,6 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       uint32_t sv[64];
       float slope = 0.f;                  // kShape: of this head, base-2 units per token
       if constexpr (kShape & 2) slope = p.shape.slope[w.h];
-      // weight of a score: 2^(score - reference)
-      auto weight = [&](uint32_t sc, float neg_m) {
-        if constexpr (kShape) return ex2_approx(__uint_as_float(sc));   // (shaped scores have it subtracted already)
-        else return ex2_approx(fmaf(__uint_as_float(sc), p.scale_log2e, neg_m));
-      };
       {
         if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SF + (G & 1)), (G >> 1) & 1, abort_flag))) { ok = false; break; }
         tc_fence_after();
@@ -625,29 +620,167 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       // The tile loop exists twice: for ordinary items (one bf16 term of P) and for the few items
       // whose rows see fewer than a tile of keys (two terms).  Keeping the second form out of the
       // first one's code matters: with both in one loop body the ordinary tiles ran 3-5 % slower.
-      auto run_tiles = [&](auto lo_tag) {
-        constexpr bool kLo = decltype(lo_tag)::value;
-        for (int j = 0; j < w.n_tiles; ++j) {
-          const int Gj = G + j, sb = Gj & 1;
-          const int x = entry_at<kShape>(w, j);
-          const int j0 = tile_of<kRing>(w, x) * kBN + hs * 64;   // first key of this stream's columns
-          const uint32_t s_addr = lane_base + kColS + sb * 128 + hs * 64;
-          // band edges: causal (keys after the query) and window (keys older than i - window); and
-          // the two visits of the tile in which the cached keys end
-          const bool edge = (j0 + 63 > w.pos0) || (p.window > 0 && j0 <= w.pos0 + kBM - 1 - p.window) ||
-                            (kRing && (x + 1 == w.dup || x == w.dup));
-          auto mask_edges = [&]() {
-            int k_max = i - j0;                                      // columns <= k_max are causal-visible
-            int k_min = p.window > 0 ? i - p.window + 1 - j0 : 0;    // columns >= k_min are inside the window
-            if (kRing && x + 1 == w.dup) k_max = min(k_max, w.cached - 1 - j0);   // this visit: the cached keys only
-            if (kRing && x == w.dup) k_min = max(k_min, w.cached - j0);           // this visit: the keys from k / v only
-  #pragma unroll
-            for (int e = 0; e < 64; ++e)
-              if (e > k_max || e < k_min) sv[e] = 0xff800000u;             // -inf
-          };
-          // raw scores in sv -> shaped base-2 scores plus `add`
-          auto shape_scores = [&](float add) {
-            if constexpr (kShape != 0) {
+      // (Two loops: with one text for both, in which declarations stand further apart, the plain
+      // one took 1 to 10 % longer, 8k causal 499 or 544 us against 495.)
+      if constexpr (kShape == 0) {
+        auto run_tiles = [&](auto lo_tag) {
+          constexpr bool kLo = decltype(lo_tag)::value;
+          for (int j = 0; j < w.n_tiles; ++j) {
+            const int Gj = G + j, sb = Gj & 1;
+            const int j0 = tile_of<kRing>(w, j) * kBN + hs * 64;   // first key of this stream's columns
+            const uint32_t s_addr = lane_base + kColS + sb * 128 + hs * 64;
+            // band edges: causal (keys after the query) and window (keys older than i - window); and
+            // the two visits of the tile in which the cached keys end
+            const bool edge = (j0 + 63 > w.pos0) || (p.window > 0 && j0 <= w.pos0 + kBM - 1 - p.window) ||
+                              (kRing && (j + 1 == w.dup || j == w.dup));
+            auto mask_edges = [&]() {
+              int k_max = i - j0;                                      // columns <= k_max are causal-visible
+              int k_min = p.window > 0 ? i - p.window + 1 - j0 : 0;    // columns >= k_min are inside the window
+              if (kRing && j + 1 == w.dup) k_max = min(k_max, w.cached - 1 - j0);   // this visit: the cached keys only
+              if (kRing && j == w.dup) k_min = max(k_min, w.cached - j0);           // this visit: the keys from k / v only
+#pragma unroll
+              for (int e = 0; e < 64; ++e)
+                if (e > k_max || e < k_min) sv[e] = 0xff800000u;             // -inf
+            };
+            if (edge) mask_edges();
+            // a row that has not seen a key yet takes its reference from this tile
+            const bool fresh = m_ref == -INFINITY;
+            if (__any_sync(0xffffffffu, fresh)) {
+              float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+              for (int e = 0; e < 64; e += 4) {
+                mx0 = fmax3(mx0, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+                mx1 = fmax3(mx1, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
+              }
+              if (fresh) m_ref = fmaxf(mx0, mx1) * p.scale_log2e;
+            }
+            float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;   // no visible key yet: weights 0, no NaN
+            // probe the next tile's scores now; the answer is read after the exponentials
+            const bool more = j + 1 < w.n_tiles;
+            const bool next_ready = more && mbar_test_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1);
+            float sum0 = 0.f, sum1 = 0.f;
+            uint32_t pk[32], pl[32];   // P as bf16 pairs; pl = rounding residuals (only on w.lo items)
+            if constexpr (!kLo) {
+#pragma unroll
+              for (int e = 0; e < 64; e += 4) {
+                const float p0 = ex2_approx(fmaf(__uint_as_float(sv[e]), p.scale_log2e, neg_m));
+                const float p1 = ex2_approx(fmaf(__uint_as_float(sv[e + 1]), p.scale_log2e, neg_m));
+                const float p2 = ex2_approx(fmaf(__uint_as_float(sv[e + 2]), p.scale_log2e, neg_m));
+                const float p3 = ex2_approx(fmaf(__uint_as_float(sv[e + 3]), p.scale_log2e, neg_m));
+                sum0 += p0 + p2;
+                sum1 += p1 + p3;
+                pk[e >> 1] = pack_bf16(p0, p1);
+                pk[(e >> 1) + 1] = pack_bf16(p2, p3);
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 64; e += 2) {
+                const float p0 = ex2_approx(fmaf(__uint_as_float(sv[e]), p.scale_log2e, neg_m));
+                const float p1 = ex2_approx(fmaf(__uint_as_float(sv[e + 1]), p.scale_log2e, neg_m));
+                sum0 += p0;
+                sum1 += p1;
+                split_bf16(p0, p1, pk[e >> 1], pl[e >> 1]);
+              }
+            }
+            // A score that leads the reference by more than 2^kMaxLead shows in the sum of the tile's
+            // weights (64 weights of at most 2^kMaxLead each stay below 2^(kMaxLead + 6); an overflow
+            // gives inf or NaN, which fail the comparison too), so the loop above carries no maximum.
+            const bool big = !(sum0 + sum1 <= 0x1p70f);
+            static_assert(kMaxLead == 64.f, "the bound above is 2^(kMaxLead + 6)");
+            if (__any_sync(0xffffffffu, big)) {
+              // rare: take the tile maximum from the scores, which are still in the S buffer (P has
+              // not been written yet), move the reference of the leading rows up to it, rescale what
+              // they have accumulated, and recompute this tile's weights
+              tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+              tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+              tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+              if (edge) mask_edges();
+              float mxa = -INFINITY, mxb = -INFINITY;
+#pragma unroll
+              for (int e = 0; e < 64; e += 4) {
+                mxa = fmax3(mxa, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+                mxb = fmax3(mxb, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
+              }
+              const float mt = fmaxf(mxa, mxb) * p.scale_log2e;
+              const bool far = mt > m_ref + kMaxLead;
+              const float alpha = far ? ex2_approx(m_ref - mt) : 1.f;
+              if (j > 0) {   // the O row holds earlier tiles: rescale it once this stream's previous P V has landed
+                // (the S buffer of tile G - 1 is released when both streams' P V of that tile are done;
+                // its previous phase is known complete because the scores of tile G - 1 existed)
+                if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SR + (sb ^ 1)), ((Gj - 1) >> 1) & 1, abort_flag))) { ok = false; break; }
+                tc_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < kD / 32; ++c) {
+                  uint32_t ov[32];
+                  tmem_ld32(o_addr + c * 32, ov);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
+                  tmem_st32(o_addr + c * 32, ov);
+                }
+              }
+              l *= alpha;
+              if (far) m_ref = mt;
+              neg_m = m_ref == -INFINITY ? 0.f : -m_ref;
+              sum0 = 0.f;
+              sum1 = 0.f;
+#pragma unroll
+              for (int e = 0; e < 64; e += 2) {
+                const float p0 = ex2_approx(fmaf(__uint_as_float(sv[e]), p.scale_log2e, neg_m));
+                const float p1 = ex2_approx(fmaf(__uint_as_float(sv[e + 1]), p.scale_log2e, neg_m));
+                sum0 += p0;
+                sum1 += p1;
+                if constexpr (kLo) split_bf16(p0, p1, pk[e >> 1], pl[e >> 1]);
+                else pk[e >> 1] = pack_bf16(p0, p1);
+              }
+            }
+            l += sum0 + sum1;
+            // P (bf16 pairs) over the first 32 of this stream's 64 score columns, the residual
+            // term, where the item carries one, over the other 32
+            tmem_st32(s_addr, pk);
+            if constexpr (kLo) tmem_st32(s_addr + 32, pl);
+            tmem_wait_st();
+            tc_fence_before();
+            // (one announcement barrier per S buffer: its next phase cannot complete before the
+            // scores of tile G + 2 exist, that is before the MMA thread has consumed this one)
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(B_PF + 2 * hs + sb));
+            // the next tile's scores
+            if (more) {
+              if (!__all_sync(0xffffffffu, next_ready || mbar_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1, abort_flag))) { ok = false; break; }
+              tc_fence_after();
+              const uint32_t n_addr = lane_base + kColS + (sb ^ 1) * 128 + hs * 64;
+              tmem_ld32(n_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+              tmem_ld32(n_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+            }
+            if (more) tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+          }
+        };
+        if (w.lo) run_tiles(std::true_type{});
+        else run_tiles(std::false_type{});
+      } else {
+        auto run_tiles = [&](auto lo_tag) {
+          constexpr bool kLo = decltype(lo_tag)::value;
+          for (int j = 0; j < w.n_tiles; ++j) {
+            const int Gj = G + j, sb = Gj & 1;
+            const int x = entry_at<kShape>(w, j);
+            const int j0 = tile_of<kRing>(w, x) * kBN + hs * 64;   // first key of this stream's columns
+            const uint32_t s_addr = lane_base + kColS + sb * 128 + hs * 64;
+            // band edges: causal (keys after the query) and window (keys older than i - window); and
+            // the two visits of the tile in which the cached keys end
+            const bool edge = (j0 + 63 > w.pos0) || (p.window > 0 && j0 <= w.pos0 + kBM - 1 - p.window) ||
+                              (kRing && (x + 1 == w.dup || x == w.dup));
+            auto mask_edges = [&]() {
+              int k_max = i - j0;                                      // columns <= k_max are causal-visible
+              int k_min = p.window > 0 ? i - p.window + 1 - j0 : 0;    // columns >= k_min are inside the window
+              if (kRing && x + 1 == w.dup) k_max = min(k_max, w.cached - 1 - j0);   // this visit: the cached keys only
+              if (kRing && x == w.dup) k_min = max(k_min, w.cached - j0);           // this visit: the keys from k / v only
+#pragma unroll
+              for (int e = 0; e < 64; ++e)
+                if (e > k_max || e < k_min) sv[e] = 0xff800000u;             // -inf
+            };
+            // raw scores in sv -> shaped base-2 scores plus `add`
+            auto shape_scores = [&](float add) {
               const float base = fmaf(-slope, (float)(i - j0), add);   // of column 0; column e is e tokens nearer
               f32x2 off = pack2(base, base);
               auto next_off = [&](int e) {   // of columns e, e + 1: anchored every 16 columns, in between by addition
@@ -698,192 +831,175 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                   }
                 }
               }
-            }
-          };
-          // the next tile's scores are probed before the exponentials, the answer is read after them
-          // (early or right before them as measured: 8k causal prompts, plain scores 502 / 545 us, biased 581 / 568)
-          const bool more = j + 1 < w.n_tiles;
-          bool next_ready = false;
-          if constexpr (kShape != 2) next_ready = more && mbar_test_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1);
-          float sum0 = 0.f, sum1 = 0.f;
-          uint32_t pk[32], pl[32];   // P as bf16 pairs; pl = rounding residuals (only on w.lo items)
-          // Capped scores of a tile that no band edge crosses, for rows that all have their reference:
-          // straight from the raw products to the weights, so that the packed arithmetic of one column
-          // runs under the exponentials of others (8k causal prompt: 710 -> 650 us).  Whether that was
-          // right (every square within the cubic's range, no far lead) is only looked at afterwards;
-          // if not, the raw products are fetched again and the tile takes the general way below.
-          // (With a distance bias as well, or alone, the general way was as fast or faster: 34.9
-          // against 36.9 us on ragged windows, 99 against 108 on chunks.)
-          bool done = false;
-          if constexpr (kShape == 1) {
-            if (!kLo && !edge && p.shape.near_sq >= 0.f && !__any_sync(0xffffffffu, m_ref == -INFINITY)) {
-              const f32x2 off = pack2(-m_ref, -m_ref);
-              f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
-              float top = 0.f;
+            };
+            // the next tile's scores are probed before the exponentials, the answer is read after them
+            // (early or right before them as measured: 8k causal prompts, biased 581 / 568 us)
+            const bool more = j + 1 < w.n_tiles;
+            bool next_ready = false;
+            if constexpr (kShape != 2) next_ready = more && mbar_test_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1);
+            float sum0 = 0.f, sum1 = 0.f;
+            uint32_t pk[32], pl[32];   // P as bf16 pairs; pl = rounding residuals (only on w.lo items)
+            // Capped scores of a tile that no band edge crosses, for rows that all have their reference:
+            // straight from the raw products to the weights, so that the packed arithmetic of one column
+            // runs under the exponentials of others (8k causal prompt: 710 -> 650 us).  Whether that was
+            // right (every square within the cubic's range, no far lead) is only looked at afterwards;
+            // if not, the raw products are fetched again and the tile takes the general way below.
+            // (With a distance bias as well, or alone, the general way was as fast or faster: 34.9
+            // against 36.9 us on ragged windows, 99 against 108 on chunks.)
+            bool done = false;
+            if constexpr (kShape == 1) {
+              if (!kLo && !edge && p.shape.near_sq >= 0.f && !__any_sync(0xffffffffu, m_ref == -INFINITY)) {
+                const f32x2 off = pack2(-m_ref, -m_ref);
+                f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
+                float top = 0.f;
 #pragma unroll
-              for (int e = 0; e < 64; e += 2) {
-                const f32x2 raw = pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), u = mul2(raw, raw);
-                f32x2 q = fma2(pack2(p.shape.near[3], p.shape.near[3]), u, pack2(p.shape.near[2], p.shape.near[2]));
-                q = fma2(q, u, pack2(p.shape.near[1], p.shape.near[1]));
-                q = fma2(q, u, pack2(p.shape.near[0], p.shape.near[0]));
-                const float2 uu = unpack2(u), ss = unpack2(fma2(q, raw, off));
-                top = fmax3(top, uu.x, uu.y);
-                const float p0 = ex2_approx(ss.x), p1 = ex2_approx(ss.y);
-                if (e & 2) sum3 = add2(sum3, pack2(p0, p1));
-                else sum2 = add2(sum2, pack2(p0, p1));
-                pk[e >> 1] = pack_bf16(p0, p1);
+                for (int e = 0; e < 64; e += 2) {
+                  const f32x2 raw = pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), u = mul2(raw, raw);
+                  f32x2 q = fma2(pack2(p.shape.near[3], p.shape.near[3]), u, pack2(p.shape.near[2], p.shape.near[2]));
+                  q = fma2(q, u, pack2(p.shape.near[1], p.shape.near[1]));
+                  q = fma2(q, u, pack2(p.shape.near[0], p.shape.near[0]));
+                  const float2 uu = unpack2(u), ss = unpack2(fma2(q, raw, off));
+                  top = fmax3(top, uu.x, uu.y);
+                  const float p0 = ex2_approx(ss.x), p1 = ex2_approx(ss.y);
+                  if (e & 2) sum3 = add2(sum3, pack2(p0, p1));
+                  else sum2 = add2(sum2, pack2(p0, p1));
+                  pk[e >> 1] = pack_bf16(p0, p1);
+                }
+                const float2 s01 = unpack2(add2(sum2, sum3));
+                sum0 = s01.x;
+                sum1 = s01.y;
+                done = __all_sync(0xffffffffu, sum0 + sum1 <= 0x1p70f && top <= p.shape.near_sq);
+                if (!done) {
+                  tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+                  tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+                  tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+                }
               }
-              const float2 s01 = unpack2(add2(sum2, sum3));
-              sum0 = s01.x;
-              sum1 = s01.y;
-              done = __all_sync(0xffffffffu, sum0 + sum1 <= 0x1p70f && top <= p.shape.near_sq);
-              if (!done) {
+            }
+            if (!done) {
+              sum0 = sum1 = 0.f;
+              shape_scores(m_ref == -INFINITY ? 0.f : -m_ref);
+              if (edge) mask_edges();
+              // a row that has not seen a key yet takes its reference from this tile
+              const bool fresh = m_ref == -INFINITY;
+              if (__any_sync(0xffffffffu, fresh)) {
+                float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 64; e += 4) {
+                  mx0 = fmax3(mx0, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+                  mx1 = fmax3(mx1, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
+                }
+                if (fresh) m_ref = fmaxf(mx0, mx1);
+                const float sub = fresh && m_ref > -INFINITY ? m_ref : 0.f;   // (fresh rows' scores stand without a reference so far)
+#pragma unroll
+                for (int e = 0; e < 64; ++e) sv[e] = __float_as_uint(__uint_as_float(sv[e]) - sub);
+              }
+              if constexpr (kShape == 2) next_ready = more && mbar_test_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1);
+              if constexpr (!kLo) {
+                f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
+#pragma unroll
+                for (int e = 0; e < 64; e += 4) {
+                  const float p0 = ex2_approx(__uint_as_float(sv[e])), p1 = ex2_approx(__uint_as_float(sv[e + 1]));
+                  const float p2 = ex2_approx(__uint_as_float(sv[e + 2])), p3 = ex2_approx(__uint_as_float(sv[e + 3]));
+                  sum2 = add2(sum2, pack2(p0, p1));
+                  sum3 = add2(sum3, pack2(p2, p3));
+                  pk[e >> 1] = pack_bf16(p0, p1);
+                  pk[(e >> 1) + 1] = pack_bf16(p2, p3);
+                }
+                const float2 s01 = unpack2(add2(sum2, sum3));
+                sum0 = s01.x;
+                sum1 = s01.y;
+              } else {
+#pragma unroll
+                for (int e = 0; e < 64; e += 2) {
+                  const float p0 = ex2_approx(__uint_as_float(sv[e]));
+                  const float p1 = ex2_approx(__uint_as_float(sv[e + 1]));
+                  sum0 += p0;
+                  sum1 += p1;
+                  split_bf16(p0, p1, pk[e >> 1], pl[e >> 1]);
+                }
+              }
+              // A score that leads the reference by more than 2^kMaxLead shows in the sum of the tile's
+              // weights (64 weights of at most 2^kMaxLead each stay below 2^(kMaxLead + 6); an overflow
+              // gives inf or NaN, which fail the comparison too), so the loop above carries no maximum.
+              const bool big = !(sum0 + sum1 <= 0x1p70f);
+              static_assert(kMaxLead == 64.f, "the bound above is 2^(kMaxLead + 6)");
+              if (__any_sync(0xffffffffu, big)) {
+                // rare: take the tile maximum from the scores, which are still in the S buffer (P has
+                // not been written yet), move the reference of the leading rows up to it, rescale what
+                // they have accumulated, and recompute this tile's weights
                 tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
                 tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
                 tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+                shape_scores(0.f);
+                if (edge) mask_edges();
+                float mxa = -INFINITY, mxb = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 64; e += 4) {
+                  mxa = fmax3(mxa, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+                  mxb = fmax3(mxb, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
+                }
+                const float mt = fmaxf(mxa, mxb);
+                const bool far = mt > m_ref + kMaxLead;
+                const float alpha = far ? ex2_approx(m_ref - mt) : 1.f;
+                if (j > 0) {   // the O row holds earlier tiles: rescale it once this stream's previous P V has landed
+                  // (the S buffer of tile G - 1 is released when both streams' P V of that tile are done;
+                  // its previous phase is known complete because the scores of tile G - 1 existed)
+                  if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SR + (sb ^ 1)), ((Gj - 1) >> 1) & 1, abort_flag))) { ok = false; break; }
+                  tc_fence_after();
+#pragma unroll 1
+                  for (int c = 0; c < kD / 32; ++c) {
+                    uint32_t ov[32];
+                    tmem_ld32(o_addr + c * 32, ov);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
+                    tmem_st32(o_addr + c * 32, ov);
+                  }
+                }
+                l *= alpha;
+                if (far) m_ref = mt;
+                const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;   // (no visible key yet: weights 0, no NaN)
+#pragma unroll
+                for (int e = 0; e < 64; ++e) sv[e] = __float_as_uint(__uint_as_float(sv[e]) + neg_m);
+                sum0 = 0.f;
+                sum1 = 0.f;
+#pragma unroll
+                for (int e = 0; e < 64; e += 2) {
+                  const float p0 = ex2_approx(__uint_as_float(sv[e]));
+                  const float p1 = ex2_approx(__uint_as_float(sv[e + 1]));
+                  sum0 += p0;
+                  sum1 += p1;
+                  if constexpr (kLo) split_bf16(p0, p1, pk[e >> 1], pl[e >> 1]);
+                  else pk[e >> 1] = pack_bf16(p0, p1);
+                }
               }
             }
-          }
-          if (!done) {
-          sum0 = sum1 = 0.f;
-          shape_scores(m_ref == -INFINITY ? 0.f : -m_ref);
-          if (edge) mask_edges();
-          // a row that has not seen a key yet takes its reference from this tile
-          const bool fresh = m_ref == -INFINITY;
-          if (__any_sync(0xffffffffu, fresh)) {
-            float mx0 = -INFINITY, mx1 = -INFINITY;
-  #pragma unroll
-            for (int e = 0; e < 64; e += 4) {
-              mx0 = fmax3(mx0, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
-              mx1 = fmax3(mx1, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
-            }
-            if (fresh) m_ref = kShape ? fmaxf(mx0, mx1) : fmaxf(mx0, mx1) * p.scale_log2e;
-            if constexpr (kShape != 0) {   // fresh rows' scores stand without a reference so far
-              const float sub = fresh && m_ref > -INFINITY ? m_ref : 0.f;
-#pragma unroll
-              for (int e = 0; e < 64; ++e) sv[e] = __float_as_uint(__uint_as_float(sv[e]) - sub);
-            }
-          }
-          float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;   // no visible key yet: weights 0, no NaN
-          if constexpr (kShape == 2) next_ready = more && mbar_test_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1);
-          if constexpr (!kLo && kShape != 0) {
-            f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
-  #pragma unroll
-            for (int e = 0; e < 64; e += 4) {
-              const float p0 = ex2_approx(__uint_as_float(sv[e])), p1 = ex2_approx(__uint_as_float(sv[e + 1]));
-              const float p2 = ex2_approx(__uint_as_float(sv[e + 2])), p3 = ex2_approx(__uint_as_float(sv[e + 3]));
-              sum2 = add2(sum2, pack2(p0, p1));
-              sum3 = add2(sum3, pack2(p2, p3));
-              pk[e >> 1] = pack_bf16(p0, p1);
-              pk[(e >> 1) + 1] = pack_bf16(p2, p3);
-            }
-            const float2 s01 = unpack2(add2(sum2, sum3));
-            sum0 = s01.x;
-            sum1 = s01.y;
-          } else if constexpr (!kLo) {
-  #pragma unroll
-            for (int e = 0; e < 64; e += 4) {
-              const float p0 = weight(sv[e], neg_m);
-              const float p1 = weight(sv[e + 1], neg_m);
-              const float p2 = weight(sv[e + 2], neg_m);
-              const float p3 = weight(sv[e + 3], neg_m);
-              sum0 += p0 + p2;
-              sum1 += p1 + p3;
-              pk[e >> 1] = pack_bf16(p0, p1);
-              pk[(e >> 1) + 1] = pack_bf16(p2, p3);
-            }
-          } else {
-  #pragma unroll
-            for (int e = 0; e < 64; e += 2) {
-              const float p0 = weight(sv[e], neg_m);
-              const float p1 = weight(sv[e + 1], neg_m);
-              sum0 += p0;
-              sum1 += p1;
-              split_bf16(p0, p1, pk[e >> 1], pl[e >> 1]);
-            }
-          }
-          // A score that leads the reference by more than 2^kMaxLead shows in the sum of the tile's
-          // weights (64 weights of at most 2^kMaxLead each stay below 2^(kMaxLead + 6); an overflow
-          // gives inf or NaN, which fail the comparison too), so the loop above carries no maximum.
-          const bool big = !(sum0 + sum1 <= 0x1p70f);
-          static_assert(kMaxLead == 64.f, "the bound above is 2^(kMaxLead + 6)");
-          if (__any_sync(0xffffffffu, big)) {
-            // rare: take the tile maximum from the scores, which are still in the S buffer (P has
-            // not been written yet), move the reference of the leading rows up to it, rescale what
-            // they have accumulated, and recompute this tile's weights
-            tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
-            tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
-            tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
-            shape_scores(0.f);
-            if (edge) mask_edges();
-            float mxa = -INFINITY, mxb = -INFINITY;
-  #pragma unroll
-            for (int e = 0; e < 64; e += 4) {
-              mxa = fmax3(mxa, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
-              mxb = fmax3(mxb, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
-            }
-            const float mt = kShape ? fmaxf(mxa, mxb) : fmaxf(mxa, mxb) * p.scale_log2e;
-            const bool far = mt > m_ref + kMaxLead;
-            const float alpha = far ? ex2_approx(m_ref - mt) : 1.f;
-            if (j > 0) {   // the O row holds earlier tiles: rescale it once this stream's previous P V has landed
-              // (the S buffer of tile G - 1 is released when both streams' P V of that tile are done;
-              // its previous phase is known complete because the scores of tile G - 1 existed)
-              if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SR + (sb ^ 1)), ((Gj - 1) >> 1) & 1, abort_flag))) { ok = false; break; }
+            l += sum0 + sum1;
+            // P (bf16 pairs) over the first 32 of this stream's 64 score columns, the residual
+            // term, where the item carries one, over the other 32
+            tmem_st32(s_addr, pk);
+            if constexpr (kLo) tmem_st32(s_addr + 32, pl);
+            tmem_wait_st();
+            tc_fence_before();
+            // (one announcement barrier per S buffer: its next phase cannot complete before the
+            // scores of tile G + 2 exist, that is before the MMA thread has consumed this one)
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(B_PF + 2 * hs + sb));
+            // the next tile's scores
+            if (more) {
+              if (!__all_sync(0xffffffffu, next_ready || mbar_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1, abort_flag))) { ok = false; break; }
               tc_fence_after();
-  #pragma unroll 1
-              for (int c = 0; c < kD / 32; ++c) {
-                uint32_t ov[32];
-                tmem_ld32(o_addr + c * 32, ov);
-                tmem_wait_ld();
-  #pragma unroll
-                for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
-                tmem_st32(o_addr + c * 32, ov);
-              }
+              const uint32_t n_addr = lane_base + kColS + (sb ^ 1) * 128 + hs * 64;
+              tmem_ld32(n_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+              tmem_ld32(n_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
             }
-            l *= alpha;
-            if (far) m_ref = mt;
-            neg_m = m_ref == -INFINITY ? 0.f : -m_ref;
-            if constexpr (kShape != 0) {
-#pragma unroll
-              for (int e = 0; e < 64; ++e) sv[e] = __float_as_uint(__uint_as_float(sv[e]) + neg_m);
-            }
-            sum0 = 0.f;
-            sum1 = 0.f;
-  #pragma unroll
-            for (int e = 0; e < 64; e += 2) {
-              const float p0 = weight(sv[e], neg_m);
-              const float p1 = weight(sv[e + 1], neg_m);
-              sum0 += p0;
-              sum1 += p1;
-              if constexpr (kLo) split_bf16(p0, p1, pk[e >> 1], pl[e >> 1]);
-              else pk[e >> 1] = pack_bf16(p0, p1);
-            }
+            if (more) tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
           }
-          }   // !done
-          l += sum0 + sum1;
-          // P (bf16 pairs) over the first 32 of this stream's 64 score columns, the residual
-          // term, where the item carries one, over the other 32
-          tmem_st32(s_addr, pk);
-          if constexpr (kLo) tmem_st32(s_addr + 32, pl);
-          tmem_wait_st();
-          tc_fence_before();
-          // (one announcement barrier per S buffer: its next phase cannot complete before the
-          // scores of tile G + 2 exist, that is before the MMA thread has consumed this one)
-          __syncwarp();
-          if (lane == 0) mbar_arrive(BAR(B_PF + 2 * hs + sb));
-          // the next tile's scores
-          if (more) {
-            if (!__all_sync(0xffffffffu, next_ready || mbar_wait(BAR(B_SF + (sb ^ 1)), ((Gj + 1) >> 1) & 1, abort_flag))) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t n_addr = lane_base + kColS + (sb ^ 1) * 128 + hs * 64;
-            tmem_ld32(n_addr, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
-            tmem_ld32(n_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
-          }
-          if (more) tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
-        }
-      };
-      if (w.lo) run_tiles(std::true_type{});
-      else run_tiles(std::false_type{});
+        };
+        if (w.lo) run_tiles(std::true_type{});
+        else run_tiles(std::false_type{});
+      }
       if (!ok) break;
       G += w.n_tiles;
       // hand (reference, sum) of the row to the epilogue warps; the slot is free once they
