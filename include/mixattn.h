@@ -185,10 +185,10 @@ int mixattn_append_kv_rope(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, cons
  * dtype and kv_format, and for that layer alone (a layer that reuses a cache has scores of its
  * own).  softcap = 0 with slopes = NULL restores plain scores.
  *   slopes   host, n_q_heads values in [0, MIXATTN_SLOPE_MAX], copied
- * The cap is evaluated to about six fp32 roundings (the fp32 mode: tanhf).  Keys and values must be
- * finite.  (Decode calls do not look at what earlier sequences left behind a sequence's last
- * token; prompt and chunk calls give masked rows, those of the next sequence of the call and stale
- * ring slots among them, a weight of zero, which an infinity or a NaN would survive.)
+ * The cap is evaluated to about six fp32 roundings (the fp32 mode: tanhf).  A sequence's
+ * keys and values must be finite, those that the masks hide from some of its rows included.  What
+ * is not the sequence's own does not matter: the other sequences of the call, and what earlier
+ * ones left behind its last token, in pages or in a ring.
  * Errors: INVALID_ARG (layer, a softcap that is neither 0 nor in [MIXATTN_SOFTCAP_MIN,
  * MIXATTN_SOFTCAP_MAX] or whose quotient with softmax_scale leaves fp32, a slope out of range or NaN), UNSUPPORTED (slopes with more than
  * MIXATTN_MAX_SLOPE_HEADS query heads).  A call that fails changes nothing. */
