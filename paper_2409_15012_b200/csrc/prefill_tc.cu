@@ -245,6 +245,7 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int b_mn, uint32_t n = 128) {
 // in L2 (a pass over all sequences at once re-read K/V from HBM 5x), heaviest tiles first,
 // and the heads of a KV group, which read the same K/V tiles, run at the same time.
 constexpr int kNoDup = 1 << 30;
+constexpr float kSteepSlope = 0.125f * 1.4426950408889634f;   // base-2 units per token
 struct WorkItem {
   int h, g, row_base, krow_base, S, i0, pos0, jt_lo, n_tiles;   // pos0 = position of query row i0 among the keys
   // Keys cached in a ring are read from the ring, the others from k / v.  When the cached keys
@@ -252,7 +253,7 @@ struct WorkItem {
   // its cached keys from the ring, entry dup the rest from k / v (each masks the other's keys).
   int cached, ring_page0, dup;                                  // dup = kNoDup when no tile is visited twice
   bool valid;
-  bool lo;   // rows of this tile may see fewer than a tile of keys: P enters P V as two bf16 terms
+  bool lo;   // rows of this tile are mixes of few keys: P enters P V as two bf16 terms
 };
 // (Launches with shaped scores number the items that exist through, so that ragged batches spread
 // evenly over the CTAs: prompts of 1 to 2500 tokens in one call 37 -> 32 us; `seq` is the caller's
@@ -298,6 +299,13 @@ __device__ __forceinline__ WorkItem get_item(const Params& p, int id, int& seq) 
   // tile) carry the rounding residual of P as a second bf16 term, like the decode kernel; all
   // other tiles, whose rows average over at least a tile of keys, keep the single term.
   w.lo = w.pos0 < kBM || (p.window > 0 && p.window < kBN);
+  // So do heads whose distance bias leaves a row as few keys: weights e^(-slope d) are worth 2 / slope
+  // equal ones, and from 16 on the rounding (half a step, 2^-8 at most, of each weight) stays below
+  // the output's own.  Price, slopes 2^-8/H ... 2^-8 of 32 heads: chunks behind a window 101.8 ->
+  // 107.9 us, 8k causal 554 -> 578; for all heads worth less than a tile of keys (slope 1/64) it
+  // would be 114 and 608.
+  if constexpr (std::is_same_v<Params, ShapedTcParams>)
+    w.lo = w.lo || (p.shape.biased && p.shape.slope[w.h] >= kSteepSlope);
   return w;
 }
 
@@ -646,7 +654,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         tmem_wait_ld_pin(*reinterpret_cast<uint32_t(*)[32]>(&sv[0]), *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
       }
       // The tile loop exists twice: for ordinary items (one bf16 term of P) and for the few items
-      // whose rows see fewer than a tile of keys (two terms).  Keeping the second form out of the
+      // whose rows are mixes of few keys (two terms).  Keeping the second form out of the
       // first one's code matters: with both in one loop body the ordinary tiles ran 3-5 % slower.
       // (Two loops: with one text for both, in which declarations stand further apart, the plain
       // one took 1 to 10 % longer, 8k causal 499 or 544 us against 495.)
