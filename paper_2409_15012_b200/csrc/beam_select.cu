@@ -238,7 +238,7 @@ __device__ __forceinline__ void merge_group(const BeamParams& p, int group, unsi
   const int r0 = (n + lists - 1) / lists - 1, k = (n + r0) / (r0 + 1);
 
   // What the other CTAs left is a trip to L2 away: everything most groups need is asked for at once.
-  // (Entries of finished beams were never written; they are not looked at.)
+  // (Entries of finished beams are zeros, their sums empty; neither is used.)
   constexpr int kEarly = 4;
   uint64_t early[kEarly], head = 0;
   float2 part = make_float2(-INFINITY, 0.f);

@@ -133,34 +133,34 @@ decode_split_f32_kernel(const __grid_constant__ std::conditional_t<SH != 0, Shap
         }
       }
     } else {
-        for (int t = t0 + warp; t < t1; t += kWarps) {
-      const int64_t page = tbl ? (int64_t)tbl[t / kPage] : (int64_t)seq * p.ring_pages + t / kPage;
-      const char* blk = p.pool + page * ge.page_bytes + (int64_t)g * ge.blk_bytes;
-      const float* kr = reinterpret_cast<const float*>(blk + (int64_t)(t % kPage) * ge.row_bytes) + lane * V;
-      const float* vr = kr + kPage * D;
-      float kv[V], vv[V];
+      for (int t = t0 + warp; t < t1; t += kWarps) {
+        const int64_t page = tbl ? (int64_t)tbl[t / kPage] : (int64_t)seq * p.ring_pages + t / kPage;
+        const char* blk = p.pool + page * ge.page_bytes + (int64_t)g * ge.blk_bytes;
+        const float* kr = reinterpret_cast<const float*>(blk + (int64_t)(t % kPage) * ge.row_bytes) + lane * V;
+        const float* vr = kr + kPage * D;
+        float kv[V], vv[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        kv[e] = kr[e];
-        vv[e] = vr[e];
+        for (int e = 0; e < V; ++e) {
+          kv[e] = kr[e];
+          vv[e] = vr[e];
+        }
+#pragma unroll
+        for (int r = 0; r < kRowsPerPass; ++r) {
+          float s = 0.f;
+#pragma unroll
+          for (int e = 0; e < V; ++e) s = fmaf(q[r][e], kv[e], s);
+#pragma unroll
+          for (int sh = 16; sh > 0; sh >>= 1) s += __shfl_xor_sync(0xffffffffu, s, sh);
+          s *= p.scale_log2e;
+          const float mn = fmaxf(m[r], s);
+          const float a = exp2f(m[r] - mn);
+          const float pe = exp2f(s - mn);
+          m[r] = mn;
+          l[r] = l[r] * a + pe;
+#pragma unroll
+          for (int e = 0; e < V; ++e) o[r][e] = fmaf(pe, vv[e], o[r][e] * a);
+        }
       }
-#pragma unroll
-      for (int r = 0; r < kRowsPerPass; ++r) {
-        float s = 0.f;
-#pragma unroll
-        for (int e = 0; e < V; ++e) s = fmaf(q[r][e], kv[e], s);
-#pragma unroll
-        for (int sh = 16; sh > 0; sh >>= 1) s += __shfl_xor_sync(0xffffffffu, s, sh);
-        s *= p.scale_log2e;
-        const float mn = fmaxf(m[r], s);
-        const float a = exp2f(m[r] - mn);
-        const float pe = exp2f(s - mn);
-        m[r] = mn;
-        l[r] = l[r] * a + pe;
-#pragma unroll
-        for (int e = 0; e < V; ++e) o[r][e] = fmaf(pe, vv[e], o[r][e] * a);
-      }
-    }
     }
 #pragma unroll
     for (int r = 0; r < kRowsPerPass; ++r) {
