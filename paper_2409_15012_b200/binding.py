@@ -176,18 +176,6 @@ def _ints(a):
     return ((C.c_int32 * n).from_buffer(b) if n else (C.c_int32 * 1)()), n
 
 
-def _empty(like, shape, stream):
-    """like.new_empty(shape), its memory taken from the stream that the call's kernels run on: a block
-    that was let go on another stream may still be written to there."""
-    torch = _get_torch()
-    handle, dev = _stream(stream) or 0, like.get_device()
-    if handle == torch._C._cuda_getCurrentRawStream(dev):
-        return like.new_empty(shape)
-    on = torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)
-    with torch.cuda.stream(on):
-        return like.new_empty(shape)
-
-
 def _dev(t) -> Optional[int]:
     return None if t is None else int(t.data_ptr())
 
@@ -250,6 +238,7 @@ class Context:
             self.arena = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{device}")
             self._like = torch.empty(0, dtype=torch.bfloat16 if dtype == BF16 else torch.float32, device=self.arena.device)
             self._ints_like = torch.empty(0, dtype=torch.int32, device=self.arena.device)
+            self._device, self._current_stream = device, torch._C._cuda_getCurrentRawStream   # (a handle, without an object)
             self.cfg.arena = self.arena.data_ptr()
             self.cfg.arena_bytes = nbytes
         h = C.c_void_p()
@@ -270,6 +259,16 @@ class Context:
             self.close()
         except Exception:
             pass
+
+    def _empty(self, like, shape, handle):
+        """like.new_empty(shape), its memory taken from the stream that the call's kernels run on: a block
+        that was let go on another stream may still be written to there."""
+        if (handle or 0) == self._current_stream(self._device):
+            return like.new_empty(shape)
+        cuda = _get_torch().cuda
+        on = cuda.ExternalStream(handle, device=self._device) if handle else cuda.default_stream(self._device)
+        with cuda.stream(on):
+            return like.new_empty(shape)
 
     # -- calls -------------------------------------------------------------
     def rc_append_kv(self, layer, seq_ids, n_new=None, k=None, v=None, stream=None) -> int:
@@ -413,10 +412,10 @@ class Context:
         if self._like is None:
             raise MixAttnError(ERR_CUDA, "mixattn_read_kv")
         hkv, d = self.n_kv_heads, self.head_dim
-        kv = _empty(self._like, (2, rows, hkv, d), stream)
+        stream = _stream(stream)
+        kv = self._empty(self._like, (2, rows, hkv, d), stream)
         at = kv.data_ptr()
-        rc = lib.mixattn_read_kv(self.h, layer, m, s, p, n, at, at + rows * hkv * d * (2 if self.dtype == BF16 else 4),
-                                 _stream(stream))
+        rc = lib.mixattn_read_kv(self.h, layer, m, s, p, n, at, at + rows * hkv * d * (2 if self.dtype == BF16 else 4), stream)
         if rc:
             raise MixAttnError(rc, "mixattn_read_kv")
         return kv.unbind(0)
@@ -475,7 +474,8 @@ class Context:
         if self._ints_like is None or n_out < 1:
             raise MixAttnError(ERR_INVALID_ARG if n_out < 1 else ERR_CUDA, "mixattn_beam_select")
         g = logits.shape[0]
-        out = _empty(self._ints_like, (3, g, n_out), stream)
+        stream = _stream(stream)
+        out = self._empty(self._ints_like, (3, g, n_out), stream)
         at, step = out.data_ptr(), 4 * g * n_out
         rc = self._beam_select(logits, scores, n_out, at, at + step, at + 2 * step, finished, eos_token, stream)
         if rc:
