@@ -13,7 +13,8 @@
 //   warp 1     one elected thread issues the tcgen05.mma (K16 steps, bf16 -> fp32 in TMEM) of
 //              S = Q K^T (M128 N128, both operands from shared memory) into one of two S
 //              buffers, two tiles ahead of the softmax
-//   warps 2-3  one elected thread per stream issues O_h += P_h V_h with P_h read from
+//   warps 2-3  one elected thread per stream issues O_h += P_h V_h (without the steps of 16
+//              keys that are not the sequence's) with P_h read from
 //              tensor memory and V MN-major from its row-major tile
 //   warps 4-7  softmax stream "lo": key columns 0-63 of every tile; warps 8-11 stream "hi":
 //              columns 64-127.  The two streams are independent flash-attention passes
