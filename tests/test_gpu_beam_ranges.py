@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from gpu_common import load_lib
+from test_gpu_beam_sums import check as check_values
 
 pytestmark = pytest.mark.gpu
 
@@ -51,8 +52,7 @@ def context(mx):
 @pytest.mark.parametrize("groups,beams,vocab,n_out", [
     (1100, 1, 300, 3), (2100, 2, 130, 64),     # more groups than one launch has counters for
     (40, 64, 2500, 64),                        # batches by the workspace
-    (1, 64, 40000, 64), (2, 64, 70003, 63),    # chunks as long as the workspace makes them
-    (1, 8, 128256, 8), (1, 4, 151936, 16), (1, 8, 50257, 64), (1, 16, 18000, 32), (1, 1, 400003, 64)])   # many lists
+    (1, 64, 40000, 64), (2, 64, 70003, 63), (1, 8, 128256, 8), (1, 4, 151936, 16), (1, 8, 50257, 64), (1, 16, 18000, 32), (1, 1, 400003, 64)])   # many lists
 def test_other_ways_through_the_launch(dtype, groups, beams, vocab, n_out):
     mx, _ = load_lib()
     ctx = context(mx)
@@ -63,6 +63,20 @@ def test_other_ways_through_the_launch(dtype, groups, beams, vocab, n_out):
     for _ in range(2):       # (the second call finds counters and workspace as the first one left them)
         check(ctx, logits, scores, n_out, finished, eos=5)
     check(ctx, logits, scores, n_out)
+    assert ctx.get_device_status() == 0
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype,groups,beams,vocab", [(torch.float32, 2, 54, 1326344), (torch.bfloat16, 2, 60, 1861771)])
+def test_chunks_made_longer_to_fit_the_workspace(dtype, groups, beams, vocab):
+    # (14 and 16 chunks per row would be best, of which the lists of one group do not fit)
+    mx, _ = load_lib()
+    ctx = context(mx)
+    gen = torch.Generator("cuda").manual_seed(84)
+    logits = torch.randn(groups, beams, vocab, generator=gen, device="cuda", dtype=dtype) * 3
+    scores = -torch.rand(groups, beams, generator=gen, device="cuda")
+    check_values(ctx, logits, scores, 64)
+    check_values(ctx, logits, scores, 64)
     assert ctx.get_device_status() == 0
     ctx.close()
 
