@@ -174,6 +174,51 @@ int mixattn_append_kv_rope(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, cons
                            const int32_t* n_new, const void* k, const void* v, float rope_theta,
                            void* stream);
 
+/* A rotary embedding (Section 3: the models use RoPE with a base that grows with the context
+ * length; RoFormer's definition, and the variants that models served beside the paper's use).
+ * Channel pair p of a head vector at position t turns by the angle t * f_p:
+ *     x' = (x cos - y sin) * scale      y' = (x sin + y cos) * scale
+ *   rotary_dim  channels that take part, a multiple of 16 up to head_dim; the others stay as they are
+ *   halves      0: pair p is channels (2p, 2p + 1); otherwise (p, p + rotary_dim / 2)
+ *   theta       f_p = theta^(-2p / rotary_dim); finite and > 1
+ *   inv_freq    host, rotary_dim / 2 values f_p of any kind (up to 1e6) instead (theta is then ignored), or NULL
+ *   scale       finite and > 0; 0 = 1
+ * Angles are formed and reduced in double precision, the rotation runs in fp32, bf16 is rounded once. */
+typedef struct {
+  int32_t rotary_dim;
+  int32_t halves;
+  double theta;
+  const double* inv_freq;
+  float scale;
+} mixattn_rope;
+
+/* Takes the rows of a projection to where attention wants them: rotates queries and keys at their
+ * positions, and stores keys and values in the cache of `layer` and / or hands them back as plain
+ * tensors.  One call per layer and step or chunk, for every kind of layer:
+ *   - an owner before mixattn_decode: store = 1, q_out
+ *   - a layer that reuses a cache (it computes queries only), after its owner's append: k = v = NULL
+ *     and first_pos = the positions of the tokens; or before the append: first_pos = NULL
+ *   - ahead of mixattn_attend_chunk or _prefill: store = 0, q_out, k_out, v_out
+ *   n_new      host, tokens per sequence (>= 0), or NULL for one token each
+ *   first_pos  host, position that the first token of each sequence is rotated at (>= 0), or NULL: the
+ *              length of the cache that `layer` reads.  With store = 1 it sets the angles only; the
+ *              tokens are stored behind what the cache holds, as always
+ *   q, k, v    device, one row of heads x head_dim per token, sequences in call order, rows
+ *              q_stride / k_stride / v_stride elements apart (views of one projection's output are
+ *              fine); NULL = not there.  Pointers and strides in bytes are multiples of 16
+ *   q_out, k_out, v_out
+ *              device, dense, 16-byte aligned, not overlapping the inputs; NULL = not wanted
+ *   store      0 or 1: append k and v (both must be there) to the cache, which `layer` must own
+ * What is stored are the bits of k_out and v_out (quantised storage: quantised from them), as
+ * mixattn_append_kv would store them.
+ * Errors: those of mixattn_append_kv (with store = 0 a layer need not own its cache), INVALID_ARG (a
+ * bad embedding, no input, an output without its input, strides too small, unaligned or so large that 64-bit byte offsets overflow, a position
+ * beyond 2^31 - 1). */
+int mixattn_rope_qkv(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32_t* seq_ids,
+                     const int32_t* n_new, const int32_t* first_pos, const mixattn_rope* rope,
+                     const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                     int64_t v_stride, int32_t store, void* q_out, void* k_out, void* v_out, void* stream);
+
 /* Shaped attention scores of one layer, from the next call on.  (The paper's models use plain
  * scores; models served beside them cap their scores or bias them by distance instead of, or
  * next to, a rotary embedding.)  With s = softmax_scale * q . k of a query at position i and a key
@@ -226,6 +271,29 @@ int mixattn_decode(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32_
 int mixattn_decode_layers(mixattn_ctx* ctx, int32_t layer_begin, int32_t layer_end, int32_t n_seqs,
                           const int32_t* seq_ids, const void* const* q, const void* const* k,
                           const void* const* v, void* const* out, void* stream, int32_t* layers_done);
+
+/* mixattn_decode for sequences that share cached prefixes: every page is read once for all the
+ * sequences that hold it.  (Section 5.4 serves many requests at once; requests behind one
+ * instruction, or several hypotheses of one prompt, are forks of a common sequence, and
+ * mixattn_fork_seqs shares the pages of what they have in common.)  The library finds the tree of
+ * common prefixes in the block tables, whatever the order of seq_ids; nothing has to be declared.
+ * Arguments, results and errors are those of mixattn_decode, and so is the computation apart from
+ * the order in which partial results are added (kept to the same precision).  A sequence may be listed more
+ * than once.  Layers with a sliding window (rings are never shared) and calls without a common prefix of at
+ * least MIXATTN_MIN_SHARED_TOKENS tokens run as mixattn_decode, with its bits. */
+#define MIXATTN_MIN_SHARED_TOKENS 128
+int mixattn_decode_shared(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32_t* seq_ids,
+                          const void* q, void* out, void* stream);
+
+/* Makes mixattn_decode and mixattn_decode_layers take the path of mixattn_decode_shared (enable != 0)
+ * or not (0, as at first).  Errors: INVALID_ARG for a null context. */
+int mixattn_set_prefix_sharing(mixattn_ctx* ctx, int32_t enable);
+
+/* Cached tokens of `layer` that a mixattn_decode_shared of these sequences reads (a token that
+ * several sequences read at once counts once); mixattn_decode reads the sum of their lengths (of what their
+ * windows hold).  Errors: INVALID_ARG, BAD_SEQ. */
+int mixattn_get_distinct_tokens(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32_t* seq_ids,
+                                int64_t* tokens);
 
 /* Prompt attention of `layer` for n_seqs sequences that start at position 0
  * (Section 3; causal as in Section 1).  Query i attends to keys j <= i
@@ -365,6 +433,60 @@ int mixattn_beam_select(mixattn_ctx* ctx, int32_t n_groups, int32_t n_beams, int
                         const uint8_t* finished, int32_t eos_token, int32_t n_out, float* out_scores,
                         int32_t* out_beams, int32_t* out_tokens, void* stream);
 
+/* What mixattn_adjust_logits applies; members that are NULL or 0 are left out.  All arrays are device memory.
+ *   tokens       [n_rows] lists of up to max_tokens tokens, token_stride elements apart: what the row
+ *                has read and written so far.  n_tokens[row] of them count (all max_tokens if
+ *                NULL; values outside 0 .. max_tokens are taken to the nearest), the first
+ *                n_prompt[row] (0 if NULL) are the prompt, the others were generated.  Entries outside the
+ *                vocabulary are ignored
+ *   repetition, frequency, presence, temperature
+ *                one value per row; repetition and temperature must be > 0
+ *   bias_tokens, bias_values
+ *                [n_rows, n_bias], dense; entries outside the vocabulary are ignored, of several for
+ *                one token the last one counts
+ *   allowed      [n_allowed] bit masks of the vocabulary, allowed_stride 32-bit words apart: bit t % 32 of word
+ *                t / 32 is set if token t may follow
+ *   allowed_rows [n_rows] mask of each row; a value outside 0 .. n_allowed - 1 = no mask.  NULL: row r
+ *                has mask r */
+typedef struct {
+  const int32_t* tokens;
+  int64_t token_stride;
+  int32_t max_tokens;
+  const int32_t* n_tokens;
+  const int32_t* n_prompt;
+  const float* repetition;
+  const float* frequency;
+  const float* presence;
+  const float* temperature;
+  const int32_t* bias_tokens;
+  const float* bias_values;
+  int32_t n_bias;
+  const uint32_t* allowed;
+  int64_t allowed_stride;
+  int32_t n_allowed;
+  const int32_t* allowed_rows;
+} mixattn_logit_rules;
+
+/* Adjusts logits ahead of the choice of the next token (mixattn_beam_select, sampling).  Per row and
+ * token, with x its logit, c the times the row has generated it and `seen` whether it is in the list at all:
+ *     a = seen ? (x > 0 ? x / repetition : x * repetition) : x
+ *     b = a - frequency * c - (c > 0 ? presence : 0)
+ *     y = (b + bias) / temperature        tokens that the mask does not allow: -infinity
+ * in fp32, rounded once where the output is bf16.  Infinite and NaN logits go through the formula as
+ * they are; a row whose mask allows nothing is all -infinity.
+ *   logits, out  device, n_rows rows of `vocab` elements of logits_dtype / out_dtype (MIXATTN_F32 or
+ *                MIXATTN_BF16; an fp32 row cannot become a bf16 one), row_stride / out_stride elements
+ *                apart, any alignment.  out == logits with the same type and stride adjusts in place (elements that
+ *                nothing changes are then not touched); otherwise the two must not overlap
+ * Errors: INVALID_ARG (null, sizes out of range: vocab 1 .. MIXATTN_MAX_VOCAB, max_tokens 0 ..
+ * MIXATTN_MAX_RULE_TOKENS, n_bias 0 .. MIXATTN_MAX_RULE_BIASES; a stride below the row's size or so large that 64-bit byte
+ * offsets overflow; an array without its partner), UNSUPPORTED (fp32 to bf16), CUDA. */
+#define MIXATTN_MAX_RULE_TOKENS ((1 << 20) - 1)
+#define MIXATTN_MAX_RULE_BIASES 2047
+int mixattn_adjust_logits(mixattn_ctx* ctx, int32_t n_rows, int32_t vocab, int32_t logits_dtype, const void* logits,
+                          int64_t row_stride, int32_t out_dtype, void* out, int64_t out_stride,
+                          const mixattn_logit_rules* rules, void* stream);
+
 /* Size of the static device array behind mixattn_decode_static_scratch. */
 #define MIXATTN_STATIC_SCRATCH_BYTES (8u << 20)
 
@@ -469,7 +591,11 @@ enum {
   MIXATTN_K_FORK = 7,           /* copies of a fork                                         */
   MIXATTN_K_READ = 8,           /* mixattn_read_kv                                          */
   MIXATTN_K_SELECT = 9,         /* beam selection                                           */
-  MIXATTN_K_COUNT = 10
+  MIXATTN_K_SHARED = 10,        /* mixattn_decode_shared: attention over the tree            */
+  MIXATTN_K_MERGE = 11,         /* the merge of its partial results                         */
+  MIXATTN_K_ROPE = 12,          /* mixattn_rope_qkv                                         */
+  MIXATTN_K_ADJUST = 13,        /* mixattn_adjust_logits                                    */
+  MIXATTN_K_COUNT = 14
 };
 
 /* enable != 0: from now on every kernel launch is bracketed by CUDA events on

@@ -30,6 +30,9 @@ ERR_CUDA = -8
 ERR_TOO_LARGE = -9
 
 K_APPEND, K_DECODE_FULL, K_DECODE_SLIDING, K_COMBINE, K_PREFILL_FULL, K_PREFILL_SLIDING, K_GATHER, K_FORK, K_READ, K_SELECT = range(10)
+K_SHARED, K_MERGE, K_ROPE, K_ADJUST = range(10, 14)
+MIN_SHARED_TOKENS = 128
+MAX_RULE_TOKENS, MAX_RULE_BIASES = (1 << 20) - 1, 2047
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmixattn.so")
 
@@ -58,6 +61,47 @@ class Config(C.Structure):
         ("chunk_scratch_tokens", C.c_int32),
         ("kv_format", C.c_int32),
     ]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("halves", C.c_int32), ("theta", C.c_double),
+                ("inv_freq", C.POINTER(C.c_double)), ("scale", C.c_float)]
+
+
+class LogitRules(C.Structure):
+    _fields_ = [
+        ("tokens", C.c_void_p),
+        ("token_stride", C.c_int64),
+        ("max_tokens", C.c_int32),
+        ("n_tokens", C.c_void_p),
+        ("n_prompt", C.c_void_p),
+        ("repetition", C.c_void_p),
+        ("frequency", C.c_void_p),
+        ("presence", C.c_void_p),
+        ("temperature", C.c_void_p),
+        ("bias_tokens", C.c_void_p),
+        ("bias_values", C.c_void_p),
+        ("n_bias", C.c_int32),
+        ("allowed", C.c_void_p),
+        ("allowed_stride", C.c_int64),
+        ("n_allowed", C.c_int32),
+        ("allowed_rows", C.c_void_p),
+    ]
+
+
+class Rope:
+    """A rotary embedding (mixattn_rope): `rotary_dim` channels, pairs (2p, 2p + 1) or, with `halves`,
+    (p, p + rotary_dim / 2), turned by position * theta^(-2p / rotary_dim), or by position * inv_freq[p]."""
+
+    def __init__(self, rotary_dim: int, theta: float = 10000.0, inv_freq=None, halves: bool = False, scale: float = 1.0):
+        self._freq = None
+        if inv_freq is not None:
+            self._freq = np.array(inv_freq, dtype=np.float64)
+            if self._freq.shape != (rotary_dim // 2,):
+                raise MixAttnError(ERR_INVALID_ARG, "Rope: one frequency per pair of channels")
+        self.desc = RopeDesc(int(rotary_dim), int(bool(halves)), float(theta),
+                             None if self._freq is None else self._freq.ctypes.data_as(C.POINTER(C.c_double)), float(scale))
+        self.ref = C.byref(self.desc)
 
 
 def _load() -> C.CDLL:
@@ -94,6 +138,12 @@ def _load() -> C.CDLL:
         "mixattn_get_stored": [vp, i32, i32, p32, p32],
         "mixattn_read_kv": [vp, i32, i32, p32, p32, p32, vp, vp, vp],
         "mixattn_beam_select": [vp, i32, i32, i32, i32, vp, C.c_int64, vp, vp, i32, i32, vp, vp, vp, vp],
+        "mixattn_decode_shared": [vp, i32, i32, p32, vp, vp, vp],
+        "mixattn_set_prefix_sharing": [vp, i32],
+        "mixattn_get_distinct_tokens": [vp, i32, i32, p32, C.POINTER(C.c_int64)],
+        "mixattn_rope_qkv": [vp, i32, i32, p32, p32, p32, C.POINTER(RopeDesc), vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, i32,
+                             vp, vp, vp, vp],
+        "mixattn_adjust_logits": [vp, i32, i32, i32, vp, C.c_int64, i32, vp, C.c_int64, C.POINTER(LogitRules), vp],
         "mixattn_set_split_tokens": [vp, i32],
         "mixattn_set_chunk_gather_reuse": [vp, i32],
         "mixattn_set_chunk_ring_direct": [vp, i32],
@@ -115,6 +165,7 @@ EXPORTS = [
     "mixattn_arena_bytes", "mixattn_cache_bytes", "mixattn_create", "mixattn_destroy",
     "mixattn_seq_reset", "mixattn_append_kv", "mixattn_append_kv_rope", "mixattn_decode", "mixattn_decode_static_scratch", "mixattn_decode_layers", "mixattn_prefill",
     "mixattn_attend_chunk", "mixattn_set_layer_scores", "mixattn_fork_seqs", "mixattn_read_kv", "mixattn_beam_select",
+    "mixattn_decode_shared", "mixattn_set_prefix_sharing", "mixattn_get_distinct_tokens", "mixattn_rope_qkv", "mixattn_adjust_logits",
     "mixattn_get_stored",
     "mixattn_get_len", "mixattn_get_block_table", "mixattn_get_n_free_pages",
     "mixattn_get_ring_state", "mixattn_locate", "mixattn_debug_read_kv", "mixattn_debug_read_kv_fp8",
@@ -312,6 +363,98 @@ class Context:
         return lib.mixattn_decode_static_scratch(self.h, layer, len(s), _p32(s), _dev(q), _dev(out),
                                                  _stream(stream))
 
+    def rc_decode_shared(self, layer, seq_ids, q, out, stream=None) -> int:
+        s, n = _ints(seq_ids)
+        return lib.mixattn_decode_shared(self.h, layer, n, s, _dev(q), _dev(out), _stream(stream))
+
+    def decode_shared(self, layer, seq_ids, q, out, stream=None):
+        """decode() that reads pages shared by several of the sequences (forks of one prompt) once for all."""
+        rc = self.rc_decode_shared(layer, seq_ids, q, out, stream)
+        if rc:
+            raise MixAttnError(rc, "mixattn_decode_shared")
+
+    def set_prefix_sharing(self, enable: bool):
+        """decode() and decode_layers() go the way of decode_shared() (off at first)."""
+        rc = lib.mixattn_set_prefix_sharing(self.h, 1 if enable else 0)
+        if rc:
+            raise MixAttnError(rc, "mixattn_set_prefix_sharing")
+
+    def get_distinct_tokens(self, layer, seq_ids) -> int:
+        """Cached tokens that a decode_shared() of these sequences reads."""
+        s, n = _ints(seq_ids)
+        out = C.c_int64()
+        rc = lib.mixattn_get_distinct_tokens(self.h, layer, n, s, C.byref(out))
+        if rc:
+            raise MixAttnError(rc, "mixattn_get_distinct_tokens")
+        return out.value
+
+    def _rows(self, t, heads):
+        """(pointer, elements between tokens) of a [tokens, heads, head_dim] tensor whose head vectors lie
+        one after the other; None if it is not one of this context."""
+        if t is None:
+            return None, 0
+        d = self.head_dim
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or t.dtype is not self._like.dtype or t.get_device() != self._device:
+            return None
+        a, b, c = t.stride()
+        if c != 1 or (heads > 1 and b != d):
+            return None
+        return t.data_ptr(), a
+
+    def rope_qkv(self, layer, seq_ids, n_new, rope, q=None, k=None, v=None, store=False, first_pos=None, out=True, stream=None):
+        """Rotates q [tokens, Hq, D] and k [tokens, Hkv, D] (views of one projection are fine) at their
+        positions (default: behind what the cache holds) and returns (q, k, v) as dense tensors, None for
+        what was not given; with `store`, k and v are appended to the cache instead of being returned.
+        `out`: False if nothing is to be returned, or a triple of dense tensors (or None) to write to.
+        The new tensors belong to `stream` (default: the default stream)."""
+        def refuse():
+            raise MixAttnError(ERR_INVALID_ARG, "mixattn_rope_qkv")
+        s, m = _ints(seq_ids)
+        n = p = None
+        if n_new is not None:
+            n, mn = _ints(n_new)
+            if mn != m:
+                refuse()
+        if first_pos is not None:
+            p, mp = _ints(first_pos)
+            if mp != m:
+                refuse()
+        if self._like is None:
+            if q is not None or k is not None or v is not None or not store:
+                raise MixAttnError(ERR_CUDA, "mixattn_rope_qkv")
+            rc = lib.mixattn_rope_qkv(self.h, layer, m, s, n, p, rope.ref, None, 0, None, 0, None, 0, 1, None, None, None, None)
+            if rc:
+                raise MixAttnError(rc, "mixattn_rope_qkv")
+            return None, None, None
+        tokens = m if n is None else sum(n[:m])
+        hq, hkv, d = self.n_q_heads, self.n_kv_heads, self.head_dim
+        rq, rk, rv = self._rows(q, hq), self._rows(k, hkv), self._rows(v, hkv)
+        if rq is None or rk is None or rv is None:
+            refuse()
+        for t in (q, k, v):
+            if t is not None and t.shape[0] != tokens:
+                refuse()
+        stream = _stream(stream)
+        outs = [None, None, None]
+        if out is True:
+            if q is not None:
+                outs[0] = self._empty(self._like, (tokens, hq, d), stream)
+            if not store:
+                if k is not None:
+                    outs[1] = self._empty(self._like, (tokens, hkv, d), stream)
+                if v is not None:
+                    outs[2] = self._empty(self._like, (tokens, hkv, d), stream)
+        elif out:
+            outs = list(out)
+            for t, h in zip(outs, (hq, hkv, hkv)):
+                if t is not None and (self._rows(t, h) is None or t.shape[0] != tokens or not t.is_contiguous()):
+                    refuse()
+        rc = lib.mixattn_rope_qkv(self.h, layer, m, s, n, p, rope.ref, rq[0], rq[1], rk[0], rk[1], rv[0], rv[1], 1 if store else 0,
+                                  _dev(outs[0]), _dev(outs[1]), _dev(outs[2]), stream)
+        if rc:
+            raise MixAttnError(rc, "mixattn_rope_qkv")
+        return tuple(outs)
+
     def pointer_table(self, tensors):
         """Host array of device pointers, one per layer (None -> NULL), for mixattn_decode_layers.
         `tensors` maps a layer index to a tensor, or is a sequence indexed by layer."""
@@ -482,6 +625,73 @@ class Context:
             raise MixAttnError(rc, "mixattn_beam_select")
         s, b, t = out.unbind(0)      # (while the kernel runs)
         return s.view(_get_torch().float32), b, t
+
+    def rc_adjust_logits(self, logits, out=None, tokens=None, n_tokens=None, n_prompt=None, repetition=None, frequency=None,
+                         presence=None, temperature=None, bias_tokens=None, bias_values=None, allowed=None, allowed_rows=None,
+                         stream=None) -> int:
+        torch = _get_torch()
+        if self._like is None:
+            return ERR_CUDA
+        out = logits if out is None else out
+        if logits.dim() != 2 or out.shape != logits.shape:
+            return ERR_INVALID_ARG
+        types = {torch.bfloat16: BF16, torch.float32: F32}
+        rows, vocab = logits.shape
+        dev = self._device
+        r = LogitRules()
+
+        def matrix(t, dtype):       # rows of a tensor, its last dimension dense: (pointer, elements between rows), or None
+            if t.dim() != 2 or (dtype is not None and t.dtype is not dtype) or t.get_device() != dev or (t.shape[1] > 1 and t.stride(1) != 1):
+                return None
+            # (a single row or an expanded one has no stride of its own to check)
+            return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+        strides = []
+        for t in (logits, out):
+            at = matrix(t, None)
+            if t.dtype not in types or at is None:
+                return ERR_INVALID_ARG
+            strides.append(at[1])
+        for name, t, dtype in (("n_tokens", n_tokens, torch.int32), ("n_prompt", n_prompt, torch.int32), ("repetition", repetition, torch.float32),
+                               ("frequency", frequency, torch.float32), ("presence", presence, torch.float32),
+                               ("temperature", temperature, torch.float32), ("allowed_rows", allowed_rows, torch.int32)):
+            if t is not None:
+                if t.dtype is not dtype or t.shape != (rows,) or not t.is_contiguous() or t.get_device() != dev:
+                    return ERR_INVALID_ARG
+                setattr(r, name, t.data_ptr())
+        if tokens is not None and tokens.dim() == 2 and tokens.shape[1] == 0:    # (empty lists)
+            tokens, r.n_tokens, r.n_prompt = None, None, None
+        if tokens is not None:
+            at = matrix(tokens, torch.int32)
+            if at is None or tokens.shape[0] != rows:
+                return ERR_INVALID_ARG
+            r.tokens, r.token_stride = at
+            r.max_tokens = tokens.shape[1]
+        if (bias_tokens is None) != (bias_values is None):
+            return ERR_INVALID_ARG
+        if bias_tokens is not None:
+            for t, dtype in ((bias_tokens, torch.int32), (bias_values, torch.float32)):
+                if t.dtype is not dtype or t.dim() != 2 or t.shape != (rows, bias_tokens.shape[1]) or not t.is_contiguous() or t.get_device() != dev:
+                    return ERR_INVALID_ARG
+            r.bias_tokens, r.bias_values, r.n_bias = bias_tokens.data_ptr(), bias_values.data_ptr(), bias_tokens.shape[1]
+        if allowed is not None:
+            at = matrix(allowed, torch.int32)
+            if at is None or allowed.shape[1] < (vocab + 31) // 32:
+                return ERR_INVALID_ARG
+            r.allowed, r.allowed_stride = at
+            r.n_allowed = allowed.shape[0]
+        return lib.mixattn_adjust_logits(self.h, rows, vocab, types[logits.dtype], logits.data_ptr(), strides[0], types[out.dtype],
+                                         out.data_ptr(), strides[1], C.byref(r), _stream(stream))
+
+    def adjust_logits(self, logits, out=None, **rules):
+        """Penalties for the tokens of a row's list, biases, temperature and grammar masks on logits [rows, vocab], in
+        place or into `out`.  Rules, all optional: tokens int32 [rows, n] with n_tokens and n_prompt int32
+        [rows]; repetition, frequency, presence, temperature fp32 [rows]; bias_tokens int32 and bias_values
+        fp32 [rows, n]; allowed int32 [masks, words] (bit t % 32 of word t // 32) with allowed_rows int32 [rows];
+        stream (default: the default stream)."""
+        rc = self.rc_adjust_logits(logits, out, **rules)
+        if rc:
+            raise MixAttnError(rc, "mixattn_adjust_logits")
 
     def seq_reset(self, seq):
         rc = lib.mixattn_seq_reset(self.h, seq)

@@ -11,6 +11,7 @@
 
 #include "cache_manager.hpp"
 #include "internal.h"
+#include "share_plan.hpp"
 
 using namespace mixattn;
 
@@ -111,6 +112,7 @@ struct mixattn_ctx {
   // Chunk calls of sliding-window layers whose window is a whole number of key tiles read the
   // cached keys in place from the ring (no copy); off = every chunk call copies.
   bool chunk_ring_direct = true;
+  bool prefix_sharing = false;   // decode calls go the way of mixattn_decode_shared
   uint64_t cache_epoch = 0;   // bumped by every call that changes a cache
   struct GatherKey {
     bool valid = false;
@@ -186,6 +188,26 @@ int validate_config(const mixattn_config* cfg, CacheManager* cm, bool allocate =
   return MIXATTN_OK;
 }
 
+// Block-table entries of a bulk append: they travel in kernel parameters (no host copy that would
+// wait for the stream or depend on pageable memory) and are set by a small kernel ahead of the one
+// that stores the tokens, which reads the table.
+int enqueue_grants(mixattn_ctx* c, const std::vector<PageGrant>& grants, cudaStream_t st) {
+  const int stride = c->cm.max_blocks();
+  TableSetParams tp;
+  tp.table = c->dev_table();
+  for (size_t a = 0; a < grants.size(); a += kTableSetMax) {
+    const size_t n = grants.size() - a < (size_t)kTableSetMax ? grants.size() - a : (size_t)kTableSetMax;
+    for (size_t i = 0; i < n; ++i) {
+      tp.idx[i] = c->cm.slot(grants[a + i].seq) * stride + grants[a + i].block;
+      tp.page[i] = grants[a + i].page;
+    }
+    tp.n = (int32_t)n;
+    cudaError_t e = launch_recorded(c, MIXATTN_K_APPEND, st, [&] { return launch_table_set(tp, st); });
+    if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
+  }
+  return MIXATTN_OK;
+}
+
 // Enqueues the device side of an append the host bookkeeping has already applied.
 int enqueue_append(mixattn_ctx* c, int layer, int n_seqs, const int32_t* seq_ids,
                    const int32_t* n_new, const std::vector<int32_t>& start_pos,
@@ -197,21 +219,8 @@ int enqueue_append(mixattn_ctx* c, int layer, int n_seqs, const int32_t* seq_ids
   for (int i = 0; i < n_seqs; ++i) single = single && (n_new == nullptr || n_new[i] == 1);
   const int stride = c->cm.max_blocks();
   if (!ring && !single && !grants.empty()) {
-    // bulk append: the new table entries travel in kernel parameters (no host copy that would
-    // wait for the stream or depend on pageable memory) and are set by a small kernel ahead of
-    // the copy kernel, which reads the table
-    TableSetParams tp;
-    tp.table = c->dev_table();
-    for (size_t a = 0; a < grants.size(); a += kTableSetMax) {
-      const size_t n = grants.size() - a < (size_t)kTableSetMax ? grants.size() - a : (size_t)kTableSetMax;
-      for (size_t i = 0; i < n; ++i) {
-        tp.idx[i] = c->cm.slot(grants[a + i].seq) * stride + grants[a + i].block;
-        tp.page[i] = grants[a + i].page;
-      }
-      tp.n = (int32_t)n;
-      cudaError_t e = launch_recorded(c, MIXATTN_K_APPEND, st, [&] { return launch_table_set(tp, st); });
-      if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
-    }
+    const int rc = enqueue_grants(c, grants, st);
+    if (rc != MIXATTN_OK) return rc;
   }
   AppendParams p;
   p.k = k;
@@ -316,7 +325,8 @@ int mixattn_create(const mixattn_config* cfg, mixattn_ctx** out) {
     c->sm_count = sms;
     c->l2_bytes = l2;
     if (prepare_decode_bf16() != cudaSuccess || prepare_prefill_tc() != cudaSuccess ||
-        prepare_beam_select() != cudaSuccess) { delete c; return MIXATTN_ERR_CUDA; }
+        prepare_beam_select() != cudaSuccess || prepare_decode_shared() != cudaSuccess ||
+        prepare_adjust_logits() != cudaSuccess) { delete c; return MIXATTN_ERR_CUDA; }
     if (cudaMemsetAsync(c->arena, 0, c->plan.total, 0) != cudaSuccess ||
         cudaStreamSynchronize(0) != cudaSuccess) {
       delete c;
@@ -589,6 +599,188 @@ int mixattn_append_kv_rope(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const 
   return append_impl(c, layer, n_seqs, seq_ids, n_new, k, v, stream, log2((double)rope_theta));
 }
 
+int mixattn_rope_qkv(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t* seq_ids, const int32_t* n_new,
+                     const int32_t* first_pos, const mixattn_rope* rope, const void* q, int64_t q_stride, const void* k,
+                     int64_t k_stride, const void* v, int64_t v_stride, int32_t store, void* q_out, void* k_out,
+                     void* v_out, void* stream) {
+  if (c == nullptr || !c->cm.valid_layer(layer) || n_seqs < 0 || (n_seqs > 0 && seq_ids == nullptr) || rope == nullptr ||
+      (store != 0 && store != 1))
+    return MIXATTN_ERR_INVALID_ARG;
+  RopeParams p;
+  p.rotary = rope->rotary_dim;
+  if (p.rotary < 16 || p.rotary > c->cfg.head_dim || p.rotary % 16 != 0) return MIXATTN_ERR_INVALID_ARG;
+  if (rope->inv_freq == nullptr && !(rope->theta > 1.0 && isfinite(rope->theta))) return MIXATTN_ERR_INVALID_ARG;
+  if (!(rope->scale >= 0.f) || !isfinite(rope->scale)) return MIXATTN_ERR_INVALID_ARG;
+  for (int i = 0; i < p.rotary / 2; ++i) {
+    p.freq[i] = rope->inv_freq ? rope->inv_freq[i] : pow(rope->theta, -2.0 * i / p.rotary);
+    if (!(fabs(p.freq[i]) <= 1e6)) return MIXATTN_ERR_INVALID_ARG;   // (NaN, or more than a double's angle can carry)
+  }
+  p.scale = rope->scale > 0.f ? rope->scale : 1.f;
+  p.halves = rope->halves != 0;
+  const LayerInfo& li = c->cm.layer(layer);
+  const int Hq = c->cfg.n_q_heads, Hkv = c->cfg.n_kv_heads, D = c->cfg.head_dim, esz = c->geom.elem_bytes;
+  if (store) {
+    try {
+      const int rc = c->cm.check_append(layer, n_seqs, seq_ids, n_new);
+      if (rc != MIXATTN_OK) return rc;
+    } catch (const std::bad_alloc&) {
+      return MIXATTN_ERR_CUDA;
+    }
+  }
+  int64_t total = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    if (!c->cm.valid_seq(seq_ids[i])) return MIXATTN_ERR_BAD_SEQ;
+    const int64_t n = n_new ? n_new[i] : 1, at = first_pos ? first_pos[i] : c->cm.len(layer, seq_ids[i]);
+    if (n < 0 || at < 0 || at + n > INT32_MAX) return MIXATTN_ERR_INVALID_ARG;
+    total += n;
+  }
+  if (total > INT32_MAX) return MIXATTN_ERR_INVALID_ARG;
+  if (!c->host_only && c->sticky_cuda_error) return MIXATTN_ERR_CUDA;
+  if (c->host_only && !store) return MIXATTN_ERR_CUDA;
+  if (!c->host_only && total > 0) {
+    if ((q == nullptr && k == nullptr && v == nullptr) || (store && (k == nullptr || v == nullptr)) ||
+        (q_out != nullptr && q == nullptr) || (k_out != nullptr && k == nullptr) || (v_out != nullptr && v == nullptr))
+      return MIXATTN_ERR_INVALID_ARG;
+    const void* in[3] = {q, k, v};
+    const int64_t stride[3] = {q_stride, k_stride, v_stride};
+    for (int i = 0; i < 3; ++i) {
+      if (in[i] == nullptr) continue;
+      const int64_t least = (int64_t)(i == 0 ? Hq : Hkv) * D;
+      if (total > 1 && (stride[i] < least || stride[i] > INT64_MAX / esz / total || stride[i] * esz % 16 != 0)) return MIXATTN_ERR_INVALID_ARG;
+    }
+    if (((size_t)q | (size_t)k | (size_t)v | (size_t)q_out | (size_t)k_out | (size_t)v_out) & 15) return MIXATTN_ERR_INVALID_ARG;
+  }
+  std::vector<int32_t> start;
+  std::vector<PageGrant> grants;
+  bool moved = false;
+  try {
+    start.resize(n_seqs);
+    for (int i = 0; i < n_seqs; ++i) start[i] = c->cm.len(layer, seq_ids[i]);
+    if (store) {
+      moved = true;
+      c->cm.apply_append(layer, n_seqs, seq_ids, n_new, &grants);
+      ++c->cache_epoch;
+    }
+  } catch (const std::bad_alloc&) {   // no host memory: the bookkeeping may have moved
+    if (moved) c->sticky_cuda_error = true;
+    return MIXATTN_ERR_CUDA;
+  }
+  if (c->host_only || total == 0) return MIXATTN_OK;
+  DeviceGuard g(c->device);
+  if (!g.ok) {
+    if (store) c->sticky_cuda_error = true;
+    return MIXATTN_ERR_CUDA;
+  }
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool ring = li.kind == MIXATTN_SLIDING;
+  bool single = true;
+  for (int i = 0; i < n_seqs; ++i) single = single && (n_new == nullptr || n_new[i] == 1);
+  if (store && !ring && !single && !grants.empty()) {
+    const int rc = enqueue_grants(c, grants, st);
+    if (rc != MIXATTN_OK) return rc;
+  }
+  p.q_stride = total > 1 ? q_stride * esz : 0;
+  p.k_stride = total > 1 ? k_stride * esz : 0;
+  p.v_stride = total > 1 ? v_stride * esz : 0;
+  // (inputs that nothing is done with are not read)
+  p.q = static_cast<const char*>(q_out ? q : nullptr);
+  p.k = static_cast<const char*>(k_out || store ? k : nullptr);
+  p.v = static_cast<const char*>(v_out || store ? v : nullptr);
+  p.q_out = static_cast<char*>(q_out);
+  p.k_out = static_cast<char*>(k_out);
+  p.v_out = static_cast<char*>(v_out);
+  if (p.q == nullptr && p.k == nullptr && p.v == nullptr) return MIXATTN_OK;   // nothing is wanted
+  p.pool = store ? c->owner_storage(layer) : nullptr;
+  p.table = c->dev_table();
+  p.table_stride = c->cm.max_blocks();
+  p.is_ring = ring;
+  p.window = ring ? li.window : 0;
+  p.ring_pages = ring ? ring_pages_of(li.window) : 0;
+  p.geom = c->geom;
+  p.n_q_heads = Hq;
+  int32_t row = 0;
+  size_t gi = 0;
+  for (int i0 = 0; i0 < n_seqs; i0 += kMaxCallSeqs) {
+    p.n_entries = std::min(n_seqs - i0, kMaxCallSeqs);
+    int most = 0;
+    for (int j = 0; j < p.n_entries; ++j) {
+      const int i = i0 + j;
+      RopeEntry& e = p.e[j];
+      e.seq = c->cm.slot(seq_ids[i]);
+      e.start_pos = start[i];
+      e.pos0 = first_pos ? first_pos[i] : start[i];
+      e.n_new = n_new ? n_new[i] : 1;
+      e.row0 = row;
+      e.page_hint = e.tbl_idx = -1;
+      if (store && !ring && single) {
+        e.page_hint = c->cm.table_row(seq_ids[i])[e.start_pos / kPage];
+        if (gi < grants.size() && grants[gi].seq == seq_ids[i]) {
+          e.tbl_idx = e.seq * p.table_stride + grants[gi].block;
+          ++gi;
+        }
+      }
+      row += e.n_new;
+      most = std::max(most, e.n_new);
+    }
+    if (most == 0) continue;
+    if (launch_recorded(c, MIXATTN_K_ROPE, st, [&] { return launch_rope_qkv(p, most, st); }) != cudaSuccess)
+      return MIXATTN_ERR_CUDA;
+  }
+  return MIXATTN_OK;
+}
+
+int mixattn_adjust_logits(mixattn_ctx* c, int32_t n_rows, int32_t vocab, int32_t logits_dtype, const void* logits,
+                          int64_t row_stride, int32_t out_dtype, void* out, int64_t out_stride,
+                          const mixattn_logit_rules* rules, void* stream) {
+  if (c == nullptr || rules == nullptr || n_rows < 0 || vocab < 1 || vocab > MIXATTN_MAX_VOCAB ||
+      (logits_dtype != MIXATTN_F32 && logits_dtype != MIXATTN_BF16) || (out_dtype != MIXATTN_F32 && out_dtype != MIXATTN_BF16))
+    return MIXATTN_ERR_INVALID_ARG;
+  if (logits_dtype == MIXATTN_F32 && out_dtype == MIXATTN_BF16) return MIXATTN_ERR_UNSUPPORTED;
+  const mixattn_logit_rules& r = *rules;
+  const int64_t rows = std::max<int64_t>(n_rows, 1), limit = INT64_MAX / 8 / rows;
+  if (rows > INT32_MAX / 8) return MIXATTN_ERR_INVALID_ARG;
+  if (row_stride < vocab || out_stride < vocab || row_stride > limit || out_stride > limit) return MIXATTN_ERR_INVALID_ARG;
+  if (r.max_tokens < 0 || r.max_tokens > MIXATTN_MAX_RULE_TOKENS || r.n_bias < 0 || r.n_bias > MIXATTN_MAX_RULE_BIASES)
+    return MIXATTN_ERR_INVALID_ARG;
+  if (r.tokens != nullptr ? (r.token_stride < r.max_tokens || r.token_stride > limit)
+                          : (r.max_tokens != 0 || r.n_tokens != nullptr || r.n_prompt != nullptr))
+    return MIXATTN_ERR_INVALID_ARG;
+  if ((r.bias_tokens != nullptr) != (r.bias_values != nullptr) || (r.bias_tokens == nullptr && r.n_bias != 0)) return MIXATTN_ERR_INVALID_ARG;
+  if (r.allowed != nullptr) {
+    if (r.n_allowed < 1 || r.allowed_stride < ((int64_t)vocab + 31) / 32 || r.allowed_stride > INT64_MAX / 8 / r.n_allowed ||
+        (r.allowed_rows == nullptr && r.n_allowed < n_rows))
+      return MIXATTN_ERR_INVALID_ARG;
+  } else if (r.n_allowed != 0 || r.allowed_rows != nullptr) {
+    return MIXATTN_ERR_INVALID_ARG;
+  }
+  if (c->host_only || c->sticky_cuda_error) return MIXATTN_ERR_CUDA;
+  if (n_rows == 0) return MIXATTN_OK;
+  if (logits == nullptr || out == nullptr || (size_t)logits % (logits_dtype == MIXATTN_BF16 ? 2 : 4) != 0 ||
+      (size_t)out % (out_dtype == MIXATTN_BF16 ? 2 : 4) != 0)
+    return MIXATTN_ERR_INVALID_ARG;
+  const void* words[9] = {r.tokens, r.n_tokens, r.n_prompt, r.repetition, r.frequency, r.presence, r.temperature, r.bias_tokens, r.allowed};
+  for (const void* w : words)
+    if ((size_t)w % 4 != 0) return MIXATTN_ERR_INVALID_ARG;
+  if (((size_t)r.bias_values | (size_t)r.allowed_rows) % 4 != 0) return MIXATTN_ERR_INVALID_ARG;
+  if (logits == out && (logits_dtype != out_dtype || row_stride != out_stride)) return MIXATTN_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return MIXATTN_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  AdjustParams p;
+  p.logits = logits;
+  p.out = out;
+  p.row_stride = row_stride;
+  p.out_stride = out_stride;
+  p.n_rows = n_rows;
+  p.vocab = vocab;
+  p.in_place = logits == out;
+  p.rules = r;
+  if (r.max_tokens == 0) p.rules.tokens = nullptr;
+  if (launch_recorded(c, MIXATTN_K_ADJUST, st, [&] { return launch_adjust_logits(p, logits_dtype, out_dtype, c->sm_count, st); }) != cudaSuccess)
+    return MIXATTN_ERR_CUDA;
+  return MIXATTN_OK;
+}
+
 // L2 policy of a decode launch (see l2_policy_of in decode_bf16.cu).  Only a ring that a later
 // layer reads again (Section 3's cache sharing makes consecutive layers read the same bytes) is
 // worth keeping: the leading part of its storage, up to a share of the L2 that a cyclic scan was
@@ -703,8 +895,8 @@ static int plan_splits(const mixattn_ctx* c, int layer, const int32_t* ids, int 
   return base;
 }
 
-int mixattn_decode(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t* seq_ids,
-                   const void* q, void* out, void* stream) {
+static int decode_plain(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t* seq_ids, const void* q, void* out,
+                        void* stream) {
   if (c == nullptr || !c->cm.valid_layer(layer) || n_seqs < 0) return MIXATTN_ERR_INVALID_ARG;
   if (n_seqs > 0 && (seq_ids == nullptr || q == nullptr || out == nullptr)) return MIXATTN_ERR_INVALID_ARG;
   for (int i = 0; i < n_seqs; ++i) {
@@ -757,6 +949,154 @@ int mixattn_decode(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t*
       if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
     }
   }
+  return MIXATTN_OK;
+}
+
+// Lays the items of a tree's pieces out on the line of work units (internal.h) and cuts the line into equal
+// parts for at most max_ctas CTAs, fewer if the partial results would not fit `room` rows.  Returns
+// false if they do not fit at all.
+static bool lay_out_shared(const ShareTree& t, int max_ctas, int64_t room, SharedDecodeParams* p) {
+  const int Hkv = p->geom.n_kv_heads;
+  int64_t units = 0;
+  for (size_t v = 0; v < t.pieces.size(); ++v) {
+    const SharePiece& s = t.pieces[v];
+    const int64_t tiles = ((int64_t)s.t1 - s.t0 + p->tile_keys - 1) / p->tile_keys;
+    const int64_t chunks = ((int64_t)s.ns * p->group + p->row_chunk - 1) / p->row_chunk;
+    p->node[v] = ShareNode{s.t0, s.t1, s.slot, s.s0, s.ns, s.parent, (int32_t)units, 0, 0};
+    units += (tiles + p->item_units) * Hkv * chunks;
+    if (units > (1 << 30)) return false;
+  }
+  p->n_nodes = (int32_t)t.pieces.size();
+  p->node[p->n_nodes] = ShareNode{0, 0, 0, 0, 0, -1, (int32_t)units, 0, 0};
+  for (int64_t ctas = max_ctas;; ctas = ctas * 3 / 4) {
+    const int64_t quota = std::max<int64_t>((units + ctas - 1) / ctas, p->item_units + 1);
+    int64_t rows = 0;
+    for (int v = 0; v < p->n_nodes; ++v) {
+      ShareNode& nd = p->node[v];
+      const int64_t tiles = ((int64_t)nd.t1 - nd.t0 + p->tile_keys - 1) / p->tile_keys;
+      nd.max_segs = (int32_t)std::min<int64_t>((tiles + quota - 2) / quota + 1, ctas);
+      nd.row0 = (int32_t)rows;
+      rows += (int64_t)nd.ns * p->n_q_heads * nd.max_segs;
+      if (rows > room) break;
+    }
+    if (rows <= room) {
+      p->quota = (int32_t)quota;
+      p->n_ctas = (int32_t)((units + quota - 1) / quota);
+      return true;
+    }
+    if (ctas == 1) return false;
+  }
+}
+
+static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t* seq_ids, const void* q,
+                              void* out, void* stream) {
+  if (c == nullptr || !c->cm.valid_layer(layer) || n_seqs < 0) return MIXATTN_ERR_INVALID_ARG;
+  if (n_seqs > 0 && (seq_ids == nullptr || q == nullptr || out == nullptr)) return MIXATTN_ERR_INVALID_ARG;
+  for (int i = 0; i < n_seqs; ++i)
+    if (!c->cm.valid_seq(seq_ids[i])) return MIXATTN_ERR_BAD_SEQ;
+  for (int i = 0; i < n_seqs; ++i)
+    if (c->cm.len(layer, seq_ids[i]) < 1) return MIXATTN_ERR_EMPTY_CONTEXT;
+  if (c->host_only || c->sticky_cuda_error) return MIXATTN_ERR_CUDA;
+  if (n_seqs < 2 || c->cm.layer(layer).kind == MIXATTN_SLIDING) return decode_plain(c, layer, n_seqs, seq_ids, q, out, stream);
+  DeviceGuard g(c->device);
+  if (!g.ok) return MIXATTN_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int Hq = c->cfg.n_q_heads, Hkv = c->cfg.n_kv_heads, D = c->cfg.head_dim;
+  const size_t row_bytes = (size_t)Hq * D * c->geom.elem_bytes;
+  try {
+    ShareTree tree;
+    SharedDecodeParams p;
+    p.pool = c->owner_storage(layer);
+    p.table = c->dev_table();
+    p.table_stride = c->cm.max_blocks();
+    p.n_pages = c->cm.n_pages();
+    p.geom = c->geom;
+    p.n_q_heads = Hq;
+    p.group = Hq / Hkv;
+    p.scale_log2e = c->scale * kLog2e;
+    p.part_o = reinterpret_cast<float*>(c->arena + c->plan.part_o_off);
+    p.part_ml = reinterpret_cast<float2*>(c->arena + c->plan.part_ml_off);
+    p.status = c->dev_status();
+    p.shaped = score_shape_of(c, layer, &p.shape) ? 1 : 0;
+    p.tile_keys = 32;
+    p.row_chunk = 32;
+    p.item_units = 1;
+    const int64_t room = (int64_t)kWsChunks * Hq;
+    // (launches of kMaxCallSeqs sequences: a larger batch is cut in the caller's order)
+    for (int i0 = 0; i0 < n_seqs; i0 += kMaxCallSeqs) {
+      const int nb = std::min(n_seqs - i0, kMaxCallSeqs);
+      const int32_t* ids = seq_ids + i0;
+      const char* qb = static_cast<const char*>(q) + (size_t)i0 * row_bytes;
+      char* ob = static_cast<char*>(out) + (size_t)i0 * row_bytes;
+      bool fits = false;
+      for (int32_t least = MIXATTN_MIN_SHARED_TOKENS; !fits; least *= 2) {   // (deep trees of short pieces: only the longer ones)
+        build_share_tree(c->cm, layer, nb, ids, least, &tree);
+        if (!tree.shared) break;
+        fits = lay_out_shared(tree, 2 * c->sm_count, room, &p);
+        if (least > (1 << 29)) break;
+      }
+      if (!fits) {
+        const int rc = decode_plain(c, layer, nb, ids, qb, ob, stream);
+        if (rc != MIXATTN_OK) return rc;
+        continue;
+      }
+      p.q = qb;
+      p.out = ob;
+      p.n_seqs = nb;
+      for (int j = 0; j < nb; ++j) {
+        p.order[j] = tree.order[j];
+        p.newest[j] = c->cm.len(layer, ids[tree.order[j]]) - 1;
+        p.leaf[j] = tree.leaf[j];
+      }
+      cudaError_t e = launch_recorded(c, MIXATTN_K_SHARED, st, [&] { return launch_decode_shared(p, st); });
+      if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
+      e = launch_recorded(c, MIXATTN_K_MERGE, st, [&] { return launch_merge_shared(p, c->cfg.dtype, st); });
+      if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
+    }
+  } catch (const std::bad_alloc&) {
+    return MIXATTN_ERR_CUDA;
+  }
+  return MIXATTN_OK;
+}
+
+int mixattn_decode(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t* seq_ids,
+                   const void* q, void* out, void* stream) {
+  return c != nullptr && c->prefix_sharing ? decode_shared_impl(c, layer, n_seqs, seq_ids, q, out, stream)
+                                           : decode_plain(c, layer, n_seqs, seq_ids, q, out, stream);
+}
+
+int mixattn_decode_shared(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t* seq_ids,
+                          const void* q, void* out, void* stream) {
+  return decode_shared_impl(c, layer, n_seqs, seq_ids, q, out, stream);
+}
+
+int mixattn_set_prefix_sharing(mixattn_ctx* c, int32_t enable) {
+  if (c == nullptr) return MIXATTN_ERR_INVALID_ARG;
+  c->prefix_sharing = enable != 0;
+  return MIXATTN_OK;
+}
+
+int mixattn_get_distinct_tokens(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t* seq_ids, int64_t* tokens) {
+  if (c == nullptr || tokens == nullptr || !c->cm.valid_layer(layer) || n_seqs < 0 || (n_seqs > 0 && seq_ids == nullptr))
+    return MIXATTN_ERR_INVALID_ARG;
+  int64_t sum = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    if (!c->cm.valid_seq(seq_ids[i])) return MIXATTN_ERR_BAD_SEQ;
+    sum += c->cm.n_attended(layer, seq_ids[i]);
+  }
+  if (c->cm.layer(layer).kind == MIXATTN_FULL) {
+    try {
+      ShareTree tree;
+      sum = 0;
+      for (int i0 = 0; i0 < n_seqs; i0 += kMaxCallSeqs) {
+        build_share_tree(c->cm, layer, std::min(n_seqs - i0, kMaxCallSeqs), seq_ids + i0, MIXATTN_MIN_SHARED_TOKENS, &tree);
+        sum += tree.tokens;
+      }
+    } catch (const std::bad_alloc&) {
+      return MIXATTN_ERR_CUDA;
+    }
+  }
+  *tokens = sum;
   return MIXATTN_OK;
 }
 

@@ -1,0 +1,230 @@
+// Decode attention over a tree of shared prefixes: the form for every storage format in exact fp32 arithmetic, and
+// the merge of the partial results.
+//
+// Section 5.4's kind of workload has many requests behind the same instruction, and generation with
+// several hypotheses many behind the same prompt: their caches share pages, which a decode that goes
+// sequence by sequence reads once per sequence.  Here a node of the tree (a range of keys and the sequences that
+// have it in common) is read once for the query heads of all of its sequences: they are the rows of
+// one flash-attention pass, out = sum_j p_j v_j with p_j = e^(b_j - m), running maximum m and sum l
+// per row.  A sequence's result is the merge of the passes along its path from the root,
+//     out = sum_c o_c 2^(m_c - M) / sum_c l_c 2^(m_c - M),   M = max_c m_c.
+// How the work is cut is described with SharedDecodeParams (internal.h).
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+
+#include "internal.h"
+#include "score_shape.cuh"
+
+namespace mixattn {
+
+namespace {
+
+// ---------------------------------------------------------------- any storage, fp32 arithmetic
+// 32 rows x 32 keys per step on the CUDA cores; eight threads per row.  Serves the fp32 mode (whose
+// point is exact arithmetic); bf16 caches and quantised ones run on the tensor cores.
+constexpr int kRows = 32, kKeys = 32, kThreads = 256, kPerRow = kThreads / kRows;
+constexpr int kPad = 4;   // floats between rows: eight rows' 16-byte words fall into different banks
+
+template <int D>
+constexpr int simple_smem() { return (2 * kRows * (D + kPad) + kKeys * D + kRows * (kKeys + 1)) * 4; }
+
+// four channels 4 c .. 4 c + 3 of a stored row as fp32
+__device__ __forceinline__ float4 stored4(const char* pool, const KvGeom& ge, int64_t page, int g, int which, int tok, int c) {
+  if (ge.fp8) {
+    const float x = exp2f((float)(*reinterpret_cast<const unsigned char*>(pool + kv_exp_offset(ge, page, g, which, tok))) - 127.f);
+    float f[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int ch = 4 * c + e;
+      const int64_t at = which ? kv_fp8_v_offset(ge, page, g, ch, tok) : kv_chunk_offset(ge, page, g, 0, tok, ch >> 4) + (ch & 15);
+      f[e] = (float)*reinterpret_cast<const __nv_fp8_e4m3*>(pool + at) * x;
+    }
+    return make_float4(f[0], f[1], f[2], f[3]);
+  }
+  if (ge.elem_bytes == 4) return *reinterpret_cast<const float4*>(pool + kv_chunk_offset(ge, page, g, which, tok, c));
+  const uint2 w = *reinterpret_cast<const uint2*>(pool + kv_chunk_offset(ge, page, g, which, tok, c >> 1) + (c & 1) * 8);
+  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                     __uint_as_float(w.y & 0xffff0000u));
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads) decode_shared_kernel(const __grid_constant__ SharedDecodeParams p) {
+  extern __shared__ __align__(16) float sm[];
+  float* sq = sm;                              // [kRows][D + kPad]
+  float* sk = sq + kRows * (D + kPad);         // [kKeys][D + kPad]
+  float* sv = sk + kKeys * (D + kPad);         // [kKeys][D]
+  float* sp = sv + kKeys * D;                  // [kRows][kKeys + 1]
+  const int tid = threadIdx.x, r = tid / kPerRow, sub = tid % kPerRow;
+  const KvGeom& ge = p.geom;
+  ShareWalk w = share_begin(p, blockIdx.x);
+  ShareSegment s;
+  while (share_next(p, blockIdx.x, w, s)) {
+    const ShareNode& nd = p.node[s.node];
+    const int32_t* tbl = p.table + (int64_t)nd.slot * p.table_stride;
+    __syncthreads();   // the previous segment's reads
+    for (int e = tid; e < kRows * (D / 4); e += kThreads) {
+      const int row = e / (D / 4), c = e - row * (D / 4);
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (row < s.rows) {
+        const int R = s.row_first + row;
+        const int64_t at = ((int64_t)p.order[s.s0 + R / p.group] * p.n_q_heads + s.g * p.group + R % p.group) * D + 4 * c;
+        if (ge.elem_bytes == 4) {
+          x = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.q) + at);
+        } else {
+          const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q) + at;
+          x = make_float4(__bfloat162float(q[0]), __bfloat162float(q[1]), __bfloat162float(q[2]), __bfloat162float(q[3]));
+        }
+      }
+      *reinterpret_cast<float4*>(sq + row * (D + kPad) + 4 * c) = x;
+    }
+    const int R = s.row_first + min(r, s.rows - 1);
+    const int newest = p.newest[s.s0 + R / p.group];
+    const float slope = p.shaped && p.shape.biased ? p.shape.slope[s.g * p.group + R % p.group] : 0.f;
+    float m = -INFINITY, l = 0.f, o[D / kPerRow];
+#pragma unroll
+    for (int j = 0; j < D / kPerRow; ++j) o[j] = 0.f;
+    for (int t = s.t0; t < s.t1; t += kKeys) {
+      __syncthreads();
+      for (int e = tid; e < 2 * kKeys * (D / 4); e += kThreads) {
+        const int which = e / (kKeys * (D / 4)), f = e - which * kKeys * (D / 4), key = f / (D / 4), c = f - key * (D / 4);
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);   // (what lies behind the last key is not read)
+        if (t + key < s.t1) x = stored4(p.pool, ge, tbl[(t + key) / kPage], s.g, which, (t + key) % kPage, c);
+        *reinterpret_cast<float4*>(which ? sv + key * D + 4 * c : sk + key * (D + kPad) + 4 * c) = x;
+      }
+      __syncthreads();
+      float x[kKeys / kPerRow];   // keys sub, sub + 8, ...
+#pragma unroll
+      for (int j = 0; j < kKeys / kPerRow; ++j) x[j] = 0.f;
+#pragma unroll 4
+      for (int c = 0; c < D; c += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(sq + r * (D + kPad) + c);
+#pragma unroll
+        for (int j = 0; j < kKeys / kPerRow; ++j) {
+          const float4 k = *reinterpret_cast<const float4*>(sk + (sub + kPerRow * j) * (D + kPad) + c);
+          x[j] = fmaf(q.w, k.w, fmaf(q.z, k.z, fmaf(q.y, k.y, fmaf(q.x, k.x, x[j]))));
+        }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < kKeys / kPerRow; ++j) {
+        const int key = t + sub + kPerRow * j;
+        const float y = p.shaped ? shaped_score_exact(x[j], p.shape, -slope * (float)(newest - key)) : x[j] * p.scale_log2e;
+        x[j] = key < s.t1 ? y : -INFINITY;
+        mx = fmaxf(mx, x[j]);
+      }
+#pragma unroll
+      for (int sh = 1; sh < kPerRow; sh <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, sh));
+      const float mn = fmaxf(m, mx), a = exp2f(m - mn);   // (the step's first key is there, so mn is finite)
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < kKeys / kPerRow; ++j) {
+        x[j] = exp2f(x[j] - mn);
+        sum += x[j];
+        sp[r * (kKeys + 1) + sub + kPerRow * j] = x[j];
+      }
+#pragma unroll
+      for (int sh = 1; sh < kPerRow; sh <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, sh);
+      m = mn;
+      l = l * a + sum;
+      __syncwarp();   // (a row's eight threads are in one warp)
+#pragma unroll
+      for (int j = 0; j < D / kPerRow; ++j) o[j] *= a;
+#pragma unroll 4
+      for (int key = 0; key < kKeys; ++key) {
+        const float pe = sp[r * (kKeys + 1) + key];
+#pragma unroll
+        for (int j = 0; j < D / kPerRow; ++j) o[j] = fmaf(pe, sv[key * D + sub + kPerRow * j], o[j]);
+      }
+      __syncwarp();
+    }
+    if (r < s.rows) {
+      float* to = p.part_o + (int64_t)s.seg_row * D;
+#pragma unroll
+      for (int j = 0; j < D / kPerRow; ++j) {
+        const int d = sub + kPerRow * j;
+        to[(d / 4) * s.rows * 4 + r * 4 + d % 4] = o[j];
+      }
+      if (sub == 0) p.part_ml[s.seg_row + r] = make_float2(m, l);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- merge
+// One thread per four channels of an output row; the partials of a segment lie [D / 4][rows][4], so
+// that the tensor-core kernel, which has a row per thread, writes them in whole lines.
+constexpr int kMergeThreads = 128;
+
+template <typename T>
+__global__ void __launch_bounds__(kMergeThreads) merge_shared_kernel(const __grid_constant__ SharedDecodeParams p) {
+  const int D = p.geom.head_dim, per_row = D / 4;
+  const int e = blockIdx.x * kMergeThreads + threadIdx.x, h = e / per_row, c4 = e - h * per_row;
+  const int i = blockIdx.y;
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // (a no-op after an ordinary launch)
+  if (h >= p.n_q_heads) return;
+  const int g = h / p.group, hh = h - g * p.group;
+  float M = -INFINITY, L = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int v = p.leaf[i]; v >= 0; v = p.node[v].parent) {
+    const ShareNode& nd = p.node[v];
+    const int tiles = (nd.t1 - nd.t0 + p.tile_keys - 1) / p.tile_keys;
+    const int all = nd.ns * p.group, chunks = (all + p.row_chunk - 1) / p.row_chunk;
+    const int R = (i - nd.s0) * p.group + hh, rc = R / p.row_chunk, rows = min(p.row_chunk, all - rc * p.row_chunk);
+    const int a = nd.unit0 + (g * chunks + rc) * (tiles + p.item_units) + p.item_units;
+    const int n = (a + tiles - 1) / p.quota - a / p.quota + 1;
+    const int base = nd.row0 + (g * all + rc * p.row_chunk) * nd.max_segs, r = R - rc * p.row_chunk;
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+      const int row0 = base + k * rows;
+      const float2 ml = p.part_ml[row0 + r];
+      const float4 o = *reinterpret_cast<const float4*>(p.part_o + (int64_t)row0 * D + ((int64_t)c4 * rows + r) * 4);
+      const float mn = fmaxf(M, ml.x), s0 = exp2f(M - mn), s1 = exp2f(ml.x - mn);   // (every segment has a key: mn is finite)
+      M = mn;
+      L = L * s0 + ml.y * s1;
+      acc.x = acc.x * s0 + o.x * s1;
+      acc.y = acc.y * s0 + o.y * s1;
+      acc.z = acc.z * s0 + o.z * s1;
+      acc.w = acc.w * s0 + o.w * s1;
+    }
+  }
+  const float inv = 1.f / L;
+  const int64_t at = ((int64_t)p.order[i] * p.n_q_heads + h) * D + 4 * c4;
+  if constexpr (sizeof(T) == 2) {
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+    *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at) =
+        make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+  } else {
+    *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + at) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+  }
+}
+
+}  // namespace
+
+cudaError_t prepare_decode_shared() {
+  constexpr auto kAttr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(decode_shared_kernel<128>, kAttr, simple_smem<128>());
+  return e == cudaSuccess ? cudaFuncSetAttribute(decode_shared_kernel<64>, kAttr, simple_smem<64>()) : e;
+}
+
+cudaError_t launch_decode_shared(const SharedDecodeParams& p, cudaStream_t st) {
+  if (p.row_chunk > kRows) return cudaErrorInvalidValue;
+  if (p.geom.head_dim == 128) decode_shared_kernel<128><<<p.n_ctas, kThreads, simple_smem<128>(), st>>>(p);
+  else decode_shared_kernel<64><<<p.n_ctas, kThreads, simple_smem<64>(), st>>>(p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_merge_shared(const SharedDecodeParams& p, int dtype, cudaStream_t st) {
+  const int n = p.n_q_heads * (p.geom.head_dim / 4);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((n + kMergeThreads - 1) / kMergeThreads, p.n_seqs);
+  cfg.blockDim = dim3(kMergeThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return dtype == MIXATTN_BF16 ? cudaLaunchKernelEx(&cfg, merge_shared_kernel<__nv_bfloat16>, p)
+                               : cudaLaunchKernelEx(&cfg, merge_shared_kernel<float>, p);
+}
+
+}  // namespace mixattn

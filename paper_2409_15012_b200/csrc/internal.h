@@ -271,6 +271,134 @@ struct BeamParams {
   int32_t* tickets;          // [n_groups] CTAs that have finished; 0 before and after a call
 };
 
+// Decode over a tree of shared prefixes (mixattn_decode_shared; the tree is built by share_plan.hpp).
+// A node is a range of keys that the sequences [s0, s0 + ns) of the launch (in tree order) have in
+// common; its rows are their query heads of one KV head, sequence-major, handled in chunks of
+// `row_chunk`.  An item is (node, KV head, chunk of rows) with its keys cut into tiles; items are laid
+// out one after the other on a line of work units, one per tile plus `item_units` in front for
+// the item's own cost, and CTA c walks units [c quota, (c + 1) quota).  What a CTA finds of an item is a
+// segment: it leaves unnormalised partial outputs, maxima and sums for the merge.
+constexpr int kMaxShareNodes = 2 * kMaxCallSeqs;
+struct ShareNode {
+  int32_t t0, t1;     // keys [t0, t1); t0 is a multiple of the page size
+  int32_t slot;       // storage slot whose block table names the pages
+  int32_t s0, ns;     // sequences, in tree order
+  int32_t parent;     // node that ends where this one begins, -1 = none
+  int32_t unit0;      // first work unit
+  int32_t row0;       // first row of partial results
+  int32_t max_segs;   // segments of an item, at most
+};
+struct SharedDecodeParams {
+  const void* q;          // [n_seqs, Hq, D], caller's order
+  void* out;
+  const char* pool;
+  const int32_t* table;
+  int32_t table_stride;
+  int32_t n_pages;
+  KvGeom geom;
+  int32_t n_q_heads, group;
+  float scale_log2e;
+  float* part_o;          // per segment [D / 4][rows][4]
+  float2* part_ml;        // [row]: maximum (base-2 units) and sum
+  int32_t* status;
+  int32_t n_seqs, n_nodes;
+  int32_t tile_keys, row_chunk, item_units;
+  int32_t quota, n_ctas;  // work units per CTA
+  int32_t shaped;
+  ShareNode node[kMaxShareNodes + 1];   // one more: where the units end
+  int32_t order[kMaxCallSeqs];          // row of q / out of the sequence
+  int32_t newest[kMaxCallSeqs];         // its last position
+  int32_t leaf[kMaxCallSeqs];           // its last node
+  ScoreShape shape;
+};
+
+// What one CTA has to do of one item.
+struct ShareSegment {
+  int32_t node, g, s0;
+  int32_t row_first, rows;   // rows of the node that the chunk holds
+  int32_t t0, t1;            // keys
+  int32_t seg_row;           // first row of partial results
+};
+struct ShareWalk {
+  int32_t u, end, v;
+};
+__device__ __forceinline__ ShareWalk share_begin(const SharedDecodeParams& p, int cta) {
+  ShareWalk w;
+  w.u = cta * p.quota;
+  w.end = min(w.u + p.quota, p.node[p.n_nodes].unit0);
+  int lo = 0, hi = p.n_nodes;   // last node that begins at or before u
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (p.node[mid].unit0 <= w.u) lo = mid; else hi = mid;
+  }
+  w.v = lo;
+  return w;
+}
+__device__ __forceinline__ bool share_next(const SharedDecodeParams& p, int cta, ShareWalk& w, ShareSegment& s) {
+  while (w.u < w.end) {
+    while (p.node[w.v + 1].unit0 <= w.u) ++w.v;
+    const ShareNode& nd = p.node[w.v];
+    const int tiles = (nd.t1 - nd.t0 + p.tile_keys - 1) / p.tile_keys, len = tiles + p.item_units;
+    const int item = (w.u - nd.unit0) / len, a = nd.unit0 + item * len + p.item_units;   // unit of the item's first tile
+    const int hi = min(a + tiles, w.end), lo = max(a, w.u);
+    w.u = hi;
+    if (hi <= lo) {            // (only units of the item's own cost)
+      w.u = max(hi, min(a, w.end));
+      continue;
+    }
+    const int all = nd.ns * p.group, chunks = (all + p.row_chunk - 1) / p.row_chunk, rc = item % chunks;
+    s.node = w.v;
+    s.s0 = nd.s0;
+    s.g = item / chunks;
+    s.row_first = rc * p.row_chunk;
+    s.rows = min(p.row_chunk, all - s.row_first);
+    s.t0 = nd.t0 + (lo - a) * p.tile_keys;
+    s.t1 = min(nd.t1, nd.t0 + (hi - a) * p.tile_keys);
+    s.seg_row = nd.row0 + (s.g * all + s.row_first) * nd.max_segs + (cta - a / p.quota) * s.rows;
+    return true;
+  }
+  return false;
+}
+
+// Rotating a projection's rows (mixattn_rope_qkv).
+constexpr int kMaxRotary = 128;
+struct RopeEntry {
+  int32_t seq;         // storage slot
+  int32_t pos0;        // position whose angle the first token takes
+  int32_t start_pos;   // position it is stored at
+  int32_t n_new;
+  int32_t row0;        // first row of q / k / v and of the outputs
+  int32_t page_hint;   // as in AppendEntry
+  int32_t tbl_idx;
+};
+struct RopeParams {
+  const char *q, *k, *v;                 // nullptr = not there
+  int64_t q_stride, k_stride, v_stride;  // bytes between tokens
+  char *q_out, *k_out, *v_out;           // dense; nullptr = not wanted
+  char* pool;                            // nullptr = nothing is stored
+  int32_t* table;
+  int32_t table_stride;
+  int32_t is_ring, window, ring_pages;
+  KvGeom geom;
+  int32_t n_q_heads;
+  int32_t rotary, halves;
+  float scale;                           // factor on the rotated channels
+  double freq[kMaxRotary / 2];
+  int32_t n_entries;
+  RopeEntry e[kMaxCallSeqs];
+};
+
+// Rules on logits (mixattn_adjust_logits).
+struct AdjustParams {
+  const void* logits;
+  void* out;
+  int64_t row_stride, out_stride;   // elements
+  int32_t n_rows, vocab;
+  int32_t in_place;
+  mixattn_logit_rules rules;
+  int32_t part;                     // tokens per CTA, a multiple of 32
+};
+
 // device status codes written to the status word
 enum { kDevOk = 0, kDevWaitTimeout = 1 };
 
@@ -289,6 +417,12 @@ cudaError_t launch_decode_split_bf16(const DecodeParams& p, const ShapedDecodePa
                                      cudaStream_t st);   // native or quantised cache
 cudaError_t launch_decode_split_f32(const DecodeParams& p, const ShapedDecodeParams* shaped, cudaStream_t st);
 cudaError_t launch_decode_combine(const DecodeParams& p, int dtype, cudaStream_t st);
+cudaError_t prepare_decode_shared();
+cudaError_t launch_decode_shared(const SharedDecodeParams& p, cudaStream_t st);         // any storage, exact fp32 arithmetic
+cudaError_t launch_merge_shared(const SharedDecodeParams& p, int dtype, cudaStream_t st);
+cudaError_t launch_rope_qkv(const RopeParams& p, int max_n_new, cudaStream_t st);
+cudaError_t prepare_adjust_logits();
+cudaError_t launch_adjust_logits(const AdjustParams& p, int in_dtype, int out_dtype, int sm_count, cudaStream_t st);
 cudaError_t launch_prefill_simple(const PrefillParams& p, int dtype, int max_len, cudaStream_t st);
 bool prefill_tc_supported(int dtype, int head_dim, const void* q, const void* k, const void* v);
 bool prefill_tc_ring_direct_supported(const KvGeom& ge, int window);   // cached keys read in place from a ring
