@@ -326,6 +326,7 @@ int mixattn_create(const mixattn_config* cfg, mixattn_ctx** out) {
     c->l2_bytes = l2;
     if (prepare_decode_bf16() != cudaSuccess || prepare_prefill_tc() != cudaSuccess ||
         prepare_beam_select() != cudaSuccess || prepare_decode_shared() != cudaSuccess ||
+        prepare_decode_shared_tc() != cudaSuccess ||
         prepare_adjust_logits() != cudaSuccess) { delete c; return MIXATTN_ERR_CUDA; }
     if (cudaMemsetAsync(c->arena, 0, c->plan.total, 0) != cudaSuccess ||
         cudaStreamSynchronize(0) != cudaSuccess) {
@@ -1018,9 +1019,14 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
     p.part_ml = reinterpret_cast<float2*>(c->arena + c->plan.part_ml_off);
     p.status = c->dev_status();
     p.shaped = score_shape_of(c, layer, &p.shape) ? 1 : 0;
-    p.tile_keys = 32;
-    p.row_chunk = 32;
-    p.item_units = 1;
+    const bool tc = shared_tc_supported(c->geom, q);
+    if (tc) {
+      shared_tc_tiles(&p);
+    } else {
+      p.tile_keys = 32;
+      p.row_chunk = 32;
+      p.item_units = 1;
+    }
     const int64_t room = (int64_t)kWsChunks * Hq;
     // (launches of kMaxCallSeqs sequences: a larger batch is cut in the caller's order)
     for (int i0 = 0; i0 < n_seqs; i0 += kMaxCallSeqs) {
@@ -1032,7 +1038,7 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
       for (int32_t least = MIXATTN_MIN_SHARED_TOKENS; !fits; least *= 2) {   // (deep trees of short pieces: only the longer ones)
         build_share_tree(c->cm, layer, nb, ids, least, &tree);
         if (!tree.shared) break;
-        fits = lay_out_shared(tree, 2 * c->sm_count, room, &p);
+        fits = lay_out_shared(tree, tc ? c->sm_count : 2 * c->sm_count, room, &p);
         if (least > (1 << 29)) break;
       }
       if (!fits) {
@@ -1048,7 +1054,9 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
         p.newest[j] = c->cm.len(layer, ids[tree.order[j]]) - 1;
         p.leaf[j] = tree.leaf[j];
       }
-      cudaError_t e = launch_recorded(c, MIXATTN_K_SHARED, st, [&] { return launch_decode_shared(p, st); });
+      cudaError_t e = launch_recorded(c, MIXATTN_K_SHARED, st, [&] {
+        return tc ? launch_decode_shared_tc(p, st) : launch_decode_shared(p, st);
+      });
       if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
       e = launch_recorded(c, MIXATTN_K_MERGE, st, [&] { return launch_merge_shared(p, c->cfg.dtype, st); });
       if (e != cudaSuccess) return MIXATTN_ERR_CUDA;

@@ -1,0 +1,530 @@
+// Decode over a tree of shared prefixes on the 5th-generation tensor cores (tcgen05 + TMEM), bf16 caches.
+//
+// The pieces of the tree, their items and segments are described with SharedDecodeParams
+// (internal.h), the mathematics in decode_shared.cu.  Here the rows of an item, the query heads that
+// read the same keys (up to 128: sequences x heads of a KV head), are the M dimension of the
+// products, so that a page of the cache is read from HBM once for all of them, and what bounds a
+// segment is that stream: a tile of 128 keys and head_dim 128 is 64 KB, 2800 cycles of an SM's share of HBM,
+// against 1500 of products and about as many of exponentials.  A row that stands alone (a sequence's own last
+// keys) costs the same tile of products, which fits under the stream all the same.
+//
+//   warp 0     page producer: ids from the block table, 4 KB tensor copies (16 tokens x 64 channels of
+//              K and of V) into a ring of 128-key stages
+//   warp 1     one thread issues S = Q K^T into one of two S buffers
+//   warps 2-3  P V of a stream each, P in two bf16 terms (value and rounding residual: 16 bits, as
+//              the other decode kernels hold them) from tensor memory
+//   warps 4-7, 8-11  the softmax of stream 0 and 1, a row per thread
+//   warps 12-15  rows of Q into shared memory for the next segment, then the results of this one
+//
+// Operands straight from the pages.  A page block holds 16 rows of K and 16 of V whose 16-byte
+// chunks are stored permuted by (token & 7), inside 128 bytes the image of a 128-byte-swizzled operand; a
+// copy of one 64-channel half lays the page down as K [2 groups of 8 tokens][1 KB], V likewise.  The
+// groups g of all pages then lie a fixed 4 KB apart, which a matrix descriptor can name: stream g takes
+// tokens 8 g .. 8 g + 7 of every page, as N = 64 columns of S (column 8 j + t = token 8 g + t of the tile's
+// page j) and as 4 steps of 16 keys (two pages each) of its P V.  So the two halves of S are two independent
+// flash-attention passes with their own reference, sum and accumulator, merged at the end.
+//
+// TMEM: S0, S1, O_0, O_1 = 4 x 128 columns.  All mbarrier waits are bounded; on time-out a status
+// word is raised and every role leaves its loop.
+#include <type_traits>
+
+#include "f32x2.cuh"
+#include "internal.h"
+#include "score_shape.cuh"
+#include "tc_ops.cuh"
+
+namespace mixattn {
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kRows = 128, kTile = 128;          // rows of an item, keys per tile
+constexpr int kTilePages = kTile / kPage;
+constexpr int kBlk = 4096;                       // one page's K and V, 64 channels
+constexpr int kHalf = kTilePages * kBlk;         // 64 channels of a tile's K and V
+constexpr int kQHalf = kRows * 128;              // 64 channels of Q
+constexpr int kSmBarBytes = 256;
+constexpr uint32_t kColS = 0, kColO = 256;
+constexpr float kMaxLead = 32.f;                 // a score this far (base 2) above its row's reference moves it
+
+template <int D>
+struct Layout {
+  static constexpr int kHalves = D / 64;
+  static constexpr int kStageBytes = kHalves * kHalf;
+  static constexpr int kStages = D == 128 ? 3 : 6;
+  static constexpr int kSmQ = 0;
+  static constexpr int kSmKV = kHalves * kQHalf;
+  static constexpr int kSmBar = kSmKV + kStages * kStageBytes;
+  static constexpr int kSmXchg = kSmBar + kSmBarBytes;
+  static constexpr int kBytes = kSmXchg + 2 * kRows * 8 + 768;   // + slack to align a 256-byte aligned base to 1024
+  static_assert(kBytes <= 227 * 1024, "shared memory");
+};
+
+enum {
+  B_QF = 0, B_QE = 1,        // Q there / consumed by the segment's score products
+  B_F = 2, B_E = 8,          // stage full / free (both P V issuers)
+  B_SF = 14, B_SR = 16,      // S buffer: scores there / P in it consumed by both streams
+  B_PF = 18,                 // 18 + 2 stream + buffer: P written
+  B_OF = 22,                 // per stream: the segment's last P V done
+  B_XC = 24, B_OR = 25,      // references and sums published / results read
+  B_N = 26
+};
+static_assert(B_N * 8 + 16 <= kSmBarBytes, "barriers");
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
+}
+
+// Column e of a stream's 64 is key key_of(e) + 8 g behind the tile's first.
+__device__ __forceinline__ constexpr int key_of(int e) { return 16 * (e >> 3) + (e & 7); }
+
+// kShape: scores capped (1), biased (2), both (3)
+template <int D, int kShape>
+__global__ void __launch_bounds__(kThreads, 1)
+decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_constant__ SharedDecodeParams p) {
+  using L = Layout<D>;
+  constexpr int kStages = L::kStages;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  unsigned char* gbase = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t bar0 = base + L::kSmBar;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gbase + L::kSmBar + B_N * 8);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gbase + L::kSmBar + B_N * 8 + 8);
+#define BAR(i) (bar0 + 8u * (i))
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (threadIdx.x == 0) {
+    mbar_init(BAR(B_QF), 4);
+    mbar_init(BAR(B_QE), 1);
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(BAR(B_F + s), 1);
+      mbar_init(BAR(B_E + s), 2);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(BAR(B_SF + s), 1);
+      mbar_init(BAR(B_SR + s), 2);
+      mbar_init(BAR(B_PF + s), 4);
+      mbar_init(BAR(B_PF + 2 + s), 4);
+      mbar_init(BAR(B_OF + s), 1);
+    }
+    mbar_init(BAR(B_XC), 8);
+    mbar_init(BAR(B_OR), 4);
+    abort_flag[0] = 0;   // any role gave up
+    abort_flag[1] = 0;   // never set: the producer's last wait runs to its own limit
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // the kernels ahead in the stream are done
+
+  // Every role walks the same segments with the same counters: G tiles, it segments so far.
+  ShareWalk walk = share_begin(p, blockIdx.x);
+  ShareSegment s;
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (warp == 0) {
+      // ------------------------------ page producer ------------------------------
+      bool ok = true;
+      int G = 0;
+      if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&pages) : "memory");
+      while (ok && share_next(p, blockIdx.x, walk, s)) {
+        const int32_t* tbl = p.table + (int64_t)p.node[s.node].slot * p.table_stride;
+        const int page_lo = s.t0 / kPage, page_hi = (s.t1 + kPage - 1) / kPage;
+        // ids are fetched 32 at a time, one batch ahead of their use
+        int ids_next = page_lo + lane < page_hi ? tbl[page_lo + lane] : 0, ids = 0;
+        for (int pg = page_lo; pg < page_hi; pg += kTilePages, ++G) {
+          const int rel = (pg - page_lo) & 31;
+          if (rel == 0) {
+            ids = ids_next;
+            if (pg + 32 + lane < page_hi) ids_next = tbl[pg + 32 + lane];
+          }
+          const int st = G % kStages, turn = G / kStages;
+          if (turn > 0) {   // lane 0 waits; the verdict is made warp-uniform
+            int w = 1;
+            if (lane == 0) w = mbar_wait(BAR(B_E + st), (turn - 1) & 1, abort_flag);
+            if (!__shfl_sync(0xffffffffu, w, 0)) { ok = false; break; }
+          }
+          const int n_pg = min(kTilePages, page_hi - pg);
+          if (lane == 0) mbar_expect_tx(BAR(B_F + st), n_pg * L::kHalves * kBlk);
+          const int j = lane & (kTilePages - 1), h = lane / kTilePages;
+          const int id = __shfl_sync(0xffffffffu, ids, rel + j);
+          if (h < L::kHalves && j < n_pg)
+            tma_load_4d(base + L::kSmKV + st * L::kStageBytes + h * kHalf + j * kBlk, &pages, 64 * h, 0, 0,
+                        id * p.geom.n_kv_heads + s.g, BAR(B_F + st));
+        }
+      }
+      if (!ok && lane == 0) {   // leave only after the copies already issued have landed (bounded)
+        atomicExch(p.status, kDevWaitTimeout);
+        for (int back = 1; back <= kStages && G - back >= 0; ++back)
+          mbar_wait(BAR(B_F + (G - back) % kStages), ((G - back) / kStages) & 1, abort_flag + 1);
+      }
+    } else if (warp == 1) {
+      // ------------------------------ score products ------------------------------
+      if (lane == 0) {
+        constexpr uint32_t kIdesc = idesc_bf16(0, 64);
+        bool ok = true;
+        int G = 0;
+        for (int it = 0; ok && share_next(p, blockIdx.x, walk, s); ++it) {
+          ok = mbar_wait(BAR(B_QF), it & 1, abort_flag);
+          for (int t = s.t0; t < s.t1 && ok; t += kTile, ++G) {
+            const int sb = G & 1, st = G % kStages;
+            ok = mbar_wait(BAR(B_F + st), (G / kStages) & 1, abort_flag);
+            if (ok && G >= 2) ok = mbar_wait(BAR(B_SR + sb), ((G >> 1) - 1) & 1, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              const uint64_t kdesc = smem_desc(base + L::kSmKV + st * L::kStageBytes + g * 1024, 16, kBlk);
+              const uint64_t qdesc = smem_desc(base + L::kSmQ, 16, 1024);
+#pragma unroll
+              for (int ks = 0; ks < D / 16; ++ks)
+                umma_bf16(tmem + kColS + sb * 128 + g * 64, qdesc + (uint64_t)((ks >> 2) * (kQHalf >> 4) + (ks & 3) * 2),
+                          kdesc + (uint64_t)((ks >> 2) * (kHalf >> 4) + (ks & 3) * 2), kIdesc, ks > 0);
+            }
+            umma_commit(BAR(B_SF + sb));
+          }
+          if (ok) umma_commit(BAR(B_QE));
+        }
+        if (!ok) atomicExch(p.status, kDevWaitTimeout);
+      }
+    } else {
+      // ------------------------------ P V of a stream ------------------------------
+      constexpr uint32_t kIdesc = idesc_bf16(1, D);
+      const int g = warp - 2;
+      bool ok = true;
+      int G = 0;
+      for (int it = 0; ok && share_next(p, blockIdx.x, walk, s); ++it) {
+        // the segment's first P V overwrites the accumulator
+        if (it >= 1) ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_OR), (it - 1) & 1, abort_flag));
+        for (int t = s.t0; t < s.t1 && ok; t += kTile, ++G) {
+          const int sb = G & 1, st = G % kStages;
+          ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_F + st), (G / kStages) & 1, abort_flag));
+          if (!ok) break;
+          // steps of 16 keys = two pages' groups; the segment's last tile may hold fewer, and rows that
+          // are no keys (behind the last one, or a page that was not loaded), whose weight of zero an
+          // infinity or a NaN would survive, are cleared meanwhile
+          const int left = s.t1 - t, steps = left >= kTile ? 4 : (left + 31) / 32;
+          if (left < kTile) {
+            unsigned char* v = gbase + L::kSmKV + st * L::kStageBytes + 2048 + g * 1024;
+            for (int r = (left / kPage) * 8; r < steps * 16; ++r) {   // row 8 j + token of page j
+              if (16 * (r >> 3) + 8 * g + (r & 7) < left) continue;
+              for (int c = lane; c < D / 8; c += 32)
+                *reinterpret_cast<uint4*>(v + (c >> 3) * kHalf + (r >> 3) * kBlk + (r & 7) * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the products read through the async proxy
+            __syncwarp();
+          }
+          ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_PF + 2 * g + sb), (G >> 1) & 1, abort_flag));
+          if (!ok) break;
+          if (lane == 0) {
+            tc_fence_after();
+            const uint64_t vdesc = smem_desc(base + L::kSmKV + st * L::kStageBytes + 2048 + g * 1024, kHalf, kBlk);
+#pragma unroll
+            for (int term = 0; term < 2; ++term)
+#pragma unroll
+              for (int ks = 0; ks < 4; ++ks)
+                if (ks < steps)
+                  umma_bf16_ts(tmem + kColO + g * 128, tmem + kColS + sb * 128 + g * 64 + term * 32 + ks * 8,
+                               vdesc + (uint64_t)(ks * (2 * kBlk >> 4)), kIdesc, (t > s.t0 || term > 0 || ks > 0) ? 1u : 0u);
+            if (t + kTile >= s.t1) umma_commit(BAR(B_OF + g));
+            umma_commit(BAR(B_E + st));
+            umma_commit(BAR(B_SR + sb));
+          }
+          __syncwarp();
+        }
+      }
+      if (!ok && lane == 0) atomicExch(p.status, kDevWaitTimeout);
+    }
+  } else if (warp >= 12) {
+    // ------------------------------ Q in, results out ------------------------------
+    const int qd = warp & 3, r = qd * 32 + lane;
+    const uint32_t lane_base = tmem + ((uint32_t)(qd * 32) << 16);
+    const float2* xchg = reinterpret_cast<const float2*>(gbase + L::kSmXchg);
+    auto put_q = [&](const ShareSegment& q, int it) {   // this thread's row of Q, rows behind the last as zeros
+      uint4 x[D / 8];
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) x[c] = make_uint4(0u, 0u, 0u, 0u);
+      if (r < q.rows) {
+        const int R = q.row_first + r;
+        const uint4* src = reinterpret_cast<const uint4*>(
+            reinterpret_cast<const __nv_bfloat16*>(p.q) +
+            ((int64_t)p.order[q.s0 + R / p.group] * p.n_q_heads + q.g * p.group + R % p.group) * D);
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) x[c] = src[c];
+      }
+      if (it >= 1 && !__all_sync(0xffffffffu, mbar_wait(BAR(B_QE), (it - 1) & 1, abort_flag))) return false;
+      unsigned char* to = gbase + L::kSmQ + r * 128;
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(to + (c >> 3) * kQHalf + (((c & 7) ^ (r & 7)) << 4)) = x[c];
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(B_QF));
+      return true;
+    };
+    bool more = share_next(p, blockIdx.x, walk, s), ok = true;
+    if (more) ok = put_q(s, 0);
+    for (int it = 0; ok && more; ++it) {
+      const ShareSegment now = s;
+      more = share_next(p, blockIdx.x, walk, s);
+      if (more) ok = put_q(s, it + 1);
+      if (!ok) break;
+      ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_XC), it & 1, abort_flag));
+      if (!ok) break;
+      const float2 lo = xchg[r], hi = xchg[kRows + r];
+      ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_OF + 0), it & 1, abort_flag) && mbar_wait(BAR(B_OF + 1), it & 1, abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      const float m = fmaxf(lo.x, hi.x);   // (finite: token 0 of the segment's first page is a key)
+      const float e_lo = ex2_approx(lo.x - m), e_hi = ex2_approx(hi.x - m);
+      float* to = p.part_o + (int64_t)now.seg_row * D + r * 4;
+      const bool mine = r < now.rows;
+      if (qd * 32 < now.rows) {            // (warps without a row have nothing to read)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t a[32], b[32];
+          tmem_ld32(lane_base + kColO + c * 32, a);
+          tmem_ld32(lane_base + kColO + 128 + c * 32, b);
+          tmem_wait_ld_pin(a, b);
+          if (mine) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              float4 o;
+              // (a stream without a key has a weight of zero and an accumulator of zeros)
+              o.x = __uint_as_float(a[e]) * e_lo + __uint_as_float(b[e]) * e_hi;
+              o.y = __uint_as_float(a[e + 1]) * e_lo + __uint_as_float(b[e + 1]) * e_hi;
+              o.z = __uint_as_float(a[e + 2]) * e_lo + __uint_as_float(b[e + 2]) * e_hi;
+              o.w = __uint_as_float(a[e + 3]) * e_lo + __uint_as_float(b[e + 3]) * e_hi;
+              *reinterpret_cast<float4*>(to + (int64_t)(c * 8 + e / 4) * now.rows * 4) = o;
+            }
+          }
+        }
+        if (mine) p.part_ml[now.seg_row + r] = make_float2(m, lo.y * e_lo + hi.y * e_hi);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(B_OR));
+    }
+    if (!ok && lane == 0) atomicExch(p.status, kDevWaitTimeout);
+  } else {
+    // ------------------------------ softmax ------------------------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    const int g = (warp - 4) >> 2, qd = warp & 3, r = qd * 32 + lane;
+    const uint32_t lane_base = tmem + ((uint32_t)(qd * 32) << 16);
+    const uint32_t o_addr = lane_base + kColO + g * 128;
+    float2* xchg = reinterpret_cast<float2*>(gbase + L::kSmXchg);
+    bool ok = true;
+    int G = 0;
+    for (int it = 0; ok && share_next(p, blockIdx.x, walk, s); ++it) {
+      const bool idle = qd * 32 >= s.rows;    // none of this warp's rows exists
+      float m_ref = -INFINITY, l = 0.f;
+      float slope = 0.f;
+      int newest = 0;
+      if constexpr (kShape & 2) {
+        const int R = s.row_first + min(r, s.rows - 1);
+        slope = p.shape.slope[s.g * p.group + R % p.group];
+        newest = p.newest[s.s0 + R / p.group];
+      }
+      for (int t = s.t0; t < s.t1; t += kTile, ++G) {
+        const int sb = G & 1;
+        if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SF + sb), (G >> 1) & 1, abort_flag))) { ok = false; break; }
+        if (!idle) {
+          tc_fence_after();
+          const uint32_t s_addr = lane_base + kColS + sb * 128 + g * 64;
+          uint32_t sv[64];
+          auto& s0 = *reinterpret_cast<uint32_t(*)[32]>(&sv[0]);
+          auto& s1 = *reinterpret_cast<uint32_t(*)[32]>(&sv[32]);
+          tmem_ld32(s_addr, s0);
+          tmem_ld32(s_addr + 32, s1);
+          tmem_wait_ld_pin(s0, s1);
+          if constexpr (kShape != 0) {   // raw products -> shaped base-2 scores
+            const float first = -slope * (float)(newest - t - 8 * g);   // bias of column 0
+            float top = 0.f;
+#pragma unroll
+            for (int e = 0; e < 64; e += 2) {
+              f32x2 x = mul2(pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), pack2(p.shape.pre, p.shape.pre));
+              if constexpr (kShape & 1) {
+                const f32x2 u = mul2(x, x);
+                f32x2 q = fma2(pack2(tanh_coefficient(5), tanh_coefficient(5)), u, pack2(tanh_coefficient(4), tanh_coefficient(4)));
+                q = fma2(q, u, pack2(tanh_coefficient(3), tanh_coefficient(3)));
+                q = fma2(q, u, pack2(tanh_coefficient(2), tanh_coefficient(2)));
+                q = fma2(q, u, pack2(tanh_coefficient(1), tanh_coefficient(1)));
+                q = fma2(q, u, pack2(tanh_coefficient(0), tanh_coefficient(0)));
+                const float2 uu = unpack2(u);
+                top = fmax3(top, uu.x, uu.y);
+                x = mul2(mul2(q, x), pack2(p.shape.post, p.shape.post));
+              }
+              if constexpr (kShape & 2) x = add2(x, pack2(fmaf(slope, (float)key_of(e), first), fmaf(slope, (float)key_of(e + 1), first)));
+              const float2 y = unpack2(x);
+              sv[e] = __float_as_uint(y.x);
+              sv[e + 1] = __float_as_uint(y.y);
+            }
+            if constexpr (kShape & 1) {
+              if (__any_sync(0xffffffffu, !(top <= 1.f))) {   // beyond the polynomial: again from the raw products
+                tmem_ld32(s_addr, s0);
+                tmem_ld32(s_addr + 32, s1);
+                tmem_wait_ld_pin(s0, s1);
+#pragma unroll
+                for (int e = 0; e < 64; ++e) {
+                  const float x = __uint_as_float(sv[e]) * p.shape.pre, o = (kShape & 2) ? fmaf(slope, (float)key_of(e), first) : 0.f;
+                  const float a = tanh_poly(x), b = tanh_exp(x);
+                  sv[e] = __float_as_uint(fmaf(fabsf(x) <= 1.f ? a : b, p.shape.post, o));
+                }
+              }
+            }
+          }
+          const float scale = kShape ? 1.f : p.scale_log2e;
+          if (t + kTile > s.t1) {
+            const int left = s.t1 - t - 8 * g;
+#pragma unroll
+            for (int e = 0; e < 64; ++e)
+              if (key_of(e) >= left) sv[e] = 0xff800000u;
+          }
+          float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 64; e += 4) {
+            mx0 = fmax3(mx0, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+            mx1 = fmax3(mx1, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
+          }
+          const float mt = fmaxf(mx0, mx1) * scale;
+          if (t == s.t0) {
+            m_ref = mt;
+          } else if (__any_sync(0xffffffffu, mt > m_ref + kMaxLead)) {
+            // rare: move the reference of the leading rows and rescale what they have accumulated, once
+            // this stream's previous P V has landed (the S buffer of tile G - 1 is released when both streams' are)
+            const bool far = mt > m_ref + kMaxLead;
+            const float alpha = far ? ex2_approx(m_ref - mt) : 1.f;
+            if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SR + (sb ^ 1)), ((G - 1) >> 1) & 1, abort_flag))) { ok = false; break; }
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t ov[32];
+              tmem_ld32(o_addr + c * 32, ov);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
+              tmem_st32(o_addr + c * 32, ov);
+            }
+            l *= alpha;
+            if (far) m_ref = mt;
+          }
+          const float neg = m_ref == -INFINITY ? 0.f : -m_ref;   // (a stream without a key: weights 0, no NaN)
+          f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
+          uint32_t pk[32], pl[32];
+#pragma unroll
+          for (int e = 0; e < 64; e += 2) {
+            const float a = ex2_approx(fmaf(__uint_as_float(sv[e]), scale, neg));
+            const float b = ex2_approx(fmaf(__uint_as_float(sv[e + 1]), scale, neg));
+            if (e & 2) sum1 = add2(sum1, pack2(a, b));
+            else sum0 = add2(sum0, pack2(a, b));
+            split_bf16(a, b, pk[e >> 1], pl[e >> 1]);
+          }
+          const float2 sum = unpack2(add2(sum0, sum1));
+          l += sum.x + sum.y;
+          tmem_st32(s_addr, pk);          // value over the first 32 of the stream's columns, residual over the others
+          tmem_st32(s_addr + 32, pl);
+          tmem_wait_st();
+          tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(B_PF + 2 * g + sb));
+      }
+      if (!ok) break;
+      if (it >= 1) ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_OR), (it - 1) & 1, abort_flag));   // the slot is free
+      if (!ok) break;
+      xchg[g * kRows + r] = make_float2(m_ref, l);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(B_XC));
+    }
+    if (!ok && lane == 0) atomicExch(p.status, kDevWaitTimeout);
+  }
+  // common exit: everyone is past its last TMEM access
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+#undef BAR
+}
+
+// Paged storage of one owner layer, native bf16 format, as [page and head][K | V][16 tokens][channels];
+// box = 64 channels of 16 tokens of K and V.  The stored chunks are permuted already, so the copy does not swizzle.
+bool make_page_map(CUtensorMap* map, const void* pool, const KvGeom& ge, int64_t pages) {
+  EncodeTiledFn fn = encode_fn();
+  if (fn == nullptr) return false;
+  cuuint64_t dims[4] = {(cuuint64_t)ge.head_dim, (cuuint64_t)kPage, 2, (cuuint64_t)(pages * ge.n_kv_heads)};
+  cuuint64_t strides[3] = {(cuuint64_t)ge.row_bytes, (cuuint64_t)kPage * ge.row_bytes, (cuuint64_t)ge.blk_bytes};
+  cuuint32_t box[4] = {64, (cuuint32_t)kPage, 2, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int kShape>
+cudaError_t launch(const SharedDecodeParams& p, const CUtensorMap& map, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.n_ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Layout<D>::kBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, decode_shared_tc_kernel<D, kShape>, map, p);
+}
+
+template <int D>
+cudaError_t prepare() {
+  constexpr auto kAttr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 0>, kAttr, Layout<D>::kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 1>, kAttr, Layout<D>::kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 2>, kAttr, Layout<D>::kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 3>, kAttr, Layout<D>::kBytes);
+  return e;
+}
+
+}  // namespace
+
+bool shared_tc_supported(const KvGeom& ge, const void* q) {
+  return !ge.fp8 && ge.elem_bytes == 2 && ((size_t)q & 15) == 0 && encode_fn() != nullptr;
+}
+
+void shared_tc_tiles(SharedDecodeParams* p) {
+  p->tile_keys = kTile;
+  p->row_chunk = kRows;
+  p->item_units = 1;
+}
+
+cudaError_t prepare_decode_shared_tc() {
+  cudaError_t e = prepare<128>();
+  return e == cudaSuccess ? prepare<64>() : e;
+}
+
+cudaError_t launch_decode_shared_tc(const SharedDecodeParams& p, cudaStream_t st) {
+  if (p.tile_keys != kTile || p.row_chunk != kRows) return cudaErrorInvalidValue;
+  CUtensorMap map;
+  if (!make_page_map(&map, p.pool, p.geom, p.n_pages)) return cudaErrorInvalidValue;
+  const int shape = !p.shaped ? 0 : (p.shape.post > 0.f ? 1 : 0) | (p.shape.biased ? 2 : 0);
+  if (p.geom.head_dim == 128) {
+    if (shape == 0) return launch<128, 0>(p, map, st);
+    if (shape == 1) return launch<128, 1>(p, map, st);
+    return shape == 2 ? launch<128, 2>(p, map, st) : launch<128, 3>(p, map, st);
+  }
+  if (shape == 0) return launch<64, 0>(p, map, st);
+  if (shape == 1) return launch<64, 1>(p, map, st);
+  return shape == 2 ? launch<64, 2>(p, map, st) : launch<64, 3>(p, map, st);
+}
+
+}  // namespace mixattn

@@ -419,6 +419,10 @@ cudaError_t launch_decode_split_f32(const DecodeParams& p, const ShapedDecodePar
 cudaError_t launch_decode_combine(const DecodeParams& p, int dtype, cudaStream_t st);
 cudaError_t prepare_decode_shared();
 cudaError_t launch_decode_shared(const SharedDecodeParams& p, cudaStream_t st);         // any storage, exact fp32 arithmetic
+bool shared_tc_supported(const KvGeom& ge, const void* q);      // on the tensor cores: bf16 caches
+void shared_tc_tiles(SharedDecodeParams* p);
+cudaError_t prepare_decode_shared_tc();
+cudaError_t launch_decode_shared_tc(const SharedDecodeParams& p, cudaStream_t st);
 cudaError_t launch_merge_shared(const SharedDecodeParams& p, int dtype, cudaStream_t st);
 cudaError_t launch_rope_qkv(const RopeParams& p, int max_n_new, cudaStream_t st);
 cudaError_t prepare_adjust_logits();
