@@ -32,9 +32,13 @@ struct ArenaPlan {
   std::vector<size_t> owner_bytes;
   size_t table_off = 0, table_bytes = 0;
   size_t part_o_off = 0, part_ml_off = 0, status_off = 0, ticket_off = 0;
+  size_t shared_o_off = 0, shared_ml_off = 0;   // partial results of shared decode, shared_rows() of them
   size_t chunk_k_off = 0, chunk_v_off = 0;   // [chunk_scratch_tokens, Hkv, D] each
   size_t cache_bytes = 0, total = 0;
 };
+
+// Rows of partial results that a shared decode leaves at most: a segment of 128 rows per CTA, and where items end another.
+int64_t shared_rows(int n_q_heads) { return 160 * 128 + 2 * (int64_t)kMaxCallSeqs * n_q_heads; }
 
 int ring_pages_of(int window) { return (window + kPage - 1) / kPage; }
 
@@ -63,6 +67,12 @@ ArenaPlan plan_arena(const CacheManager& cm, const mixattn_config& cfg) {
   off += kAlign;
   pl.ticket_off = off;
   off += align_up(kBeamTickets * sizeof(int32_t));
+  if (cm.n_full_owners() > 0 && cfg.dtype == MIXATTN_BF16) {
+    pl.shared_o_off = off;
+    off += align_up((size_t)shared_rows(cfg.n_q_heads) * cfg.head_dim * sizeof(float));
+    pl.shared_ml_off = off;
+    off += align_up((size_t)shared_rows(cfg.n_q_heads) * sizeof(float2));
+  }
   if (cfg.chunk_scratch_tokens > 0) {
     const size_t bytes = align_up((size_t)cfg.chunk_scratch_tokens * ge.n_kv_heads * ge.row_bytes);
     pl.chunk_k_off = off;
@@ -841,23 +851,9 @@ static cudaError_t launch_split_pass(const mixattn_ctx* c, const ShapedDecodePar
                                       : launch_decode_split_f32(p, sp, st);
 }
 
-// Split plan of one decode launch over sequences ids[0 .. nb): fills the per-sequence fields of
-// *p (seq_id, n_eff, chunk_len, chunk_base, n_seqs, total_items; group and head_chunks must be
-// set) and returns the number of split slots the launch writes; *any_split tells whether a
-// combine pass is needed.  Long caches are cut into splits of kSplitTokens keys (large splits
-// keep the per-item epilogue negligible; thousands of items balance over the SMs).  When there
-// are fewer (sequence, KV head) pairs than SMs, short caches are cut further, but only up to one
-// item per SM, so the launch stays a single wave.  Both decode entry points use this one
-// function, so they add the partial results in the same order.
-static int plan_splits(const mixattn_ctx* c, int layer, const int32_t* ids, int nb, DecodeParams* p,
-                       bool* any_split) {
+// The cutting itself: n_eff[0 .. nb) are set, `total` is their sum.
+static int cut_splits(const mixattn_ctx* c, int layer, int nb, int64_t total, DecodeParams* p, bool* any_split) {
   const int Hkv = c->cfg.n_kv_heads;
-  int64_t total = 0;
-  for (int j = 0; j < nb; ++j) {
-    p->seq_id[j] = c->cm.slot(ids[j]);
-    p->n_eff[j] = c->cm.n_attended(layer, ids[j]);
-    total += p->n_eff[j];
-  }
   int64_t T = c->split_tokens > 0 ? (c->split_tokens + kPage - 1) / kPage * kPage : kSplitTokens;
   // Shaped scores, and too few items of that size to even out over the SMs: half the size.  (17
   // sequences of 1 to 64k tokens, quantised cache: 86 -> 67 us; 5 of 9k to 20k: 68 -> 49; with
@@ -876,6 +872,9 @@ static int plan_splits(const mixattn_ctx* c, int layer, const int32_t* ids, int 
   *any_split = false;
   for (int j = 0; j < nb; ++j) {
     const int64_t n = p->n_eff[j];
+    p->chunk_base[j] = base;
+    p->chunk_len[j] = kPage;
+    if (n == 0) continue;   // (a shared decode: nothing of the sequence's own)
     int64_t nc = (n + T - 1) / T;
     if (nc < nc_wave) {
       int64_t by_len = n / kMinSplitTokens;
@@ -885,7 +884,6 @@ static int plan_splits(const mixattn_ctx* c, int layer, const int32_t* ids, int 
     int64_t len = (n + nc - 1) / nc;
     len = (len + kPage - 1) / kPage * kPage;
     nc = (n + len - 1) / len;
-    p->chunk_base[j] = base;
     p->chunk_len[j] = (int32_t)len;
     base += (int)nc;
     *any_split = *any_split || nc > 1;
@@ -894,6 +892,25 @@ static int plan_splits(const mixattn_ctx* c, int layer, const int32_t* ids, int 
   p->n_seqs = nb;
   p->total_items = base * Hkv * p->head_chunks;
   return base;
+}
+
+// Split plan of one decode launch over sequences ids[0 .. nb): fills the per-sequence fields of
+// *p (seq_id, n_eff, chunk_len, chunk_base, n_seqs, total_items; group and head_chunks must be
+// set) and returns the number of split slots the launch writes; *any_split tells whether a
+// combine pass is needed.  Long caches are cut into splits of kSplitTokens keys (large splits
+// keep the per-item epilogue negligible; thousands of items balance over the SMs).  When there
+// are fewer (sequence, KV head) pairs than SMs, short caches are cut further, but only up to one
+// item per SM, so the launch stays a single wave.  Both decode entry points use this one
+// function, so they add the partial results in the same order.
+static int plan_splits(const mixattn_ctx* c, int layer, const int32_t* ids, int nb, DecodeParams* p,
+                       bool* any_split) {
+  int64_t total = 0;
+  for (int j = 0; j < nb; ++j) {
+    p->seq_id[j] = c->cm.slot(ids[j]);
+    p->n_eff[j] = c->cm.n_attended(layer, ids[j]);
+    total += p->n_eff[j];
+  }
+  return cut_splits(c, layer, nb, total, p, any_split);
 }
 
 static int decode_plain(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_t* seq_ids, const void* q, void* out,
@@ -954,21 +971,34 @@ static int decode_plain(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int
 }
 
 // Lays the items of a tree's pieces out on the line of work units (internal.h) and cuts the line into equal
-// parts for at most max_ctas CTAs, fewer if the partial results would not fit `room` rows.  Returns
-// false if they do not fit at all.
-static bool lay_out_shared(const ShareTree& t, int max_ctas, int64_t room, SharedDecodeParams* p) {
+// parts for at most max_ctas CTAs, fewer if the partial results would not fit `room` rows.  With `leaves`
+// the pieces of a single sequence are left to the split pass.  Returns false if it does not fit at all.
+static bool lay_out_shared(const ShareTree& t, bool leaves, int max_ctas, int64_t room, SharedDecodeParams* p, int* n_leaves) {
   const int Hkv = p->geom.n_kv_heads;
   int64_t units = 0;
+  std::vector<int32_t> at(t.pieces.size(), -1);   // node of each piece
+  p->n_nodes = 0;
   for (size_t v = 0; v < t.pieces.size(); ++v) {
     const SharePiece& s = t.pieces[v];
+    if (leaves && s.ns == 1) continue;
     const int64_t tiles = ((int64_t)s.t1 - s.t0 + p->tile_keys - 1) / p->tile_keys;
     const int64_t chunks = ((int64_t)s.ns * p->group + p->row_chunk - 1) / p->row_chunk;
-    p->node[v] = ShareNode{s.t0, s.t1, s.slot, s.s0, s.ns, s.parent, (int32_t)units, 0, 0};
+    at[v] = p->n_nodes;
+    p->node[p->n_nodes++] = ShareNode{s.t0, s.t1, s.slot, s.s0, s.ns, s.parent < 0 ? -1 : at[s.parent], (int32_t)units, 0, 0};
     units += (tiles + p->item_units) * Hkv * chunks;
     if (units > (1 << 30)) return false;
   }
-  p->n_nodes = (int32_t)t.pieces.size();
   p->node[p->n_nodes] = ShareNode{0, 0, 0, 0, 0, -1, (int32_t)units, 0, 0};
+  int end = p->n_nodes;
+  if (leaves)
+    for (size_t v = 0; v < t.pieces.size(); ++v) {
+      const SharePiece& s = t.pieces[v];
+      if (s.ns != 1) continue;
+      at[v] = ++end;
+      p->node[end] = ShareNode{s.t0, s.t1, s.slot, s.s0, 1, s.parent < 0 ? -1 : at[s.parent], 0, 0, -1};
+    }
+  *n_leaves = end - p->n_nodes;
+  for (size_t i = 0; i < t.leaf.size(); ++i) p->leaf[i] = at[t.leaf[i]];
   for (int64_t ctas = max_ctas;; ctas = ctas * 3 / 4) {
     const int64_t quota = std::max<int64_t>((units + ctas - 1) / ctas, p->item_units + 1);
     int64_t rows = 0;
@@ -986,6 +1016,31 @@ static bool lay_out_shared(const ShareTree& t, int max_ctas, int64_t room, Share
       return true;
     }
     if (ctas == 1) return false;
+  }
+}
+
+// The keys that only one sequence has, as a launch of the ordinary split pass over the sequences in the
+// caller's order: each with its block table from its first own page on.  Completes the nodes behind p's items.
+static void plan_own_keys(const mixattn_ctx* c, int layer, int n_leaves, SharedDecodeParams* p, ShapedDecodeParams* d) {
+  ShareNode* leaf = p->node + p->n_nodes + 1;
+  int64_t total = 0;
+  for (int i = 0; i < p->n_seqs; ++i) d->seq_id[i] = d->n_eff[i] = d->newest[i] = 0;
+  for (int v = 0; v < n_leaves; ++v) {
+    const int i = p->order[leaf[v].s0];
+    d->seq_id[i] = leaf[v].slot * p->table_stride + leaf[v].t0 / kPage;   // (a table's entries are indexed in 32 bits)
+    d->n_eff[i] = leaf[v].t1 - leaf[v].t0;
+    d->newest[i] = p->newest[leaf[v].s0] - leaf[v].t0;
+    total += d->n_eff[i];
+  }
+  d->n_seqs = p->n_seqs;
+  d->total_items = 0;
+  if (n_leaves == 0) return;
+  bool any = false;
+  cut_splits(c, layer, p->n_seqs, total, d, &any);
+  for (int v = 0; v < n_leaves; ++v) {
+    const int i = p->order[leaf[v].s0];
+    leaf[v].row0 = d->chunk_base[i];
+    leaf[v].max_segs = -(d->chunk_base[i + 1] - d->chunk_base[i]);
   }
 }
 
@@ -1007,6 +1062,7 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
   try {
     ShareTree tree;
     SharedDecodeParams p;
+    ShapedDecodeParams d;
     p.pool = c->owner_storage(layer);
     p.table = c->dev_table();
     p.table_stride = c->cm.max_blocks();
@@ -1015,19 +1071,49 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
     p.n_q_heads = Hq;
     p.group = Hq / Hkv;
     p.scale_log2e = c->scale * kLog2e;
-    p.part_o = reinterpret_cast<float*>(c->arena + c->plan.part_o_off);
-    p.part_ml = reinterpret_cast<float2*>(c->arena + c->plan.part_ml_off);
+    p.split_o = reinterpret_cast<float*>(c->arena + c->plan.part_o_off);
+    p.split_ml = reinterpret_cast<float2*>(c->arena + c->plan.part_ml_off);
     p.status = c->dev_status();
     p.shaped = score_shape_of(c, layer, &p.shape) ? 1 : 0;
     const bool tc = shared_tc_supported(c->geom, q);
+    int64_t room;
     if (tc) {
       shared_tc_tiles(&p);
+      p.part_o = reinterpret_cast<float*>(c->arena + c->plan.shared_o_off);
+      p.part_ml = reinterpret_cast<float2*>(c->arena + c->plan.shared_ml_off);
+      room = shared_rows(Hq);
+      d.pool = p.pool;
+      d.table = p.table;
+      d.table_stride = 1;
+      d.ring_pages = 0;
+      d.geom = c->geom;
+      d.n_q_heads = Hq;
+      d.group = p.group;
+      d.head_chunks = (p.group + kMaxGroupRows - 1) / kMaxGroupRows;
+      d.scale_log2e = p.scale_log2e;
+      d.part_o = const_cast<float*>(p.split_o);
+      d.part_ml = const_cast<float2*>(p.split_ml);
+      d.status = p.status;
+      d.l2_keep_bytes = d.l2_pool_bytes = 0;
+      d.partial = 1;
+      d.wrap = 0;
+      // (always the kernel of shaped scores, here without cap or bias where the layer has none: it clears
+      // what earlier sequences left behind the last key)
+      if (p.shaped) {
+        d.shape = p.shape;
+      } else {
+        d.shape.pre = p.scale_log2e;
+        d.shape.post = 0.f;
+        d.shape.biased = 0;
+      }
     } else {
       p.tile_keys = 32;
       p.row_chunk = 32;
       p.item_units = 1;
+      p.part_o = const_cast<float*>(p.split_o);
+      p.part_ml = const_cast<float2*>(p.split_ml);
+      room = (int64_t)kWsChunks * Hq;
     }
-    const int64_t room = (int64_t)kWsChunks * Hq;
     // (launches of kMaxCallSeqs sequences: a larger batch is cut in the caller's order)
     for (int i0 = 0; i0 < n_seqs; i0 += kMaxCallSeqs) {
       const int nb = std::min(n_seqs - i0, kMaxCallSeqs);
@@ -1035,10 +1121,11 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
       const char* qb = static_cast<const char*>(q) + (size_t)i0 * row_bytes;
       char* ob = static_cast<char*>(out) + (size_t)i0 * row_bytes;
       bool fits = false;
+      int n_leaves = 0;
       for (int32_t least = MIXATTN_MIN_SHARED_TOKENS; !fits; least *= 2) {   // (deep trees of short pieces: only the longer ones)
         build_share_tree(c->cm, layer, nb, ids, least, &tree);
         if (!tree.shared) break;
-        fits = lay_out_shared(tree, tc ? c->sm_count : 2 * c->sm_count, room, &p);
+        fits = lay_out_shared(tree, tc, tc ? c->sm_count : 2 * c->sm_count, room, &p, &n_leaves);
         if (least > (1 << 29)) break;
       }
       if (!fits) {
@@ -1052,12 +1139,20 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
       for (int j = 0; j < nb; ++j) {
         p.order[j] = tree.order[j];
         p.newest[j] = c->cm.len(layer, ids[tree.order[j]]) - 1;
-        p.leaf[j] = tree.leaf[j];
       }
       cudaError_t e = launch_recorded(c, MIXATTN_K_SHARED, st, [&] {
         return tc ? launch_decode_shared_tc(p, st) : launch_decode_shared(p, st);
       });
       if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
+      if (tc) {
+        plan_own_keys(c, layer, n_leaves, &p, &d);
+        d.q = qb;
+        d.out = nullptr;
+        if (d.total_items > 0) {
+          e = launch_recorded(c, MIXATTN_K_DECODE_FULL, st, [&] { return launch_split_pass(c, d, true, st); });
+          if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
+        }
+      }
       e = launch_recorded(c, MIXATTN_K_MERGE, st, [&] { return launch_merge_shared(p, c->cfg.dtype, st); });
       if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
     }

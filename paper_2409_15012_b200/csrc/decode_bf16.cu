@@ -303,7 +303,9 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
   if constexpr (CL > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   // ... and do not touch global memory before the kernels ahead in the stream have
   // completed and flushed (a no-op when this kernel was launched the ordinary way)
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // (partial launches: the kernel ahead let this one start once everything before it was done, and
+  // nothing here depends on it; it is waited for at the end, for the sake of the merge that follows)
+  if (!p.partial) asm volatile("griddepcontrol.wait;" ::: "memory");
 
   const KvGeom& ge = p.geom;
 
@@ -373,6 +375,7 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
       __syncwarp();
       asm volatile("barrier.cluster.wait.acquire.aligned;\n\tbarrier.cluster.arrive.release.aligned;" ::: "memory");
     }
+    if (p.partial) asm volatile("griddepcontrol.wait;" ::: "memory");
     return;
   }
 
@@ -669,7 +672,7 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
         continue;
       }
       const int h = h0 + r;
-      if (x.n_splits == 1) {
+      if (x.n_splits == 1 && !p.partial) {
         reinterpret_cast<__nv_bfloat16*>(p.out)[((int64_t)x.i * p.n_q_heads + h) * D + d] =
             __float2bfloat16_rn(acc / L);
       } else {
@@ -690,7 +693,7 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
           const float L = xml[r * 2 + 1] * s0 + xml[(rows_cap + r) * 2 + 1] * s1;
           const float acc = xo[(size_t)r * D + d] * s0 + xo[((size_t)rows_cap + r) * D + d] * s1;
           const int h = h0 + r;
-          if (x.n_splits == 1) {
+          if (x.n_splits == 1 && !p.partial) {
             reinterpret_cast<__nv_bfloat16*>(p.out)[((int64_t)x.i * p.n_q_heads + h) * D + d] =
                 __float2bfloat16_rn(acc / L);
           } else {
@@ -703,6 +706,7 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
     }
     consumer_bar<NCW>();
   }
+  if (p.partial) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 size_t smem_bytes(int D, int group, int n_stages, int ncw, int cl, int kv8) {

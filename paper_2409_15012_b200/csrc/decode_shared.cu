@@ -150,50 +150,104 @@ __global__ void __launch_bounds__(kThreads) decode_shared_kernel(const __grid_co
 }
 
 // ---------------------------------------------------------------- merge
-// One thread per four channels of an output row; the partials of a segment lie [D / 4][rows][4], so
-// that the tensor-core kernel, which has a row per thread, writes them in whole lines.
-constexpr int kMergeThreads = 128;
+// kMergeLanes threads per four channels of an output row take turns over the partial results of the row's path,
+// four loads in flight each, and join in shared memory: a row behind a long prefix has some twenty segments,
+// and one after the other their latencies were the whole kernel (20 us of 8 sequences' 79).  The partials
+// of a segment lie [D / 4][rows][4], so that the tensor-core kernel, which has a row per thread, writes whole lines.
+constexpr int kMergeThreads = 256, kMergeLanes = 4;
+
+struct Partial {
+  float M, L;
+  float4 o;
+};
+__device__ __forceinline__ void join(Partial& a, float m, float l, float4 o) {
+  const float mn = fmaxf(a.M, m);
+  const float s0 = mn == -INFINITY ? 1.f : exp2f(a.M - mn), s1 = mn == -INFINITY ? 0.f : exp2f(m - mn);
+  a.M = mn;
+  a.L = a.L * s0 + l * s1;
+  a.o.x = a.o.x * s0 + o.x * s1;
+  a.o.y = a.o.y * s0 + o.y * s1;
+  a.o.z = a.o.z * s0 + o.z * s1;
+  a.o.w = a.o.w * s0 + o.w * s1;
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kMergeThreads) merge_shared_kernel(const __grid_constant__ SharedDecodeParams p) {
+  __shared__ Partial sm[kMergeThreads];
   const int D = p.geom.head_dim, per_row = D / 4;
-  const int e = blockIdx.x * kMergeThreads + threadIdx.x, h = e / per_row, c4 = e - h * per_row;
+  const int per_block = kMergeThreads / kMergeLanes;                  // (row, channels) pairs per block
+  const int kl = threadIdx.x / per_block, local = threadIdx.x % per_block;
+  const int e = blockIdx.x * per_block + local, h = e / per_row, c4 = e - h * per_row;
   const int i = blockIdx.y;
+  const bool there = h < p.n_q_heads;
   asm volatile("griddepcontrol.wait;" ::: "memory");   // (a no-op after an ordinary launch)
-  if (h >= p.n_q_heads) return;
-  const int g = h / p.group, hh = h - g * p.group;
-  float M = -INFINITY, L = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int v = p.leaf[i]; v >= 0; v = p.node[v].parent) {
-    const ShareNode& nd = p.node[v];
-    const int tiles = (nd.t1 - nd.t0 + p.tile_keys - 1) / p.tile_keys;
-    const int all = nd.ns * p.group, chunks = (all + p.row_chunk - 1) / p.row_chunk;
-    const int R = (i - nd.s0) * p.group + hh, rc = R / p.row_chunk, rows = min(p.row_chunk, all - rc * p.row_chunk);
-    const int a = nd.unit0 + (g * chunks + rc) * (tiles + p.item_units) + p.item_units;
-    const int n = (a + tiles - 1) / p.quota - a / p.quota + 1;
-    const int base = nd.row0 + (g * all + rc * p.row_chunk) * nd.max_segs, r = R - rc * p.row_chunk;
-#pragma unroll 4
-    for (int k = 0; k < n; ++k) {
-      const int row0 = base + k * rows;
-      const float2 ml = p.part_ml[row0 + r];
-      const float4 o = *reinterpret_cast<const float4*>(p.part_o + (int64_t)row0 * D + ((int64_t)c4 * rows + r) * 4);
-      const float mn = fmaxf(M, ml.x), s0 = exp2f(M - mn), s1 = exp2f(ml.x - mn);   // (every segment has a key: mn is finite)
-      M = mn;
-      L = L * s0 + ml.y * s1;
-      acc.x = acc.x * s0 + o.x * s1;
-      acc.y = acc.y * s0 + o.y * s1;
-      acc.z = acc.z * s0 + o.z * s1;
-      acc.w = acc.w * s0 + o.w * s1;
+  Partial acc{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+  if (there) {
+    const int g = h / p.group, hh = h - g * p.group;
+    int turn = kl;   // this thread's next segment, counted from the node's first
+    for (int v = p.leaf[i]; v >= 0; v = p.node[v].parent) {
+      const ShareNode& nd = p.node[v];
+      int n, step, row;       // segments, rows between them, first row
+      int64_t at;             // of the channels, in floats
+      const float* po = p.part_o;
+      const float2* pm = p.part_ml;
+      int64_t o_step;
+      if (nd.max_segs < 0) {
+        n = -nd.max_segs;
+        step = p.n_q_heads;
+        row = nd.row0 * p.n_q_heads + h;
+        at = (int64_t)row * D + 4 * c4;
+        o_step = (int64_t)step * D;
+        po = p.split_o;
+        pm = p.split_ml;
+      } else {
+        const int tiles = (nd.t1 - nd.t0 + p.tile_keys - 1) / p.tile_keys;
+        const int all = nd.ns * p.group, chunks = (all + p.row_chunk - 1) / p.row_chunk;
+        const int R = (i - nd.s0) * p.group + hh, rc = R / p.row_chunk, rows = min(p.row_chunk, all - rc * p.row_chunk);
+        const int a = nd.unit0 + (g * chunks + rc) * (tiles + p.item_units) + p.item_units;
+        n = (a + tiles - 1) / p.quota - a / p.quota + 1;
+        const int row0 = nd.row0 + (g * all + rc * p.row_chunk) * nd.max_segs, r = R - rc * p.row_chunk;
+        step = rows;
+        row = row0 + r;
+        at = (int64_t)row0 * D + ((int64_t)c4 * rows + r) * 4;
+        o_step = (int64_t)rows * D;
+      }
+      int k = turn;
+      for (; k < n; k += 4 * kMergeLanes) {
+        float2 ml[4];
+        float4 o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int kj = k + j * kMergeLanes;
+          ml[j] = make_float2(-INFINITY, 0.f);
+          o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (kj < n) {
+            ml[j] = pm[row + kj * step];
+            o[j] = *reinterpret_cast<const float4*>(po + at + kj * o_step);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) join(acc, ml[j].x, ml[j].y, o[j]);
+      }
+      turn = ((turn - n) % kMergeLanes + kMergeLanes) % kMergeLanes;   // the lanes go on where the others stopped
     }
+    if (kl > 0) sm[threadIdx.x] = acc;
   }
-  const float inv = 1.f / L;
+  __syncthreads();
+  if (kl > 0 || !there) return;
+#pragma unroll
+  for (int j = 1; j < kMergeLanes; ++j) {
+    const Partial& x = sm[j * per_block + local];
+    join(acc, x.M, x.L, x.o);
+  }
+  const float inv = 1.f / acc.L;
   const int64_t at = ((int64_t)p.order[i] * p.n_q_heads + h) * D + 4 * c4;
   if constexpr (sizeof(T) == 2) {
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.o.x * inv, acc.o.y * inv), hi = __floats2bfloat162_rn(acc.o.z * inv, acc.o.w * inv);
     *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at) =
         make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
   } else {
-    *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + at) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + at) = make_float4(acc.o.x * inv, acc.o.y * inv, acc.o.z * inv, acc.o.w * inv);
   }
 }
 
@@ -215,7 +269,7 @@ cudaError_t launch_decode_shared(const SharedDecodeParams& p, cudaStream_t st) {
 cudaError_t launch_merge_shared(const SharedDecodeParams& p, int dtype, cudaStream_t st) {
   const int n = p.n_q_heads * (p.geom.head_dim / 4);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((n + kMergeThreads - 1) / kMergeThreads, p.n_seqs);
+  cfg.gridDim = dim3((n * kMergeLanes + kMergeThreads - 1) / kMergeThreads, p.n_seqs);
   cfg.blockDim = dim3(kMergeThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];

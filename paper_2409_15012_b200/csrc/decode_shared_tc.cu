@@ -95,7 +95,6 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
 #define BAR(i) (bar0 + 8u * (i))
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) {
     mbar_init(BAR(B_QF), 4);
     mbar_init(BAR(B_QE), 1);
@@ -124,10 +123,12 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  asm volatile("griddepcontrol.wait;" ::: "memory");   // the kernels ahead in the stream are done
-
   // Every role walks the same segments with the same counters: G tiles, it segments so far.
   ShareWalk walk = share_begin(p, blockIdx.x);
+  // The kernels ahead in the stream are done; only then may the next one start: the split pass of the
+  // sequences' own keys does not wait for this kernel before it begins.
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   ShareSegment s;
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");

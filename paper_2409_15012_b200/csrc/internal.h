@@ -149,6 +149,8 @@ struct DecodeParams {
   int32_t* status;        // device error word (0 = fine)
   int32_t n_seqs;
   int32_t total_items;    // chunks * Hkv * head_chunks
+  int32_t partial = 0;    // 1: every item leaves a partial result, and the launch does not wait for the one ahead of it
+                          // before it starts (the tensor-core kernel of a shared decode), but before it ends
   int32_t seq_id[kMaxCallSeqs];          // storage slots of the sequences
   int32_t n_eff[kMaxCallSeqs];           // keys attended: min(len, window) or len
   int32_t chunk_len[kMaxCallSeqs];       // keys per split of this sequence (multiple of 16)
@@ -287,6 +289,8 @@ struct ShareNode {
   int32_t unit0;      // first work unit
   int32_t row0;       // first row of partial results
   int32_t max_segs;   // segments of an item, at most
+  // max_segs < 0: keys of one sequence, taken by the split pass of the ordinary decode kernels in
+  // -max_segs splits, whose results begin at split slot row0 of its workspace ([slot][Hq][D])
 };
 struct SharedDecodeParams {
   const void* q;          // [n_seqs, Hq, D], caller's order
@@ -300,12 +304,15 @@ struct SharedDecodeParams {
   float scale_log2e;
   float* part_o;          // per segment [D / 4][rows][4]
   float2* part_ml;        // [row]: maximum (base-2 units) and sum
+  const float* split_o;   // results of the split pass
+  const float2* split_ml;
   int32_t* status;
-  int32_t n_seqs, n_nodes;
+  int32_t n_seqs;
+  int32_t n_nodes;        // nodes that are laid out as items; those of the split pass come behind the one that ends the units
   int32_t tile_keys, row_chunk, item_units;
   int32_t quota, n_ctas;  // work units per CTA
   int32_t shaped;
-  ShareNode node[kMaxShareNodes + 1];   // one more: where the units end
+  ShareNode node[kMaxShareNodes + 1];   // [n_nodes]: where the units end
   int32_t order[kMaxCallSeqs];          // row of q / out of the sequence
   int32_t newest[kMaxCallSeqs];         // its last position
   int32_t leaf[kMaxCallSeqs];           // its last node
