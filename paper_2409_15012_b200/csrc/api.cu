@@ -971,52 +971,70 @@ static int decode_plain(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int
 }
 
 // Lays the items of a tree's pieces out on the line of work units (internal.h) and cuts the line into equal
-// parts for at most max_ctas CTAs, fewer if the partial results would not fit `room` rows.  With `leaves`
-// the pieces of a single sequence are left to the split pass.  Returns false if it does not fit at all.
+// parts for at most max_ctas CTAs, fewer if the partial results would not fit `room` rows.  Items whose rows
+// make several chunks read the same keys: where they are long, each begins with a CTA of its own, so that all
+// chunks get to a key at about the same time and it comes from HBM once (128k keys, 64 sequences x 4 heads:
+// WAS -> NOW us).  With `leaves` the pieces of a single sequence are left to the split pass.  Returns false if
+// it does not fit at all.
 static bool lay_out_shared(const ShareTree& t, bool leaves, int max_ctas, int64_t room, SharedDecodeParams* p, int* n_leaves) {
   const int Hkv = p->geom.n_kv_heads;
-  int64_t units = 0;
   std::vector<int32_t> at(t.pieces.size(), -1);   // node of each piece
   p->n_nodes = 0;
   for (size_t v = 0; v < t.pieces.size(); ++v) {
     const SharePiece& s = t.pieces[v];
     if (leaves && s.ns == 1) continue;
-    const int64_t tiles = ((int64_t)s.t1 - s.t0 + p->tile_keys - 1) / p->tile_keys;
-    const int64_t chunks = ((int64_t)s.ns * p->group + p->row_chunk - 1) / p->row_chunk;
     at[v] = p->n_nodes;
-    p->node[p->n_nodes++] = ShareNode{s.t0, s.t1, s.slot, s.s0, s.ns, s.parent < 0 ? -1 : at[s.parent], (int32_t)units, 0, 0};
-    units += (tiles + p->item_units) * Hkv * chunks;
-    if (units > (1 << 30)) return false;
+    p->node[p->n_nodes++] = ShareNode{s.t0, s.t1, s.slot, s.s0, s.ns, s.parent < 0 ? -1 : at[s.parent], 0, 0, 0, 0};
   }
-  p->node[p->n_nodes] = ShareNode{0, 0, 0, 0, 0, -1, (int32_t)units, 0, 0};
   int end = p->n_nodes;
+  p->node[end] = ShareNode{0, 0, 0, 0, 0, -1, 0, 0, 0, 0};
   if (leaves)
     for (size_t v = 0; v < t.pieces.size(); ++v) {
       const SharePiece& s = t.pieces[v];
       if (s.ns != 1) continue;
       at[v] = ++end;
-      p->node[end] = ShareNode{s.t0, s.t1, s.slot, s.s0, 1, s.parent < 0 ? -1 : at[s.parent], 0, 0, -1};
+      p->node[end] = ShareNode{s.t0, s.t1, s.slot, s.s0, 1, s.parent < 0 ? -1 : at[s.parent], 0, 0, 0, -1};
     }
   *n_leaves = end - p->n_nodes;
   for (size_t i = 0; i < t.leaf.size(); ++i) p->leaf[i] = at[t.leaf[i]];
-  for (int64_t ctas = max_ctas;; ctas = ctas * 3 / 4) {
-    const int64_t quota = std::max<int64_t>((units + ctas - 1) / ctas, p->item_units + 1);
-    int64_t rows = 0;
+
+  // units and rows for a given quota
+  auto lay = [&](int64_t quota, int64_t* units, int64_t* rows) {
+    *units = *rows = 0;
     for (int v = 0; v < p->n_nodes; ++v) {
       ShareNode& nd = p->node[v];
       const int64_t tiles = ((int64_t)nd.t1 - nd.t0 + p->tile_keys - 1) / p->tile_keys;
-      nd.max_segs = (int32_t)std::min<int64_t>((tiles + quota - 2) / quota + 1, ctas);
-      nd.row0 = (int32_t)rows;
-      rows += (int64_t)nd.ns * p->n_q_heads * nd.max_segs;
-      if (rows > room) break;
+      const int64_t chunks = ((int64_t)nd.ns * p->group + p->row_chunk - 1) / p->row_chunk;
+      int64_t len = tiles + p->item_units;
+      if (chunks > 1 && len > 2 * quota) {
+        len = (len + quota - 1) / quota * quota;
+        *units = (*units + quota - 1) / quota * quota;
+      }
+      if (*units + len * Hkv * chunks > (1 << 30)) return false;
+      nd.unit0 = (int32_t)*units;
+      nd.item_len = (int32_t)len;
+      *units += len * Hkv * chunks;
+      nd.max_segs = (int32_t)((tiles + quota - 2) / quota + 1);
+      nd.row0 = (int32_t)std::min<int64_t>(*rows, INT32_MAX);
+      *rows += (int64_t)nd.ns * p->n_q_heads * nd.max_segs;
     }
-    if (rows <= room) {
+    p->node[p->n_nodes].unit0 = (int32_t)*units;
+    return true;
+  };
+  int64_t units, rows;
+  if (!lay(INT32_MAX, &units, &rows)) return false;
+  int64_t quota = std::max<int64_t>((units + max_ctas - 1) / max_ctas, p->item_units + 1);
+  for (int step = 0; step < 1000; ++step) {
+    if (!lay(quota, &units, &rows)) return false;
+    if ((units + quota - 1) / quota <= max_ctas && rows <= room) {
       p->quota = (int32_t)quota;
       p->n_ctas = (int32_t)((units + quota - 1) / quota);
       return true;
     }
-    if (ctas == 1) return false;
+    quota += 1 + (rows > room ? quota / 4 : quota / 64);
+    if (quota > (1 << 30)) break;
   }
+  return false;
 }
 
 // The keys that only one sequence has, as a launch of the ordinary split pass over the sequences in the

@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kMergeThreads) merge_shared_kernel(const __gri
         const int tiles = (nd.t1 - nd.t0 + p.tile_keys - 1) / p.tile_keys;
         const int all = nd.ns * p.group, chunks = (all + p.row_chunk - 1) / p.row_chunk;
         const int R = (i - nd.s0) * p.group + hh, rc = R / p.row_chunk, rows = min(p.row_chunk, all - rc * p.row_chunk);
-        const int a = nd.unit0 + (g * chunks + rc) * (tiles + p.item_units) + p.item_units;
+        const int a = nd.unit0 + (g * chunks + rc) * nd.item_len + p.item_units;
         n = (a + tiles - 1) / p.quota - a / p.quota + 1;
         const int row0 = nd.row0 + (g * all + rc * p.row_chunk) * nd.max_segs, r = R - rc * p.row_chunk;
         step = rows;

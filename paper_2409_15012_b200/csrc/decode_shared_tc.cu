@@ -8,21 +8,23 @@
 // against 1500 of products and about as many of exponentials.  A row that stands alone (a sequence's own last
 // keys) costs the same tile of products, which fits under the stream all the same.
 //
-//   warp 0     page producer: ids from the block table, 4 KB tensor copies (16 tokens x 64 channels of
-//              K and of V) into a ring of 128-key stages
-//   warp 1     one thread issues S = Q K^T into one of two S buffers
-//   warps 2-3  P V of a stream each, P in two bf16 terms (value and rounding residual: 16 bits, as
+//   warps 0, 3 page producers for K and for V: ids from the block table, 2 KB tensor copies (16 tokens x
+//              64 channels) into a ring of 128-key stages each.  A warp needs about 100 cycles per
+//              copy: with one warp for both, its 32 copies per tile were the limit (3200 cycles)
+//   warp 1     issues S = Q K^T into one of two S buffers, a stream's half at a time
+//   warp 2     P V of both streams, P in two bf16 terms (value and rounding residual: 16 bits, as
 //              the other decode kernels hold them) from tensor memory
 //   warps 4-7, 8-11  the softmax of stream 0 and 1, a row per thread
 //   warps 12-15  rows of Q into shared memory for the next segment, then the results of this one
 //
 // Operands straight from the pages.  A page block holds 16 rows of K and 16 of V whose 16-byte
 // chunks are stored permuted by (token & 7), inside 128 bytes the image of a 128-byte-swizzled operand; a
-// copy of one 64-channel half lays the page down as K [2 groups of 8 tokens][1 KB], V likewise.  The
-// groups g of all pages then lie a fixed 4 KB apart, which a matrix descriptor can name: stream g takes
-// tokens 8 g .. 8 g + 7 of every page, as N = 64 columns of S (column 8 j + t = token 8 g + t of the tile's
-// page j) and as 4 steps of 16 keys (two pages each) of its P V.  So the two halves of S are two independent
-// flash-attention passes with their own reference, sum and accumulator, merged at the end.
+// copy of one 64-channel half of a page's K lays down 16 such rows, and eight pages one after the other
+// are the [128 keys x 64 channels] block that a matrix descriptor names.  Stream h takes the keys of pages 4 h .. 4 h + 3 of
+// every tile: two independent flash-attention passes with their own reference, sum and accumulator, merged at
+// the end.  K and V have rings of their own because a tile's K is done with when its scores are, a softmax and a
+// product earlier than its V: with both in one ring of three stages, the loads of the tile after next came
+// too late (2400 cycles a tile where neither HBM nor products limit, with any number of products).
 //
 // TMEM: S0, S1, O_0, O_1 = 4 x 128 columns.  All mbarrier waits are bounded; on time-out a status
 // word is raised and every role leaves its loop.
@@ -40,45 +42,42 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kRows = 128, kTile = 128;          // rows of an item, keys per tile
 constexpr int kTilePages = kTile / kPage;
-constexpr int kBlk = 4096;                       // one page's K and V, 64 channels
-constexpr int kHalf = kTilePages * kBlk;         // 64 channels of a tile's K and V
+constexpr int kPiece = 2048;                     // 64 channels of one page's K or V
+constexpr int kHalf = kTilePages * kPiece;       // 64 channels of a tile's K or V
 constexpr int kQHalf = kRows * 128;              // 64 channels of Q
-constexpr int kSmBarBytes = 256;
 constexpr uint32_t kColS = 0, kColO = 256;
-constexpr float kMaxLead = 32.f;                 // a score this far (base 2) above its row's reference moves it
+constexpr float kMaxLead = 32.f;                 // a score this far (base 2) above its row's reference moves it;
+constexpr float kMaxSum = 0x1p38f;               // 64 weights that do not lead that far add up to no more
+
+enum {
+  B_QF = 0, B_QE = 1,        // Q there / consumed by the segment's score products
+  B_SF = 2, B_SR = 6,        // + 2 stream + buffer: the stream's half of an S buffer: scores there / P in it consumed
+  B_PF = 10,                 // + 2 stream + buffer: P written
+  B_OF = 14,                 // per stream: the segment's last P V done
+  B_XC = 16, B_OR = 17,      // references and sums published / results read
+  B_KF = 18                  // K stages full, then free, V stages full, then free
+};
 
 template <int D>
 struct Layout {
   static constexpr int kHalves = D / 64;
   static constexpr int kStageBytes = kHalves * kHalf;
   static constexpr int kStages = D == 128 ? 3 : 6;
+  static constexpr int kKE = B_KF + kStages, kVF = B_KF + 2 * kStages, kVE = B_KF + 3 * kStages, kBars = B_KF + 4 * kStages;
   static constexpr int kSmQ = 0;
-  static constexpr int kSmKV = kHalves * kQHalf;
-  static constexpr int kSmBar = kSmKV + kStages * kStageBytes;
-  static constexpr int kSmXchg = kSmBar + kSmBarBytes;
+  static constexpr int kSmK = kHalves * kQHalf;
+  static constexpr int kSmV = kSmK + kStages * kStageBytes;
+  static constexpr int kSmBar = kSmV + kStages * kStageBytes;
+  static constexpr int kSmXchg = kSmBar + (kBars * 8 + 16 + 255) / 256 * 256;
   static constexpr int kBytes = kSmXchg + 2 * kRows * 8 + 768;   // + slack to align a 256-byte aligned base to 1024
   static_assert(kBytes <= 227 * 1024, "shared memory");
 };
-
-enum {
-  B_QF = 0, B_QE = 1,        // Q there / consumed by the segment's score products
-  B_F = 2, B_E = 8,          // stage full / free (both P V issuers)
-  B_SF = 14, B_SR = 16,      // S buffer: scores there / P in it consumed by both streams
-  B_PF = 18,                 // 18 + 2 stream + buffer: P written
-  B_OF = 22,                 // per stream: the segment's last P V done
-  B_XC = 24, B_OR = 25,      // references and sums published / results read
-  B_N = 26
-};
-static_assert(B_N * 8 + 16 <= kSmBarBytes, "barriers");
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
       ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
 }
-
-// Column e of a stream's 64 is key key_of(e) + 8 g behind the tile's first.
-__device__ __forceinline__ constexpr int key_of(int e) { return 16 * (e >> 3) + (e & 7); }
 
 // kShape: scores capped (1), biased (2), both (3)
 template <int D, int kShape>
@@ -90,8 +89,8 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* gbase = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t bar0 = base + L::kSmBar;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gbase + L::kSmBar + B_N * 8);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(gbase + L::kSmBar + B_N * 8 + 8);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gbase + L::kSmBar + L::kBars * 8);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gbase + L::kSmBar + L::kBars * 8 + 8);
 #define BAR(i) (bar0 + 8u * (i))
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -99,16 +98,18 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
     mbar_init(BAR(B_QF), 4);
     mbar_init(BAR(B_QE), 1);
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(BAR(B_F + s), 1);
-      mbar_init(BAR(B_E + s), 2);
+      mbar_init(BAR(B_KF + s), 1);
+      mbar_init(BAR(L::kKE + s), 1);
+      mbar_init(BAR(L::kVF + s), 1);
+      mbar_init(BAR(L::kVE + s), 1);
     }
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < 4; ++s) {
       mbar_init(BAR(B_SF + s), 1);
-      mbar_init(BAR(B_SR + s), 2);
+      mbar_init(BAR(B_SR + s), 1);
       mbar_init(BAR(B_PF + s), 4);
-      mbar_init(BAR(B_PF + 2 + s), 4);
-      mbar_init(BAR(B_OF + s), 1);
     }
+    mbar_init(BAR(B_OF + 0), 1);
+    mbar_init(BAR(B_OF + 1), 1);
     mbar_init(BAR(B_XC), 8);
     mbar_init(BAR(B_OR), 4);
     abort_flag[0] = 0;   // any role gave up
@@ -132,8 +133,11 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
   ShareSegment s;
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    if (warp == 0) {
-      // ------------------------------ page producer ------------------------------
+    if (warp == 0 || warp == 3) {
+      // ------------------------------ page producers ------------------------------
+      const int v = warp == 3;   // K or V
+      const int full = v ? L::kVF : B_KF, free = v ? L::kVE : L::kKE;
+      const uint32_t ring = base + (v ? L::kSmV : L::kSmK);
       bool ok = true;
       int G = 0;
       if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&pages) : "memory");
@@ -148,99 +152,108 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
             ids = ids_next;
             if (pg + 32 + lane < page_hi) ids_next = tbl[pg + 32 + lane];
           }
-          const int st = G % kStages, turn = G / kStages;
-          if (turn > 0) {   // lane 0 waits; the verdict is made warp-uniform
-            int w = 1;
-            if (lane == 0) w = mbar_wait(BAR(B_E + st), (turn - 1) & 1, abort_flag);
-            if (!__shfl_sync(0xffffffffu, w, 0)) { ok = false; break; }
-          }
-          const int n_pg = min(kTilePages, page_hi - pg);
-          if (lane == 0) mbar_expect_tx(BAR(B_F + st), n_pg * L::kHalves * kBlk);
+          const int st = G % kStages, turn = G / kStages, n_pg = min(kTilePages, page_hi - pg);
           const int j = lane & (kTilePages - 1), h = lane / kTilePages;
           const int id = __shfl_sync(0xffffffffu, ids, rel + j);
+          if (turn > 0) {   // lane 0 waits; the verdict is made warp-uniform
+            int w = 1;
+            if (lane == 0) w = mbar_wait(BAR(free + st), (turn - 1) & 1, abort_flag);
+            if (!__shfl_sync(0xffffffffu, w, 0)) { ok = false; break; }
+          }
+          if (lane == 0) mbar_expect_tx(BAR(full + st), n_pg * L::kHalves * kPiece);
+          __syncwarp();
           if (h < L::kHalves && j < n_pg)
-            tma_load_4d(base + L::kSmKV + st * L::kStageBytes + h * kHalf + j * kBlk, &pages, 64 * h, 0, 0,
-                        id * p.geom.n_kv_heads + s.g, BAR(B_F + st));
+            tma_load_4d(ring + st * L::kStageBytes + h * kHalf + j * kPiece, &pages, 64 * h, 0, v,
+                        id * p.geom.n_kv_heads + s.g, BAR(full + st));
         }
       }
       if (!ok && lane == 0) {   // leave only after the copies already issued have landed (bounded)
         atomicExch(p.status, kDevWaitTimeout);
         for (int back = 1; back <= kStages && G - back >= 0; ++back)
-          mbar_wait(BAR(B_F + (G - back) % kStages), ((G - back) / kStages) & 1, abort_flag + 1);
+          mbar_wait(BAR(full + (G - back) % kStages), ((G - back) / kStages) & 1, abort_flag + 1);
       }
     } else if (warp == 1) {
       // ------------------------------ score products ------------------------------
-      if (lane == 0) {
-        constexpr uint32_t kIdesc = idesc_bf16(0, 64);
-        bool ok = true;
-        int G = 0;
-        for (int it = 0; ok && share_next(p, blockIdx.x, walk, s); ++it) {
-          ok = mbar_wait(BAR(B_QF), it & 1, abort_flag);
-          for (int t = s.t0; t < s.t1 && ok; t += kTile, ++G) {
-            const int sb = G & 1, st = G % kStages;
-            ok = mbar_wait(BAR(B_F + st), (G / kStages) & 1, abort_flag);
-            if (ok && G >= 2) ok = mbar_wait(BAR(B_SR + sb), ((G >> 1) - 1) & 1, abort_flag);
-            if (!ok) break;
-            tc_fence_after();
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-              const uint64_t kdesc = smem_desc(base + L::kSmKV + st * L::kStageBytes + g * 1024, 16, kBlk);
-              const uint64_t qdesc = smem_desc(base + L::kSmQ, 16, 1024);
-#pragma unroll
-              for (int ks = 0; ks < D / 16; ++ks)
-                umma_bf16(tmem + kColS + sb * 128 + g * 64, qdesc + (uint64_t)((ks >> 2) * (kQHalf >> 4) + (ks & 3) * 2),
-                          kdesc + (uint64_t)((ks >> 2) * (kHalf >> 4) + (ks & 3) * 2), kIdesc, ks > 0);
-            }
-            umma_commit(BAR(B_SF + sb));
-          }
-          if (ok) umma_commit(BAR(B_QE));
-        }
-        if (!ok) atomicExch(p.status, kDevWaitTimeout);
-      }
-    } else {
-      // ------------------------------ P V of a stream ------------------------------
-      constexpr uint32_t kIdesc = idesc_bf16(1, D);
-      const int g = warp - 2;
+      constexpr uint32_t kIdesc = idesc_bf16(0, 64);
+      const uint64_t qdesc = smem_desc(base + L::kSmQ, 16, 1024);
       bool ok = true;
       int G = 0;
       for (int it = 0; ok && share_next(p, blockIdx.x, walk, s); ++it) {
-        // the segment's first P V overwrites the accumulator
+        ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_QF), it & 1, abort_flag));
+        for (int t = s.t0; t < s.t1 && ok; t += kTile, ++G) {
+          const int sb = G & 1, st = G % kStages;
+          ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_KF + st), (G / kStages) & 1, abort_flag));
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {   // a stream's half waits for its own P V alone
+            if (ok && G >= 2) ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_SR + 2 * g + sb), ((G >> 1) - 1) & 1, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t kdesc = smem_desc(base + L::kSmK + st * L::kStageBytes + g * 64 * 128, 16, 1024);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks)
+              umma_bf16_warp(tmem + kColS + sb * 128 + g * 64, qdesc + (uint64_t)((ks >> 2) * (kQHalf >> 4) + (ks & 3) * 2),
+                             kdesc + (uint64_t)((ks >> 2) * (kHalf >> 4) + (ks & 3) * 2), kIdesc, ks > 0);
+            umma_commit_warp(BAR(B_SF + 2 * g + sb));
+          }
+          if (!ok) break;
+          umma_commit_warp(BAR(L::kKE + st));
+        }
+        if (ok) umma_commit_warp(BAR(B_QE));
+      }
+      if (!ok && lane == 0) atomicExch(p.status, kDevWaitTimeout);
+    } else {
+      // ------------------------------ P V ------------------------------
+      constexpr uint32_t kIdesc = idesc_bf16(1, D);
+      bool ok = true;
+      int G = 0;
+      for (int it = 0; ok && share_next(p, blockIdx.x, walk, s); ++it) {
+        // the segment's first P V overwrites the accumulators
         if (it >= 1) ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_OR), (it - 1) & 1, abort_flag));
         for (int t = s.t0; t < s.t1 && ok; t += kTile, ++G) {
           const int sb = G & 1, st = G % kStages;
-          ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_F + st), (G / kStages) & 1, abort_flag));
+          ok = __all_sync(0xffffffffu, mbar_wait(BAR(L::kVF + st), (G / kStages) & 1, abort_flag));
           if (!ok) break;
-          // steps of 16 keys = two pages' groups; the segment's last tile may hold fewer, and rows that
-          // are no keys (behind the last one, or a page that was not loaded), whose weight of zero an
-          // infinity or a NaN would survive, are cleared meanwhile
-          const int left = s.t1 - t, steps = left >= kTile ? 4 : (left + 31) / 32;
+          // A stream's steps of 16 keys are pages; the segment's last tile may hold fewer (one at least is taken: the
+          // accumulator is read), and rows that are no keys (behind the last one, or of a page that was not
+          // loaded), whose weight of zero an infinity or a NaN would survive, are cleared meanwhile.
+          const int left = s.t1 - t;
           if (left < kTile) {
-            unsigned char* v = gbase + L::kSmKV + st * L::kStageBytes + 2048 + g * 1024;
-            for (int r = (left / kPage) * 8; r < steps * 16; ++r) {   // row 8 j + token of page j
-              if (16 * (r >> 3) + 8 * g + (r & 7) < left) continue;
-              for (int c = lane; c < D / 8; c += 32)
-                *reinterpret_cast<uint4*>(v + (c >> 3) * kHalf + (r >> 3) * kBlk + (r & 7) * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              const int steps = min(max((left - 64 * g + 15) >> 4, 1), 4), first = min(max(left - 64 * g, 0), 16 * steps);
+              unsigned char* v = gbase + L::kSmV + st * L::kStageBytes + g * 64 * 128;
+              for (int x = lane; x < (16 * steps - first) * (D / 8); x += 32) {   // 16-byte chunks
+                const int row = first + x / (D / 8), c = x % (D / 8);
+                *reinterpret_cast<uint4*>(v + (c >> 3) * kHalf + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+              }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the products read through the async proxy
             __syncwarp();
           }
-          ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_PF + 2 * g + sb), (G >> 1) & 1, abort_flag));
-          if (!ok) break;
-          if (lane == 0) {
+          const bool last = t + kTile >= s.t1;
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(BAR(B_PF + 2 * g + sb), (G >> 1) & 1, abort_flag));
+            if (!ok) break;
             tc_fence_after();
-            const uint64_t vdesc = smem_desc(base + L::kSmKV + st * L::kStageBytes + 2048 + g * 1024, kHalf, kBlk);
+            const uint64_t vdesc = smem_desc(base + L::kSmV + st * L::kStageBytes + g * 64 * 128, kHalf, 1024);
+            const uint32_t o = tmem + kColO + g * 128, pcol = tmem + kColS + sb * 128 + g * 64;
+            if (left - 64 * g >= 64) {
+              umma_bf16_ts_warp(o, pcol, vdesc, kIdesc, t > s.t0);
 #pragma unroll
-            for (int term = 0; term < 2; ++term)
-#pragma unroll
-              for (int ks = 0; ks < 4; ++ks)
-                if (ks < steps)
-                  umma_bf16_ts(tmem + kColO + g * 128, tmem + kColS + sb * 128 + g * 64 + term * 32 + ks * 8,
-                               vdesc + (uint64_t)(ks * (2 * kBlk >> 4)), kIdesc, (t > s.t0 || term > 0 || ks > 0) ? 1u : 0u);
-            if (t + kTile >= s.t1) umma_commit(BAR(B_OF + g));
-            umma_commit(BAR(B_E + st));
-            umma_commit(BAR(B_SR + sb));
+              for (int x = 1; x < 8; ++x)   // four steps of the values, four of the residuals
+                umma_bf16_ts_warp(o, pcol + 8 * x, vdesc + (uint64_t)((x & 3) * (kPiece >> 4)), kIdesc, 1u);
+            } else {
+              const int steps = max((left - 64 * g + 15) >> 4, 1);
+#pragma unroll 1
+              for (int x = 0; x < 8; ++x)
+                if ((x & 3) < steps)
+                  umma_bf16_ts_warp(o, pcol + 8 * x, vdesc + (uint64_t)((x & 3) * (kPiece >> 4)), kIdesc, t > s.t0 || x > 0);
+            }
+            if (last) umma_commit_warp(BAR(B_OF + g));
+            umma_commit_warp(BAR(B_SR + 2 * g + sb));
+            if (g == 1) umma_commit_warp(BAR(L::kVE + st));
           }
-          __syncwarp();
         }
       }
       if (!ok && lane == 0) atomicExch(p.status, kDevWaitTimeout);
@@ -284,7 +297,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
       ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_OF + 0), it & 1, abort_flag) && mbar_wait(BAR(B_OF + 1), it & 1, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      const float m = fmaxf(lo.x, hi.x);   // (finite: token 0 of the segment's first page is a key)
+      const float m = fmaxf(lo.x, hi.x);   // (finite: stream 0 has the segment's first key)
       const float e_lo = ex2_approx(lo.x - m), e_hi = ex2_approx(hi.x - m);
       float* to = p.part_o + (int64_t)now.seg_row * D + r * 4;
       const bool mine = r < now.rows;
@@ -336,7 +349,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
       }
       for (int t = s.t0; t < s.t1; t += kTile, ++G) {
         const int sb = G & 1;
-        if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SF + sb), (G >> 1) & 1, abort_flag))) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SF + 2 * g + sb), (G >> 1) & 1, abort_flag))) { ok = false; break; }
         if (!idle) {
           tc_fence_after();
           const uint32_t s_addr = lane_base + kColS + sb * 128 + g * 64;
@@ -347,7 +360,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
           tmem_ld32(s_addr + 32, s1);
           tmem_wait_ld_pin(s0, s1);
           if constexpr (kShape != 0) {   // raw products -> shaped base-2 scores
-            const float first = -slope * (float)(newest - t - 8 * g);   // bias of column 0
+            const float first = -slope * (float)(newest - t - 64 * g);   // bias of column 0
             float top = 0.f;
 #pragma unroll
             for (int e = 0; e < 64; e += 2) {
@@ -363,7 +376,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
                 top = fmax3(top, uu.x, uu.y);
                 x = mul2(mul2(q, x), pack2(p.shape.post, p.shape.post));
               }
-              if constexpr (kShape & 2) x = add2(x, pack2(fmaf(slope, (float)key_of(e), first), fmaf(slope, (float)key_of(e + 1), first)));
+              if constexpr (kShape & 2) x = add2(x, pack2(fmaf(slope, (float)e, first), fmaf(slope, (float)(e + 1), first)));
               const float2 y = unpack2(x);
               sv[e] = __float_as_uint(y.x);
               sv[e + 1] = __float_as_uint(y.y);
@@ -375,7 +388,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
                 tmem_wait_ld_pin(s0, s1);
 #pragma unroll
                 for (int e = 0; e < 64; ++e) {
-                  const float x = __uint_as_float(sv[e]) * p.shape.pre, o = (kShape & 2) ? fmaf(slope, (float)key_of(e), first) : 0.f;
+                  const float x = __uint_as_float(sv[e]) * p.shape.pre, o = (kShape & 2) ? fmaf(slope, (float)e, first) : 0.f;
                   const float a = tanh_poly(x), b = tanh_exp(x);
                   sv[e] = __float_as_uint(fmaf(fabsf(x) <= 1.f ? a : b, p.shape.post, o));
                 }
@@ -384,54 +397,73 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
           }
           const float scale = kShape ? 1.f : p.scale_log2e;
           if (t + kTile > s.t1) {
-            const int left = s.t1 - t - 8 * g;
+            const int left = s.t1 - t - 64 * g;
 #pragma unroll
             for (int e = 0; e < 64; ++e)
-              if (key_of(e) >= left) sv[e] = 0xff800000u;
+              if (e >= left) sv[e] = 0xff800000u;
           }
-          float mx0 = -INFINITY, mx1 = -INFINITY;
+          // A row's reference is the maximum of its first tile and only moves when a later score leads it
+          // by more than 2^kMaxLead, which shows in the sum of the tile's weights: so the exponentials
+          // wait for no maximum, and none is computed.
+          auto tile_max = [&]() {
+            float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
-          for (int e = 0; e < 64; e += 4) {
-            mx0 = fmax3(mx0, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
-            mx1 = fmax3(mx1, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
-          }
-          const float mt = fmaxf(mx0, mx1) * scale;
-          if (t == s.t0) {
-            m_ref = mt;
-          } else if (__any_sync(0xffffffffu, mt > m_ref + kMaxLead)) {
-            // rare: move the reference of the leading rows and rescale what they have accumulated, once
-            // this stream's previous P V has landed (the S buffer of tile G - 1 is released when both streams' are)
+            for (int e = 0; e < 64; e += 4) {
+              mx0 = fmax3(mx0, __uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+              mx1 = fmax3(mx1, __uint_as_float(sv[e + 2]), __uint_as_float(sv[e + 3]));
+            }
+            return fmaxf(mx0, mx1) * scale;
+          };
+          if (t == s.t0) m_ref = tile_max();
+          float sum;
+          // P: values over the first 32 of the stream's columns, residuals over the others (the scores are
+          // all in registers by now); in two halves, which keeps the registers within the launch's 128
+          auto weights = [&]() {
+            const float neg = m_ref == -INFINITY ? 0.f : -m_ref;   // (a stream without a key: weights 0, no NaN)
+            f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              uint32_t pk[16], pl[16];
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) {
+                const int e = 32 * half + i;
+                const float a = ex2_approx(fmaf(__uint_as_float(sv[e]), scale, neg));
+                const float b = ex2_approx(fmaf(__uint_as_float(sv[e + 1]), scale, neg));
+                if (i & 2) sum1 = add2(sum1, pack2(a, b));
+                else sum0 = add2(sum0, pack2(a, b));
+                split_bf16(a, b, pk[i >> 1], pl[i >> 1]);
+              }
+              tmem_st16(s_addr + 16 * half, pk);
+              tmem_st16(s_addr + 32 + 16 * half, pl);
+            }
+            const float2 x = unpack2(add2(sum0, sum1));
+            sum = x.x + x.y;
+          };
+          weights();
+          if (__any_sync(0xffffffffu, !(sum <= kMaxSum))) {
+            // rare (an overflow gives infinity or NaN, which fail the comparison too): move the reference of
+            // the leading rows and rescale what they have accumulated, once this stream's previous P V has landed
+            const float mt = tile_max();
             const bool far = mt > m_ref + kMaxLead;
             const float alpha = far ? ex2_approx(m_ref - mt) : 1.f;
-            if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SR + (sb ^ 1)), ((G - 1) >> 1) & 1, abort_flag))) { ok = false; break; }
-            tc_fence_after();
+            if (t > s.t0) {
+              if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SR + 2 * g + (sb ^ 1)), ((G - 1) >> 1) & 1, abort_flag))) { ok = false; break; }
+              tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-              uint32_t ov[32];
-              tmem_ld32(o_addr + c * 32, ov);
-              tmem_wait_ld();
+              for (int c = 0; c < D / 32; ++c) {
+                uint32_t ov[32];
+                tmem_ld32(o_addr + c * 32, ov);
+                tmem_wait_ld();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
-              tmem_st32(o_addr + c * 32, ov);
+                for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
+                tmem_st32(o_addr + c * 32, ov);
+              }
             }
             l *= alpha;
             if (far) m_ref = mt;
+            weights();
           }
-          const float neg = m_ref == -INFINITY ? 0.f : -m_ref;   // (a stream without a key: weights 0, no NaN)
-          f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
-          uint32_t pk[32], pl[32];
-#pragma unroll
-          for (int e = 0; e < 64; e += 2) {
-            const float a = ex2_approx(fmaf(__uint_as_float(sv[e]), scale, neg));
-            const float b = ex2_approx(fmaf(__uint_as_float(sv[e + 1]), scale, neg));
-            if (e & 2) sum1 = add2(sum1, pack2(a, b));
-            else sum0 = add2(sum0, pack2(a, b));
-            split_bf16(a, b, pk[e >> 1], pl[e >> 1]);
-          }
-          const float2 sum = unpack2(add2(sum0, sum1));
-          l += sum.x + sum.y;
-          tmem_st32(s_addr, pk);          // value over the first 32 of the stream's columns, residual over the others
-          tmem_st32(s_addr + 32, pl);
+          l += sum;
           tmem_wait_st();
           tc_fence_before();
         }
@@ -458,13 +490,13 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
 }
 
 // Paged storage of one owner layer, native bf16 format, as [page and head][K | V][16 tokens][channels];
-// box = 64 channels of 16 tokens of K and V.  The stored chunks are permuted already, so the copy does not swizzle.
+// box = 64 channels of 16 tokens of K or V.  The stored chunks are permuted already, so the copy does not swizzle.
 bool make_page_map(CUtensorMap* map, const void* pool, const KvGeom& ge, int64_t pages) {
   EncodeTiledFn fn = encode_fn();
   if (fn == nullptr) return false;
   cuuint64_t dims[4] = {(cuuint64_t)ge.head_dim, (cuuint64_t)kPage, 2, (cuuint64_t)(pages * ge.n_kv_heads)};
   cuuint64_t strides[3] = {(cuuint64_t)ge.row_bytes, (cuuint64_t)kPage * ge.row_bytes, (cuuint64_t)ge.blk_bytes};
-  cuuint32_t box[4] = {64, (cuuint32_t)kPage, 2, 1};
+  cuuint32_t box[4] = {64, (cuuint32_t)kPage, 1, 1};
   cuuint32_t estr[4] = {1, 1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,

@@ -287,6 +287,7 @@ struct ShareNode {
   int32_t s0, ns;     // sequences, in tree order
   int32_t parent;     // node that ends where this one begins, -1 = none
   int32_t unit0;      // first work unit
+  int32_t item_len;   // units of an item (there may be some left over at its end)
   int32_t row0;       // first row of partial results
   int32_t max_segs;   // segments of an item, at most
   // max_segs < 0: keys of one sequence, taken by the split pass of the ordinary decode kernels in
@@ -345,14 +346,16 @@ __device__ __forceinline__ bool share_next(const SharedDecodeParams& p, int cta,
   while (w.u < w.end) {
     while (p.node[w.v + 1].unit0 <= w.u) ++w.v;
     const ShareNode& nd = p.node[w.v];
-    const int tiles = (nd.t1 - nd.t0 + p.tile_keys - 1) / p.tile_keys, len = tiles + p.item_units;
-    const int item = (w.u - nd.unit0) / len, a = nd.unit0 + item * len + p.item_units;   // unit of the item's first tile
+    const int tiles = (nd.t1 - nd.t0 + p.tile_keys - 1) / p.tile_keys;
+    const int item = (w.u - nd.unit0) / nd.item_len, a = nd.unit0 + item * nd.item_len + p.item_units;   // unit of the item's first tile
     const int hi = min(a + tiles, w.end), lo = max(a, w.u);
-    w.u = hi;
-    if (hi <= lo) {            // (only units of the item's own cost)
-      w.u = max(hi, min(a, w.end));
+    w.u = min(a - p.item_units + nd.item_len, w.end);
+    // (units left over in front of the next node belong to none: the last node before them takes them)
+    if (item >= p.geom.n_kv_heads * ((nd.ns * p.group + p.row_chunk - 1) / p.row_chunk)) {
+      w.u = min(p.node[w.v + 1].unit0, w.end);
       continue;
     }
+    if (hi <= lo) continue;    // (only units of the item's own cost, or left over)
     const int all = nd.ns * p.group, chunks = (all + p.row_chunk - 1) / p.row_chunk, rc = item % chunks;
     s.node = w.v;
     s.s0 = nd.s0;
