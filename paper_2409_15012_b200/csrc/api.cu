@@ -851,30 +851,35 @@ static cudaError_t launch_split_pass(const mixattn_ctx* c, const ShapedDecodePar
                                       : launch_decode_split_f32(p, sp, st);
 }
 
+// Splits of a shared decode's own keys: about four items for each of the launch's CTAs, which evens out
+// lengths from a few tokens to thousands (64 sequences of 16 to 2048 own tokens: WAS us with splits of 2048).
+static int64_t own_split(const mixattn_ctx* c, int64_t total, const DecodeParams* p) {
+  if (c->split_tokens > 0) return (c->split_tokens + kPage - 1) / kPage * kPage;
+  const int64_t t = total * c->cfg.n_kv_heads * p->head_chunks / (4 * (int64_t)p->partial);
+  return std::min<int64_t>(std::max<int64_t>((t + kPage - 1) / kPage * kPage, 512), kSplitTokens);
+}
+
 // The cutting itself: n_eff[0 .. nb) are set, `total` is their sum.
 static int cut_splits(const mixattn_ctx* c, int layer, int nb, int64_t total, DecodeParams* p, bool* any_split) {
   const int Hkv = c->cfg.n_kv_heads;
-  int64_t T = c->split_tokens > 0 ? (c->split_tokens + kPage - 1) / kPage * kPage : kSplitTokens;
+  int64_t T = p->partial ? own_split(c, total, p) : c->split_tokens > 0 ? (c->split_tokens + kPage - 1) / kPage * kPage : kSplitTokens;
   // Shaped scores, and too few items of that size to even out over the SMs: half the size.  (17
   // sequences of 1 to 64k tokens, quantised cache: 86 -> 67 us; 5 of 9k to 20k: 68 -> 49; with
   // 14 items per SM it makes no difference.  Layers with plain scores keep the splits, and with them
   // the order of summation, that they have had.)
-  if (c->split_tokens == 0 && !c->scores[layer].plain() &&
+  if (!p->partial && c->split_tokens == 0 && !c->scores[layer].plain() &&
       total * c->cfg.n_kv_heads * p->head_chunks < (int64_t)kFewItems * c->sm_count * T)
     T = kSplitTokens / 2;
   int64_t t_min = (total + kWsExtraChunks - 1) / kWsExtraChunks;
   t_min = (t_min + kPage - 1) / kPage * kPage;
   if (T < t_min) T = t_min;
   const int64_t pairs = (int64_t)nb * Hkv * p->head_chunks;
-  int64_t nc_wave = c->split_tokens > 0 ? 1 : c->sm_count / pairs;
+  int64_t nc_wave = c->split_tokens > 0 || p->partial ? 1 : c->sm_count / pairs;
   if (nc_wave > kWsWaveChunks / nb) nc_wave = kWsWaveChunks / nb;   // the workspace bounds the extra splits
   int base = 0;
   *any_split = false;
   for (int j = 0; j < nb; ++j) {
     const int64_t n = p->n_eff[j];
-    p->chunk_base[j] = base;
-    p->chunk_len[j] = kPage;
-    if (n == 0) continue;   // (a shared decode: nothing of the sequence's own)
     int64_t nc = (n + T - 1) / T;
     if (nc < nc_wave) {
       int64_t by_len = n / kMinSplitTokens;
@@ -884,6 +889,7 @@ static int cut_splits(const mixattn_ctx* c, int layer, int nb, int64_t total, De
     int64_t len = (n + nc - 1) / nc;
     len = (len + kPage - 1) / kPage * kPage;
     nc = (n + len - 1) / len;
+    p->chunk_base[j] = base;
     p->chunk_len[j] = (int32_t)len;
     base += (int)nc;
     *any_split = *any_split || nc > 1;
@@ -1037,28 +1043,56 @@ static bool lay_out_shared(const ShareTree& t, bool leaves, int max_ctas, int64_
   return false;
 }
 
-// The keys that only one sequence has, as a launch of the ordinary split pass over the sequences in the
-// caller's order: each with its block table from its first own page on.  Completes the nodes behind p's items.
+// SMs that are left to the split pass of the sequences' own keys: the two kernels run side by side, and their
+// shares follow what each has to do, in microseconds of an SM as measured: the split pass 1.0 for 128 keys and 3
+// for an item (64 one-token items on four CTAs: 53 us), the tensor-core kernel 1.5 for a tile of few rows (its
+// bytes), 1.75 for one of many (its products) and 4 for an item.
+static int own_key_ctas(const ShareTree& t, const SharedDecodeParams& p, const DecodeParams& d, int sm_count) {
+  double own = 0, common = 0;
+  for (const SharePiece& s : t.pieces) {
+    const double tiles = (s.t1 - s.t0) / 128.0;
+    if (s.ns == 1) {
+      own += (tiles + 3.0) * d.head_chunks;
+    } else {
+      const int rows = s.ns * p.group, chunks = (rows + p.row_chunk - 1) / p.row_chunk;
+      common += (tiles * (rows > 64 ? 1.75 : 1.5) + 4.0) * chunks;
+    }
+  }
+  if (own == 0) return 0;
+  return std::min((int)(sm_count * own / (own + common)) + 1, sm_count - 1);
+}
+
+// The keys that only one sequence has, as a launch of the ordinary split pass: each sequence with its block
+// table from its first own page on, the longest ones first (the CTAs take the items in turns: 64
+// sequences of 16 to 2048 own tokens in the caller's order kept some CTAs busy for 70 us and others for 39).
+// Completes the nodes behind p's items.
 static void plan_own_keys(const mixattn_ctx* c, int layer, int n_leaves, SharedDecodeParams* p, ShapedDecodeParams* d) {
   ShareNode* leaf = p->node + p->n_nodes + 1;
+  int32_t by_length[kMaxCallSeqs];
   int64_t total = 0;
-  for (int i = 0; i < p->n_seqs; ++i) d->seq_id[i] = d->n_eff[i] = d->newest[i] = 0;
   for (int v = 0; v < n_leaves; ++v) {
-    const int i = p->order[leaf[v].s0];
-    d->seq_id[i] = leaf[v].slot * p->table_stride + leaf[v].t0 / kPage;   // (a table's entries are indexed in 32 bits)
-    d->n_eff[i] = leaf[v].t1 - leaf[v].t0;
-    d->newest[i] = p->newest[leaf[v].s0] - leaf[v].t0;
-    total += d->n_eff[i];
+    by_length[v] = v;
+    total += leaf[v].t1 - leaf[v].t0;
   }
-  d->n_seqs = p->n_seqs;
+  std::sort(by_length, by_length + n_leaves, [&](int a, int b) {
+    const int na = leaf[a].t1 - leaf[a].t0, nb = leaf[b].t1 - leaf[b].t0;
+    return na != nb ? na > nb : a < b;
+  });
+  d->n_seqs = n_leaves;
   d->total_items = 0;
   if (n_leaves == 0) return;
+  for (int i = 0; i < n_leaves; ++i) {
+    const ShareNode& nd = leaf[by_length[i]];
+    d->q_row[i] = p->order[nd.s0];
+    d->seq_id[i] = nd.slot * p->table_stride + nd.t0 / kPage;   // (a table's entries are indexed in 32 bits)
+    d->n_eff[i] = nd.t1 - nd.t0;
+    d->newest[i] = p->newest[nd.s0] - nd.t0;
+  }
   bool any = false;
-  cut_splits(c, layer, p->n_seqs, total, d, &any);
-  for (int v = 0; v < n_leaves; ++v) {
-    const int i = p->order[leaf[v].s0];
-    leaf[v].row0 = d->chunk_base[i];
-    leaf[v].max_segs = -(d->chunk_base[i + 1] - d->chunk_base[i]);
+  cut_splits(c, layer, n_leaves, total, d, &any);
+  for (int i = 0; i < n_leaves; ++i) {
+    leaf[by_length[i]].row0 = d->chunk_base[i];
+    leaf[by_length[i]].max_segs = -(d->chunk_base[i + 1] - d->chunk_base[i]);
   }
 }
 
@@ -1113,7 +1147,6 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
       d.part_ml = const_cast<float2*>(p.split_ml);
       d.status = p.status;
       d.l2_keep_bytes = d.l2_pool_bytes = 0;
-      d.partial = 1;
       d.wrap = 0;
       // (always the kernel of shaped scores, here without cap or bias where the layer has none: it clears
       // what earlier sequences left behind the last key)
@@ -1143,7 +1176,9 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
       for (int32_t least = MIXATTN_MIN_SHARED_TOKENS; !fits; least *= 2) {   // (deep trees of short pieces: only the longer ones)
         build_share_tree(c->cm, layer, nb, ids, least, &tree);
         if (!tree.shared) break;
-        fits = lay_out_shared(tree, tc, tc ? c->sm_count : 2 * c->sm_count, room, &p, &n_leaves);
+        const int own_ctas = tc ? own_key_ctas(tree, p, d, c->sm_count) : 0;
+        d.partial = own_ctas;
+        fits = lay_out_shared(tree, tc, tc ? c->sm_count - own_ctas : 2 * c->sm_count, room, &p, &n_leaves);
         if (least > (1 << 29)) break;
       }
       if (!fits) {
@@ -1171,7 +1206,7 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
           if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
         }
       }
-      e = launch_recorded(c, MIXATTN_K_MERGE, st, [&] { return launch_merge_shared(p, c->cfg.dtype, st); });
+      e = launch_recorded(c, MIXATTN_K_MERGE, st, [&] { return launch_merge_shared(p, c->cfg.dtype, c->sm_count, st); });
       if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
     }
   } catch (const std::bad_alloc&) {

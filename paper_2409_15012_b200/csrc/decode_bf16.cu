@@ -375,7 +375,7 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
       __syncwarp();
       asm volatile("barrier.cluster.wait.acquire.aligned;\n\tbarrier.cluster.arrive.release.aligned;" ::: "memory");
     }
-    if (p.partial) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (CL == 1 && p.partial) asm volatile("griddepcontrol.wait;" ::: "memory");
     return;
   }
 
@@ -405,11 +405,12 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
     const int rows = min(kMaxGroupRows, p.group - x.hc * kMaxGroupRows);
     const int h0 = x.g * p.group + x.hc * kMaxGroupRows;
 
+    const int q_row = p.partial ? p.q_row[x.i] : x.i;
     // Q^T fragments (B operand): thread holds head (lane >> 2), channels 16 ks + fcol (+8)
     uint32_t qb[kKSteps][2];
     if constexpr (!KV8) {
       const __nv_bfloat16* qp = reinterpret_cast<const __nv_bfloat16*>(p.q) +
-                                ((int64_t)x.i * p.n_q_heads + h0 + frow) * D + fcol;
+                                ((int64_t)q_row * p.n_q_heads + h0 + frow) * D + fcol;
 #pragma unroll
       for (int ks = 0; ks < kKSteps; ++ks) {
         qb[ks][0] = frow < rows ? *reinterpret_cast<const uint32_t*>(qp + ks * 16) : 0u;
@@ -420,7 +421,7 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
       // pair 2t, 2t+1 and two to 2t+8, 2t+9), so this thread's Q values of a 16-channel step
       // are the four channels 4t .. 4t+3, as fp16
       const __nv_bfloat16* qp = reinterpret_cast<const __nv_bfloat16*>(p.q) +
-                                ((int64_t)x.i * p.n_q_heads + h0 + frow) * D + 2 * fcol;
+                                ((int64_t)q_row * p.n_q_heads + h0 + frow) * D + 2 * fcol;
 #pragma unroll
       for (int ks = 0; ks < kKSteps; ++ks) {
         uint2 w = make_uint2(0u, 0u);
@@ -693,7 +694,7 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
           const float L = xml[r * 2 + 1] * s0 + xml[(rows_cap + r) * 2 + 1] * s1;
           const float acc = xo[(size_t)r * D + d] * s0 + xo[((size_t)rows_cap + r) * D + d] * s1;
           const int h = h0 + r;
-          if (x.n_splits == 1 && !p.partial) {
+          if (x.n_splits == 1) {
             reinterpret_cast<__nv_bfloat16*>(p.out)[((int64_t)x.i * p.n_q_heads + h) * D + d] =
                 __float2bfloat16_rn(acc / L);
           } else {
@@ -706,7 +707,7 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
     }
     consumer_bar<NCW>();
   }
-  if (p.partial) asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (CL == 1 && p.partial) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 size_t smem_bytes(int D, int group, int n_stages, int ncw, int cl, int kv8) {
@@ -770,9 +771,9 @@ cudaError_t launch_decode_split_bf16(const DecodeParams& p, const ShapedDecodePa
   // launch is bound by HBM instead of by the SM that drew two items.
   int64_t max_keys = 0;
   for (int i = 0; i < p.n_seqs; ++i) max_keys = p.chunk_len[i] > max_keys ? p.chunk_len[i] : max_keys;
-  const bool small = p.total_items > sm_count && p.total_items <= 2 * sm_count && max_keys <= 2048;
+  const bool small = !p.partial && p.total_items > sm_count && p.total_items <= 2 * sm_count && max_keys <= 2048;
   // At most one item per two SMs, and items of several stages: a cluster of two CTAs per item.
-  const bool paired = 2 * p.total_items <= sm_count && max_keys >= 4 * kTileKeys;
+  const bool paired = !p.partial && 2 * p.total_items <= sm_count && max_keys >= 4 * kTileKeys;
   const int cl = paired ? 2 : 1;
   const int kv8 = p.geom.fp8;
   const int ncw = small ? 4 : 8;
@@ -789,7 +790,7 @@ cudaError_t launch_decode_split_bf16(const DecodeParams& p, const ShapedDecodePa
   n_stages -= n_stages % unit;
   if (n_stages < unit) return cudaErrorInvalidConfiguration;
   const size_t smem = smem_bytes(D, p.group, n_stages, ncw, cl, kv8);
-  const int slots = small ? 2 * sm_count : sm_count;
+  const int slots = p.partial ? p.partial : small ? 2 * sm_count : sm_count;
   const int grid = paired ? 2 * p.total_items : (p.total_items < slots ? p.total_items : slots);
   // launched with programmatic stream serialization: the kernel's set-up may overlap the
   // tail of the previous kernel in the stream; it waits (griddepcontrol.wait) before its

@@ -150,11 +150,12 @@ __global__ void __launch_bounds__(kThreads) decode_shared_kernel(const __grid_co
 }
 
 // ---------------------------------------------------------------- merge
-// kMergeLanes threads per four channels of an output row take turns over the partial results of the row's path,
+// kLanes threads per four channels of an output row take turns over the partial results of the row's path,
 // four loads in flight each, and join in shared memory: a row behind a long prefix has some twenty segments,
-// and one after the other their latencies were the whole kernel (20 us of 8 sequences' 79).  The partials
+// and one after the other their latencies were the whole kernel (20 us of 8 sequences' 79).  As many lanes
+// as keep the grid within one wave.  The partials
 // of a segment lie [D / 4][rows][4], so that the tensor-core kernel, which has a row per thread, writes whole lines.
-constexpr int kMergeThreads = 256, kMergeLanes = 4;
+constexpr int kMergeThreads = 256;
 
 struct Partial {
   float M, L;
@@ -171,19 +172,20 @@ __device__ __forceinline__ void join(Partial& a, float m, float l, float4 o) {
   a.o.w = a.o.w * s0 + o.w * s1;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kMergeThreads) merge_shared_kernel(const __grid_constant__ SharedDecodeParams p) {
+template <typename T, int kLanes>
+__global__ void __launch_bounds__(kMergeThreads, 4) merge_shared_kernel(const __grid_constant__ SharedDecodeParams p) {
   __shared__ Partial sm[kMergeThreads];
   const int D = p.geom.head_dim, per_row = D / 4;
-  const int per_block = kMergeThreads / kMergeLanes;                  // (row, channels) pairs per block
+  const int per_block = kMergeThreads / kLanes;                  // (row, channels) pairs per block
   const int kl = threadIdx.x / per_block, local = threadIdx.x % per_block;
-  const int e = blockIdx.x * per_block + local, h = e / per_row, c4 = e - h * per_row;
+  // the heads of a group next to each other (they are neighbouring rows of a segment), then the channels
+  const int e = blockIdx.x * per_block + local, g = e / (p.group * per_row), c4 = (e - g * p.group * per_row) / p.group;
+  const int hh = e % p.group, h = g * p.group + hh;
   const int i = blockIdx.y;
   const bool there = h < p.n_q_heads;
   asm volatile("griddepcontrol.wait;" ::: "memory");   // (a no-op after an ordinary launch)
   Partial acc{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
   if (there) {
-    const int g = h / p.group, hh = h - g * p.group;
     int turn = kl;   // this thread's next segment, counted from the node's first
     for (int v = p.leaf[i]; v >= 0; v = p.node[v].parent) {
       const ShareNode& nd = p.node[v];
@@ -213,12 +215,12 @@ __global__ void __launch_bounds__(kMergeThreads) merge_shared_kernel(const __gri
         o_step = (int64_t)rows * D;
       }
       int k = turn;
-      for (; k < n; k += 4 * kMergeLanes) {
+      for (; k < n; k += 4 * kLanes) {
         float2 ml[4];
         float4 o[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int kj = k + j * kMergeLanes;
+          const int kj = k + j * kLanes;
           ml[j] = make_float2(-INFINITY, 0.f);
           o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
           if (kj < n) {
@@ -229,14 +231,14 @@ __global__ void __launch_bounds__(kMergeThreads) merge_shared_kernel(const __gri
 #pragma unroll
         for (int j = 0; j < 4; ++j) join(acc, ml[j].x, ml[j].y, o[j]);
       }
-      turn = ((turn - n) % kMergeLanes + kMergeLanes) % kMergeLanes;   // the lanes go on where the others stopped
+      turn = ((turn - n) % kLanes + kLanes) % kLanes;   // the lanes go on where the others stopped
     }
     if (kl > 0) sm[threadIdx.x] = acc;
   }
   __syncthreads();
   if (kl > 0 || !there) return;
 #pragma unroll
-  for (int j = 1; j < kMergeLanes; ++j) {
+  for (int j = 1; j < kLanes; ++j) {
     const Partial& x = sm[j * per_block + local];
     join(acc, x.M, x.L, x.o);
   }
@@ -266,10 +268,13 @@ cudaError_t launch_decode_shared(const SharedDecodeParams& p, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-cudaError_t launch_merge_shared(const SharedDecodeParams& p, int dtype, cudaStream_t st) {
-  const int n = p.n_q_heads * (p.geom.head_dim / 4);
+template <typename T>
+static cudaError_t launch_merge(const SharedDecodeParams& p, int sm_count, cudaStream_t st) {
+  const int64_t n = (int64_t)p.n_q_heads * (p.geom.head_dim / 4), room = (int64_t)sm_count * 4 * kMergeThreads;
+  int lanes = 8;
+  while (lanes > 1 && n * p.n_seqs * lanes > room) lanes /= 2;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((n * kMergeLanes + kMergeThreads - 1) / kMergeThreads, p.n_seqs);
+  cfg.gridDim = dim3((unsigned)((n * lanes + kMergeThreads - 1) / kMergeThreads), p.n_seqs);
   cfg.blockDim = dim3(kMergeThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -277,8 +282,14 @@ cudaError_t launch_merge_shared(const SharedDecodeParams& p, int dtype, cudaStre
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return dtype == MIXATTN_BF16 ? cudaLaunchKernelEx(&cfg, merge_shared_kernel<__nv_bfloat16>, p)
-                               : cudaLaunchKernelEx(&cfg, merge_shared_kernel<float>, p);
+  if (lanes == 8) return cudaLaunchKernelEx(&cfg, merge_shared_kernel<T, 8>, p);
+  if (lanes == 4) return cudaLaunchKernelEx(&cfg, merge_shared_kernel<T, 4>, p);
+  if (lanes == 2) return cudaLaunchKernelEx(&cfg, merge_shared_kernel<T, 2>, p);
+  return cudaLaunchKernelEx(&cfg, merge_shared_kernel<T, 1>, p);
+}
+
+cudaError_t launch_merge_shared(const SharedDecodeParams& p, int dtype, int sm_count, cudaStream_t st) {
+  return dtype == MIXATTN_BF16 ? launch_merge<__nv_bfloat16>(p, sm_count, st) : launch_merge<float>(p, sm_count, st);
 }
 
 }  // namespace mixattn

@@ -361,28 +361,29 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
           tmem_wait_ld_pin(s0, s1);
           if constexpr (kShape != 0) {   // raw products -> shaped base-2 scores
             const float first = -slope * (float)(newest - t - 64 * g);   // bias of column 0
-            float top = 0.f;
+            float top = 0.f;   // largest square of a product
 #pragma unroll
             for (int e = 0; e < 64; e += 2) {
-              f32x2 x = mul2(pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1])), pack2(p.shape.pre, p.shape.pre));
-              if constexpr (kShape & 1) {
-                const f32x2 u = mul2(x, x);
-                f32x2 q = fma2(pack2(tanh_coefficient(5), tanh_coefficient(5)), u, pack2(tanh_coefficient(4), tanh_coefficient(4)));
-                q = fma2(q, u, pack2(tanh_coefficient(3), tanh_coefficient(3)));
-                q = fma2(q, u, pack2(tanh_coefficient(2), tanh_coefficient(2)));
-                q = fma2(q, u, pack2(tanh_coefficient(1), tanh_coefficient(1)));
-                q = fma2(q, u, pack2(tanh_coefficient(0), tanh_coefficient(0)));
+              const f32x2 raw = pack2(__uint_as_float(sv[e]), __uint_as_float(sv[e + 1]));
+              const f32x2 off = pack2(fmaf(slope, (float)e, first), fmaf(slope, (float)(e + 1), first));
+              f32x2 x;
+              if constexpr (kShape & 1) {   // a cubic in the product's square, good to half the cap (score_shape.cuh)
+                const f32x2 u = mul2(raw, raw);
+                f32x2 q = fma2(pack2(p.shape.near[3], p.shape.near[3]), u, pack2(p.shape.near[2], p.shape.near[2]));
+                q = fma2(q, u, pack2(p.shape.near[1], p.shape.near[1]));
+                q = fma2(q, u, pack2(p.shape.near[0], p.shape.near[0]));
                 const float2 uu = unpack2(u);
                 top = fmax3(top, uu.x, uu.y);
-                x = mul2(mul2(q, x), pack2(p.shape.post, p.shape.post));
+                x = (kShape & 2) ? fma2(q, raw, off) : mul2(q, raw);
+              } else {
+                x = fma2(raw, pack2(p.shape.pre, p.shape.pre), off);
               }
-              if constexpr (kShape & 2) x = add2(x, pack2(fmaf(slope, (float)e, first), fmaf(slope, (float)(e + 1), first)));
               const float2 y = unpack2(x);
               sv[e] = __float_as_uint(y.x);
               sv[e + 1] = __float_as_uint(y.y);
             }
             if constexpr (kShape & 1) {
-              if (__any_sync(0xffffffffu, !(top <= 1.f))) {   // beyond the polynomial: again from the raw products
+              if (__any_sync(0xffffffffu, !(top <= p.shape.near_sq))) {   // beyond it: again from the raw products
                 tmem_ld32(s_addr, s0);
                 tmem_ld32(s_addr + 32, s1);
                 tmem_wait_ld_pin(s0, s1);

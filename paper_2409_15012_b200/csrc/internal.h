@@ -149,8 +149,10 @@ struct DecodeParams {
   int32_t* status;        // device error word (0 = fine)
   int32_t n_seqs;
   int32_t total_items;    // chunks * Hkv * head_chunks
-  int32_t partial = 0;    // 1: every item leaves a partial result, and the launch does not wait for the one ahead of it
-                          // before it starts (the tensor-core kernel of a shared decode), but before it ends
+  int32_t partial = 0;    // > 0: every item leaves a partial result, the launch has at most so many CTAs, and it does
+                          // not wait for the one ahead of it (the tensor-core kernel of a shared decode, which
+                          // leaves SMs free for it) before it starts, but before it ends
+  int32_t q_row[kMaxCallSeqs];           // partial launches: row of q of each sequence
   int32_t seq_id[kMaxCallSeqs];          // storage slots of the sequences
   int32_t n_eff[kMaxCallSeqs];           // keys attended: min(len, window) or len
   int32_t chunk_len[kMaxCallSeqs];       // keys per split of this sequence (multiple of 16)
@@ -433,7 +435,7 @@ bool shared_tc_supported(const KvGeom& ge, const void* q);      // on the tensor
 void shared_tc_tiles(SharedDecodeParams* p);
 cudaError_t prepare_decode_shared_tc();
 cudaError_t launch_decode_shared_tc(const SharedDecodeParams& p, cudaStream_t st);
-cudaError_t launch_merge_shared(const SharedDecodeParams& p, int dtype, cudaStream_t st);
+cudaError_t launch_merge_shared(const SharedDecodeParams& p, int dtype, int sm_count, cudaStream_t st);
 cudaError_t launch_rope_qkv(const RopeParams& p, int max_n_new, cudaStream_t st);
 cudaError_t prepare_adjust_logits();
 cudaError_t launch_adjust_logits(const AdjustParams& p, int in_dtype, int out_dtype, int sm_count, cudaStream_t st);
