@@ -1,4 +1,4 @@
-// Decode over a tree of shared prefixes on the 5th-generation tensor cores (tcgen05 + TMEM), bf16 caches.
+// Decode over a tree of shared prefixes on the 5th-generation tensor cores (tcgen05 + TMEM), bf16 and quantised caches.
 //
 // The pieces of the tree, their items and segments are described with SharedDecodeParams
 // (internal.h), the mathematics in decode_shared.cu.  Here the rows of an item, the query heads that
@@ -25,6 +25,14 @@
 // the end.  K and V have rings of their own because a tile's K is done with when its scores are, a softmax and a
 // product earlier than its V: with both in one ring of three stages, the loads of the tile after next came
 // too late (2400 cycles a tile where neither HBM nor products limit, with any number of products).
+//
+// Quantised caches (kFp8; format in internal.h).  A page block is one untiled copy of 4128 bytes into a ring of
+// 64-key stages, and the warps of Q and of the results turn its codes into operands between those duties: K codes to
+// fp16 (one conversion per pair, exact; Q is taken to fp16 as in the other decode kernel), rows as above;
+// V codes to bf16 (bits moved into place and one product with 2^120, exact), which are stored transposed and stay
+// so: the second product takes V with its keys contiguous.  A K row's exponent multiplies its scores, a V row's
+// its weight before that is split in two bf16 terms, whose range holds any exponent.  K has one operand
+// buffer (its scores come early), V two, so that a stage is free again as soon as it is converted.
 //
 // TMEM: S0, S1, O_0, O_1 = 4 x 128 columns.  All mbarrier waits are bounded; on time-out a status
 // word is raised and every role leaves its loop.
@@ -58,19 +66,27 @@ enum {
   B_KF = 18                  // K stages full, then free, V stages full, then free
 };
 
-template <int D>
+template <int D, bool kFp8>
 struct Layout {
   static constexpr int kHalves = D / 64;
-  static constexpr int kStageBytes = kHalves * kHalf;
-  static constexpr int kStages = D == 128 ? 3 : 6;
-  static constexpr int kKE = B_KF + kStages, kVF = B_KF + 2 * kStages, kVE = B_KF + 3 * kStages, kBars = B_KF + 4 * kStages;
+  static constexpr int kTileBytes = kHalves * kHalf;              // K or V of a tile as operand
+  // native: rings of operand tiles for K and V.  Quantised: a ring of raw stages (64 keys, K and V), one
+  // operand buffer for K and two for V; a tile's exponents as factors, four tiles deep (K, V)
+  static constexpr int kStages = kFp8 ? 5 : D == 128 ? 3 : 6;
+  static constexpr int kKBufs = kFp8 ? 1 : kStages, kVBufs = kFp8 ? 2 : kStages;
+  static constexpr int kRawBlk = 2 * kPage * D + 2 * kPage, kRawStage = 4 * kRawBlk;
+  static constexpr int kKE = B_KF + kKBufs, kVF = kKE + kKBufs, kVE = kVF + kVBufs, kRF = kVE + kVBufs;
+  static constexpr int kRE = kRF + (kFp8 ? kStages : 0), kXF = kRE + (kFp8 ? kStages : 0), kBars = kXF + (kFp8 ? 4 : 0);
   static constexpr int kSmQ = 0;
   static constexpr int kSmK = kHalves * kQHalf;
-  static constexpr int kSmV = kSmK + kStages * kStageBytes;
-  static constexpr int kSmBar = kSmV + kStages * kStageBytes;
+  static constexpr int kSmV = kSmK + kKBufs * kTileBytes;
+  static constexpr int kSmRaw = kSmV + kVBufs * kTileBytes;
+  static constexpr int kSmX = kSmRaw + (kFp8 ? kStages * kRawStage : 0);
+  static constexpr int kSmBar = kSmX + (kFp8 ? 4 * 2 * kTile * 4 : 0);
   static constexpr int kSmXchg = kSmBar + (kBars * 8 + 16 + 255) / 256 * 256;
   static constexpr int kBytes = kSmXchg + 2 * kRows * 8 + 768;   // + slack to align a 256-byte aligned base to 1024
   static_assert(kBytes <= 227 * 1024, "shared memory");
+  static_assert(!kFp8 || D == 128, "quantised caches have 128 channels");
 };
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
@@ -79,11 +95,37 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
 }
 
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+// four E4M3 codes -> fp16 pairs (bytes 0, 1 and bytes 2, 3), exact
+__device__ __forceinline__ void codes_to_f16(uint32_t x, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\t"
+      "mov.b32 {l, h}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, l;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi) : "r"(x));
+}
+// The same as bf16: sign, and exponent and mantissa moved to the bf16 field's low end, are the value times
+// 2^-120 (subnormal codes become subnormal numbers), which the product puts right.
+__device__ __forceinline__ void codes_to_bf16(uint32_t x, uint32_t& lo, uint32_t& hi) {
+  const uint32_t a = __byte_perm(x, 0u, 0x1404), b = __byte_perm(x, 0u, 0x3424);   // codes in the high bytes of the halves
+  uint32_t p = (a & 0x80008000u) | ((a >> 4) & 0x07f007f0u), q = (b & 0x80008000u) | ((b >> 4) & 0x07f007f0u);
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(lo) : "r"(p), "r"(0x7b807b80u));           // 2^120
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(hi) : "r"(q), "r"(0x7b807b80u));
+}
+__device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t x) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(__uint_as_float(x & 0xffff0000u)), "f"(__uint_as_float(x << 16)));
+  return d;
+}
+
 // kShape: scores capped (1), biased (2), both (3)
-template <int D, int kShape>
+template <int D, int kShape, bool kFp8>
 __global__ void __launch_bounds__(kThreads, 1)
 decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_constant__ SharedDecodeParams p) {
-  using L = Layout<D>;
+  using L = Layout<D, kFp8>;
   constexpr int kStages = L::kStages;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -97,11 +139,20 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
   if (threadIdx.x == 0) {
     mbar_init(BAR(B_QF), 4);
     mbar_init(BAR(B_QE), 1);
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(BAR(B_KF + s), 1);
+    for (int s = 0; s < L::kKBufs; ++s) {
+      mbar_init(BAR(B_KF + s), kFp8 ? 4 : 1);   // by the four converting warps
       mbar_init(BAR(L::kKE + s), 1);
-      mbar_init(BAR(L::kVF + s), 1);
+    }
+    for (int s = 0; s < L::kVBufs; ++s) {
+      mbar_init(BAR(L::kVF + s), kFp8 ? 4 : 1);
       mbar_init(BAR(L::kVE + s), 1);
+    }
+    if constexpr (kFp8) {
+      for (int s = 0; s < kStages; ++s) {
+        mbar_init(BAR(L::kRF + s), 1);
+        mbar_init(BAR(L::kRE + s), 4);
+      }
+      for (int s = 0; s < 4; ++s) mbar_init(BAR(L::kXF + s), 4);
     }
     for (int s = 0; s < 4; ++s) {
       mbar_init(BAR(B_SF + s), 1);
@@ -133,7 +184,40 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
   ShareSegment s;
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    if (warp == 0 || warp == 3) {
+    if (kFp8 && warp == 0) {
+      // ------------------------------ page producer, quantised ------------------------------
+      bool ok = true;
+      int H = 0;   // stages of four pages so far
+      while (ok && share_next(p, blockIdx.x, walk, s)) {
+        const int32_t* tbl = p.table + (int64_t)p.node[s.node].slot * p.table_stride;
+        const int page_lo = s.t0 / kPage, page_hi = (s.t1 + kPage - 1) / kPage;
+        int ids_next = page_lo + lane < page_hi ? tbl[page_lo + lane] : 0, ids = 0;
+        for (int pg = page_lo; pg < page_hi; pg += 4, ++H) {
+          const int rel = (pg - page_lo) & 31;
+          if (rel == 0) {
+            ids = ids_next;
+            if (pg + 32 + lane < page_hi) ids_next = tbl[pg + 32 + lane];
+          }
+          const int st = H % kStages, turn = H / kStages, n_pg = min(4, page_hi - pg);
+          const int id = __shfl_sync(0xffffffffu, ids, rel + (lane & 3));
+          if (turn > 0) {
+            int w = 1;
+            if (lane == 0) w = mbar_wait(BAR(L::kRE + st), (turn - 1) & 1, abort_flag);
+            if (!__shfl_sync(0xffffffffu, w, 0)) { ok = false; break; }
+          }
+          if (lane == 0) mbar_expect_tx(BAR(L::kRF + st), n_pg * L::kRawBlk);
+          __syncwarp();
+          if (lane < n_pg)
+            bulk_load(base + L::kSmRaw + st * L::kRawStage + lane * L::kRawBlk,
+                      p.pool + (int64_t)id * p.geom.page_bytes + (int64_t)s.g * L::kRawBlk, L::kRawBlk, BAR(L::kRF + st));
+        }
+      }
+      if (!ok && lane == 0) {
+        atomicExch(p.status, kDevWaitTimeout);
+        for (int back = 1; back <= kStages && H - back >= 0; ++back)
+          mbar_wait(BAR(L::kRF + (H - back) % kStages), ((H - back) / kStages) & 1, abort_flag + 1);
+      }
+    } else if (!kFp8 && (warp == 0 || warp == 3)) {
       // ------------------------------ page producers ------------------------------
       const int v = warp == 3;   // K or V
       const int full = v ? L::kVF : B_KF, free = v ? L::kVE : L::kKE;
@@ -163,7 +247,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
           if (lane == 0) mbar_expect_tx(BAR(full + st), n_pg * L::kHalves * kPiece);
           __syncwarp();
           if (h < L::kHalves && j < n_pg)
-            tma_load_4d(ring + st * L::kStageBytes + h * kHalf + j * kPiece, &pages, 64 * h, 0, v,
+            tma_load_4d(ring + st * L::kTileBytes + h * kHalf + j * kPiece, &pages, 64 * h, 0, v,
                         id * p.geom.n_kv_heads + s.g, BAR(full + st));
         }
       }
@@ -174,21 +258,21 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
       }
     } else if (warp == 1) {
       // ------------------------------ score products ------------------------------
-      constexpr uint32_t kIdesc = idesc_bf16(0, 64);
+      constexpr uint32_t kIdesc = kFp8 ? idesc_f16(0, 64) : idesc_bf16(0, 64);
       const uint64_t qdesc = smem_desc(base + L::kSmQ, 16, 1024);
       bool ok = true;
       int G = 0;
       for (int it = 0; ok && share_next(p, blockIdx.x, walk, s); ++it) {
         ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_QF), it & 1, abort_flag));
         for (int t = s.t0; t < s.t1 && ok; t += kTile, ++G) {
-          const int sb = G & 1, st = G % kStages;
-          ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_KF + st), (G / kStages) & 1, abort_flag));
+          const int sb = G & 1, st = G % L::kKBufs;
+          ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_KF + st), (G / L::kKBufs) & 1, abort_flag));
 #pragma unroll
           for (int g = 0; g < 2; ++g) {   // a stream's half waits for its own P V alone
             if (ok && G >= 2) ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_SR + 2 * g + sb), ((G >> 1) - 1) & 1, abort_flag));
             if (!ok) break;
             tc_fence_after();
-            const uint64_t kdesc = smem_desc(base + L::kSmK + st * L::kStageBytes + g * 64 * 128, 16, 1024);
+            const uint64_t kdesc = smem_desc(base + L::kSmK + st * L::kTileBytes + g * 64 * 128, 16, 1024);
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks)
               umma_bf16_warp(tmem + kColS + sb * 128 + g * 64, qdesc + (uint64_t)((ks >> 2) * (kQHalf >> 4) + (ks & 3) * 2),
@@ -201,27 +285,29 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
         if (ok) umma_commit_warp(BAR(B_QE));
       }
       if (!ok && lane == 0) atomicExch(p.status, kDevWaitTimeout);
-    } else {
+    } else if (warp == 2) {
       // ------------------------------ P V ------------------------------
-      constexpr uint32_t kIdesc = idesc_bf16(1, D);
+      constexpr uint32_t kIdesc = idesc_bf16(kFp8 ? 0 : 1, D);   // V with its channels contiguous, or its keys
+      constexpr int kGStep = kFp8 ? 128 * 128 : 64 * 128;         // a stream's keys behind the other's
+      constexpr int kStep = kFp8 ? 32 : kPiece;                   // 16 keys
       bool ok = true;
       int G = 0;
       for (int it = 0; ok && share_next(p, blockIdx.x, walk, s); ++it) {
         // the segment's first P V overwrites the accumulators
         if (it >= 1) ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_OR), (it - 1) & 1, abort_flag));
         for (int t = s.t0; t < s.t1 && ok; t += kTile, ++G) {
-          const int sb = G & 1, st = G % kStages;
-          ok = __all_sync(0xffffffffu, mbar_wait(BAR(L::kVF + st), (G / kStages) & 1, abort_flag));
+          const int sb = G & 1, st = G % L::kVBufs;
+          ok = __all_sync(0xffffffffu, mbar_wait(BAR(L::kVF + st), (G / L::kVBufs) & 1, abort_flag));
           if (!ok) break;
           // A stream's steps of 16 keys are pages; the segment's last tile may hold fewer (one at least is taken: the
           // accumulator is read), and rows that are no keys (behind the last one, or of a page that was not
           // loaded), whose weight of zero an infinity or a NaN would survive, are cleared meanwhile.
           const int left = s.t1 - t;
-          if (left < kTile) {
+          if (!kFp8 && left < kTile) {
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
               const int steps = min(max((left - 64 * g + 15) >> 4, 1), 4), first = min(max(left - 64 * g, 0), 16 * steps);
-              unsigned char* v = gbase + L::kSmV + st * L::kStageBytes + g * 64 * 128;
+              unsigned char* v = gbase + L::kSmV + st * L::kTileBytes + g * 64 * 128;
               for (int x = lane; x < (16 * steps - first) * (D / 8); x += 32) {   // 16-byte chunks
                 const int row = first + x / (D / 8), c = x % (D / 8);
                 *reinterpret_cast<uint4*>(v + (c >> 3) * kHalf + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
@@ -236,19 +322,19 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
             ok = ok && __all_sync(0xffffffffu, mbar_wait(BAR(B_PF + 2 * g + sb), (G >> 1) & 1, abort_flag));
             if (!ok) break;
             tc_fence_after();
-            const uint64_t vdesc = smem_desc(base + L::kSmV + st * L::kStageBytes + g * 64 * 128, kHalf, 1024);
+            const uint64_t vdesc = smem_desc(base + L::kSmV + st * L::kTileBytes + g * kGStep, kFp8 ? 16 : kHalf, 1024);
             const uint32_t o = tmem + kColO + g * 128, pcol = tmem + kColS + sb * 128 + g * 64;
             if (left - 64 * g >= 64) {
               umma_bf16_ts_warp(o, pcol, vdesc, kIdesc, t > s.t0);
 #pragma unroll
               for (int x = 1; x < 8; ++x)   // four steps of the values, four of the residuals
-                umma_bf16_ts_warp(o, pcol + 8 * x, vdesc + (uint64_t)((x & 3) * (kPiece >> 4)), kIdesc, 1u);
+                umma_bf16_ts_warp(o, pcol + 8 * x, vdesc + (uint64_t)((x & 3) * (kStep >> 4)), kIdesc, 1u);
             } else {
               const int steps = max((left - 64 * g + 15) >> 4, 1);
 #pragma unroll 1
               for (int x = 0; x < 8; ++x)
                 if ((x & 3) < steps)
-                  umma_bf16_ts_warp(o, pcol + 8 * x, vdesc + (uint64_t)((x & 3) * (kPiece >> 4)), kIdesc, t > s.t0 || x > 0);
+                  umma_bf16_ts_warp(o, pcol + 8 * x, vdesc + (uint64_t)((x & 3) * (kStep >> 4)), kIdesc, t > s.t0 || x > 0);
             }
             if (last) umma_commit_warp(BAR(B_OF + g));
             umma_commit_warp(BAR(B_SR + 2 * g + sb));
@@ -275,6 +361,11 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
 #pragma unroll
         for (int c = 0; c < D / 8; ++c) x[c] = src[c];
       }
+      if constexpr (kFp8) {   // the score products run on fp16
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c)
+          x[c] = make_uint4(bf16x2_to_f16x2(x[c].x), bf16x2_to_f16x2(x[c].y), bf16x2_to_f16x2(x[c].z), bf16x2_to_f16x2(x[c].w));
+      }
       if (it >= 1 && !__all_sync(0xffffffffu, mbar_wait(BAR(B_QE), (it - 1) & 1, abort_flag))) return false;
       unsigned char* to = gbase + L::kSmQ + r * 128;
 #pragma unroll
@@ -284,10 +375,94 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
       if (lane == 0) mbar_arrive(BAR(B_QF));
       return true;
     };
+    // Quantised: a tile's codes into operands; every thread of the four warps takes 8 chunks of 16 codes of K and of V.
+    auto convert = [&](const ShareSegment& q, int t, int G, int H) {
+      const int n = threadIdx.x - 12 * 32, left = q.t1 - t, stages = left > 64 ? 2 : 1;
+      const unsigned char* raw[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        raw[x] = gbase + L::kSmRaw + (H + x) % kStages * L::kRawStage;
+        if (x < stages && !__all_sync(0xffffffffu, mbar_wait(BAR(L::kRF + (H + x) % kStages), ((H + x) / kStages) & 1, abort_flag))) return false;
+      }
+      if (G >= 1 && !__all_sync(0xffffffffu, mbar_wait(BAR(L::kKE), (G - 1) & 1, abort_flag))) return false;
+      // K: chunk c of key's row is 16 channels
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const int key = x * 16 + (n >> 3), c = n & 7, tok = key & 15;
+        if (key >= left) break;   // (what the operand holds there are other keys' rows, masked later)
+        const uint4 w = *reinterpret_cast<const uint4*>(raw[x >> 2] + (x & 3) * L::kRawBlk + tok * D + ((c ^ fp8_k_swizzle(tok)) << 4));
+        uint4 lo, hi;
+        codes_to_f16(w.x, lo.x, lo.y);
+        codes_to_f16(w.y, lo.z, lo.w);
+        codes_to_f16(w.z, hi.x, hi.y);
+        codes_to_f16(w.w, hi.z, hi.w);
+        unsigned char* to = gbase + L::kSmK + (c >> 2) * kHalf + key * 128;
+        const int at = (c & 3) * 2;
+        *reinterpret_cast<uint4*>(to + ((at ^ (key & 7)) << 4)) = lo;
+        *reinterpret_cast<uint4*>(to + (((at + 1) ^ (key & 7)) << 4)) = hi;
+      }
+      {   // exponents as factors; keys that are not there have a weight of zero times a factor of zero
+        float* f = reinterpret_cast<float*>(gbase + L::kSmX) + (G & 3) * 2 * kTile;
+        const float fold = kShape == 0 ? p.scale_log2e : kShape == 2 ? p.shape.pre : 1.f;
+        const unsigned char* xs = raw[n >> 6] + ((n >> 4) & 3) * L::kRawBlk + 2 * kPage * D + (n & 15);
+        float fk = 0.f, fv = 0.f;
+        if (n < left) {
+          fk = __int_as_float((int)xs[0] << 23) * fold;   // 2^(byte - 127); byte 0 is a vector of zeros
+          fv = __int_as_float((int)xs[kPage] << 23);
+        }
+        f[n] = fk;
+        f[kTile + n] = fv;
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(BAR(B_KF));
+        mbar_arrive(BAR(L::kXF + (G & 3)));
+      }
+      if (G >= 2 && !__all_sync(0xffffffffu, mbar_wait(BAR(L::kVE + (G & 1)), ((G >> 1) - 1) & 1, abort_flag))) return false;
+      // V: a channel's 16 keys of a page; rows are channels, 64 keys of a stream each
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+        const int there = left - 16 * x;   // keys of this page
+        if (there > 0) w = *reinterpret_cast<const uint4*>(raw[x >> 2] + (x & 3) * L::kRawBlk + kPage * D + n * kPage);
+        if (there < 16) {                  // what lies behind the last key may be any code, a NaN too
+          auto keep = [&](uint32_t v, int first) {
+            const int m = there - first;
+            return m >= 4 ? v : m <= 0 ? 0u : v & ((1u << (8 * m)) - 1u);
+          };
+          w = make_uint4(keep(w.x, 0), keep(w.y, 4), keep(w.z, 8), keep(w.w, 12));
+        }
+        uint4 lo, hi;
+        codes_to_bf16(w.x, lo.x, lo.y);
+        codes_to_bf16(w.y, lo.z, lo.w);
+        codes_to_bf16(w.z, hi.x, hi.y);
+        codes_to_bf16(w.w, hi.z, hi.w);
+        unsigned char* to = gbase + L::kSmV + (G & 1) * L::kTileBytes + (x >> 2) * (128 * 128) + n * 128;
+        const int at = (x & 3) * 2;
+        *reinterpret_cast<uint4*>(to + ((at ^ (n & 7)) << 4)) = lo;
+        *reinterpret_cast<uint4*>(to + (((at + 1) ^ (n & 7)) << 4)) = hi;
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(BAR(L::kVF + (G & 1)));
+        for (int x = 0; x < stages; ++x) mbar_arrive(BAR(L::kRE + (H + x) % kStages));
+      }
+      return true;
+    };
+    int G = 0, H = 0;   // quantised: tiles and raw stages so far
     bool more = share_next(p, blockIdx.x, walk, s), ok = true;
     if (more) ok = put_q(s, 0);
     for (int it = 0; ok && more; ++it) {
       const ShareSegment now = s;
+      if constexpr (kFp8) {
+        for (int t = now.t0; ok && t < now.t1; t += kTile, ++G) {
+          ok = convert(now, t, G, H);
+          H += now.t1 - t > 64 ? 2 : 1;
+        }
+        if (!ok) break;
+      }
       more = share_next(p, blockIdx.x, walk, s);
       if (more) ok = put_q(s, it + 1);
       if (!ok) break;
@@ -359,6 +534,21 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
           tmem_ld32(s_addr, s0);
           tmem_ld32(s_addr + 32, s1);
           tmem_wait_ld_pin(s0, s1);
+          const float* factor = reinterpret_cast<const float*>(gbase + L::kSmX) + (G & 3) * 2 * kTile + 64 * g;   // kFp8
+          auto scale_keys = [&]() {   // products of codes -> products (or base-2 scores, see above)
+#pragma unroll
+            for (int e = 0; e < 64; e += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(factor + e);
+              sv[e] = __float_as_uint(__uint_as_float(sv[e]) * f.x);
+              sv[e + 1] = __float_as_uint(__uint_as_float(sv[e + 1]) * f.y);
+              sv[e + 2] = __float_as_uint(__uint_as_float(sv[e + 2]) * f.z);
+              sv[e + 3] = __float_as_uint(__uint_as_float(sv[e + 3]) * f.w);
+            }
+          };
+          if constexpr (kFp8) {
+            if (!__all_sync(0xffffffffu, mbar_wait(BAR(L::kXF + (G & 3)), (G >> 2) & 1, abort_flag))) { ok = false; break; }
+            scale_keys();
+          }
           if constexpr (kShape != 0) {   // raw products -> shaped base-2 scores
             const float first = -slope * (float)(newest - t - 64 * g);   // bias of column 0
             float top = 0.f;   // largest square of a product
@@ -376,7 +566,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
                 top = fmax3(top, uu.x, uu.y);
                 x = (kShape & 2) ? fma2(q, raw, off) : mul2(q, raw);
               } else {
-                x = fma2(raw, pack2(p.shape.pre, p.shape.pre), off);
+                x = kFp8 ? add2(raw, off) : fma2(raw, pack2(p.shape.pre, p.shape.pre), off);
               }
               const float2 y = unpack2(x);
               sv[e] = __float_as_uint(y.x);
@@ -387,6 +577,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
                 tmem_ld32(s_addr, s0);
                 tmem_ld32(s_addr + 32, s1);
                 tmem_wait_ld_pin(s0, s1);
+                if constexpr (kFp8) scale_keys();
 #pragma unroll
                 for (int e = 0; e < 64; ++e) {
                   const float x = __uint_as_float(sv[e]) * p.shape.pre, o = (kShape & 2) ? fmaf(slope, (float)e, first) : 0.f;
@@ -396,7 +587,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
               }
             }
           }
-          const float scale = kShape ? 1.f : p.scale_log2e;
+          const float scale = kShape || kFp8 ? 1.f : p.scale_log2e;
           if (t + kTile > s.t1) {
             const int left = s.t1 - t - 64 * g;
 #pragma unroll
@@ -432,7 +623,12 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
                 const float b = ex2_approx(fmaf(__uint_as_float(sv[e + 1]), scale, neg));
                 if (i & 2) sum1 = add2(sum1, pack2(a, b));
                 else sum0 = add2(sum0, pack2(a, b));
-                split_bf16(a, b, pk[i >> 1], pl[i >> 1]);
+                if constexpr (kFp8) {
+                  const float2 f = *reinterpret_cast<const float2*>(factor + kTile + e);
+                  split_bf16(a * f.x, b * f.y, pk[i >> 1], pl[i >> 1]);
+                } else {
+                  split_bf16(a, b, pk[i >> 1], pl[i >> 1]);
+                }
               }
               tmem_st16(s_addr + 16 * half, pk);
               tmem_st16(s_addr + 32 + 16 * half, pl);
@@ -504,35 +700,43 @@ bool make_page_map(CUtensorMap* map, const void* pool, const KvGeom& ge, int64_t
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int kShape>
+template <int D, int kShape, bool kFp8>
 cudaError_t launch(const SharedDecodeParams& p, const CUtensorMap& map, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.n_ctas);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Layout<D>::kBytes;
+  cfg.dynamicSmemBytes = Layout<D, kFp8>::kBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, decode_shared_tc_kernel<D, kShape>, map, p);
+  return cudaLaunchKernelEx(&cfg, decode_shared_tc_kernel<D, kShape, kFp8>, map, p);
+}
+template <int D, bool kFp8>
+cudaError_t launch_shape(const SharedDecodeParams& p, const CUtensorMap& map, cudaStream_t st) {
+  const int shape = !p.shaped ? 0 : (p.shape.post > 0.f ? 1 : 0) | (p.shape.biased ? 2 : 0);
+  if (shape == 0) return launch<D, 0, kFp8>(p, map, st);
+  if (shape == 1) return launch<D, 1, kFp8>(p, map, st);
+  return shape == 2 ? launch<D, 2, kFp8>(p, map, st) : launch<D, 3, kFp8>(p, map, st);
 }
 
-template <int D>
+template <int D, bool kFp8>
 cudaError_t prepare() {
   constexpr auto kAttr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 0>, kAttr, Layout<D>::kBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 1>, kAttr, Layout<D>::kBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 2>, kAttr, Layout<D>::kBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 3>, kAttr, Layout<D>::kBytes);
+  constexpr int kBytes = Layout<D, kFp8>::kBytes;
+  cudaError_t e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 0, kFp8>, kAttr, kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 1, kFp8>, kAttr, kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 2, kFp8>, kAttr, kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(decode_shared_tc_kernel<D, 3, kFp8>, kAttr, kBytes);
   return e;
 }
 
 }  // namespace
 
 bool shared_tc_supported(const KvGeom& ge, const void* q) {
-  return !ge.fp8 && ge.elem_bytes == 2 && ((size_t)q & 15) == 0 && encode_fn() != nullptr;
+  return ge.elem_bytes == 2 && ((size_t)q & 15) == 0 && (ge.fp8 || encode_fn() != nullptr);
 }
 
 void shared_tc_tiles(SharedDecodeParams* p) {
@@ -542,23 +746,17 @@ void shared_tc_tiles(SharedDecodeParams* p) {
 }
 
 cudaError_t prepare_decode_shared_tc() {
-  cudaError_t e = prepare<128>();
-  return e == cudaSuccess ? prepare<64>() : e;
+  cudaError_t e = prepare<128, false>();
+  if (e == cudaSuccess) e = prepare<64, false>();
+  return e == cudaSuccess ? prepare<128, true>() : e;
 }
 
 cudaError_t launch_decode_shared_tc(const SharedDecodeParams& p, cudaStream_t st) {
   if (p.tile_keys != kTile || p.row_chunk != kRows) return cudaErrorInvalidValue;
-  CUtensorMap map;
+  CUtensorMap map = {};
+  if (p.geom.fp8) return p.geom.head_dim == 128 ? launch_shape<128, true>(p, map, st) : cudaErrorInvalidValue;
   if (!make_page_map(&map, p.pool, p.geom, p.n_pages)) return cudaErrorInvalidValue;
-  const int shape = !p.shaped ? 0 : (p.shape.post > 0.f ? 1 : 0) | (p.shape.biased ? 2 : 0);
-  if (p.geom.head_dim == 128) {
-    if (shape == 0) return launch<128, 0>(p, map, st);
-    if (shape == 1) return launch<128, 1>(p, map, st);
-    return shape == 2 ? launch<128, 2>(p, map, st) : launch<128, 3>(p, map, st);
-  }
-  if (shape == 0) return launch<64, 0>(p, map, st);
-  if (shape == 1) return launch<64, 1>(p, map, st);
-  return shape == 2 ? launch<64, 2>(p, map, st) : launch<64, 3>(p, map, st);
+  return p.geom.head_dim == 128 ? launch_shape<128, false>(p, map, st) : launch_shape<64, false>(p, map, st);
 }
 
 }  // namespace mixattn

@@ -185,9 +185,12 @@ __device__ __forceinline__ void split_bf16(float x, float y, uint32_t& hi, uint3
   lo = pack_bf16(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
 }
 
-// instruction descriptor: D fp32, A/B bf16, M = 128, N = n; b_mn = 1 for an MN-major B
+// instruction descriptor: D fp32, A/B bf16 (or both fp16), M = 128, N = n; b_mn = 1 for an MN-major B
 __host__ __device__ constexpr uint32_t idesc_bf16(int b_mn, uint32_t n = 128) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)b_mn << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+__host__ __device__ constexpr uint32_t idesc_f16(int b_mn, uint32_t n = 128) {
+  return idesc_bf16(b_mn, n) & ~((1u << 7) | (1u << 10));
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
