@@ -27,12 +27,15 @@
 // too late (2400 cycles a tile where neither HBM nor products limit, with any number of products).
 //
 // Quantised caches (kFp8; format in internal.h).  A page block is one untiled copy of 4128 bytes into a ring of
-// 64-key stages, and the warps of Q and of the results turn its codes into operands between those duties: K codes to
-// fp16 (one conversion per pair, exact; Q is taken to fp16 as in the other decode kernel), rows as above;
-// V codes to bf16 (bits moved into place and one product with 2^120, exact), which are stored transposed and stay
-// so: the second product takes V with its keys contiguous.  A K row's exponent multiplies its scores, a V row's
-// its weight before that is split in two bf16 terms, whose range holds any exponent.  K has one operand
-// buffer (its scores come early), V two, so that a stage is free again as soon as it is converted.
+// 64-key stages, and the warps of Q and of the results turn its codes into fp16 operands between those duties (one
+// conversion per pair, exact; Q is taken to fp16 as in the other decode kernel): K rows as above, V, which is
+// stored transposed, with its keys contiguous.  A K row's exponent multiplies its scores.  A V row's exponent X
+// is added to its base-2 score: the weight 2^(s + X - n) is what multiplies the row's codes, and with
+// n the row's reference for s + X, its fp16 rounding (2^-12 of it, or 2^-25 of the largest) is
+// relative to what the keys contribute, however their magnitudes differ.  The sum of the softmax takes the
+// weights times 2^-X in fp32, so reference, sum and accumulator are as ever.  (V as bf16, the weight in two terms:
+// 2500 cycles a tile for the conversion alone.)  K has one operand buffer (its scores come early), V
+// two, so that a stage is free again as soon as it is converted.
 //
 // TMEM: S0, S1, O_0, O_1 = 4 x 128 columns.  All mbarrier waits are bounded; on time-out a status
 // word is raised and every role leaves its loop.
@@ -54,8 +57,6 @@ constexpr int kPiece = 2048;                     // 64 channels of one page's K 
 constexpr int kHalf = kTilePages * kPiece;       // 64 channels of a tile's K or V
 constexpr int kQHalf = kRows * 128;              // 64 channels of Q
 constexpr uint32_t kColS = 0, kColO = 256;
-constexpr float kMaxLead = 32.f;                 // a score this far (base 2) above its row's reference moves it;
-constexpr float kMaxSum = 0x1p38f;               // 64 weights that do not lead that far add up to no more
 
 enum {
   B_QF = 0, B_QE = 1,        // Q there / consumed by the segment's score products
@@ -71,7 +72,7 @@ struct Layout {
   static constexpr int kHalves = D / 64;
   static constexpr int kTileBytes = kHalves * kHalf;              // K or V of a tile as operand
   // native: rings of operand tiles for K and V.  Quantised: a ring of raw stages (64 keys, K and V), one
-  // operand buffer for K and two for V; a tile's exponents as factors, four tiles deep (K, V)
+  // operand buffer for K and two for V; what a tile's exponents come to, four tiles deep
   static constexpr int kStages = kFp8 ? 5 : D == 128 ? 3 : 6;
   static constexpr int kKBufs = kFp8 ? 1 : kStages, kVBufs = kFp8 ? 2 : kStages;
   static constexpr int kRawBlk = 2 * kPage * D + 2 * kPage, kRawStage = 4 * kRawBlk;
@@ -82,7 +83,7 @@ struct Layout {
   static constexpr int kSmV = kSmK + kKBufs * kTileBytes;
   static constexpr int kSmRaw = kSmV + kVBufs * kTileBytes;
   static constexpr int kSmX = kSmRaw + (kFp8 ? kStages * kRawStage : 0);
-  static constexpr int kSmBar = kSmX + (kFp8 ? 4 * 2 * kTile * 4 : 0);
+  static constexpr int kSmBar = kSmX + (kFp8 ? 4 * 3 * kTile * 4 : 0);
   static constexpr int kSmXchg = kSmBar + (kBars * 8 + 16 + 255) / 256 * 256;
   static constexpr int kBytes = kSmXchg + 2 * kRows * 8 + 768;   // + slack to align a 256-byte aligned base to 1024
   static_assert(kBytes <= 227 * 1024, "shared memory");
@@ -107,14 +108,6 @@ __device__ __forceinline__ void codes_to_f16(uint32_t x, uint32_t& lo, uint32_t&
       "cvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
       : "=r"(lo), "=r"(hi) : "r"(x));
 }
-// The same as bf16: sign, and exponent and mantissa moved to the bf16 field's low end, are the value times
-// 2^-120 (subnormal codes become subnormal numbers), which the product puts right.
-__device__ __forceinline__ void codes_to_bf16(uint32_t x, uint32_t& lo, uint32_t& hi) {
-  const uint32_t a = __byte_perm(x, 0u, 0x1404), b = __byte_perm(x, 0u, 0x3424);   // codes in the high bytes of the halves
-  uint32_t p = (a & 0x80008000u) | ((a >> 4) & 0x07f007f0u), q = (b & 0x80008000u) | ((b >> 4) & 0x07f007f0u);
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(lo) : "r"(p), "r"(0x7b807b80u));           // 2^120
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(hi) : "r"(q), "r"(0x7b807b80u));
-}
 __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t x) {
   uint32_t d;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(__uint_as_float(x & 0xffff0000u)), "f"(__uint_as_float(x << 16)));
@@ -127,6 +120,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_constant__ SharedDecodeParams p) {
   using L = Layout<D, kFp8>;
   constexpr int kStages = L::kStages;
+  // A score this far (base 2) above its row's reference moves it; 64 weights that do not lead that far
+  // add up to no more than kMaxSum (fp16 weights have to stay below 65504 themselves).
+  constexpr float kMaxLead = kFp8 ? 9.f : 32.f, kMaxSum = kFp8 ? 0x1p15f : 0x1p38f;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* gbase = smem_raw + (base - smem_u32(smem_raw));
@@ -287,7 +283,8 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
       if (!ok && lane == 0) atomicExch(p.status, kDevWaitTimeout);
     } else if (warp == 2) {
       // ------------------------------ P V ------------------------------
-      constexpr uint32_t kIdesc = idesc_bf16(kFp8 ? 0 : 1, D);   // V with its channels contiguous, or its keys
+      constexpr uint32_t kIdesc = kFp8 ? idesc_f16(0, D) : idesc_bf16(1, D);   // V with its keys contiguous, or its channels
+      constexpr int kTerms = kFp8 ? 4 : 8;                        // four steps of the weights, four of their residuals
       constexpr int kGStep = kFp8 ? 128 * 128 : 64 * 128;         // a stream's keys behind the other's
       constexpr int kStep = kFp8 ? 32 : kPiece;                   // 16 keys
       bool ok = true;
@@ -327,12 +324,12 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
             if (left - 64 * g >= 64) {
               umma_bf16_ts_warp(o, pcol, vdesc, kIdesc, t > s.t0);
 #pragma unroll
-              for (int x = 1; x < 8; ++x)   // four steps of the values, four of the residuals
+              for (int x = 1; x < kTerms; ++x)
                 umma_bf16_ts_warp(o, pcol + 8 * x, vdesc + (uint64_t)((x & 3) * (kStep >> 4)), kIdesc, 1u);
             } else {
               const int steps = max((left - 64 * g + 15) >> 4, 1);
 #pragma unroll 1
-              for (int x = 0; x < 8; ++x)
+              for (int x = 0; x < kTerms; ++x)
                 if ((x & 3) < steps)
                   umma_bf16_ts_warp(o, pcol + 8 * x, vdesc + (uint64_t)((x & 3) * (kStep >> 4)), kIdesc, t > s.t0 || x > 0);
             }
@@ -385,33 +382,43 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
         if (x < stages && !__all_sync(0xffffffffu, mbar_wait(BAR(L::kRF + (H + x) % kStages), ((H + x) / kStages) & 1, abort_flag))) return false;
       }
       if (G >= 1 && !__all_sync(0xffffffffu, mbar_wait(BAR(L::kKE), (G - 1) & 1, abort_flag))) return false;
+      // (All of a thread's loads come before its stores, which the compiler could not pass: taken one by one, each
+      // chunk waited for its own load, 2800 cycles a tile for K and V together.)
+      uint4 w[8];
       // K: chunk c of key's row is 16 channels
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
         const int key = x * 16 + (n >> 3), c = n & 7, tok = key & 15;
-        if (key >= left) break;   // (what the operand holds there are other keys' rows, masked later)
-        const uint4 w = *reinterpret_cast<const uint4*>(raw[x >> 2] + (x & 3) * L::kRawBlk + tok * D + ((c ^ fp8_k_swizzle(tok)) << 4));
+        w[x] = make_uint4(0u, 0u, 0u, 0u);
+        if (key < left)   // (the others are masked later)
+          w[x] = *reinterpret_cast<const uint4*>(raw[x >> 2] + (x & 3) * L::kRawBlk + tok * D + ((c ^ fp8_k_swizzle(tok)) << 4));
+      }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const int key = x * 16 + (n >> 3), c = n & 7, at = (c & 3) * 2;
         uint4 lo, hi;
-        codes_to_f16(w.x, lo.x, lo.y);
-        codes_to_f16(w.y, lo.z, lo.w);
-        codes_to_f16(w.z, hi.x, hi.y);
-        codes_to_f16(w.w, hi.z, hi.w);
+        codes_to_f16(w[x].x, lo.x, lo.y);
+        codes_to_f16(w[x].y, lo.z, lo.w);
+        codes_to_f16(w[x].z, hi.x, hi.y);
+        codes_to_f16(w[x].w, hi.z, hi.w);
         unsigned char* to = gbase + L::kSmK + (c >> 2) * kHalf + key * 128;
-        const int at = (c & 3) * 2;
         *reinterpret_cast<uint4*>(to + ((at ^ (key & 7)) << 4)) = lo;
         *reinterpret_cast<uint4*>(to + (((at + 1) ^ (key & 7)) << 4)) = hi;
       }
-      {   // exponents as factors; keys that are not there have a weight of zero times a factor of zero
-        float* f = reinterpret_cast<float*>(gbase + L::kSmX) + (G & 3) * 2 * kTile;
+      {   // the exponents: factor of the scores, summand of the weight's, factor of the sum's
+        float* f = reinterpret_cast<float*>(gbase + L::kSmX) + (G & 3) * 3 * kTile;
         const float fold = kShape == 0 ? p.scale_log2e : kShape == 2 ? p.shape.pre : 1.f;
         const unsigned char* xs = raw[n >> 6] + ((n >> 4) & 3) * L::kRawBlk + 2 * kPage * D + (n & 15);
-        float fk = 0.f, fv = 0.f;
+        float fk = 0.f, xv = 0.f, gv = 0.f;   // (keys that are not there are masked)
         if (n < left) {
-          fk = __int_as_float((int)xs[0] << 23) * fold;   // 2^(byte - 127); byte 0 is a vector of zeros
-          fv = __int_as_float((int)xs[kPage] << 23);
+          fk = __int_as_float((int)xs[0] << 23) * fold;           // 2^(byte - 127); byte 0 is a vector of zeros,
+          const int e = xs[kPage] == 0 ? -100 : (int)xs[kPage] - 127;   // which in V may have any exponent
+          xv = (float)e;
+          gv = __int_as_float(min(127 - e, 254) << 23);
         }
         f[n] = fk;
-        f[kTile + n] = fv;
+        f[kTile + n] = xv;
+        f[2 * kTile + n] = gv;
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
@@ -421,23 +428,31 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
       }
       if (G >= 2 && !__all_sync(0xffffffffu, mbar_wait(BAR(L::kVE + (G & 1)), ((G >> 1) - 1) & 1, abort_flag))) return false;
       // V: a channel's 16 keys of a page; rows are channels, 64 keys of a stream each
+      if (left >= kTile) {
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        uint4 w = make_uint4(0u, 0u, 0u, 0u);
-        const int there = left - 16 * x;   // keys of this page
-        if (there > 0) w = *reinterpret_cast<const uint4*>(raw[x >> 2] + (x & 3) * L::kRawBlk + kPage * D + n * kPage);
-        if (there < 16) {                  // what lies behind the last key may be any code, a NaN too
+        for (int x = 0; x < 8; ++x) w[x] = *reinterpret_cast<const uint4*>(raw[x >> 2] + (x & 3) * L::kRawBlk + kPage * D + n * kPage);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const int there = left - 16 * x;   // keys of this page; what lies behind the last key may be any code, a NaN too
           auto keep = [&](uint32_t v, int first) {
             const int m = there - first;
             return m >= 4 ? v : m <= 0 ? 0u : v & ((1u << (8 * m)) - 1u);
           };
-          w = make_uint4(keep(w.x, 0), keep(w.y, 4), keep(w.z, 8), keep(w.w, 12));
+          w[x] = make_uint4(0u, 0u, 0u, 0u);
+          if (there > 0) {
+            w[x] = *reinterpret_cast<const uint4*>(raw[x >> 2] + (x & 3) * L::kRawBlk + kPage * D + n * kPage);
+            w[x] = make_uint4(keep(w[x].x, 0), keep(w[x].y, 4), keep(w[x].z, 8), keep(w[x].w, 12));
+          }
         }
+      }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
         uint4 lo, hi;
-        codes_to_bf16(w.x, lo.x, lo.y);
-        codes_to_bf16(w.y, lo.z, lo.w);
-        codes_to_bf16(w.z, hi.x, hi.y);
-        codes_to_bf16(w.w, hi.z, hi.w);
+        codes_to_f16(w[x].x, lo.x, lo.y);
+        codes_to_f16(w[x].y, lo.z, lo.w);
+        codes_to_f16(w[x].z, hi.x, hi.y);
+        codes_to_f16(w[x].w, hi.z, hi.w);
         unsigned char* to = gbase + L::kSmV + (G & 1) * L::kTileBytes + (x >> 2) * (128 * 128) + n * 128;
         const int at = (x & 3) * 2;
         *reinterpret_cast<uint4*>(to + ((at ^ (n & 7)) << 4)) = lo;
@@ -534,23 +549,31 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
           tmem_ld32(s_addr, s0);
           tmem_ld32(s_addr + 32, s1);
           tmem_wait_ld_pin(s0, s1);
-          const float* factor = reinterpret_cast<const float*>(gbase + L::kSmX) + (G & 3) * 2 * kTile + 64 * g;   // kFp8
-          auto scale_keys = [&]() {   // products of codes -> products (or base-2 scores, see above)
+          const float* factor = reinterpret_cast<const float*>(gbase + L::kSmX) + (G & 3) * 3 * kTile + 64 * g;   // kFp8
+          const float first = (kShape & 2) ? -slope * (float)(newest - t - 64 * g) : 0.f;   // bias of column 0
+          auto scale_keys = [&]() {   // products of codes -> products, or (no cap) what the weights are taken of
 #pragma unroll
             for (int e = 0; e < 64; e += 4) {
               const float4 f = *reinterpret_cast<const float4*>(factor + e);
-              sv[e] = __float_as_uint(__uint_as_float(sv[e]) * f.x);
-              sv[e + 1] = __float_as_uint(__uint_as_float(sv[e + 1]) * f.y);
-              sv[e + 2] = __float_as_uint(__uint_as_float(sv[e + 2]) * f.z);
-              sv[e + 3] = __float_as_uint(__uint_as_float(sv[e + 3]) * f.w);
+              float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+              if constexpr (!(kShape & 1)) x = *reinterpret_cast<const float4*>(factor + kTile + e);
+              if constexpr (kShape == 2) {
+                x.x += fmaf(slope, (float)e, first);
+                x.y += fmaf(slope, (float)(e + 1), first);
+                x.z += fmaf(slope, (float)(e + 2), first);
+                x.w += fmaf(slope, (float)(e + 3), first);
+              }
+              sv[e] = __float_as_uint(fmaf(__uint_as_float(sv[e]), f.x, x.x));
+              sv[e + 1] = __float_as_uint(fmaf(__uint_as_float(sv[e + 1]), f.y, x.y));
+              sv[e + 2] = __float_as_uint(fmaf(__uint_as_float(sv[e + 2]), f.z, x.z));
+              sv[e + 3] = __float_as_uint(fmaf(__uint_as_float(sv[e + 3]), f.w, x.w));
             }
           };
           if constexpr (kFp8) {
             if (!__all_sync(0xffffffffu, mbar_wait(BAR(L::kXF + (G & 3)), (G >> 2) & 1, abort_flag))) { ok = false; break; }
             scale_keys();
           }
-          if constexpr (kShape != 0) {   // raw products -> shaped base-2 scores
-            const float first = -slope * (float)(newest - t - 64 * g);   // bias of column 0
+          if constexpr (kShape != 0 && !(kFp8 && kShape == 2)) {   // raw products -> shaped base-2 scores
             float top = 0.f;   // largest square of a product
 #pragma unroll
             for (int e = 0; e < 64; e += 2) {
@@ -566,7 +589,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
                 top = fmax3(top, uu.x, uu.y);
                 x = (kShape & 2) ? fma2(q, raw, off) : mul2(q, raw);
               } else {
-                x = kFp8 ? add2(raw, off) : fma2(raw, pack2(p.shape.pre, p.shape.pre), off);
+                x = fma2(raw, pack2(p.shape.pre, p.shape.pre), off);
               }
               const float2 y = unpack2(x);
               sv[e] = __float_as_uint(y.x);
@@ -585,6 +608,14 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
                   sv[e] = __float_as_uint(fmaf(fabsf(x) <= 1.f ? a : b, p.shape.post, o));
                 }
               }
+            }
+          }
+          if constexpr (kFp8 && (kShape & 1)) {
+#pragma unroll
+            for (int e = 0; e < 64; e += 2) {
+              const float2 x = *reinterpret_cast<const float2*>(factor + kTile + e);
+              sv[e] = __float_as_uint(__uint_as_float(sv[e]) + x.x);
+              sv[e + 1] = __float_as_uint(__uint_as_float(sv[e + 1]) + x.y);
             }
           }
           const float scale = kShape || kFp8 ? 1.f : p.scale_log2e;
@@ -607,12 +638,12 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
             return fmaxf(mx0, mx1) * scale;
           };
           if (t == s.t0) m_ref = tile_max();
-          float sum;
+          float sum, part;   // of the weights, and what they add to the row's sum
           // P: values over the first 32 of the stream's columns, residuals over the others (the scores are
           // all in registers by now); in two halves, which keeps the registers within the launch's 128
           auto weights = [&]() {
             const float neg = m_ref == -INFINITY ? 0.f : -m_ref;   // (a stream without a key: weights 0, no NaN)
-            f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
+            f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0, part0 = sum0;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               uint32_t pk[16], pl[16];
@@ -624,17 +655,22 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
                 if (i & 2) sum1 = add2(sum1, pack2(a, b));
                 else sum0 = add2(sum0, pack2(a, b));
                 if constexpr (kFp8) {
-                  const float2 f = *reinterpret_cast<const float2*>(factor + kTile + e);
-                  split_bf16(a * f.x, b * f.y, pk[i >> 1], pl[i >> 1]);
+                  const float2 f = *reinterpret_cast<const float2*>(factor + 2 * kTile + e);
+                  part0 = fma2(pack2(a, b), pack2(f.x, f.y), part0);
+                  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(pk[i >> 1]) : "f"(b), "f"(a));
                 } else {
                   split_bf16(a, b, pk[i >> 1], pl[i >> 1]);
                 }
               }
               tmem_st16(s_addr + 16 * half, pk);
-              tmem_st16(s_addr + 32 + 16 * half, pl);
+              if constexpr (!kFp8) tmem_st16(s_addr + 32 + 16 * half, pl);
             }
-            const float2 x = unpack2(add2(sum0, sum1));
-            sum = x.x + x.y;
+            float2 x = unpack2(add2(sum0, sum1));
+            part = sum = x.x + x.y;
+            if constexpr (kFp8) {
+              x = unpack2(part0);
+              part = x.x + x.y;
+            }
           };
           weights();
           if (__any_sync(0xffffffffu, !(sum <= kMaxSum))) {
@@ -660,7 +696,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
             if (far) m_ref = mt;
             weights();
           }
-          l += sum;
+          l += part;
           tmem_wait_st();
           tc_fence_before();
         }
