@@ -123,6 +123,11 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
   // A score this far (base 2) above its row's reference moves it; 64 weights that do not lead that far
   // add up to no more than kMaxSum (fp16 weights have to stay below 65504 themselves).
   constexpr float kMaxLead = kFp8 ? 9.f : 32.f, kMaxSum = kFp8 ? 0x1p15f : 0x1p38f;
+  // A segment's j-th tile (of n) and its first key.  With a distance bias, which lifts the scores towards the query,
+  // the newest tile comes first: from the oldest on, a steep head would move its reference at every tile
+  // (32 sequences of 64k, quantised cache: 124 -> 105 us).
+  auto tiles_of = [](const ShareSegment& q) { return (q.t1 - q.t0 + kTile - 1) / kTile; };
+  auto tile_key = [](const ShareSegment& q, int j, int n) { return q.t0 + ((kShape & 2) ? n - 1 - j : j) * kTile; };
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* gbase = smem_raw + (base - smem_u32(smem_raw));
@@ -186,16 +191,18 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
       int H = 0;   // stages of four pages so far
       while (ok && share_next(p, blockIdx.x, walk, s)) {
         const int32_t* tbl = p.table + (int64_t)p.node[s.node].slot * p.table_stride;
-        const int page_lo = s.t0 / kPage, page_hi = (s.t1 + kPage - 1) / kPage;
-        int ids_next = page_lo + lane < page_hi ? tbl[page_lo + lane] : 0, ids = 0;
-        for (int pg = page_lo; pg < page_hi; pg += 4, ++H) {
-          const int rel = (pg - page_lo) & 31;
-          if (rel == 0) {
-            ids = ids_next;
-            if (pg + 32 + lane < page_hi) ids_next = tbl[pg + 32 + lane];
-          }
-          const int st = H % kStages, turn = H / kStages, n_pg = min(4, page_hi - pg);
-          const int id = __shfl_sync(0xffffffffu, ids, rel + (lane & 3));
+        const int page_hi = (s.t1 + kPage - 1) / kPage, n_tiles = tiles_of(s);
+        // a tile's ids are fetched while the one before is on its way
+        auto ids_of = [&](int j) {
+          const int pg = tile_key(s, j, n_tiles) / kPage + (lane & (kTilePages - 1));
+          return j < n_tiles && pg < page_hi ? tbl[pg] : 0;
+        };
+        int ids = ids_of(0);
+        for (int j = 0; ok && j < n_tiles; ++j) {
+          const int ids_next = ids_of(j + 1), pages_here = min(kTilePages, page_hi - tile_key(s, j, n_tiles) / kPage);
+          for (int pg = 0; pg < pages_here; pg += 4, ++H) {
+          const int st = H % kStages, turn = H / kStages, n_pg = min(4, pages_here - pg);
+          const int id = __shfl_sync(0xffffffffu, ids, pg + (lane & 3));
           if (turn > 0) {
             int w = 1;
             if (lane == 0) w = mbar_wait(BAR(L::kRE + st), (turn - 1) & 1, abort_flag);
@@ -206,6 +213,8 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
           if (lane < n_pg)
             bulk_load(base + L::kSmRaw + st * L::kRawStage + lane * L::kRawBlk,
                       p.pool + (int64_t)id * p.geom.page_bytes + (int64_t)s.g * L::kRawBlk, L::kRawBlk, BAR(L::kRF + st));
+          }
+          ids = ids_next;
         }
       }
       if (!ok && lane == 0) {
@@ -223,18 +232,17 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
       if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&pages) : "memory");
       while (ok && share_next(p, blockIdx.x, walk, s)) {
         const int32_t* tbl = p.table + (int64_t)p.node[s.node].slot * p.table_stride;
-        const int page_lo = s.t0 / kPage, page_hi = (s.t1 + kPage - 1) / kPage;
-        // ids are fetched 32 at a time, one batch ahead of their use
-        int ids_next = page_lo + lane < page_hi ? tbl[page_lo + lane] : 0, ids = 0;
-        for (int pg = page_lo; pg < page_hi; pg += kTilePages, ++G) {
-          const int rel = (pg - page_lo) & 31;
-          if (rel == 0) {
-            ids = ids_next;
-            if (pg + 32 + lane < page_hi) ids_next = tbl[pg + 32 + lane];
-          }
-          const int st = G % kStages, turn = G / kStages, n_pg = min(kTilePages, page_hi - pg);
-          const int j = lane & (kTilePages - 1), h = lane / kTilePages;
-          const int id = __shfl_sync(0xffffffffu, ids, rel + j);
+        const int page_hi = (s.t1 + kPage - 1) / kPage, n_tiles = tiles_of(s), j = lane & (kTilePages - 1), h = lane / kTilePages;
+        // a tile's ids are fetched while the one before is on its way
+        auto id_of = [&](int x) {
+          const int pg = tile_key(s, x, n_tiles) / kPage + j;
+          return x < n_tiles && pg < page_hi ? tbl[pg] : 0;
+        };
+        int id_next = id_of(0);
+        for (int x = 0; x < n_tiles; ++x, ++G) {
+          const int id = id_next;
+          id_next = id_of(x + 1);
+          const int st = G % kStages, turn = G / kStages, n_pg = min(kTilePages, page_hi - tile_key(s, x, n_tiles) / kPage);
           if (turn > 0) {   // lane 0 waits; the verdict is made warp-uniform
             int w = 1;
             if (lane == 0) w = mbar_wait(BAR(free + st), (turn - 1) & 1, abort_flag);
@@ -260,7 +268,8 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
       int G = 0;
       for (int it = 0; ok && share_next(p, blockIdx.x, walk, s); ++it) {
         ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_QF), it & 1, abort_flag));
-        for (int t = s.t0; t < s.t1 && ok; t += kTile, ++G) {
+        const int n_tiles = tiles_of(s);
+        for (int j = 0; j < n_tiles && ok; ++j, ++G) {
           const int sb = G & 1, st = G % L::kKBufs;
           ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_KF + st), (G / L::kKBufs) & 1, abort_flag));
 #pragma unroll
@@ -292,14 +301,15 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
       for (int it = 0; ok && share_next(p, blockIdx.x, walk, s); ++it) {
         // the segment's first P V overwrites the accumulators
         if (it >= 1) ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_OR), (it - 1) & 1, abort_flag));
-        for (int t = s.t0; t < s.t1 && ok; t += kTile, ++G) {
+        const int n_tiles = tiles_of(s);
+        for (int j = 0; j < n_tiles && ok; ++j, ++G) {
           const int sb = G & 1, st = G % L::kVBufs;
           ok = __all_sync(0xffffffffu, mbar_wait(BAR(L::kVF + st), (G / L::kVBufs) & 1, abort_flag));
           if (!ok) break;
           // A stream's steps of 16 keys are pages; the segment's last tile may hold fewer (one at least is taken: the
           // accumulator is read), and rows that are no keys (behind the last one, or of a page that was not
           // loaded), whose weight of zero an infinity or a NaN would survive, are cleared meanwhile.
-          const int left = s.t1 - t;
+          const int left = s.t1 - tile_key(s, j, n_tiles);
           if (!kFp8 && left < kTile) {
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
@@ -313,7 +323,6 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the products read through the async proxy
             __syncwarp();
           }
-          const bool last = t + kTile >= s.t1;
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             ok = ok && __all_sync(0xffffffffu, mbar_wait(BAR(B_PF + 2 * g + sb), (G >> 1) & 1, abort_flag));
@@ -322,7 +331,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
             const uint64_t vdesc = smem_desc(base + L::kSmV + st * L::kTileBytes + g * kGStep, kFp8 ? 16 : kHalf, 1024);
             const uint32_t o = tmem + kColO + g * 128, pcol = tmem + kColS + sb * 128 + g * 64;
             if (left - 64 * g >= 64) {
-              umma_bf16_ts_warp(o, pcol, vdesc, kIdesc, t > s.t0);
+              umma_bf16_ts_warp(o, pcol, vdesc, kIdesc, j > 0);
 #pragma unroll
               for (int x = 1; x < kTerms; ++x)
                 umma_bf16_ts_warp(o, pcol + 8 * x, vdesc + (uint64_t)((x & 3) * (kStep >> 4)), kIdesc, 1u);
@@ -331,9 +340,9 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
 #pragma unroll 1
               for (int x = 0; x < kTerms; ++x)
                 if ((x & 3) < steps)
-                  umma_bf16_ts_warp(o, pcol + 8 * x, vdesc + (uint64_t)((x & 3) * (kStep >> 4)), kIdesc, t > s.t0 || x > 0);
+                  umma_bf16_ts_warp(o, pcol + 8 * x, vdesc + (uint64_t)((x & 3) * (kStep >> 4)), kIdesc, j > 0 || x > 0);
             }
-            if (last) umma_commit_warp(BAR(B_OF + g));
+            if (j == n_tiles - 1) umma_commit_warp(BAR(B_OF + g));
             umma_commit_warp(BAR(B_SR + 2 * g + sb));
             if (g == 1) umma_commit_warp(BAR(L::kVE + st));
           }
@@ -472,7 +481,9 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
     for (int it = 0; ok && more; ++it) {
       const ShareSegment now = s;
       if constexpr (kFp8) {
-        for (int t = now.t0; ok && t < now.t1; t += kTile, ++G) {
+        const int n_tiles = tiles_of(now);
+        for (int j = 0; ok && j < n_tiles; ++j, ++G) {
+          const int t = tile_key(now, j, n_tiles);
           ok = convert(now, t, G, H);
           H += now.t1 - t > 64 ? 2 : 1;
         }
@@ -537,7 +548,9 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
         slope = p.shape.slope[s.g * p.group + R % p.group];
         newest = p.newest[s.s0 + R / p.group];
       }
-      for (int t = s.t0; t < s.t1; t += kTile, ++G) {
+      const int n_tiles = tiles_of(s);
+      for (int j = 0; j < n_tiles; ++j, ++G) {
+        const int t = tile_key(s, j, n_tiles);
         const int sb = G & 1;
         if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SF + 2 * g + sb), (G >> 1) & 1, abort_flag))) { ok = false; break; }
         if (!idle) {
@@ -625,7 +638,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
             for (int e = 0; e < 64; ++e)
               if (e >= left) sv[e] = 0xff800000u;
           }
-          // A row's reference is the maximum of its first tile and only moves when a later score leads it
+          // A row's reference is the maximum of the first tile in which it has a key and only moves when a later score leads it
           // by more than 2^kMaxLead, which shows in the sum of the tile's weights: so the exponentials
           // wait for no maximum, and none is computed.
           auto tile_max = [&]() {
@@ -637,7 +650,10 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
             }
             return fmaxf(mx0, mx1) * scale;
           };
-          if (t == s.t0) m_ref = tile_max();
+          if (__any_sync(0xffffffffu, m_ref == -INFINITY)) {
+            const float mt = tile_max();
+            if (m_ref == -INFINITY) m_ref = mt;
+          }
           float sum, part;   // of the weights, and what they add to the row's sum
           // P: values over the first 32 of the stream's columns, residuals over the others (the scores are
           // all in registers by now); in two halves, which keeps the registers within the launch's 128
@@ -679,7 +695,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
             const float mt = tile_max();
             const bool far = mt > m_ref + kMaxLead;
             const float alpha = far ? ex2_approx(m_ref - mt) : 1.f;
-            if (t > s.t0) {
+            if (j > 0) {
               if (!__all_sync(0xffffffffu, mbar_wait(BAR(B_SR + 2 * g + (sb ^ 1)), ((G - 1) >> 1) & 1, abort_flag))) { ok = false; break; }
               tc_fence_after();
 #pragma unroll 1
