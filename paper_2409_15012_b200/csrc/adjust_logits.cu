@@ -1,17 +1,18 @@
 // Penalties for repeated tokens, biases and grammar masks on logits (mixattn_adjust_logits).
 //
-// What stands between a model's logits and the selection of the next token, per row:
+// What stands between a model's logits and the choice of the next token, per row:
 //     a = seen ? (x > 0 ? x / repetition : x * repetition) : x
 //     b = a - frequency * c - (c > 0 ? presence : 0)
 //     y = (b + bias) / temperature,   -inf where the mask forbids
 // Bound by memory: the logits are read and written once.  What a row has seen is a short list of tokens, what the
-// logits need is a count per token of the vocabulary: a cluster of CTAs takes a row, each CTA a
-// part of the vocabulary with one word per token in its shared memory; each scans its share of the list
-// and adds to the word of the CTA that owns the token, through distributed shared memory.  So the list is read once,
-// nothing per token of the vocabulary is ever in global memory, and whole-number sums make the result
-// independent of their order.  A CTA's part of the row is small enough to be asked for at the very start, 16 bytes
-// by 16 into registers, and is on its way while the words are cleared and the list is read; then it is
-// adjusted and written.
+// logits need is a count per token of the vocabulary.  A CTA takes parts of rows (up to 16384 bf16 or 8192
+// fp32 logits): it asks for the part's logits, 16 bytes by 16 into registers, reads the row's list meanwhile and
+// adds up, in one word per token of the part in shared memory, what is said about the token (whole-number
+// sums: the result does not depend on their order), then adjusts and writes, and clears the words that were not
+// zero for its next part.  512 rows x 131072 bf16 with lists of 100 to 9000 tokens: WAS us.  On the way: a cluster of CTAs per
+// row that shared one reading of the list, through distributed shared memory, 317 against 312; the tokens of the list
+// taken out of the words one by one beside the stream, 286, by warps of their own, 258; quotients instead of
+// products with a reciprocal, 278.
 #include <cuda_bf16.h>
 
 #include "internal.h"
@@ -21,30 +22,20 @@ namespace mixattn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kLongList = 32768;
-constexpr int kPer = 8;           // 16-byte pieces of the row per thread: 16384 bf16 or 8192 fp32 logits per CTA
+constexpr int kPer = 8;           // 16-byte pieces per thread
+constexpr int kCtasPerSm = 3;     // (the words: 64 KB)
 // a token's word: times it was generated | occurs in the prompt | 1 + its place in the list of biases
 constexpr uint32_t kCountMask = (1u << 20) - 1, kPromptBit = 1u << 20;
 constexpr int kBiasShift = 21;
 static_assert(MIXATTN_MAX_RULE_TOKENS <= (int)kCountMask && MIXATTN_MAX_RULE_BIASES < (1 << (32 - kBiasShift)), "fields");
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ uint32_t map_to_cta(uint32_t local, int cta) {
-  uint32_t remote;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(cta));
-  return remote;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-struct Row {                 // one row's rules
-  float repetition, inv_repetition, frequency, presence, scale;   // scale: 1 / temperature
+struct Row {                      // one row's rules
+  float repetition, inv_repetition, frequency, presence;
   const float* bias;
 };
 
-// one logit, w = its word, without the division by the temperature.  (Quotients as products with a reciprocal: one more rounding of 2^-24,
-// at a fifth of the instructions.)
+// A logit whose token's word is w, but for the temperature.  (Quotients as products with a reciprocal: one more rounding
+// of 2^-24, at a fifth of the instructions.)
 __device__ __forceinline__ float adjusted(float x, uint32_t w, const Row& r) {
   const uint32_t c = w & kCountMask;
   if (w & (kCountMask | kPromptBit)) x *= x > 0.f ? r.inv_repetition : r.repetition;
@@ -68,162 +59,208 @@ __device__ __forceinline__ uint32_t mask_bits(const uint32_t* mask, int at, int 
   return __funnelshift_r(lo, hi, at & 31);
 }
 
-template <typename T, int N>
-struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Vec { T v[N]; };
-
-// kTable: some token may have a word (a list of tokens or of biases is there)
-template <typename TI, typename TO, bool kTable>
-__global__ void __launch_bounds__(kThreads, 3)
-adjust_logits_kernel(const __grid_constant__ AdjustParams p, const int cluster, const int spans) {
-  extern __shared__ __align__(16) uint32_t words[];
-  constexpr int kVec = 16 / sizeof(TI);           // logits per 16-byte load
-  constexpr uint32_t kAll = (1u << kVec) - 1;
-  const mixattn_logit_rules& ru = p.rules;
-  const int rank = blockIdx.x % cluster, at_span = blockIdx.x / cluster;
-  const int64_t row = at_span / spans;
-  const int span = at_span % spans;
-  const int first = (span * cluster + rank) * p.part;             // this CTA's tokens [first, last)
-  const int last = min(p.vocab, first + p.part);
-  asm volatile("griddepcontrol.wait;" ::: "memory");              // (a no-op after an ordinary launch)
-
-  Row r;
-  r.repetition = ru.repetition ? ru.repetition[row] : 1.f;
-  r.inv_repetition = 1.f / r.repetition;
-  r.frequency = ru.frequency ? ru.frequency[row] : 0.f;
-  r.presence = ru.presence ? ru.presence[row] : 0.f;
-  const float temperature = ru.temperature ? ru.temperature[row] : 1.f;
-  r.scale = fminf(1.f / temperature, 3.4028235e38f);              // (finite: 0 stays 0)
-  r.bias = ru.bias_values + row * ru.n_bias;
-  const uint32_t* mask = nullptr;
-  const int mask_words = (p.vocab + 31) / 32;
-  if (ru.allowed) {
-    const int64_t which = ru.allowed_rows ? ru.allowed_rows[row] : row;
-    if (which >= 0 && which < ru.n_allowed) mask = ru.allowed + which * ru.allowed_stride;
+// f(tokens, index of the first) for the entries of a list, eight at a time per thread; -1 where there is none
+template <typename F>
+__device__ __forceinline__ void for_each_8(const int32_t* list, int n, F f) {
+  const int tid = threadIdx.x;
+  const int lead = min((int)(-(intptr_t)((size_t)list >> 2) & 3), n), quads = (n - lead) / 4, tail = lead + 4 * quads;
+  const int4* at = reinterpret_cast<const int4*>(list + lead);
+  for (int q = 2 * tid; q < quads; q += 2 * kThreads) {
+    const int4 a = at[q], b = q + 1 < quads ? at[q + 1] : make_int4(-1, -1, -1, -1);
+    const int t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    f(t, lead + 4 * q);
   }
-  const TI* in = reinterpret_cast<const TI*>(p.logits) + row * p.row_stride;
-  TO* out = reinterpret_cast<TO*>(p.out) + row * p.out_stride;
-  const bool skip = p.in_place && temperature == 1.f;             // a token without a word stays as it is
-
-  // 16-byte accesses from the first token on at which both rows are aligned (rows of an odd vocabulary start
-  // anywhere; parts are whole 16-byte pieces, so the answer is the same in all of them); single ones where there is none
-  int head = 0;
-  while (head < kVec && ((((size_t)(in + head)) | ((size_t)(out + head))) & 15)) ++head;
-  const bool pieces = head < kVec;
-  if (!pieces) head = 0;
-  const int v0 = min(first + head, max(last, first));
-  const int body = pieces ? max(0, last - v0) / kVec : 0;
-  const int pad = (kVec - head) % kVec;                           // the words of a piece are 16-byte aligned
-  Vec<TI, kVec> x[kPer];
-  uint32_t allow[kPer];
+  if (tid < 2) {   // in front of the first 16-byte boundary, behind the last
+    const int first = tid ? tail : 0, end = tid ? n : lead;
+    int t[8];
 #pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    const int b = threadIdx.x + u * kThreads;
-    allow[u] = kAll;
-    if (b < body) {
-      if (mask) allow[u] = mask_bits(mask, v0 + b * kVec, mask_words) & kAll;
-      if (!skip && allow[u] != 0) x[u] = *reinterpret_cast<const Vec<TI, kVec>*>(in + v0 + b * kVec);
-    }
-  }
-
-  if constexpr (kTable) {
-    for (int i = threadIdx.x; i < (p.part + kVec) / 4; i += kThreads) reinterpret_cast<uint4*>(words)[i] = make_uint4(0u, 0u, 0u, 0u);
-    __syncthreads();
-    // the last of several biases for one token counts
-    for (int i = threadIdx.x; i < ru.n_bias; i += kThreads) {
-      const int t = ru.bias_tokens[row * ru.n_bias + i];
-      if (t >= first && t < last) atomicMax(words + (t - first + pad), (uint32_t)(i + 1) << kBiasShift);
-    }
-    int n = 0, prompt = 0;
-    if (ru.tokens) {
-      n = ru.n_tokens ? min(max(ru.n_tokens[row], 0), ru.max_tokens) : ru.max_tokens;
-      prompt = ru.n_prompt ? min(max(ru.n_prompt[row], 0), n) : 0;
-    }
-    if (cluster > 1) cluster_sync();   // every CTA's words are cleared and carry their biases
-    else __syncthreads();
-    const int lo = span * cluster * p.part;                                                      // the cluster's tokens
-    const int hi = (int)min((int64_t)p.vocab, (int64_t)lo + (int64_t)cluster * p.part);
-    const int32_t* list = ru.tokens + row * ru.token_stride;
-    constexpr int kBatch = 8;          // entries in flight per thread
-    const int step = cluster * kThreads;
-    for (int i0 = rank * kThreads + threadIdx.x; i0 < n; i0 += kBatch * step) {
-      int t[kBatch];
-#pragma unroll
-      for (int j = 0; j < kBatch; ++j) t[j] = i0 + j * step < n ? list[i0 + j * step] : -1;
-#pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        if (t[j] < lo || t[j] >= hi) continue;   // (another cluster's, or no token at all)
-        const bool read = i0 + j * step < prompt;
-        if (cluster == 1) {
-          uint32_t* at = words + (t[j] - lo + pad);
-          if (read) atomicOr(at, kPromptBit);
-          else atomicAdd(at, 1u);
-        } else {
-          const int cta = (t[j] - lo) / p.part;
-          const uint32_t to = map_to_cta(smem_u32(words) + 4 * (t[j] - lo - cta * p.part + pad), cta);
-          if (read) asm volatile("red.relaxed.cluster.shared::cluster.or.b32 [%0], %1;" ::"r"(to), "r"(kPromptBit) : "memory");
-          else asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(to), "r"(1u) : "memory");
-        }
-      }
-    }
-    if (cluster > 1) cluster_sync();   // (and nobody leaves while others still add to its words)
-    else __syncthreads();
-  }
-  if (first >= last) return;
-
-  auto one = [&](int t) {
-    const uint32_t w = kTable ? words[t - first + pad] : 0u;
-    const bool ok = mask == nullptr || (__ldg(mask + (t >> 5)) >> (t & 31) & 1u);
-    if (!ok) out[t] = rounded<TO>(-INFINITY);
-    else if (!skip || w != 0) out[t] = rounded<TO>(adjusted(widened(in[t]), w, r) * r.scale);
-  };
-  if (!pieces) {
-    for (int t = first + threadIdx.x; t < last; t += kThreads) one(t);
-    return;
-  }
-  if ((int)threadIdx.x < v0 - first) one(first + threadIdx.x);
-  for (int t = v0 + body * kVec + threadIdx.x; t < last; t += kThreads) one(t);
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    const int b = threadIdx.x + u * kThreads;
-    if (b >= body) break;
-    const int t = v0 + b * kVec;
-    uint32_t w[kVec], any = 0;
-    if constexpr (kTable) {
-#pragma unroll
-      for (int i = 0; i < kVec; i += 4) {
-        const uint4 q = *reinterpret_cast<const uint4*>(words + (t - first + pad) + i);
-        w[i] = q.x; w[i + 1] = q.y; w[i + 2] = q.z; w[i + 3] = q.w;
-        any |= q.x | q.y | q.z | q.w;
-      }
-    }
-    if (skip) {
-      if (any == 0 && allow[u] == kAll) continue;
-      if (allow[u] != 0) x[u] = *reinterpret_cast<const Vec<TI, kVec>*>(in + t);
-    }
-    Vec<TO, kVec> y;
-    float f[kVec];
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) f[i] = widened(x[u].v[i]);
-    if (any != 0) {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i)
-        if (w[i] != 0) f[i] = adjusted(f[i], w[i], r);
-    }
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      f[i] *= r.scale;
-      if (!(allow[u] >> i & 1u)) f[i] = -INFINITY;
-      y.v[i] = rounded<TO>(f[i]);
-    }
-    *reinterpret_cast<Vec<TO, kVec>*>(out + t) = y;
+    for (int j = 0; j < 8; ++j) t[j] = first + j < end ? list[first + j] : -1;
+    f(t, first);
   }
 }
 
-// tokens per CTA at most
+// What a part of a row has to do with.
+template <typename TI, typename TO>
+struct Part {
+  static constexpr int kVec = 16 / sizeof(TI);    // logits per 16-byte load
+  int64_t row;
+  int first, last;                                // tokens [first, last)
+  const TI* in;
+  TO* out;
+  const uint32_t* mask;
+  int v0, body;                                   // first token and number of whole pieces
+  bool pieces;
+  float temperature;
+  __device__ __forceinline__ Part(const AdjustParams& p, int64_t item, int parts) {
+    const mixattn_logit_rules& ru = p.rules;
+    row = item / parts;
+    first = (int)(item - row * parts) * p.part;
+    last = min(p.vocab, first + p.part);
+    in = reinterpret_cast<const TI*>(p.logits) + row * p.row_stride;
+    out = reinterpret_cast<TO*>(p.out) + row * p.out_stride;
+    temperature = ru.temperature ? ru.temperature[row] : 1.f;
+    mask = nullptr;
+    if (ru.allowed) {
+      const int64_t which = ru.allowed_rows ? ru.allowed_rows[row] : row;
+      if (which >= 0 && which < ru.n_allowed) mask = ru.allowed + which * ru.allowed_stride;
+    }
+    // 16-byte accesses from the first token on at which both rows are aligned (rows of an odd vocabulary
+    // start anywhere); single ones where there is none
+    const int head_in = (int)(-(intptr_t)((size_t)(in + first) / sizeof(TI)) & (kVec - 1));
+    pieces = ((size_t)(out + first + head_in) & 15) == 0;
+    v0 = pieces ? min(first + head_in, last) : last;
+    body = max(0, last - v0) / kVec;
+  }
+  __device__ __forceinline__ float scale() const { return fminf(1.f / temperature, 3.4028235e38f); }   // (finite: 0 stays 0)
+  __device__ __forceinline__ bool allowed(int t) const { return mask == nullptr || (__ldg(mask + (t >> 5)) >> (t & 31) & 1u); }
+};
+
+// kTable: some token may have a word (a list of tokens or of biases is there).  parts: CTAs' worth of work per row
+template <typename TI, typename TO, bool kTable>
+__global__ void __launch_bounds__(kThreads, kTable ? kCtasPerSm : 4)
+adjust_logits_kernel(const __grid_constant__ AdjustParams p, const int parts) {
+  using P = Part<TI, TO>;
+  constexpr int kVec = P::kVec;
+  constexpr uint32_t kAll = (1u << kVec) - 1;
+  extern __shared__ __align__(16) uint32_t words[];
+  const mixattn_logit_rules& ru = p.rules;
+  const int tid = threadIdx.x;
+  const int64_t items = (int64_t)p.n_rows * parts;
+  if constexpr (kTable)
+    for (int i = tid; i < (p.part + 2 * kVec) / 4; i += kThreads) reinterpret_cast<uint4*>(words)[i] = make_uint4(0u, 0u, 0u, 0u);
+  asm volatile("griddepcontrol.wait;" ::: "memory");                  // (a no-op after an ordinary launch)
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const P a(p, item, parts);
+    const bool still = p.in_place && a.temperature == 1.f;            // a token that no rule names stays as it is
+    const float scale = a.scale();
+    const uint4* src = reinterpret_cast<const uint4*>(a.in + a.v0);
+    uint4 x[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u)
+      if (tid + u * kThreads < a.body && !still) x[u] = src[tid + u * kThreads];
+    Row r;
+    uint32_t* word = words;                                           // of token a.first; those of a piece are 16-byte aligned
+    if constexpr (kTable) {
+      word += a.pieces ? (kVec - (a.v0 - a.first) % kVec) % kVec : 0;
+      int n = 0, prompt = 0;
+      if (ru.tokens) {
+        n = ru.n_tokens ? min(max(ru.n_tokens[a.row], 0), ru.max_tokens) : ru.max_tokens;
+        prompt = ru.n_prompt ? min(max(ru.n_prompt[a.row], 0), n) : 0;
+      }
+      r.repetition = ru.repetition ? ru.repetition[a.row] : 1.f;
+      r.inv_repetition = 1.f / r.repetition;
+      r.frequency = ru.frequency ? ru.frequency[a.row] : 0.f;
+      r.presence = ru.presence ? ru.presence[a.row] : 0.f;
+      r.bias = ru.bias_values + a.row * ru.n_bias;
+      const unsigned span = a.last > a.first ? a.last - a.first : 0;
+      __syncthreads();                                                // the words are zero
+      if (ru.n_bias > 0) {
+        // the last of several biases for one token counts: the largest place, while nothing else is in the words
+        for (int i = tid; i < ru.n_bias; i += kThreads) {
+          const unsigned at = (unsigned)(ru.bias_tokens[a.row * ru.n_bias + i] - a.first);
+          if (at < span) atomicMax(word + at, (uint32_t)(i + 1) << kBiasShift);
+        }
+        __syncthreads();
+      }
+      for_each_8(ru.tokens + a.row * ru.token_stride, n, [&](const int (&t)[8], int i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const unsigned at = (unsigned)(t[j] - a.first);             // (another part's, or no token at all)
+          if (t[j] < 0 || at >= span) continue;
+          if (i + j < prompt) atomicOr(word + at, kPromptBit);
+          else atomicAdd(word + at, 1u);
+        }
+      });
+      __syncthreads();
+    }
+    auto one = [&](int t) {
+      uint32_t w = 0u;
+      if constexpr (kTable) {
+        w = word[t - a.first];
+        word[t - a.first] = 0u;
+      }
+      if (!a.allowed(t)) {
+        a.out[t] = rounded<TO>(-INFINITY);
+      } else if (!still || w != 0u) {
+        float f = widened(a.in[t]);
+        if (kTable && w != 0u) f = adjusted(f, w, r);
+        a.out[t] = rounded<TO>(f * scale);
+      }
+    };
+    if (!a.pieces) {
+      for (int t = a.first + tid; t < a.last; t += kThreads) one(t);
+      continue;
+    }
+    if (tid < a.v0 - a.first) one(a.first + tid);
+    for (int t = a.v0 + a.body * kVec + tid; t < a.last; t += kThreads) one(t);
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int b = tid + u * kThreads, t = a.v0 + b * kVec;
+      if (b >= a.body) break;
+      const uint32_t allow = a.mask ? mask_bits(a.mask, t, (p.vocab + 31) / 32) & kAll : kAll;
+      uint32_t w[kVec], any = 0u;
+      if constexpr (kTable) {
+        uint4* at = reinterpret_cast<uint4*>(word + (t - a.first));
+#pragma unroll
+        for (int i = 0; i < kVec / 4; ++i) {
+          const uint4 q = at[i];
+          w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+          any |= q.x | q.y | q.z | q.w;
+        }
+        if (any != 0u)
+#pragma unroll
+          for (int i = 0; i < kVec / 4; ++i) at[i] = make_uint4(0u, 0u, 0u, 0u);
+      }
+      if (still) {
+        if (any == 0u && allow == kAll) continue;
+        x[u] = src[b];
+      }
+      const uint32_t v[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+      float f[kVec];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kVec == 8) {
+          f[2 * i] = __uint_as_float(v[i] << 16);
+          f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+        } else {
+          f[i] = __uint_as_float(v[i]);
+        }
+      }
+      if (kTable && any != 0u) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+          if (w[i] != 0u) f[i] = adjusted(f[i], w[i], r);
+      }
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) f[i] *= scale;
+      if (allow != kAll) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+          if (!(allow >> i & 1u)) f[i] = -INFINITY;
+      }
+      uint4* to = reinterpret_cast<uint4*>(a.out + t);
+      if constexpr (sizeof(TO) == 2) {
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+          y[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        *to = make_uint4(y[0], y[1], y[2], y[3]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kVec / 4; ++i)
+          to[i] = make_uint4(__float_as_uint(f[4 * i]), __float_as_uint(f[4 * i + 1]), __float_as_uint(f[4 * i + 2]), __float_as_uint(f[4 * i + 3]));
+      }
+    }
+  }
+}
+
+// tokens per part at most, and the words of a part
 template <typename TI>
 constexpr int max_part() { return kThreads * kPer * (16 / (int)sizeof(TI)); }
 template <typename TI>
-constexpr int table_bytes(int part) { return (part + 16 / (int)sizeof(TI)) * 4; }
+constexpr int table_bytes(int part) { return (part + 2 * (16 / (int)sizeof(TI))) * 4; }
 
 template <typename TI, typename TO>
 cudaError_t prepare() {
@@ -233,31 +270,25 @@ cudaError_t prepare() {
 template <typename TI, typename TO>
 cudaError_t launch(AdjustParams& p, int sm_count, cudaStream_t st) {
   const bool table = p.rules.tokens != nullptr || p.rules.n_bias > 0;
-  // CTAs per row: enough for the vocabulary, more (up to eight) where rows are few
+  // parts per row: as few as registers and shared memory allow, more (down to 2048 tokens each) where rows are few
   int64_t parts = ((int64_t)p.vocab + max_part<TI>() - 1) / max_part<TI>();
-  while (parts < 8 && p.n_rows * parts < 2 * sm_count && p.vocab > parts * 2048) parts *= 2;
-  // A list of usual length is read by every CTA of the row for itself; only a long one is worth a cluster's two
-  // barriers and remote sums (512 rows x 131072: WAS
-  const int cluster = p.rules.tokens != nullptr && p.rules.max_tokens > kLongList && parts > 1 ? 8 : 1;
-  parts = (parts + cluster - 1) / cluster * cluster;
+  while (p.n_rows * parts < 2 * sm_count && p.vocab > parts * 2048) parts *= 2;
   p.part = (int)((((int64_t)p.vocab + parts - 1) / parts + 31) / 32 * 32);
-  const int spans = (int)(parts / cluster);
-  if (p.n_rows * parts > INT32_MAX) return cudaErrorInvalidValue;
+  const int64_t items = p.n_rows * parts;
+  if (parts > INT32_MAX) return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.n_rows * parts));
+  const int64_t slots = (int64_t)sm_count * (table ? kCtasPerSm : 4);
+  cfg.gridDim = dim3((unsigned)(items < slots ? items : slots));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = table ? table_bytes<TI>(p.part) : 0;
   cfg.stream = st;
-  cudaLaunchAttribute attr[2];
+  cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return table ? cudaLaunchKernelEx(&cfg, adjust_logits_kernel<TI, TO, true>, p, cluster, spans)
-               : cudaLaunchKernelEx(&cfg, adjust_logits_kernel<TI, TO, false>, p, cluster, spans);
+  cfg.numAttrs = 1;
+  return table ? cudaLaunchKernelEx(&cfg, adjust_logits_kernel<TI, TO, true>, p, (int)parts)
+               : cudaLaunchKernelEx(&cfg, adjust_logits_kernel<TI, TO, false>, p, (int)parts);
 }
 
 }  // namespace
