@@ -24,8 +24,7 @@ struct Chunk {                        // 16 bytes as fp32
   static constexpr int N = 16 / sizeof(T);
   float f[N];
 };
-__device__ __forceinline__ void load(Chunk<__nv_bfloat16>& c, const char* p) {
-  const uint4 w = *reinterpret_cast<const uint4*>(p);
+__device__ __forceinline__ void widen(Chunk<__nv_bfloat16>& c, uint4 w) {
   const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -33,9 +32,8 @@ __device__ __forceinline__ void load(Chunk<__nv_bfloat16>& c, const char* p) {
     c.f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ void load(Chunk<float>& c, const char* p) {
-  const float4 w = *reinterpret_cast<const float4*>(p);
-  c.f[0] = w.x; c.f[1] = w.y; c.f[2] = w.z; c.f[3] = w.w;
+__device__ __forceinline__ void widen(Chunk<float>& c, uint4 w) {
+  c.f[0] = __uint_as_float(w.x); c.f[1] = __uint_as_float(w.y); c.f[2] = __uint_as_float(w.z); c.f[3] = __uint_as_float(w.w);
 }
 __device__ __forceinline__ uint4 bits_of(const Chunk<__nv_bfloat16>& c) {
   uint32_t v[4];
@@ -104,21 +102,38 @@ __global__ void __launch_bounds__(kThreads) rope_qkv_kernel(const __grid_constan
   const int tok0 = blockIdx.x * kTokens;
   if (tok0 >= en.n_new) return;
   const int n_tok = min(kTokens, en.n_new - tok0), pairs = p.rotary / 2;
-  for (int i = threadIdx.x; i < n_tok * pairs; i += kThreads) {
-    const int t = i / pairs, pr = i - t * pairs;
-    double a = (double)(en.pos0 + tok0 + t) * p.freq[pr];
-    a -= 6.283185307179586476925 * rint(a * 0.15915494309189533577);
-    float sn, cs;
-    sincosf((float)a, &sn, &cs);
-    turn[t][pr] = make_float2(cs * p.scale, sn * p.scale);
-  }
-  __syncthreads();
   const int lane = threadIdx.x % kLanes, t = threadIdx.x / kLanes % kTokens, grp = threadIdx.x / (kLanes * kTokens);
-  if (t >= n_tok) return;                    // (whole head vectors: the lanes that shuffle stay together)
   // this thread's two chunks: a pair of halves, or neighbours
   const int turned = p.rotary / E;           // chunks that turn (even: rotary is a multiple of 16)
   const bool rotates = lane < turned / 2, split = p.halves && rotates;
   const int c0 = split ? lane : 2 * lane, c1 = split ? lane + turned / 2 : 2 * lane + 1;
+  const int64_t row = (int64_t)en.row0 + tok0 + t;
+  const int nq = p.q != nullptr ? p.n_q_heads : 0, nk = p.k != nullptr ? ge.n_kv_heads : 0, nv = p.v != nullptr ? ge.n_kv_heads : 0;
+  const int heads = t < n_tok ? nq + nk + nv : 0;
+  auto source = [&](int h) {
+    const char* src = h < nq ? p.q + row * p.q_stride : h < nq + nk ? p.k + row * p.k_stride : p.v + row * p.v_stride;
+    return src + (int64_t)(h < nq ? h : h < nq + nk ? h - nq : h - nq - nk) * ge.row_bytes;
+  };
+  // Rows are asked for kAhead heads before they are needed, the first ones before the sines are formed.
+  constexpr int kAhead = 2;
+  uint4 ahead[kAhead][2];
+  auto fetch = [&](int h, uint4 (&to)[2]) {
+    if (h >= heads) return;
+    const char* src = source(h);
+    to[0] = *reinterpret_cast<const uint4*>(src + c0 * 16);
+    to[1] = *reinterpret_cast<const uint4*>(src + c1 * 16);
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) fetch(grp + i * kGroups, ahead[i]);
+  for (int i = threadIdx.x; i < n_tok * pairs; i += kThreads) {
+    const int x = i / pairs, pr = i - x * pairs;
+    double a = (double)(en.pos0 + tok0 + x) * p.freq[pr];
+    a -= 6.283185307179586476925 * rint(a * 0.15915494309189533577);
+    float sn, cs;
+    sincosf((float)a, &sn, &cs);
+    turn[x][pr] = make_float2(cs * p.scale, sn * p.scale);
+  }
+  __syncthreads();
   float cs[E], sn[E];
   if (rotates) {
 #pragma unroll
@@ -128,10 +143,9 @@ __global__ void __launch_bounds__(kThreads) rope_qkv_kernel(const __grid_constan
       sn[i] = w.y;
     }
   }
-  const int64_t row = (int64_t)en.row0 + tok0 + t;
   int64_t page = 0;
   int slot = 0;
-  bool keep = p.pool != nullptr;
+  bool keep = p.pool != nullptr && t < n_tok;
   if (keep) {
     // a ring only keeps the last `window` tokens of the call
     keep = !(p.is_ring && en.n_new > p.window && tok0 + t < en.n_new - p.window);
@@ -145,56 +159,54 @@ __global__ void __launch_bounds__(kThreads) rope_qkv_kernel(const __grid_constan
       slot = pos % kPage;
     }
   }
-  const int nq = p.q != nullptr ? p.n_q_heads : 0, nk = p.k != nullptr ? ge.n_kv_heads : 0, nv = p.v != nullptr ? ge.n_kv_heads : 0;
-#pragma unroll 2
-  for (int h = grp; h < nq + nk + nv; h += kGroups) {
-    const int which = h < nq ? 0 : h < nq + nk ? 1 : 2;
-    const int hh = which == 0 ? h : which == 1 ? h - nq : h - nq - nk;
-    const char* src = which == 0 ? p.q + row * p.q_stride : which == 1 ? p.k + row * p.k_stride : p.v + row * p.v_stride;
-    src += (int64_t)hh * ge.row_bytes;
-    uint4 b0, b1;
-    if (rotates && which != 2) {
-      Chunk<T> a, b;
-      load(a, src + c0 * 16);
-      load(b, src + c1 * 16);
-      if (split) {
+  for (int h0 = grp; h0 < heads; h0 += kAhead * kGroups) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-          const float x = a.f[i], y = b.f[i];
-          a.f[i] = x * cs[i] - y * sn[i];
-          b.f[i] = x * sn[i] + y * cs[i];
-        }
-      } else {
+    for (int j = 0; j < kAhead; ++j) {
+      const int h = h0 + j * kGroups;
+      if (h >= heads) break;                 // (whole head vectors: the lanes that shuffle stay together)
+      uint4 b0 = ahead[j][0], b1 = ahead[j][1];
+      fetch(h + kAhead * kGroups, ahead[j]);
+      const int which = h < nq ? 0 : h < nq + nk ? 1 : 2, hh = which == 0 ? h : which == 1 ? h - nq : h - nq - nk;
+      if (rotates && which != 2) {
+        Chunk<T> a, b;
+        widen(a, b0);
+        widen(b, b1);
+        if (split) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-          float& fx = i < E / 2 ? a.f[2 * i] : b.f[2 * i - E];
-          float& fy = i < E / 2 ? a.f[2 * i + 1] : b.f[2 * i - E + 1];
-          const float x = fx, y = fy;
-          fx = x * cs[i] - y * sn[i];
-          fy = x * sn[i] + y * cs[i];
+          for (int i = 0; i < E; ++i) {
+            const float x = a.f[i], y = b.f[i];
+            a.f[i] = x * cs[i] - y * sn[i];
+            b.f[i] = x * sn[i] + y * cs[i];
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            float& fx = i < E / 2 ? a.f[2 * i] : b.f[2 * i - E];
+            float& fy = i < E / 2 ? a.f[2 * i + 1] : b.f[2 * i - E + 1];
+            const float x = fx, y = fy;
+            fx = x * cs[i] - y * sn[i];
+            fy = x * sn[i] + y * cs[i];
+          }
         }
+        b0 = bits_of(a);
+        b1 = bits_of(b);
       }
-      b0 = bits_of(a);
-      b1 = bits_of(b);
-    } else {
-      b0 = *reinterpret_cast<const uint4*>(src + c0 * 16);
-      b1 = *reinterpret_cast<const uint4*>(src + c1 * 16);
-    }
-    char* out = which == 0 ? p.q_out : which == 1 ? p.k_out : p.v_out;
-    if (out != nullptr) {
-      out += (row * (which == 0 ? p.n_q_heads : ge.n_kv_heads) + hh) * ge.row_bytes;
-      *reinterpret_cast<uint4*>(out + c0 * 16) = b0;
-      *reinterpret_cast<uint4*>(out + c1 * 16) = b1;
-    }
-    if (which != 0 && keep) {
-      if constexpr (sizeof(T) == 2 && D == 128) {
-        if (ge.fp8) {
-          store_fp8<kLanes>(p, page, slot, hh, which - 1, c0, c1, b0, b1, lane == 0);
-          continue;
+      char* out = which == 0 ? p.q_out : which == 1 ? p.k_out : p.v_out;
+      if (out != nullptr) {
+        out += (row * (which == 0 ? p.n_q_heads : ge.n_kv_heads) + hh) * ge.row_bytes;
+        *reinterpret_cast<uint4*>(out + c0 * 16) = b0;
+        *reinterpret_cast<uint4*>(out + c1 * 16) = b1;
+      }
+      if (which != 0 && keep) {
+        if constexpr (sizeof(T) == 2 && D == 128) {
+          if (ge.fp8) {
+            store_fp8<kLanes>(p, page, slot, hh, which - 1, c0, c1, b0, b1, lane == 0);
+            continue;
+          }
         }
+        *reinterpret_cast<uint4*>(p.pool + kv_chunk_offset(ge, page, hh, which - 1, slot, c0)) = b0;
+        *reinterpret_cast<uint4*>(p.pool + kv_chunk_offset(ge, page, hh, which - 1, slot, c1)) = b1;
       }
-      *reinterpret_cast<uint4*>(p.pool + kv_chunk_offset(ge, page, hh, which - 1, slot, c0)) = b0;
-      *reinterpret_cast<uint4*>(p.pool + kv_chunk_offset(ge, page, hh, which - 1, slot, c1)) = b1;
     }
   }
 }
