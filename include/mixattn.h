@@ -279,14 +279,16 @@ int mixattn_decode_layers(mixattn_ctx* ctx, int32_t layer_begin, int32_t layer_e
  * common prefixes in the block tables, whatever the order of seq_ids; nothing has to be declared.
  * Arguments, results and errors are those of mixattn_decode, and so is the computation apart from
  * the order in which partial results are added (kept to the same precision).  A sequence may be listed more
- * than once.  Layers with a sliding window (rings are never shared) and calls without a common prefix of at
- * least MIXATTN_MIN_SHARED_TOKENS tokens run as mixattn_decode, with its bits. */
+ * than once.  Layers with a sliding window (rings are never shared), calls without a common prefix of at
+ * least MIXATTN_MIN_SHARED_TOKENS tokens, and q or out that are not 16-byte aligned run as mixattn_decode, with
+ * its bits.  (The contents behind a sequence's last token do not matter, here for plain scores too; its own keys
+ * and values have to be finite.) */
 #define MIXATTN_MIN_SHARED_TOKENS 128
 int mixattn_decode_shared(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32_t* seq_ids,
                           const void* q, void* out, void* stream);
 
 /* Makes mixattn_decode and mixattn_decode_layers take the path of mixattn_decode_shared (enable != 0)
- * or not (0, as at first).  Errors: INVALID_ARG for a null context. */
+ * or not (0, as at first); mixattn_decode_static_scratch never does.  Errors: INVALID_ARG for a null context. */
 int mixattn_set_prefix_sharing(mixattn_ctx* ctx, int32_t enable);
 
 /* Cached tokens of `layer` that a mixattn_decode_shared of these sequences reads (a token that

@@ -394,7 +394,8 @@ class Context:
         if t is None:
             return None, 0
         d = self.head_dim
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or t.dtype is not self._like.dtype or t.get_device() != self._device:
+        shape = t.shape
+        if len(shape) != 3 or shape[1] != heads or shape[2] != d or t.dtype is not self._like.dtype or t.get_device() != self._device:
             return None
         a, b, c = t.stride()
         if c != 1 or (heads > 1 and b != d):
@@ -426,14 +427,13 @@ class Context:
             if rc:
                 raise MixAttnError(rc, "mixattn_rope_qkv")
             return None, None, None
-        tokens = m if n is None else sum(n[:m])
+        tokens = m if n is None else sum(n_new) if type(n_new) is list else sum(n[:m])
         hq, hkv, d = self.n_q_heads, self.n_kv_heads, self.head_dim
         rq, rk, rv = self._rows(q, hq), self._rows(k, hkv), self._rows(v, hkv)
         if rq is None or rk is None or rv is None:
             refuse()
-        for t in (q, k, v):
-            if t is not None and t.shape[0] != tokens:
-                refuse()
+        if (q is not None and q.shape[0] != tokens) or (k is not None and k.shape[0] != tokens) or (v is not None and v.shape[0] != tokens):
+            refuse()
         stream = _stream(stream)
         outs = [None, None, None]
         if out is True:

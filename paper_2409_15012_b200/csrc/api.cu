@@ -852,7 +852,7 @@ static cudaError_t launch_split_pass(const mixattn_ctx* c, const ShapedDecodePar
 }
 
 // Splits of a shared decode's own keys: about four items for each of the launch's CTAs, which evens out
-// lengths from a few tokens to thousands (64 sequences of 16 to 2048 own tokens: WAS us with splits of 2048).
+// lengths from a few tokens to thousands (64 sequences of 16 to 2048 own tokens behind 32k: 79 us with splits of 2048, 77).
 static int64_t own_split(const mixattn_ctx* c, int64_t total, const DecodeParams* p) {
   if (c->split_tokens > 0) return (c->split_tokens + kPage - 1) / kPage * kPage;
   const int64_t t = total * c->cfg.n_kv_heads * p->head_chunks / (4 * (int64_t)p->partial);
@@ -980,7 +980,7 @@ static int decode_plain(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int
 // parts for at most max_ctas CTAs, fewer if the partial results would not fit `room` rows.  Items whose rows
 // make several chunks read the same keys: where they are long, each begins with a CTA of its own, so that all
 // chunks get to a key at about the same time and it comes from HBM once (128k keys, 64 sequences x 4 heads:
-// WAS -> NOW us).  With `leaves` the pieces of a single sequence are left to the split pass.  Returns false if
+// 229 -> 198 us).  With `leaves` the pieces of a single sequence are left to the split pass.  Returns false if
 // it does not fit at all.
 static bool lay_out_shared(const ShareTree& t, bool leaves, int max_ctas, int64_t room, SharedDecodeParams* p, int* n_leaves) {
   const int Hkv = p->geom.n_kv_heads;
@@ -1105,7 +1105,10 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
   for (int i = 0; i < n_seqs; ++i)
     if (c->cm.len(layer, seq_ids[i]) < 1) return MIXATTN_ERR_EMPTY_CONTEXT;
   if (c->host_only || c->sticky_cuda_error) return MIXATTN_ERR_CUDA;
-  if (n_seqs < 2 || c->cm.layer(layer).kind == MIXATTN_SLIDING) return decode_plain(c, layer, n_seqs, seq_ids, q, out, stream);
+  // (nothing to share, or tensors that the wide accesses of these kernels cannot take)
+  const bool tc = c->cfg.dtype == MIXATTN_BF16;
+  if (n_seqs < 2 || c->cm.layer(layer).kind == MIXATTN_SLIDING || (((size_t)q | (size_t)out) & 15) != 0 || (tc && !shared_tc_supported(c->geom)))
+    return decode_plain(c, layer, n_seqs, seq_ids, q, out, stream);
   DeviceGuard g(c->device);
   if (!g.ok) return MIXATTN_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -1127,7 +1130,6 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
     p.split_ml = reinterpret_cast<float2*>(c->arena + c->plan.part_ml_off);
     p.status = c->dev_status();
     p.shaped = score_shape_of(c, layer, &p.shape) ? 1 : 0;
-    const bool tc = shared_tc_supported(c->geom, q);
     int64_t room;
     if (tc) {
       shared_tc_tiles(&p);

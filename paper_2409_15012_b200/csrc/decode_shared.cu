@@ -1,5 +1,5 @@
-// Decode attention over a tree of shared prefixes: the form for every storage format in exact fp32 arithmetic, and
-// the merge of the partial results.
+// Decode attention over a tree of shared prefixes: the form for fp32 caches, in exact fp32 arithmetic, and the merge
+// of the partial results.  (bf16 and quantised caches: decode_shared_tc.cu.)
 //
 // Section 5.4's kind of workload has many requests behind the same instruction, and generation with
 // several hypotheses many behind the same prompt: their caches share pages, which a decode that goes
@@ -10,7 +10,6 @@
 //     out = sum_c o_c 2^(m_c - M) / sum_c l_c 2^(m_c - M),   M = max_c m_c.
 // How the work is cut is described with SharedDecodeParams (internal.h).
 #include <cuda_bf16.h>
-#include <cuda_fp8.h>
 
 #include "internal.h"
 #include "score_shape.cuh"
@@ -19,33 +18,13 @@ namespace mixattn {
 
 namespace {
 
-// ---------------------------------------------------------------- any storage, fp32 arithmetic
-// 32 rows x 32 keys per step on the CUDA cores; eight threads per row.  Serves the fp32 mode (whose
-// point is exact arithmetic); bf16 caches and quantised ones run on the tensor cores.
+// ---------------------------------------------------------------- fp32 caches
+// 32 rows x 32 keys per step on the CUDA cores; eight threads per row.
 constexpr int kRows = 32, kKeys = 32, kThreads = 256, kPerRow = kThreads / kRows;
 constexpr int kPad = 4;   // floats between rows: eight rows' 16-byte words fall into different banks
 
 template <int D>
 constexpr int simple_smem() { return (2 * kRows * (D + kPad) + kKeys * D + kRows * (kKeys + 1)) * 4; }
-
-// four channels 4 c .. 4 c + 3 of a stored row as fp32
-__device__ __forceinline__ float4 stored4(const char* pool, const KvGeom& ge, int64_t page, int g, int which, int tok, int c) {
-  if (ge.fp8) {
-    const float x = exp2f((float)(*reinterpret_cast<const unsigned char*>(pool + kv_exp_offset(ge, page, g, which, tok))) - 127.f);
-    float f[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int ch = 4 * c + e;
-      const int64_t at = which ? kv_fp8_v_offset(ge, page, g, ch, tok) : kv_chunk_offset(ge, page, g, 0, tok, ch >> 4) + (ch & 15);
-      f[e] = (float)*reinterpret_cast<const __nv_fp8_e4m3*>(pool + at) * x;
-    }
-    return make_float4(f[0], f[1], f[2], f[3]);
-  }
-  if (ge.elem_bytes == 4) return *reinterpret_cast<const float4*>(pool + kv_chunk_offset(ge, page, g, which, tok, c));
-  const uint2 w = *reinterpret_cast<const uint2*>(pool + kv_chunk_offset(ge, page, g, which, tok, c >> 1) + (c & 1) * 8);
-  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
-                     __uint_as_float(w.y & 0xffff0000u));
-}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads) decode_shared_kernel(const __grid_constant__ SharedDecodeParams p) {
@@ -68,12 +47,7 @@ __global__ void __launch_bounds__(kThreads) decode_shared_kernel(const __grid_co
       if (row < s.rows) {
         const int R = s.row_first + row;
         const int64_t at = ((int64_t)p.order[s.s0 + R / p.group] * p.n_q_heads + s.g * p.group + R % p.group) * D + 4 * c;
-        if (ge.elem_bytes == 4) {
-          x = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.q) + at);
-        } else {
-          const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q) + at;
-          x = make_float4(__bfloat162float(q[0]), __bfloat162float(q[1]), __bfloat162float(q[2]), __bfloat162float(q[3]));
-        }
+        x = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.q) + at);
       }
       *reinterpret_cast<float4*>(sq + row * (D + kPad) + 4 * c) = x;
     }
@@ -88,7 +62,8 @@ __global__ void __launch_bounds__(kThreads) decode_shared_kernel(const __grid_co
       for (int e = tid; e < 2 * kKeys * (D / 4); e += kThreads) {
         const int which = e / (kKeys * (D / 4)), f = e - which * kKeys * (D / 4), key = f / (D / 4), c = f - key * (D / 4);
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);   // (what lies behind the last key is not read)
-        if (t + key < s.t1) x = stored4(p.pool, ge, tbl[(t + key) / kPage], s.g, which, (t + key) % kPage, c);
+        if (t + key < s.t1)
+          x = *reinterpret_cast<const float4*>(p.pool + kv_chunk_offset(ge, tbl[(t + key) / kPage], s.g, which, (t + key) % kPage, c));
         *reinterpret_cast<float4*>(which ? sv + key * D + 4 * c : sk + key * (D + kPad) + 4 * c) = x;
       }
       __syncthreads();

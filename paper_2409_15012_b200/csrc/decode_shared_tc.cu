@@ -421,7 +421,9 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
         float fk = 0.f, xv = 0.f, gv = 0.f;   // (keys that are not there are masked)
         if (n < left) {
           fk = __int_as_float((int)xs[0] << 23) * fold;           // 2^(byte - 127); byte 0 is a vector of zeros,
-          const int e = xs[kPage] == 0 ? -100 : (int)xs[kPage] - 127;   // which in V may have any exponent
+          // which in V may have any exponent: low enough not to be the reference, high enough that its weight, which
+          // the row's sum takes, is not flushed to zero beside exponents of up to 14 (that happens 126 below)
+          const int e = xs[kPage] == 0 ? -60 : (int)xs[kPage] - 127;
           xv = (float)e;
           gv = __int_as_float(min(127 - e, 254) << 23);
         }
@@ -787,9 +789,7 @@ cudaError_t prepare() {
 
 }  // namespace
 
-bool shared_tc_supported(const KvGeom& ge, const void* q) {
-  return ge.elem_bytes == 2 && ((size_t)q & 15) == 0 && (ge.fp8 || encode_fn() != nullptr);
-}
+bool shared_tc_supported(const KvGeom& ge) { return ge.elem_bytes == 2 && (ge.fp8 || encode_fn() != nullptr); }
 
 void shared_tc_tiles(SharedDecodeParams* p) {
   p->tile_keys = kTile;

@@ -430,8 +430,8 @@ cudaError_t launch_decode_split_bf16(const DecodeParams& p, const ShapedDecodePa
 cudaError_t launch_decode_split_f32(const DecodeParams& p, const ShapedDecodeParams* shaped, cudaStream_t st);
 cudaError_t launch_decode_combine(const DecodeParams& p, int dtype, cudaStream_t st);
 cudaError_t prepare_decode_shared();
-cudaError_t launch_decode_shared(const SharedDecodeParams& p, cudaStream_t st);         // any storage, exact fp32 arithmetic
-bool shared_tc_supported(const KvGeom& ge, const void* q);      // on the tensor cores: bf16 caches
+cudaError_t launch_decode_shared(const SharedDecodeParams& p, cudaStream_t st);         // fp32 caches
+bool shared_tc_supported(const KvGeom& ge);                     // on the tensor cores: bf16 and quantised caches
 void shared_tc_tiles(SharedDecodeParams* p);
 cudaError_t prepare_decode_shared_tc();
 cudaError_t launch_decode_shared_tc(const SharedDecodeParams& p, cudaStream_t st);

@@ -368,3 +368,68 @@ def test_refusals():
     assert tree.ctx.rc_decode_shared(1, [], q, out) == 0
     torch.cuda.synchronize()
     assert bool((out == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "f32"])
+def test_unaligned_tensors_give_the_bits_of_decode(dtype):
+    tree = Tree((8, 2, 128), dtype, 5, 300, 2000)
+    seqs = grow(tree, 1, 4, 600, 0, [9, 40])
+    step = 2 if dtype != "f32" else 1         # elements: 4 bytes
+    n = 4 * 8 * 128
+    spare = [torch.zeros(n + 8, device="cuda", dtype=tree.t) for _ in range(3)]
+    q = tree.queries(4)
+    odd_q, odd_out = (s[step:step + n].view(4, 8, 128) for s in spare[:2])
+    odd_q.copy_(q)
+    plain = torch.empty_like(q)
+    tree.ctx.decode(1, seqs, q, plain)
+    if dtype != "fp8":                        # (a quantised cache's decode takes queries of 8-byte alignment)
+        out = torch.empty_like(q)
+        tree.ctx.decode_shared(1, seqs, odd_q, out)
+        assert torch.equal(bits(out), bits(plain))
+    tree.ctx.decode_shared(1, seqs, q, odd_out)
+    assert torch.equal(bits(odd_out), bits(plain))
+    assert bool((spare[1][:step] == 0).all()) and bool((spare[1][step + n:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("cap,bias", [(0.0, False), (0.0, True), (30.0, True)])
+def test_own_keys_of_every_length(dtype, cap, bias):
+    """Lengths on both sides of pages, tiles and splits next to each other: the shares of the two kernels, the
+    order of the items and the merge."""
+    tree = Tree((32, 8, 128), dtype, 25, 6000, 9000, seed=3)
+    tails = [0, 1, 5000, 15, 16, 17, 63, 64, 65, 127, 128, 129, 511, 512, 513, 1023, 1025, 2, 3, 2049, 30, 700, 1, 4097]
+    seqs = grow(tree, 1, 24, 3000, 0, tails)
+    tree.shape(cap, bias)
+    tree.check(seqs)
+    tree.ctx.set_split_tokens(64)
+    tree.check(seqs)
+    tree.ctx.set_split_tokens(0)
+
+
+def test_magnitudes_that_differ_between_tokens():
+    """A quantised cache's values of 2^-20 to 2^18 beside vectors of zeros: weights are rounded relative to what
+    their keys contribute: 2^-11 of A, and 2^-24 of the largest contribution for each key (half the fp16 subnormal
+    step, 2^-25, times an element of 448 at most where the largest one's is 256 at least).  The last twelve
+    tokens, in pages of their own, are the ordinary split pass's: half that step times 448 each."""
+    tree = Tree((8, 2, 128), "fp8", 5, 200, 1200)
+    gen = torch.Generator("cuda").manual_seed(9)
+    k = on_e4m3(torch.randn(700, 2, 128, generator=gen, device="cuda").bfloat16())
+    size = torch.exp2(torch.randint(-20, 19, (700, 2, 1), generator=gen, device="cuda").float())
+    size[::5] = 0.0
+    v = on_e4m3((torch.randn(700, 2, 128, generator=gen, device="cuda") * size).bfloat16())
+    tree.ctx.append_kv(0, [4], [700], k, v)
+    tree.kv[4] = [k, v]
+    tree.fork([4] * 4, [0, 1, 2, 3])
+    q = tree.queries(4, sharp=1.0)
+    out = torch.empty_like(q)
+    tree.ctx.decode_shared(1, [0, 1, 2, 3], q, out)
+    want, A, top = tree.expect([0, 1, 2, 3], q)
+    largest = torch.zeros_like(want)
+    for i in range(4):
+        p = torch.softmax(torch.einsum("gcd,ngd->gcn", q[i].double().view(2, -1, 128), k.double()) / math.sqrt(128), -1)
+        largest[i] = (p * v.double().abs().amax(-1).T[:, None]).amax(-1).reshape(8, 1)
+    # the output's rounding: half a step of bf16, whose eps is 2^-7 (8 significant bits), so 2^-8 of the value
+    half_step = torch.finfo(torch.bfloat16).eps / 2
+    bound = half_step * want.abs() * 1.001 + (2.0 ** -11 + 2.0 ** -24 * top * 48 * 1.4 + 2.0 ** -16) * A + 700 * 2.0 ** -24 * largest + 12 * 2.0 ** -25 * 448
+    assert ((out.double() - want).abs() <= bound).all()
+    assert tree.ctx.get_device_status() == 0
