@@ -138,10 +138,10 @@ def _load() -> C.CDLL:
         "mixattn_get_stored": [vp, i32, i32, p32, p32],
         "mixattn_read_kv": [vp, i32, i32, p32, p32, p32, vp, vp, vp],
         "mixattn_beam_select": [vp, i32, i32, i32, i32, vp, C.c_int64, vp, vp, i32, i32, vp, vp, vp, vp],
-        "mixattn_decode_shared": [vp, i32, i32, p32, vp, vp, vp],
+        "mixattn_decode_shared": [vp, i32, i32, vp, vp, vp, vp],
         "mixattn_set_prefix_sharing": [vp, i32],
         "mixattn_get_distinct_tokens": [vp, i32, i32, p32, C.POINTER(C.c_int64)],
-        "mixattn_rope_qkv": [vp, i32, i32, p32, p32, p32, C.POINTER(RopeDesc), vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, i32,
+        "mixattn_rope_qkv": [vp, i32, i32, vp, vp, vp, C.POINTER(RopeDesc), vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, i32,
                              vp, vp, vp, vp],
         "mixattn_adjust_logits": [vp, i32, i32, i32, vp, C.c_int64, i32, vp, C.c_int64, C.POINTER(LogitRules), vp],
         "mixattn_set_split_tokens": [vp, i32],
@@ -225,6 +225,20 @@ def _ints(a):
             raise MixAttnError(ERR_INVALID_ARG, "sequence of integers")
     n = len(b)
     return ((C.c_int32 * n).from_buffer(b) if n else (C.c_int32 * 1)()), n
+
+
+def _ints_at(a):
+    """(address, length, owner of the memory) of a host sequence of whole numbers, for the calls that take addresses."""
+    if type(a) is list:
+        try:
+            b = array("i", a)
+        except TypeError:
+            pass
+        else:
+            at, n = b.buffer_info()
+            return at, n, b
+    b, n = _ints(a)
+    return C.addressof(b), n, b
 
 
 def _dev(t) -> Optional[int]:
@@ -364,7 +378,7 @@ class Context:
                                                  _stream(stream))
 
     def rc_decode_shared(self, layer, seq_ids, q, out, stream=None) -> int:
-        s, n = _ints(seq_ids)
+        s, n, _own = _ints_at(seq_ids)
         return lib.mixattn_decode_shared(self.h, layer, n, s, _dev(q), _dev(out), _stream(stream))
 
     def decode_shared(self, layer, seq_ids, q, out, stream=None):
@@ -410,14 +424,16 @@ class Context:
         The new tensors belong to `stream` (default: the default stream)."""
         def refuse():
             raise MixAttnError(ERR_INVALID_ARG, "mixattn_rope_qkv")
-        s, m = _ints(seq_ids)
+        s, m, _own_s = _ints_at(seq_ids)
         n = p = None
+        tokens = m
         if n_new is not None:
-            n, mn = _ints(n_new)
+            n, mn, _own_n = _ints_at(n_new)
             if mn != m:
                 refuse()
+            tokens = sum(_own_n[:mn])
         if first_pos is not None:
-            p, mp = _ints(first_pos)
+            p, mp, _own_p = _ints_at(first_pos)
             if mp != m:
                 refuse()
         if self._like is None:
@@ -427,7 +443,6 @@ class Context:
             if rc:
                 raise MixAttnError(rc, "mixattn_rope_qkv")
             return None, None, None
-        tokens = m if n is None else sum(n_new) if type(n_new) is list else sum(n[:m])
         hq, hkv, d = self.n_q_heads, self.n_kv_heads, self.head_dim
         rq, rk, rv = self._rows(q, hq), self._rows(k, hkv), self._rows(v, hkv)
         if rq is None or rk is None or rv is None:

@@ -478,21 +478,25 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
       return true;
     };
     int G = 0, H = 0;   // quantised: tiles and raw stages so far
+    auto convert_tiles = [&](const ShareSegment& q, int from, int to) {
+      bool fine = true;
+      const int n_tiles = tiles_of(q);
+      for (int j = from; fine && j < min(to, n_tiles); ++j, ++G) {
+        const int t = tile_key(q, j, n_tiles);
+        fine = convert(q, t, G, H);
+        H += q.t1 - t > 64 ? 2 : 1;
+      }
+      return fine;
+    };
     bool more = share_next(p, blockIdx.x, walk, s), ok = true;
     if (more) ok = put_q(s, 0);
+    if (kFp8 && more && ok) ok = convert_tiles(s, 0, 1);
     for (int it = 0; ok && more; ++it) {
       const ShareSegment now = s;
-      if constexpr (kFp8) {
-        const int n_tiles = tiles_of(now);
-        for (int j = 0; ok && j < n_tiles; ++j, ++G) {
-          const int t = tile_key(now, j, n_tiles);
-          ok = convert(now, t, G, H);
-          H += now.t1 - t > 64 ? 2 : 1;
-        }
-        if (!ok) break;
-      }
+      if (kFp8 && !convert_tiles(now, 1, INT32_MAX)) { ok = false; break; }
       more = share_next(p, blockIdx.x, walk, s);
-      if (more) ok = put_q(s, it + 1);
+      // (the next segment's first tile before this one's results: its scores can start under them)
+      if (more) ok = put_q(s, it + 1) && (!kFp8 || convert_tiles(s, 0, 1));
       if (!ok) break;
       ok = __all_sync(0xffffffffu, mbar_wait(BAR(B_XC), it & 1, abort_flag));
       if (!ok) break;
