@@ -280,10 +280,13 @@ int mixattn_decode_layers(mixattn_ctx* ctx, int32_t layer_begin, int32_t layer_e
  * Arguments, results and errors are those of mixattn_decode, and so is the computation apart from
  * the order in which partial results are added (kept to the same precision).  A sequence may be listed more
  * than once.  Layers with a sliding window (rings are never shared), calls without a common prefix of at
- * least MIXATTN_MIN_SHARED_TOKENS tokens, and q or out that are not 16-byte aligned run as mixattn_decode, with
- * its bits.  (The contents behind a sequence's last token do not matter, here for plain scores too; its own keys
- * and values have to be finite.) */
+ * least MIXATTN_MIN_SHARED_TOKENS tokens or (bf16) with less than MIXATTN_MIN_SAVED_BYTES to save, and q or
+ * out that are not 16-byte aligned run as mixattn_decode, with its bits.  (Where prefixes are shared, the contents
+ * behind a sequence's last token do not matter, for plain scores too; its own keys and values have to be
+ * finite.) */
 #define MIXATTN_MIN_SHARED_TOKENS 128
+#define MIXATTN_MIN_SAVED_BYTES 56000000 /* keys and values read once instead of several times; see
+                                            mixattn_set_share_min_bytes */
 int mixattn_decode_shared(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32_t* seq_ids,
                           const void* q, void* out, void* stream);
 
@@ -291,9 +294,9 @@ int mixattn_decode_shared(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const
  * or not (0, as at first); mixattn_decode_static_scratch never does.  Errors: INVALID_ARG for a null context. */
 int mixattn_set_prefix_sharing(mixattn_ctx* ctx, int32_t enable);
 
-/* Cached tokens of `layer` that a mixattn_decode_shared of these sequences reads (a token that
- * several sequences read at once counts once); mixattn_decode reads the sum of their lengths (of what their
- * windows hold).  Errors: INVALID_ARG, BAD_SEQ. */
+/* Cached tokens of `layer` that a mixattn_decode_shared of these sequences reads where it shares prefixes (a
+ * token that several sequences read at once counts once); mixattn_decode reads the sum of their lengths (of what
+ * their windows hold).  Errors: INVALID_ARG, BAD_SEQ. */
 int mixattn_get_distinct_tokens(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32_t* seq_ids,
                                 int64_t* tokens);
 
@@ -580,6 +583,10 @@ int mixattn_get_device_status(mixattn_ctx* ctx, int32_t* status);
 /* Target number of keys per split of the split-KV decode; 0 = automatic.
  * Results do not depend on it beyond fp32 summation order. */
 int mixattn_set_split_tokens(mixattn_ctx* ctx, int32_t tokens);
+
+/* Bytes of keys and values that a shared decode on a bf16 context has to save to be worth its second and third
+ * launch; < 0 = automatic (MIXATTN_MIN_SAVED_BYTES), 0 = always.  Errors: INVALID_ARG for a null context. */
+int mixattn_set_share_min_bytes(mixattn_ctx* ctx, int64_t bytes);
 
 /* Kernel classes for mixattn_profile_read. */
 enum {

@@ -31,7 +31,7 @@ ERR_TOO_LARGE = -9
 
 K_APPEND, K_DECODE_FULL, K_DECODE_SLIDING, K_COMBINE, K_PREFILL_FULL, K_PREFILL_SLIDING, K_GATHER, K_FORK, K_READ, K_SELECT = range(10)
 K_SHARED, K_MERGE, K_ROPE, K_ADJUST = range(10, 14)
-MIN_SHARED_TOKENS = 128
+MIN_SHARED_TOKENS, MIN_SAVED_BYTES = 128, 56000000
 MAX_RULE_TOKENS, MAX_RULE_BIASES = (1 << 20) - 1, 2047
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmixattn.so")
@@ -140,6 +140,7 @@ def _load() -> C.CDLL:
         "mixattn_beam_select": [vp, i32, i32, i32, i32, vp, C.c_int64, vp, vp, i32, i32, vp, vp, vp, vp],
         "mixattn_decode_shared": [vp, i32, i32, vp, vp, vp, vp],
         "mixattn_set_prefix_sharing": [vp, i32],
+        "mixattn_set_share_min_bytes": [vp, C.c_int64],
         "mixattn_get_distinct_tokens": [vp, i32, i32, p32, C.POINTER(C.c_int64)],
         "mixattn_rope_qkv": [vp, i32, i32, vp, vp, vp, C.POINTER(RopeDesc), vp, C.c_int64, vp, C.c_int64, vp, C.c_int64, i32,
                              vp, vp, vp, vp],
@@ -165,7 +166,7 @@ EXPORTS = [
     "mixattn_arena_bytes", "mixattn_cache_bytes", "mixattn_create", "mixattn_destroy",
     "mixattn_seq_reset", "mixattn_append_kv", "mixattn_append_kv_rope", "mixattn_decode", "mixattn_decode_static_scratch", "mixattn_decode_layers", "mixattn_prefill",
     "mixattn_attend_chunk", "mixattn_set_layer_scores", "mixattn_fork_seqs", "mixattn_read_kv", "mixattn_beam_select",
-    "mixattn_decode_shared", "mixattn_set_prefix_sharing", "mixattn_get_distinct_tokens", "mixattn_rope_qkv", "mixattn_adjust_logits",
+    "mixattn_decode_shared", "mixattn_set_prefix_sharing", "mixattn_set_share_min_bytes", "mixattn_get_distinct_tokens", "mixattn_rope_qkv", "mixattn_adjust_logits",
     "mixattn_get_stored",
     "mixattn_get_len", "mixattn_get_block_table", "mixattn_get_n_free_pages",
     "mixattn_get_ring_state", "mixattn_locate", "mixattn_debug_read_kv", "mixattn_debug_read_kv_fp8",
@@ -393,8 +394,14 @@ class Context:
         if rc:
             raise MixAttnError(rc, "mixattn_set_prefix_sharing")
 
+    def set_share_min_bytes(self, nbytes: int):
+        """Bytes of keys and values that a shared decode has to save (bf16 contexts); < 0 = automatic, 0 = always."""
+        rc = lib.mixattn_set_share_min_bytes(self.h, int(nbytes))
+        if rc:
+            raise MixAttnError(rc, "mixattn_set_share_min_bytes")
+
     def get_distinct_tokens(self, layer, seq_ids) -> int:
-        """Cached tokens that a decode_shared() of these sequences reads."""
+        """Cached tokens that a decode_shared() of these sequences reads where it shares prefixes."""
         s, n = _ints(seq_ids)
         out = C.c_int64()
         rc = lib.mixattn_get_distinct_tokens(self.h, layer, n, s, C.byref(out))

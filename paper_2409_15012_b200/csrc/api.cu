@@ -123,6 +123,7 @@ struct mixattn_ctx {
   // cached keys in place from the ring (no copy); off = every chunk call copies.
   bool chunk_ring_direct = true;
   bool prefix_sharing = false;   // decode calls go the way of mixattn_decode_shared
+  int64_t share_min_bytes = -1;  // what such a call has to save; < 0 = automatic
   uint64_t cache_epoch = 0;   // bumped by every call that changes a cache
   struct GatherKey {
     bool valid = false;
@@ -1178,6 +1179,17 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
       for (int32_t least = MIXATTN_MIN_SHARED_TOKENS; !fits; least *= 2) {   // (deep trees of short pieces: only the longer ones)
         build_share_tree(c->cm, layer, nb, ids, least, &tree);
         if (!tree.shared) break;
+        // Worth it?  The two launches more cost 6 to 9 us, as long as it takes to read some 60 MB.  As measured,
+        // shared / plain, with what is saved: 2 sequences behind 16k tokens of 8 heads x 128 (67 MB) 22.6 / 21.3 us, 4 behind
+        // 4k (50 MB) 15.4 / 14.5, 16 behind 1k (63 MB) 15.0 / 11.5, behind 4k (252 MB) 17.3 / 37; 16 behind 4k
+        // of 4 heads x 64 (63 MB) 13.3 / 20.6; quantised, 4 behind 4k (25 MB) 16.5 / 12.4, behind 16k (101 MB)
+        // 31 / 41.  (fp32: always, 14.5 / 28.8 at 200 tokens of 2 sequences.)
+        if (tc) {
+          int64_t apart = 0;
+          for (int j = 0; j < nb; ++j) apart += c->cm.len(layer, ids[j]);
+          const int64_t saved = (apart - tree.tokens) * (c->geom.page_bytes / kPage);
+          if (saved < (c->share_min_bytes < 0 ? MIXATTN_MIN_SAVED_BYTES : c->share_min_bytes)) break;
+        }
         const int own_ctas = tc ? own_key_ctas(tree, p, d, c->sm_count) : 0;
         d.partial = own_ctas;
         fits = lay_out_shared(tree, tc, tc ? c->sm_count - own_ctas : 2 * c->sm_count, room, &p, &n_leaves);
@@ -1231,6 +1243,12 @@ int mixattn_decode_shared(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const i
 int mixattn_set_prefix_sharing(mixattn_ctx* c, int32_t enable) {
   if (c == nullptr) return MIXATTN_ERR_INVALID_ARG;
   c->prefix_sharing = enable != 0;
+  return MIXATTN_OK;
+}
+
+int mixattn_set_share_min_bytes(mixattn_ctx* c, int64_t bytes) {
+  if (c == nullptr) return MIXATTN_ERR_INVALID_ARG;
+  c->share_min_bytes = bytes;
   return MIXATTN_OK;
 }
 

@@ -41,6 +41,7 @@ class Tree:
         self.ctx = mx.Context(layout or [(mx.FULL, 0, 0), (mx.FULL, 0, 0)], *heads, mx.F32 if dtype == "f32" else mx.BF16, seqs, pages,
                               max_seq_len=longest, device=0, kv_format=mx.KV_FP8_E4M3 if dtype == "fp8" else mx.KV_NATIVE,
                               chunk_scratch_tokens=chunk)
+        self.ctx.set_share_min_bytes(0)      # (small trees too)
         self.gen = torch.Generator("cuda").manual_seed(seed)
         self.t = torch.float32 if dtype == "f32" else torch.bfloat16
         self.kv = {}
@@ -246,6 +247,27 @@ def test_without_shared_prefixes_the_bits_of_decode(dtype):
     tree.ctx.decode(1, [2], q, a)
     tree.ctx.decode_shared(1, [2], q, b)
     assert torch.equal(bits(a), bits(b))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+def test_little_to_save_gives_the_bits_of_decode(dtype):
+    """On both sides of the least that is worth sharing."""
+    mx, _ = load_lib()
+    tree = Tree((8, 2, 128), dtype, 5, 300, 2000)
+    seqs = grow(tree, 1, 4, 600, 0, [9])
+    token = 2 * 2 * 129 if dtype == "fp8" else 2 * 2 * 128 * 2
+    saved = 3 * (600 // 16 * 16) * token
+    assert saved < mx.MIN_SAVED_BYTES
+    q = tree.queries(4)
+    plain, out = torch.empty_like(q), torch.empty_like(q)
+    tree.ctx.decode(1, seqs, q, plain)
+    for least, same in ((-1, True), (saved + 1, True), (saved, False), (0, False)):
+        tree.ctx.set_share_min_bytes(least)
+        before = tree.ctx.get_launch_count()
+        tree.ctx.decode_shared(1, seqs, q, out)
+        assert (tree.ctx.get_launch_count() - before == 3) == (not same)
+        assert not same or torch.equal(bits(out), bits(plain))
+        tree.compare(seqs, q, out)
 
 
 def test_switch_for_decode_and_decode_layers():

@@ -33,6 +33,7 @@ def test_generation_with_several_hypotheses(fp8):
     n = groups * beams
     ctx = mx.Context(layout, hq, hkv, d, mx.BF16, n, 400, max_seq_len=600, device=0, kv_format=mx.KV_FP8_E4M3 if fp8 else mx.KV_NATIVE)
     ctx.set_prefix_sharing(True)
+    ctx.set_share_min_bytes(0)
     gen = torch.Generator("cuda").manual_seed(11)
 
     def normal(*shape):
@@ -136,6 +137,7 @@ def test_two_contexts_on_two_streams():
         gen = torch.Generator("cuda").manual_seed(seed)
         ctx = mx.Context([(mx.FULL, 0, 0)], 16, 4, 128, mx.BF16, 17, 900, max_seq_len=6000, device=0)
         kv = [torch.randn(5000, 4, 128, generator=gen, device="cuda").bfloat16() for _ in range(2)]
+        ctx.set_share_min_bytes(0)
         ctx.append_kv(0, [16], [5000], *kv)
         ctx.fork_seqs([16] * 16, list(range(16)))
         for s in range(16):
@@ -159,6 +161,7 @@ def test_captured_step():
     gen = torch.Generator("cuda").manual_seed(3)
     ctx = mx.Context([(mx.FULL, 0, 0), (mx.FULL, 0, 0)], 8, 2, 64, mx.BF16, 5, 200, max_seq_len=1000, device=0)
     kv = [torch.randn(600, 2, 64, generator=gen, device="cuda").bfloat16() for _ in range(2)]
+    ctx.set_share_min_bytes(0)
     ctx.append_kv(0, [4], [600], *kv)
     ctx.fork_seqs([4] * 4, [0, 1, 2, 3])
     for s in range(4):
@@ -200,6 +203,7 @@ def test_profile_classes():
     mx, _ = load_lib()
     ctx = mx.Context([(mx.FULL, 0, 0)], 8, 2, 128, mx.BF16, 3, 100, max_seq_len=500, device=0)
     ctx.profile_enable(True)
+    ctx.set_share_min_bytes(0)
     rows = torch.randn(300, 12, 128, device="cuda").bfloat16()
     ctx.rope_qkv(0, [0], [300], mx.Rope(128), k=rows[:, 8:10], v=rows[:, 10:], store=True)
     ctx.fork_seqs([0, 0], [1, 2])

@@ -93,5 +93,6 @@ def test_refusals():
         assert e.value.code == code
     assert mx.lib.mixattn_get_distinct_tokens(ctx.h, 0, 0, None, None) == mx.ERR_INVALID_ARG
     assert mx.lib.mixattn_set_prefix_sharing(None, 1) == mx.ERR_INVALID_ARG
+    assert mx.lib.mixattn_set_share_min_bytes(None, 0) == mx.ERR_INVALID_ARG
     assert ctx.rc_decode_shared(0, [0], None, None) == mx.ERR_INVALID_ARG
     assert mx.lib.mixattn_decode_shared(ctx.h, 0, 0, None, None, None, None) == mx.ERR_CUDA     # a host-only context launches nothing
