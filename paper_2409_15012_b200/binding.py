@@ -99,6 +99,8 @@ class Rope:
             self._freq = np.array(inv_freq, dtype=np.float64)
             if self._freq.shape != (rotary_dim // 2,):
                 raise MixAttnError(ERR_INVALID_ARG, "Rope: one frequency per pair of channels")
+        elif 2 <= rotary_dim <= 1024 and 1.0 < theta < float("inf"):      # (formed once; anything else is the call's to refuse)
+            self._freq = np.float64(theta) ** (-2.0 * np.arange(rotary_dim // 2) / rotary_dim)
         self.desc = RopeDesc(int(rotary_dim), int(bool(halves)), float(theta),
                              None if self._freq is None else self._freq.ctypes.data_as(C.POINTER(C.c_double)), float(scale))
         self.ref = C.byref(self.desc)

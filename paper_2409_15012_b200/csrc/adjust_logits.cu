@@ -5,14 +5,14 @@
 //     b = a - frequency * c - (c > 0 ? presence : 0)
 //     y = (b + bias) / temperature,   -inf where the mask forbids
 // Bound by memory: the logits are read and written once.  What a row has seen is a short list of tokens, what the
-// logits need is a count per token of the vocabulary.  A CTA takes parts of rows (up to 16384 bf16 or 8192
+// logits need is a count per token of the vocabulary.  A CTA takes parts of rows (up to 12288 bf16 or 6144
 // fp32 logits): it asks for the part's logits, 16 bytes by 16 into registers, reads the row's list meanwhile and
 // adds up, in one word per token of the part in shared memory, what is said about the token (whole-number
 // sums: the result does not depend on their order), then adjusts and writes, and clears the words that were not
-// zero for its next part.  512 rows x 131072 bf16 with lists of 100 to 9000 tokens: 119 us.  On the way: a cluster of CTAs per
+// zero for its next part.  512 rows x 131072 bf16 with lists of 100 to 9000 tokens: 102 us.  On the way: a cluster of CTAs per
 // row that shared one reading of the list, through distributed shared memory, 317 against 312; the tokens of the list
-// taken out of the words one by one beside the stream, 286, by warps of their own, 258; quotients instead of
-// products with a reciprocal, 278.
+// taken out of the words one by one beside the stream, 286, by warps of their own, 258, or put adjusted in the
+// words' place by a second reading of the list, 171; quotients instead of products with a reciprocal, 278.
 #include <cuda_bf16.h>
 
 #include "internal.h"
@@ -22,8 +22,8 @@ namespace mixattn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPer = 8;           // 16-byte pieces per thread
-constexpr int kCtasPerSm = 3;     // (the words: 64 KB)
+constexpr int kPer = 6;           // 16-byte pieces per thread
+constexpr int kCtasPerSm = 4;     // (the words: 48 KB; with 8 pieces per thread and three CTAs 117 us, with 4 and four 124)
 // a token's word: times it was generated | occurs in the prompt | 1 + its place in the list of biases
 constexpr uint32_t kCountMask = (1u << 20) - 1, kPromptBit = 1u << 20;
 constexpr int kBiasShift = 21;
