@@ -87,9 +87,9 @@ __device__ __forceinline__ void store_fp8(const RopeParams& p, int64_t page, int
   if (leader) *reinterpret_cast<unsigned char*>(p.pool + kv_exp_offset(ge, page, g, which, slot)) = (unsigned char)(X + 127);
 }
 
-// kTokens tokens of a sequence per block
-template <typename T, int D, int kTokens>
-__global__ void __launch_bounds__(kThreads) rope_qkv_kernel(const __grid_constant__ RopeParams p) {
+// kTokens tokens of a sequence per block.  kFp8: what is stored is quantised
+template <typename T, int D, int kTokens, bool kFp8>
+__global__ void __launch_bounds__(kThreads, 4) rope_qkv_kernel(const __grid_constant__ RopeParams p) {
   constexpr int E = Chunk<T>::N;             // channels per chunk
   constexpr int kLanes = D / E / 2;          // threads per head vector, two chunks each
   constexpr int kGroups = kThreads / (kLanes * kTokens);   // heads in flight per token
@@ -114,17 +114,16 @@ __global__ void __launch_bounds__(kThreads) rope_qkv_kernel(const __grid_constan
     const char* src = h < nq ? p.q + row * p.q_stride : h < nq + nk ? p.k + row * p.k_stride : p.v + row * p.v_stride;
     return src + (int64_t)(h < nq ? h : h < nq + nk ? h - nq : h - nq - nk) * ge.row_bytes;
   };
-  // Rows are asked for kAhead heads before they are needed, the first ones before the sines are formed.
-  constexpr int kAhead = 2;
-  uint4 ahead[kAhead][2];
-  auto fetch = [&](int h, uint4 (&to)[2]) {
+  // A row is asked for one head before it is needed, the first one before the sines are formed; more rows under way
+  // take registers, and with them blocks, away (8192 rows: none ahead 54 us, one 40, two 46 with two or three blocks per SM).
+  uint4 ahead[2];
+  auto fetch = [&](int h) {
     if (h >= heads) return;
     const char* src = source(h);
-    to[0] = *reinterpret_cast<const uint4*>(src + c0 * 16);
-    to[1] = *reinterpret_cast<const uint4*>(src + c1 * 16);
+    ahead[0] = __ldcs(reinterpret_cast<const uint4*>(src + c0 * 16));   // (read once)
+    ahead[1] = __ldcs(reinterpret_cast<const uint4*>(src + c1 * 16));
   };
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i) fetch(grp + i * kGroups, ahead[i]);
+  fetch(grp);
   for (int i = threadIdx.x; i < n_tok * pairs; i += kThreads) {
     const int x = i / pairs, pr = i - x * pairs;
     double a = (double)(en.pos0 + tok0 + x) * p.freq[pr];
@@ -159,59 +158,52 @@ __global__ void __launch_bounds__(kThreads) rope_qkv_kernel(const __grid_constan
       slot = pos % kPage;
     }
   }
-  for (int h0 = grp; h0 < heads; h0 += kAhead * kGroups) {
+  for (int h = grp; h < heads; h += kGroups) {   // (whole head vectors: the lanes that shuffle stay together)
+    uint4 b0 = ahead[0], b1 = ahead[1];
+    fetch(h + kGroups);
+    const int which = h < nq ? 0 : h < nq + nk ? 1 : 2, hh = which == 0 ? h : which == 1 ? h - nq : h - nq - nk;
+    if (rotates && which != 2) {
+      Chunk<T> a, b;
+      widen(a, b0);
+      widen(b, b1);
+      if (split) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int h = h0 + j * kGroups;
-      if (h >= heads) break;                 // (whole head vectors: the lanes that shuffle stay together)
-      uint4 b0 = ahead[j][0], b1 = ahead[j][1];
-      fetch(h + kAhead * kGroups, ahead[j]);
-      const int which = h < nq ? 0 : h < nq + nk ? 1 : 2, hh = which == 0 ? h : which == 1 ? h - nq : h - nq - nk;
-      if (rotates && which != 2) {
-        Chunk<T> a, b;
-        widen(a, b0);
-        widen(b, b1);
-        if (split) {
-#pragma unroll
-          for (int i = 0; i < E; ++i) {
-            const float x = a.f[i], y = b.f[i];
-            a.f[i] = x * cs[i] - y * sn[i];
-            b.f[i] = x * sn[i] + y * cs[i];
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < E; ++i) {
-            float& fx = i < E / 2 ? a.f[2 * i] : b.f[2 * i - E];
-            float& fy = i < E / 2 ? a.f[2 * i + 1] : b.f[2 * i - E + 1];
-            const float x = fx, y = fy;
-            fx = x * cs[i] - y * sn[i];
-            fy = x * sn[i] + y * cs[i];
-          }
+        for (int i = 0; i < E; ++i) {
+          const float x = a.f[i], y = b.f[i];
+          a.f[i] = x * cs[i] - y * sn[i];
+          b.f[i] = x * sn[i] + y * cs[i];
         }
-        b0 = bits_of(a);
-        b1 = bits_of(b);
-      }
-      char* out = which == 0 ? p.q_out : which == 1 ? p.k_out : p.v_out;
-      if (out != nullptr) {
-        out += (row * (which == 0 ? p.n_q_heads : ge.n_kv_heads) + hh) * ge.row_bytes;
-        *reinterpret_cast<uint4*>(out + c0 * 16) = b0;
-        *reinterpret_cast<uint4*>(out + c1 * 16) = b1;
-      }
-      if (which != 0 && keep) {
-        if constexpr (sizeof(T) == 2 && D == 128) {
-          if (ge.fp8) {
-            store_fp8<kLanes>(p, page, slot, hh, which - 1, c0, c1, b0, b1, lane == 0);
-            continue;
-          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          float& fx = i < E / 2 ? a.f[2 * i] : b.f[2 * i - E];
+          float& fy = i < E / 2 ? a.f[2 * i + 1] : b.f[2 * i - E + 1];
+          const float x = fx, y = fy;
+          fx = x * cs[i] - y * sn[i];
+          fy = x * sn[i] + y * cs[i];
         }
-        *reinterpret_cast<uint4*>(p.pool + kv_chunk_offset(ge, page, hh, which - 1, slot, c0)) = b0;
-        *reinterpret_cast<uint4*>(p.pool + kv_chunk_offset(ge, page, hh, which - 1, slot, c1)) = b1;
       }
+      b0 = bits_of(a);
+      b1 = bits_of(b);
+    }
+    char* out = which == 0 ? p.q_out : which == 1 ? p.k_out : p.v_out;
+    if (out != nullptr) {
+      out += (row * (which == 0 ? p.n_q_heads : ge.n_kv_heads) + hh) * ge.row_bytes;
+      *reinterpret_cast<uint4*>(out + c0 * 16) = b0;
+      *reinterpret_cast<uint4*>(out + c1 * 16) = b1;
+    }
+    if (which != 0 && keep) {
+      if constexpr (kFp8) {
+        store_fp8<kLanes>(p, page, slot, hh, which - 1, c0, c1, b0, b1, lane == 0);
+        continue;
+      }
+      *reinterpret_cast<uint4*>(p.pool + kv_chunk_offset(ge, page, hh, which - 1, slot, c0)) = b0;
+      *reinterpret_cast<uint4*>(p.pool + kv_chunk_offset(ge, page, hh, which - 1, slot, c1)) = b1;
     }
   }
 }
 
-template <typename T, int D, int kTokens>
+template <typename T, int D, int kTokens, bool kFp8 = false>
 cudaError_t launch(const RopeParams& p, int max_n_new, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((max_n_new + kTokens - 1) / kTokens, p.n_entries);
@@ -222,7 +214,7 @@ cudaError_t launch(const RopeParams& p, int max_n_new, cudaStream_t st) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, rope_qkv_kernel<T, D, kTokens>, p);
+  return cudaLaunchKernelEx(&cfg, rope_qkv_kernel<T, D, kTokens, kFp8>, p);
 }
 
 }  // namespace
@@ -232,12 +224,14 @@ cudaError_t launch_rope_qkv(const RopeParams& p, int max_n_new, cudaStream_t st)
   if (max_n_new < 1) max_n_new = 1;
   // a token or two per sequence: a block's threads share one token's heads
   const bool step = max_n_new <= 2, wide = p.geom.head_dim == 128;
+  if (p.geom.fp8 && p.pool != nullptr)   // (head_dim 128)
+    return step ? launch<__nv_bfloat16, 128, 1, true>(p, max_n_new, st) : launch<__nv_bfloat16, 128, 4, true>(p, max_n_new, st);
   if (p.geom.elem_bytes == 2) {
     if (step) return wide ? launch<__nv_bfloat16, 128, 1>(p, max_n_new, st) : launch<__nv_bfloat16, 64, 1>(p, max_n_new, st);
-    return wide ? launch<__nv_bfloat16, 128, 8>(p, max_n_new, st) : launch<__nv_bfloat16, 64, 8>(p, max_n_new, st);
+    return wide ? launch<__nv_bfloat16, 128, 4>(p, max_n_new, st) : launch<__nv_bfloat16, 64, 4>(p, max_n_new, st);
   }
   if (step) return wide ? launch<float, 128, 1>(p, max_n_new, st) : launch<float, 64, 1>(p, max_n_new, st);
-  return wide ? launch<float, 128, 8>(p, max_n_new, st) : launch<float, 64, 8>(p, max_n_new, st);
+  return wide ? launch<float, 128, 4>(p, max_n_new, st) : launch<float, 64, 4>(p, max_n_new, st);
 }
 
 }  // namespace mixattn
