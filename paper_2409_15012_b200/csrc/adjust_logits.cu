@@ -9,7 +9,7 @@
 // fp32 logits): it asks for the part's logits, 16 bytes by 16 into registers, reads the row's list meanwhile and
 // adds up, in one word per token of the part in shared memory, what is said about the token (whole-number
 // sums: the result does not depend on their order), then adjusts and writes, and clears the words that were not
-// zero for its next part.  512 rows x 131072 bf16 with lists of 100 to 9000 tokens: 102 us.  On the way: a cluster of CTAs per
+// zero for its next part.  512 rows x 131072 bf16 with lists of 100 to 9000 tokens: 93 us.  On the way: a cluster of CTAs per
 // row that shared one reading of the list, through distributed shared memory, 317 against 312; the tokens of the list
 // taken out of the words one by one beside the stream, 286, by warps of their own, 258, or put adjusted in the
 // words' place by a second reading of the list, 171; quotients instead of products with a reciprocal, 278.
@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPer = 6;           // 16-byte pieces per thread
-constexpr int kCtasPerSm = 4;     // (the words: 48 KB; with 8 pieces per thread and three CTAs 117 us, with 4 and four 124)
+constexpr int kCtasPerSm = 4;     // (the words: 48 KB; with 8 pieces per thread and three CTAs 15 us more, with 4 and four 22)
 // a token's word: times it was generated | occurs in the prompt | 1 + its place in the list of biases
 constexpr uint32_t kCountMask = (1u << 20) - 1, kPromptBit = 1u << 20;
 constexpr int kBiasShift = 21;
@@ -52,10 +52,10 @@ __device__ __forceinline__ TO rounded(float x) {
 __device__ __forceinline__ float widened(float x) { return x; }
 __device__ __forceinline__ float widened(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// bits [at, at + 8) of a mask of `words` words; at >= 0
-__device__ __forceinline__ uint32_t mask_bits(const uint32_t* mask, int at, int words) {
+// bits [at, at + 8) of a mask of `words` words, of which lo is the one with bit `at`; at >= 0
+__device__ __forceinline__ uint32_t mask_bits(const uint32_t* mask, uint32_t lo, int at, int words) {
   const int w = at >> 5;
-  const uint32_t lo = __ldg(mask + w), hi = (at & 31) > 24 && w + 1 < words ? __ldg(mask + w + 1) : 0u;
+  const uint32_t hi = (at & 31) > 24 && w + 1 < words ? __ldg(mask + w + 1) : 0u;
   return __funnelshift_r(lo, hi, at & 31);
 }
 
@@ -173,6 +173,10 @@ adjust_logits_kernel(const __grid_constant__ AdjustParams p, const int parts) {
       });
       __syncthreads();
     }
+    uint32_t lo[kPer];                                                // the pieces' mask words, all under way at once (one after the other: 102 us)
+#pragma unroll
+    for (int u = 0; u < kPer; ++u)
+      if (a.mask && tid + u * kThreads < a.body) lo[u] = __ldg(a.mask + ((a.v0 + (tid + u * kThreads) * kVec) >> 5));
     auto one = [&](int t) {
       uint32_t w = 0u;
       if constexpr (kTable) {
@@ -197,7 +201,7 @@ adjust_logits_kernel(const __grid_constant__ AdjustParams p, const int parts) {
     for (int u = 0; u < kPer; ++u) {
       const int b = tid + u * kThreads, t = a.v0 + b * kVec;
       if (b >= a.body) break;
-      const uint32_t allow = a.mask ? mask_bits(a.mask, t, (p.vocab + 31) / 32) & kAll : kAll;
+      const uint32_t allow = a.mask ? mask_bits(a.mask, lo[u], t, (p.vocab + 31) / 32) & kAll : kAll;
       uint32_t w[kVec], any = 0u;
       if constexpr (kTable) {
         uint4* at = reinterpret_cast<uint4*>(word + (t - a.first));
