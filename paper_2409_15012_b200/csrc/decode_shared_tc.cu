@@ -592,6 +592,16 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
             if (!__all_sync(0xffffffffu, mbar_wait(BAR(L::kXF + (G & 3)), (G >> 2) & 1, abort_flag))) { ok = false; break; }
             scale_keys();
           }
+          // Columns behind the last key hold products with whatever lies there (a page's old rows, an earlier tile).  Their
+          // scores are masked below, but until then they must not have a say in which form of the cap all keys take.
+          if constexpr ((kShape & 1) && !kFp8) {
+            if (t + kTile > s.t1) {
+              const int left = s.t1 - t - 64 * g;
+#pragma unroll
+              for (int e = 0; e < 64; ++e)
+                if (e >= left) sv[e] = 0u;
+            }
+          }
           if constexpr (kShape != 0 && !(kFp8 && kShape == 2)) {   // raw products -> shaped base-2 scores
             float top = 0.f;   // largest square of a product
 #pragma unroll
