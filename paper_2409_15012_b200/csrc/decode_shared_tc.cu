@@ -33,12 +33,17 @@
 // is added to its base-2 score: the weight 2^(s + X - n) is what multiplies the row's codes, and with
 // n the row's reference for s + X, its fp16 rounding (2^-12 of it, or 2^-25 of the largest) is
 // relative to what the keys contribute, however their magnitudes differ.  The sum of the softmax takes the
-// weights times 2^-X in fp32, so reference, sum and accumulator are as ever.  (V as bf16, the weight in two terms:
+// weights times 2^-X in fp32, so reference, sum and accumulator are as ever.  X is taken as -60 at least: the sum's
+// terms stay below 2^75, and a key whose values hardly count keeps its weight in the sum beside exponents of up to
+// 14 (the weight is flushed 126 below the reference).  What a lower X, or a vector of zeros, lacks then is taken off its
+// codes while they are converted (rare): values below 2^-51 in steps of 2^-84.  (V as bf16, the weight in two terms:
 // 2500 cycles a tile for the conversion alone.)  K has one operand buffer (its scores come early), V
 // two, so that a stage is free again as soon as it is converted.
 //
 // TMEM: S0, S1, O_0, O_1 = 4 x 128 columns.  All mbarrier waits are bounded; on time-out a status
 // word is raised and every role leaves its loop.
+#include <cuda_fp16.h>
+
 #include <type_traits>
 
 #include "f32x2.cuh"
@@ -107,6 +112,15 @@ __device__ __forceinline__ void codes_to_f16(uint32_t x, uint32_t& lo, uint32_t&
       "cvt.rn.f16x2.e4m3x2 %0, l;\n\t"
       "cvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
       : "=r"(lo), "=r"(hi) : "r"(x));
+}
+// Lowest exponent of a V row that its weight and the row's sum take in (see the top): byte of 2^-60.
+constexpr uint32_t kLowByte = 127 - 60;
+// two fp16 elements times what the exponents in the two low bytes of e have below that, 2^(byte - kLowByte) (0 for byte 0)
+__device__ __forceinline__ uint32_t times_rest(uint32_t x, uint32_t e) {
+  const float a = __int_as_float((127 + min((int)(e & 0xffu) - (int)kLowByte, 0)) << 23);
+  const float b = __int_as_float((127 + min((int)(e >> 8 & 0xffu) - (int)kLowByte, 0)) << 23);
+  const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&x), __floats2half2_rn(a, b));
+  return *reinterpret_cast<const uint32_t*>(&y);
 }
 __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t x) {
   uint32_t d;
@@ -420,12 +434,10 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
         const unsigned char* xs = raw[n >> 6] + ((n >> 4) & 3) * L::kRawBlk + 2 * kPage * D + (n & 15);
         float fk = 0.f, xv = 0.f, gv = 0.f;   // (keys that are not there are masked)
         if (n < left) {
-          fk = __int_as_float((int)xs[0] << 23) * fold;           // 2^(byte - 127); byte 0 is a vector of zeros,
-          // which in V may have any exponent: low enough not to be the reference, high enough that its weight, which
-          // the row's sum takes, is not flushed to zero beside exponents of up to 14 (that happens 126 below)
-          const int e = xs[kPage] == 0 ? -60 : (int)xs[kPage] - 127;
+          fk = __int_as_float((int)xs[0] << 23) * fold;           // 2^(byte - 127); byte 0 reads as zeros
+          const int e = max((int)xs[kPage], (int)kLowByte) - 127;      // (what is missing below is in the codes)
           xv = (float)e;
-          gv = __int_as_float(min(127 - e, 254) << 23);
+          gv = __int_as_float((127 - e) << 23);
         }
         f[n] = fk;
         f[kTile + n] = xv;
@@ -437,6 +449,13 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
         mbar_arrive(BAR(B_KF));
         mbar_arrive(BAR(L::kXF + (G & 3)));
       }
+      // some V exponent of the tile below kLowByte (looked at four keys per lane)
+      bool low = false;
+      if (4 * lane < left) {
+        const uint32_t x4 = *reinterpret_cast<const uint32_t*>(raw[lane >> 4] + ((lane >> 2) & 3) * L::kRawBlk + 2 * kPage * D + kPage + 4 * (lane & 3));
+        low = ((x4 - 0x01010101u * kLowByte) & ~x4 & 0x80808080u) != 0u;
+      }
+      low = __any_sync(0xffffffffu, low);
       if (G >= 2 && !__all_sync(0xffffffffu, mbar_wait(BAR(L::kVE + (G & 1)), ((G >> 1) - 1) & 1, abort_flag))) return false;
       // V: a channel's 16 keys of a page; rows are channels, 64 keys of a stream each
       if (left >= kTile) {
@@ -468,6 +487,17 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
         const int at = (x & 3) * 2;
         *reinterpret_cast<uint4*>(to + ((at ^ (n & 7)) << 4)) = lo;
         *reinterpret_cast<uint4*>(to + (((at + 1) ^ (n & 7)) << 4)) = hi;
+      }
+      if (low) {   // (over again: with a test per page in the loop above a tree took 49 us for 42, like this 41.3 for 40.8 without)
+#pragma unroll 1
+        for (int x = 0; 16 * x < min(left, kTile); ++x) {
+          const uint4 e = *reinterpret_cast<const uint4*>(raw[x >> 2] + (x & 3) * L::kRawBlk + 2 * kPage * D + kPage);
+          unsigned char* row = gbase + L::kSmV + (G & 1) * L::kTileBytes + (x >> 2) * (128 * 128) + n * 128;
+          uint4* lo = reinterpret_cast<uint4*>(row + (((2 * x & 7) ^ (n & 7)) << 4));
+          uint4* hi = reinterpret_cast<uint4*>(row + (((2 * x & 7) + 1 ^ (n & 7)) << 4));
+          *lo = make_uint4(times_rest(lo->x, e.x), times_rest(lo->y, e.x >> 16), times_rest(lo->z, e.y), times_rest(lo->w, e.y >> 16));
+          *hi = make_uint4(times_rest(hi->x, e.z), times_rest(hi->y, e.z >> 16), times_rest(hi->z, e.w), times_rest(hi->w, e.w >> 16));
+        }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
