@@ -477,7 +477,7 @@ typedef struct {
  *     a = seen ? (x > 0 ? x / repetition : x * repetition) : x
  *     b = a - frequency * c - (c > 0 ? presence : 0)
  *     y = (b + bias) / temperature        tokens that the mask does not allow: -infinity
- * in fp32, rounded once where the output is bf16.  Infinite and NaN logits go through the formula as
+ * in fp32, rounded once where the output is bf16 (whose quotients are products with the reciprocal).  Infinite and NaN logits go through the formula as
  * they are; a row whose mask allows nothing is all -infinity.
  *   logits, out  device, n_rows rows of `vocab` elements of logits_dtype / out_dtype (MIXATTN_F32 or
  *                MIXATTN_BF16; an fp32 row cannot become a bf16 one), row_stride / out_stride elements
