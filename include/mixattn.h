@@ -183,7 +183,8 @@ int mixattn_append_kv_rope(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, cons
  *   theta       f_p = theta^(-2p / rotary_dim); finite and > 1
  *   inv_freq    host, rotary_dim / 2 values f_p of any kind (up to 1e6) instead (theta is then ignored), or NULL
  *   scale       finite and > 0; 0 = 1
- * Angles are formed and reduced in double precision, the rotation runs in fp32, bf16 is rounded once. */
+ * Angles are formed and reduced in double precision with what its products lose carried along (good to 2^-40 for every
+ * position and frequency that is taken), the rotation runs in fp32, bf16 is rounded once. */
 typedef struct {
   int32_t rotary_dim;
   int32_t halves;
@@ -213,7 +214,7 @@ typedef struct {
  * mixattn_append_kv would store them.
  * Errors: those of mixattn_append_kv (with store = 0 a layer need not own its cache), INVALID_ARG (a
  * bad embedding, no input, an output without its input, strides too small, unaligned or so large that 64-bit byte offsets overflow, a position
- * beyond 2^31 - 1). */
+ * beyond 2^31 - 2). */
 int mixattn_rope_qkv(mixattn_ctx* ctx, int32_t layer, int32_t n_seqs, const int32_t* seq_ids,
                      const int32_t* n_new, const int32_t* first_pos, const mixattn_rope* rope,
                      const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,

@@ -625,7 +625,7 @@ int mixattn_rope_qkv(mixattn_ctx* c, int32_t layer, int32_t n_seqs, const int32_
   if (!(rope->scale >= 0.f) || !isfinite(rope->scale)) return MIXATTN_ERR_INVALID_ARG;
   for (int i = 0; i < p.rotary / 2; ++i) {
     p.freq[i] = rope->inv_freq ? rope->inv_freq[i] : pow(rope->theta, -2.0 * i / p.rotary);
-    if (!(fabs(p.freq[i]) <= 1e6)) return MIXATTN_ERR_INVALID_ARG;   // (NaN, or more than a double's angle can carry)
+    if (!(fabs(p.freq[i]) <= 1e6)) return MIXATTN_ERR_INVALID_ARG;   // (NaN, or turns that a double does not count exactly)
   }
   p.scale = rope->scale > 0.f ? rope->scale : 1.f;
   p.halves = rope->halves != 0;

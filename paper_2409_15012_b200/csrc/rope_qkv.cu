@@ -7,7 +7,9 @@
 // A thread keeps one place of the head vectors of one token, two 16-byte chunks that hold whole
 // pairs, and goes over the heads: the sines it needs stay in registers.  A block's sines are
 // formed once, in shared memory: the angle in double precision (positions reach 10^5 and beyond, the first pairs turn
-// by a radian per position), reduced by whole turns, sine and cosine in fp32.
+// by a radian per position), reduced by whole turns, sine and cosine in fp32.  The product of position and
+// frequency reaches 2 10^15, where a double's step is 1/4: its rounding error and 2 pi's are carried along, which leaves
+// the reduced angle good to 2^-49 everywhere.
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 
@@ -126,8 +128,9 @@ __global__ void __launch_bounds__(kThreads, 4) rope_qkv_kernel(const __grid_cons
   fetch(grp);
   for (int i = threadIdx.x; i < n_tok * pairs; i += kThreads) {
     const int x = i / pairs, pr = i - x * pairs;
-    double a = (double)(en.pos0 + tok0 + x) * p.freq[pr];
-    a -= 6.283185307179586476925 * rint(a * 0.15915494309189533577);
+    const double at = en.pos0 + tok0 + x, f = p.freq[pr], far = at * f, turns = rint(far * 0.15915494309189533577);
+    // at f = far + what its rounding lost; 2 pi in two terms: the first difference is exact to 2^-51
+    const double a = fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, far)) + fma(at, f, -far);
     float sn, cs;
     sincosf((float)a, &sn, &cs);
     turn[x][pr] = make_float2(cs * p.scale, sn * p.scale);
