@@ -700,7 +700,8 @@ class Context:
             r.bias_tokens, r.bias_values, r.n_bias = bias_tokens.data_ptr(), bias_values.data_ptr(), bias_tokens.shape[1]
         if allowed is not None:
             at = matrix(allowed, torch.int32)
-            if at is None or allowed.shape[1] < (vocab + 31) // 32:
+            # (a set of no masks has no address, which would read as no set at all)
+            if at is None or allowed.shape[1] < (vocab + 31) // 32 or (rows > 0 and allowed.shape[0] == 0):
                 return ERR_INVALID_ARG
             r.allowed, r.allowed_stride = at
             r.n_allowed = allowed.shape[0]
