@@ -202,7 +202,13 @@ def strerror(code: int) -> str:
 
 
 def _i32(a) -> np.ndarray:
-    return np.ascontiguousarray(a, dtype=np.int32)
+    try:
+        b = np.ascontiguousarray(a, dtype=np.int32)
+    except OverflowError:
+        raise MixAttnError(ERR_INVALID_ARG, "sequence of integers") from None
+    if isinstance(a, np.ndarray) and a.dtype.kind in "iu" and a.dtype != np.int32 and not np.array_equal(a, b):   # (it wraps)
+        raise MixAttnError(ERR_INVALID_ARG, "sequence of integers")
+    return b
 
 
 def _p32(a: Optional[np.ndarray]):
@@ -219,6 +225,8 @@ def _ints(a):
             b = array("i", a)
         except TypeError:
             pass
+        except OverflowError:
+            raise MixAttnError(ERR_INVALID_ARG, "sequence of integers") from None
     if b is None:
         x = np.asarray(a)
         if x.ndim != 1 or x.dtype.kind not in "iufb":
@@ -235,7 +243,7 @@ def _ints_at(a):
     if type(a) is list:
         try:
             b = array("i", a)
-        except TypeError:
+        except (TypeError, OverflowError):      # (_ints refuses the latter)
             pass
         else:
             at, n = b.buffer_info()
