@@ -476,7 +476,9 @@ class Context:
                     outs[1] = self._empty(self._like, (tokens, hkv, d), stream)
                 if v is not None:
                     outs[2] = self._empty(self._like, (tokens, hkv, d), stream)
-        elif out:
+        elif out is not None and out is not False:
+            if type(out) not in (list, tuple) or len(out) != 3:
+                refuse()
             outs = list(out)
             for t, h in zip(outs, (hq, hkv, hkv)):
                 if t is not None and (self._rows(t, h) is None or t.shape[0] != tokens or not t.is_contiguous()):
