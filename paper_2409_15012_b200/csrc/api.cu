@@ -1212,6 +1212,10 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
       });
       if (e != cudaSuccess) return MIXATTN_ERR_CUDA;
       if (tc) {
+        // The split pass comes right behind the tensor-core kernel, and nothing may come between: it reads q, the table and
+        // the pages without a wait of its own, which is sound because that kernel lets its dependents start only after
+        // its own wait for everything ahead of it (and each way out of the split pass waits for that kernel's end, which the
+        // merge relies on).
         plan_own_keys(c, layer, n_leaves, &p, &d);
         d.q = qb;
         d.out = nullptr;

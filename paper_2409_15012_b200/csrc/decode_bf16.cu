@@ -304,7 +304,7 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
   // ... and do not touch global memory before the kernels ahead in the stream have
   // completed and flushed (a no-op when this kernel was launched the ordinary way)
   // (partial launches: the kernel ahead let this one start once everything before it was done, and
-  // nothing here depends on it; it is waited for at the end, for the sake of the merge that follows)
+  // nothing here depends on it; it is waited for on every way out, for the sake of the merge that follows)
   if (!p.partial) asm volatile("griddepcontrol.wait;" ::: "memory");
 
   const KvGeom& ge = p.geom;
@@ -643,7 +643,7 @@ decode_split_bf16_kernel(const __grid_constant__ LaunchParams<SH> p, const int n
     consumer_bar<NCW>();
     const bool gave_up = *abort_flag != 0;  // uniform: set before the barrier by whichever role gave up
     if (gave_up && threadIdx.x == 0) atomicExch(p.status, kDevWaitTimeout);
-    if (CL == 1 && gave_up) return;
+    if (CL == 1 && gave_up) break;   // (a partial launch still waits for the kernel ahead)
     // (in a cluster every consumer thread goes on to the cluster barrier below, which has no
     // time-out of its own: the other CTA's threads reach it after at most their own bounded waits)
     if constexpr (CL > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
