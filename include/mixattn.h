@@ -116,8 +116,10 @@ typedef struct {
 
 /* Bytes of device memory a context with this config carves out of `arena`:
  * K/V storage (see mixattn_cache_bytes), the device copy of the block tables
- * and the split-KV workspace.  Writes *out_bytes.  Errors: INVALID_ARG,
- * INVALID_LAYOUT. */
+ * and the split-KV workspace.  Writes *out_bytes.  (With fewer than 32 query
+ * heads a bf16 context with standard layers counts up to 10.4 MB that only let
+ * mixattn_decode_shared use every SM; an arena that ends short of them is taken
+ * as well.)  Errors: INVALID_ARG, INVALID_LAYOUT. */
 int mixattn_arena_bytes(const mixattn_config* cfg, size_t* out_bytes);
 
 /* Bytes of K/V storage alone: one paged pool of n_pages pages per

@@ -31,14 +31,33 @@ struct ArenaPlan {
   std::vector<size_t> owner_off;  // per owner slot
   std::vector<size_t> owner_bytes;
   size_t table_off = 0, table_bytes = 0;
-  size_t part_o_off = 0, part_ml_off = 0, status_off = 0, ticket_off = 0;
-  size_t shared_o_off = 0, shared_ml_off = 0;   // partial results of shared decode, shared_rows() of them
+  size_t status_off = 0, ticket_off = 0;
   size_t chunk_k_off = 0, chunk_v_off = 0;   // [chunk_scratch_tokens, Hkv, D] each
-  size_t cache_bytes = 0, total = 0;
+  // the split-KV workspace, at the end of the arena: partial results of split_bytes, and what a shared decode lacks beside them
+  size_t part_o_off = 0, part_ml_off = 0, split_bytes = 0;
+  size_t cache_bytes = 0, least = 0, total = 0;   // least: without the latter
 };
 
-// Rows of partial results that a shared decode leaves at most: a segment of 128 rows per CTA, and where items end another.
-int64_t shared_rows(int n_q_heads) { return 160 * 128 + 2 * (int64_t)kMaxCallSeqs * n_q_heads; }
+// Shared decode on the tensor cores (bf16 and quantised caches) divides the workspace: the split pass of the own keys
+// has kOwnChunks slots of a row per query head, the rest is for the tensor-core kernel: at most a segment of 128 rows
+// per CTA, and where items end another.  With 32 query heads of 128 that is the workspace of the ordinary decode; fewer
+// heads need up to 10.4 MB on top to use every SM (12 of 128: 6.7).
+constexpr int kOwnExtraChunks = 384, kOwnChunks = kMaxCallSeqs + kOwnExtraChunks;
+constexpr int kSharedCtas = 160;   // (148 SMs)
+int64_t shared_rows(int n_q_heads) { return kSharedCtas * 128 + 2 * (int64_t)kMaxCallSeqs * n_q_heads; }
+
+size_t rows_bytes(int64_t rows, int head_dim) {
+  return align_up((size_t)rows * head_dim * sizeof(float)) + align_up((size_t)rows * sizeof(float2));
+}
+
+// Rows (at most shared_rows) that fit a workspace of `bytes` behind the own keys' slots.
+int64_t shared_rows_that_fit(size_t bytes, int n_q_heads, int head_dim) {
+  const size_t own = rows_bytes((int64_t)kOwnChunks * n_q_heads, head_dim);
+  if (bytes <= own) return 0;
+  int64_t rows = std::min<int64_t>((bytes - own) / (head_dim * sizeof(float) + sizeof(float2)), shared_rows(n_q_heads));
+  while (rows > 0 && own + rows_bytes(rows, head_dim) > bytes) --rows;
+  return rows;
+}
 
 int ring_pages_of(int window) { return (window + kPage - 1) / kPage; }
 
@@ -59,20 +78,10 @@ ArenaPlan plan_arena(const CacheManager& cm, const mixattn_config& cfg) {
   pl.table_off = off;
   pl.table_bytes = (size_t)cm.max_seqs() * cm.max_blocks() * sizeof(int32_t);
   off += align_up(pl.table_bytes);
-  pl.part_o_off = off;
-  off += align_up((size_t)kWsChunks * cfg.n_q_heads * cfg.head_dim * sizeof(float));
-  pl.part_ml_off = off;
-  off += align_up((size_t)kWsChunks * cfg.n_q_heads * sizeof(float2));
   pl.status_off = off;
   off += kAlign;
   pl.ticket_off = off;
   off += align_up(kBeamTickets * sizeof(int32_t));
-  if (cm.n_full_owners() > 0 && cfg.dtype == MIXATTN_BF16) {
-    pl.shared_o_off = off;
-    off += align_up((size_t)shared_rows(cfg.n_q_heads) * cfg.head_dim * sizeof(float));
-    pl.shared_ml_off = off;
-    off += align_up((size_t)shared_rows(cfg.n_q_heads) * sizeof(float2));
-  }
   if (cfg.chunk_scratch_tokens > 0) {
     const size_t bytes = align_up((size_t)cfg.chunk_scratch_tokens * ge.n_kv_heads * ge.row_bytes);
     pl.chunk_k_off = off;
@@ -80,7 +89,14 @@ ArenaPlan plan_arena(const CacheManager& cm, const mixattn_config& cfg) {
     pl.chunk_v_off = off;
     off += bytes;
   }
-  pl.total = off;
+  const int64_t split_rows = (int64_t)kWsChunks * cfg.n_q_heads;
+  pl.part_o_off = off;
+  pl.part_ml_off = off + align_up((size_t)split_rows * cfg.head_dim * sizeof(float));
+  pl.split_bytes = rows_bytes(split_rows, cfg.head_dim);
+  pl.least = pl.total = off + pl.split_bytes;
+  if (cm.n_full_owners() > 0 && cfg.dtype == MIXATTN_BF16)
+    pl.total = std::max(pl.total, off + rows_bytes((int64_t)kOwnChunks * cfg.n_q_heads, cfg.head_dim) +
+                                      rows_bytes(shared_rows(cfg.n_q_heads), cfg.head_dim));
   return pl;
 }
 
@@ -122,6 +138,7 @@ struct mixattn_ctx {
   // Chunk calls of sliding-window layers whose window is a whole number of key tiles read the
   // cached keys in place from the ring (no copy); off = every chunk call copies.
   bool chunk_ring_direct = true;
+  int64_t shared_room = 0;       // rows of a shared decode's partial results that the arena holds
   bool prefix_sharing = false;   // decode calls go the way of mixattn_decode_shared
   int64_t share_min_bytes = -1;  // what such a call has to save; < 0 = automatic
   uint64_t cache_epoch = 0;   // bumped by every call that changes a cache
@@ -320,12 +337,14 @@ int mixattn_create(const mixattn_config* cfg, mixattn_ctx** out) {
   c->host_only = cfg->device < 0;
   c->device = cfg->device;
   if (!c->host_only) {
-    if (cfg->arena == nullptr || cfg->arena_bytes < c->plan.total ||
+    if (cfg->arena == nullptr || cfg->arena_bytes < c->plan.least ||
         (reinterpret_cast<uintptr_t>(cfg->arena) % kAlign) != 0) {
       delete c;
       return MIXATTN_ERR_INVALID_ARG;
     }
     c->arena = static_cast<char*>(cfg->arena);
+    const size_t arena_bytes = std::min(cfg->arena_bytes, c->plan.total);
+    c->shared_room = shared_rows_that_fit(arena_bytes - c->plan.part_o_off, cfg->n_q_heads, cfg->head_dim);
     DeviceGuard g(c->device);
     int sms = 0, l2 = 0;   // (single attributes: filling the whole property block takes milliseconds)
     if (!g.ok || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, c->device) != cudaSuccess ||
@@ -339,7 +358,7 @@ int mixattn_create(const mixattn_config* cfg, mixattn_ctx** out) {
         prepare_beam_select() != cudaSuccess || prepare_decode_shared() != cudaSuccess ||
         prepare_decode_shared_tc() != cudaSuccess ||
         prepare_adjust_logits() != cudaSuccess) { delete c; return MIXATTN_ERR_CUDA; }
-    if (cudaMemsetAsync(c->arena, 0, c->plan.total, 0) != cudaSuccess ||
+    if (cudaMemsetAsync(c->arena, 0, arena_bytes, 0) != cudaSuccess ||
         cudaStreamSynchronize(0) != cudaSuccess) {
       delete c;
       return MIXATTN_ERR_CUDA;
@@ -544,7 +563,7 @@ int mixattn_beam_select(mixattn_ctx* c, int32_t n_groups, int32_t n_beams, int32
   p.eos = eos_token;
   // the chunks' results live in the split-KV workspace; groups that do not fit it together run
   // one batch after the other
-  const size_t room = c->plan.status_off - c->plan.part_o_off;
+  const size_t room = c->plan.split_bytes;
   const size_t per_chunk = sizeof(float2) + (size_t)n_out * sizeof(uint64_t);
   const int64_t rows = (int64_t)n_groups * n_beams;
   p.n_chunks = beam_chunks((int)rows, vocab, elem, c->sm_count, &p.chunk_granules);
@@ -871,7 +890,8 @@ static int cut_splits(const mixattn_ctx* c, int layer, int nb, int64_t total, De
   if (!p->partial && c->split_tokens == 0 && !c->scores[layer].plain() &&
       total * c->cfg.n_kv_heads * p->head_chunks < (int64_t)kFewItems * c->sm_count * T)
     T = kSplitTokens / 2;
-  int64_t t_min = (total + kWsExtraChunks - 1) / kWsExtraChunks;
+  const int64_t extra = p->partial ? kOwnExtraChunks : kWsExtraChunks;
+  int64_t t_min = (total + extra - 1) / extra;
   t_min = (t_min + kPage - 1) / kPage * kPage;
   if (T < t_min) T = t_min;
   const int64_t pairs = (int64_t)nb * Hkv * p->head_chunks;
@@ -1128,15 +1148,19 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
     p.group = Hq / Hkv;
     p.scale_log2e = c->scale * kLog2e;
     p.split_o = reinterpret_cast<float*>(c->arena + c->plan.part_o_off);
-    p.split_ml = reinterpret_cast<float2*>(c->arena + c->plan.part_ml_off);
+    p.split_ml = reinterpret_cast<float2*>(c->arena + c->plan.part_ml_off);   // (tensor cores: set below)
     p.status = c->dev_status();
     p.shaped = score_shape_of(c, layer, &p.shape) ? 1 : 0;
     int64_t room;
     if (tc) {
       shared_tc_tiles(&p);
-      p.part_o = reinterpret_cast<float*>(c->arena + c->plan.shared_o_off);
-      p.part_ml = reinterpret_cast<float2*>(c->arena + c->plan.shared_ml_off);
-      room = shared_rows(Hq);
+      const int64_t own_rows = (int64_t)kOwnChunks * Hq;
+      char* own = c->arena + c->plan.part_o_off;
+      char* shared = own + rows_bytes(own_rows, D);
+      room = c->shared_room;
+      p.split_ml = reinterpret_cast<float2*>(own + align_up((size_t)own_rows * D * sizeof(float)));
+      p.part_o = reinterpret_cast<float*>(shared);
+      p.part_ml = reinterpret_cast<float2*>(shared + align_up((size_t)room * D * sizeof(float)));
       d.pool = p.pool;
       d.table = p.table;
       d.table_stride = 1;
