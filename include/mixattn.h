@@ -283,7 +283,8 @@ int mixattn_decode_layers(mixattn_ctx* ctx, int32_t layer_begin, int32_t layer_e
  * Arguments, results and errors are those of mixattn_decode, and so is the computation apart from
  * the order in which partial results are added (kept to the same precision).  A sequence may be listed more
  * than once.  Layers with a sliding window (rings are never shared), calls without a common prefix of at
- * least MIXATTN_MIN_SHARED_TOKENS tokens or (bf16) with less than MIXATTN_MIN_SAVED_BYTES to save, and q or
+ * least MIXATTN_MIN_SHARED_TOKENS tokens or (bf16) with less than MIXATTN_MIN_SAVED_BYTES to save or for which
+ * mixattn_decode is estimated to be the faster way (few short sequences), and q or
  * out that are not 16-byte aligned run as mixattn_decode, with its bits.  (Where prefixes are shared, the contents
  * behind a sequence's last token do not matter, for plain scores too; its own keys and values have to be
  * finite.) */
@@ -588,7 +589,7 @@ int mixattn_get_device_status(mixattn_ctx* ctx, int32_t* status);
 int mixattn_set_split_tokens(mixattn_ctx* ctx, int32_t tokens);
 
 /* Bytes of keys and values that a shared decode on a bf16 context has to save to be worth its second and third
- * launch; < 0 = automatic (MIXATTN_MIN_SAVED_BYTES), 0 = always.  Errors: INVALID_ARG for a null context. */
+ * launch; < 0 = automatic (MIXATTN_MIN_SAVED_BYTES, and an estimate of both ways), 0 = always.  Errors: INVALID_ARG for a null context. */
 int mixattn_set_share_min_bytes(mixattn_ctx* ctx, int64_t bytes);
 
 /* Kernel classes for mixattn_profile_read. */

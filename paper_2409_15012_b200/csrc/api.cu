@@ -1068,19 +1068,57 @@ static bool lay_out_shared(const ShareTree& t, bool leaves, int max_ctas, int64_
 // shares follow what each has to do, in microseconds of an SM as measured: the split pass 1.0 for 128 keys and 3
 // for an item (64 one-token items on four CTAs: 53 us), the tensor-core kernel 1.5 for a tile of few rows (its
 // bytes), 1.75 for one of many (its products) and 4 for an item.
-static int own_key_ctas(const ShareTree& t, const SharedDecodeParams& p, const DecodeParams& d, int sm_count) {
-  double own = 0, common = 0;
+struct SharedCost {
+  double own = 0, common = 0;   // per KV head
+};
+static SharedCost shared_cost(const ShareTree& t, const SharedDecodeParams& p, const DecodeParams& d, double few_rows, double many_rows) {
+  SharedCost c;
   for (const SharePiece& s : t.pieces) {
     const double tiles = (s.t1 - s.t0) / 128.0;
     if (s.ns == 1) {
-      own += (tiles + 3.0) * d.head_chunks;
+      c.own += (tiles + 3.0) * d.head_chunks;
     } else {
       const int rows = s.ns * p.group, chunks = (rows + p.row_chunk - 1) / p.row_chunk;
-      common += (tiles * (rows > 64 ? 1.75 : 1.5) + 4.0) * chunks;
+      c.common += (tiles * (rows > 64 ? many_rows : few_rows) + 4.0) * chunks;
     }
   }
-  if (own == 0) return 0;
-  return std::min((int)(sm_count * own / (own + common)) + 1, sm_count - 1);
+  return c;
+}
+static int own_key_ctas(const ShareTree& t, const SharedDecodeParams& p, const DecodeParams& d, int sm_count) {
+  const SharedCost c = shared_cost(t, p, d, 1.5, 1.75);
+  if (c.own == 0) return 0;
+  return std::min((int)(sm_count * c.own / (c.own + c.common)) + 1, sm_count - 1);
+}
+
+// Whether sharing pays: an estimate of either way in microseconds, from what either has to do.  The ordinary decode is
+// not bound by the bytes (what the sequences have in common comes from L2) but by its keys: 19000 (quantised 28000) keys
+// of a KV head per microsecond over all SMs, in rounds of an item per SM, all of a round as long as its items are.
+// The shared one costs its pieces, as above (a quantised tile 2.3), and three launches, which together with the
+// plan take the host 16 and a tenth per sequence.  Measured both ways at 504 points (2 to 64 sequences behind 512 to
+// 32k tokens, nine layouts, 64 and 512 own tokens), calls that take the slower way: by more than 4 % in GPU or
+// wall time, 1 shared (5 %); by more than 10 % in both, 12 ordinary (up to 28 %, one with less than 56 MB to save 75).
+// With the bytes saved as the only measure, 39 (up to twice the time) and 7.  16 sequences behind 1k tokens of 8 heads
+// x 128 (63 MB saved, but of 4 MB): 17.6 us shared, 11.3 ordinary; 8 behind 8k: 18.7 and 47.
+static bool worth_sharing(const mixattn_ctx* c, int layer, int nb, const int32_t* ids, const ShareTree& t, const SharedDecodeParams& p,
+                          ShapedDecodeParams* d) {
+  bool any = false;
+  d->partial = 0;
+  plan_splits(c, layer, ids, nb, d, &any);
+  int64_t keys = 0;
+  int32_t longest = 0;
+  for (int j = 0; j < nb; ++j) {
+    keys += d->n_eff[j];
+    longest = std::max(longest, d->chunk_len[j]);
+  }
+  const bool fp8 = c->geom.fp8 != 0;
+  const int sms = c->sm_count, items = d->total_items;
+  double work = (double)keys * c->cfg.n_kv_heads * d->head_chunks;
+  if (!(items > sms && items <= 2 * sms && longest <= 2048))   // (those run two to an SM, in one round)
+    work *= (double)((items + sms - 1) / sms) * sms / items;
+  const double ordinary = 2.5 + work / (fp8 ? 28000.0 : 19000.0);
+  const SharedCost cost = fp8 ? shared_cost(t, p, *d, 2.3, 2.3) : shared_cost(t, p, *d, 1.5, 1.75);
+  const double shared = (fp8 ? 14.0 : 11.5) + (cost.own + cost.common) * c->cfg.n_kv_heads / sms;
+  return ordinary > std::max(shared, 16.0 + 0.1 * nb);
 }
 
 // The keys that only one sequence has, as a launch of the ordinary split pass: each sequence with its block
@@ -1203,16 +1241,12 @@ static int decode_shared_impl(mixattn_ctx* c, int32_t layer, int32_t n_seqs, con
       for (int32_t least = MIXATTN_MIN_SHARED_TOKENS; !fits; least *= 2) {   // (deep trees of short pieces: only the longer ones)
         build_share_tree(c->cm, layer, nb, ids, least, &tree);
         if (!tree.shared) break;
-        // Worth it?  The two launches more cost 6 to 9 us, as long as it takes to read some 60 MB.  As measured,
-        // shared / plain, with what is saved: 2 sequences behind 16k tokens of 8 heads x 128 (67 MB) 22.6 / 21.3 us, 4 behind
-        // 4k (50 MB) 15.4 / 14.5, 16 behind 1k (63 MB) 15.0 / 11.5, behind 4k (252 MB) 17.3 / 37; 16 behind 4k
-        // of 4 heads x 64 (63 MB) 13.3 / 20.6; quantised, 4 behind 4k (25 MB) 16.5 / 12.4, behind 16k (101 MB)
-        // 31 / 41.  (fp32: always, 14.5 / 28.8 at 200 tokens of 2 sequences.)
-        if (tc) {
+        if (tc) {   // worth it?  (fp32: always, 14.5 against 28.8 us at 200 tokens of 2 sequences)
           int64_t apart = 0;
           for (int j = 0; j < nb; ++j) apart += c->cm.len(layer, ids[j]);
           const int64_t saved = (apart - tree.tokens) * (c->geom.page_bytes / kPage);
           if (saved < (c->share_min_bytes < 0 ? MIXATTN_MIN_SAVED_BYTES : c->share_min_bytes)) break;
+          if (c->share_min_bytes < 0 && !worth_sharing(c, layer, nb, ids, tree, p, &d)) break;
         }
         const int own_ctas = tc ? own_key_ctas(tree, p, d, c->sm_count) : 0;
         d.partial = own_ctas;
