@@ -3,10 +3,12 @@
 // The pieces of the tree, their items and segments are described with SharedDecodeParams
 // (internal.h), the mathematics in decode_shared.cu.  Here the rows of an item, the query heads that
 // read the same keys (up to 128: sequences x heads of a KV head), are the M dimension of the
-// products, so that a page of the cache is read from HBM once for all of them, and what bounds a
-// segment is that stream: a tile of 128 keys and head_dim 128 is 64 KB, 2800 cycles of an SM's share of HBM,
-// against 1500 of products and about as many of exponentials.  A row that stands alone (a sequence's own last
-// keys) costs the same tile of products, which fits under the stream all the same.
+// products, so that a page of the cache is read from HBM once for all of them; more rows are chunks of their own, which
+// read the keys again, from L2 (their CTAs walk side by side).  What bounds a segment: a tile of 128 keys and head_dim 128
+// is 64 KB, 2800 cycles of an SM's share of HBM, and costs each chunk 1536 cycles of products and about as many of
+// exponentials.  So one chunk follows the stream, and with two the products come first (64 sequences of 4 heads behind
+// 32k: tensor pipe 66 % busy, DRAM at 25 %).  The keys that only one sequence has do not come here: a row that stands
+// alone would cost a tile of products like 128 (plan_own_keys, api.cu).
 //
 //   warps 0, 3 page producers for K and for V: ids from the block table, 2 KB tensor copies (16 tokens x
 //              64 channels) into a ring of 128-key stages each.  A warp needs about 100 cycles per
