@@ -29,29 +29,42 @@ constexpr uint32_t kCountMask = (1u << 20) - 1, kPromptBit = 1u << 20;
 constexpr int kBiasShift = 21;
 static_assert(MIXATTN_MAX_RULE_TOKENS <= (int)kCountMask && MIXATTN_MAX_RULE_BIASES < (1 << (32 - kBiasShift)), "fields");
 
-// x / by, inv = 1 / by.  bf16 results take the product, one more rounding of 2^-24 beside their 2^-8.  fp32 results
-// correct it by its residual, which an fma forms exactly: the quotient within half a step (1 + 2^-22).  (fp32 rows with
-// lists of 2000 tokens, 512 x 131072: 114 us without, 126 so, 154 with divisions.)  Infinities and NaN
-// come from the product.  Divisors at the ends of fp32's range, whose reciprocal is none or an inexact
-// one, are left to the division itself: their rows go one logit at a time.
+// What a row divides by, as a factor.  bf16 results take the product with the reciprocal, one more rounding of 2^-24
+// beside their 2^-8.  fp32 results take the reciprocal in two terms, cut off and not rounded in the first, so that the
+// second is positive (for an infinity): x hi + x lo, rounded once, is the quotient within half a step (1 + 2^-21).
+// (fp32 rows with lists of 2000 tokens, 512 x 131072: 114 us with products, 117 so, 126 corrected by the quotient's residual,
+// 154 with divisions; penalties alone in place 120, 135.)  Divisors at the ends of fp32's range, whose reciprocal is none or an inexact one, are left to the
+// division itself: their rows go one logit at a time.
 __device__ __forceinline__ bool ordinary(float by) { return by >= 0x1p-120f && by <= 0x1p60f; }
-__device__ __forceinline__ float corrected(float q, float x, float by, float inv) {
-  const float y = fmaf(-fmaf(q, by, -x), inv, q);   // (so, a zero keeps its sign)
-  return fabsf(q) < INFINITY ? y : q;
-}
+__device__ __forceinline__ float cut_off_reciprocal(float x) { return __frcp_rz(x); }
+template <bool kExact>
+struct Inverse {
+  float hi, lo;
+  Inverse() = default;
+  __device__ __forceinline__ explicit Inverse(float by) : hi(kExact ? cut_off_reciprocal(by) : 1.f / by), lo(0.f) {
+    if (kExact) lo = fmaxf(fmaf(-by, hi, 1.f) / by, 0x1p-149f);
+  }
+  __device__ __forceinline__ float times(float x) const { return kExact ? fmaf(x, hi, x * lo) : x * hi; }
+};
 
+template <bool kExact>
 struct Row {                      // one row's rules
-  float repetition, inv_repetition, frequency, presence;
+  float repetition, frequency, presence;
+  Inverse<kExact> inv_repetition;
   const float* bias;
 };
 
 // A logit whose token's word is w, but for the temperature.
 template <bool kExact>
-__device__ __forceinline__ float adjusted(float x, uint32_t w, const Row& r, bool divide = false) {
+__device__ __forceinline__ float adjusted(float x, uint32_t w, const Row<kExact>& r, bool divide = false) {
   const uint32_t c = w & kCountMask;
   if (w & (kCountMask | kPromptBit)) {
-    const float q = x > 0.f && divide ? x / r.repetition : x * (x > 0.f ? r.inv_repetition : r.repetition);
-    x = kExact && x > 0.f && !divide ? corrected(q, x, r.repetition, r.inv_repetition) : q;
+    const bool up = x > 0.f;
+    if constexpr (kExact) {
+      if (divide) x = up ? x / r.repetition : x * r.repetition;
+      else x = fmaf(x, up ? r.inv_repetition.hi : r.repetition, up ? x * r.inv_repetition.lo : -0.f);   // (adding -0 changes nothing)
+    }
+    else x = up && divide ? x / r.repetition : x * (up ? r.inv_repetition.hi : r.repetition);
   }
   if (c) x -= fmaf(r.frequency, (float)c, r.presence);
   if (w >> kBiasShift) x += r.bias[(w >> kBiasShift) - 1];
@@ -146,18 +159,14 @@ adjust_logits_kernel(const __grid_constant__ AdjustParams p, const int parts) {
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const P a(p, item, parts);
     const bool still = p.in_place && a.temperature == 1.f;            // a token that no rule names stays as it is
-    const float inv_temperature = 1.f / a.temperature;
-    auto cooled = [&](float x) {
-      const float q = x * inv_temperature;
-      return kExact ? corrected(q, x, a.temperature, inv_temperature) : q;
-    };
+    const Inverse<kExact> cooled(a.temperature);
     const uint4* src = reinterpret_cast<const uint4*>(a.in + a.v0);
     uint4 x[kPer];
 #pragma unroll
     for (int u = 0; u < kPer; ++u)
       if (tid + u * kThreads < a.body && !still) x[u] = src[tid + u * kThreads];
-    Row r;
     uint32_t* word = words;                                           // of token a.first; those of a piece are 16-byte aligned
+    Row<kExact> r;
     if constexpr (kTable) {
       word += a.pieces ? (kVec - (a.v0 - a.first) % kVec) % kVec : 0;
       int n = 0, prompt = 0;
@@ -166,7 +175,7 @@ adjust_logits_kernel(const __grid_constant__ AdjustParams p, const int parts) {
         prompt = ru.n_prompt ? min(max(ru.n_prompt[a.row], 0), n) : 0;
       }
       r.repetition = ru.repetition ? ru.repetition[a.row] : 1.f;
-      r.inv_repetition = 1.f / r.repetition;
+      r.inv_repetition = Inverse<kExact>(r.repetition);
       r.frequency = ru.frequency ? ru.frequency[a.row] : 0.f;
       r.presence = ru.presence ? ru.presence[a.row] : 0.f;
       r.bias = ru.bias_values + a.row * ru.n_bias;
@@ -208,7 +217,7 @@ adjust_logits_kernel(const __grid_constant__ AdjustParams p, const int parts) {
       } else if (!still || w != 0u) {
         float f = widened(a.in[t]);
         if (kTable && w != 0u) f = adjusted<kExact>(f, w, r, divide);
-        a.out[t] = rounded<TO>(divide ? f / a.temperature : cooled(f));
+        a.out[t] = rounded<TO>(divide ? f / a.temperature : cooled.times(f));
       }
     };
     if (!a.pieces || divide) {
@@ -256,7 +265,7 @@ adjust_logits_kernel(const __grid_constant__ AdjustParams p, const int parts) {
           if (w[i] != 0u) f[i] = adjusted<kExact>(f[i], w[i], r);
       }
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) f[i] = cooled(f[i]);
+      for (int i = 0; i < kVec; ++i) f[i] = cooled.times(f[i]);
       if (allow != kAll) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
