@@ -124,6 +124,21 @@ __device__ __forceinline__ uint32_t times_rest(uint32_t x, uint32_t e) {
   const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&x), __floats2half2_rn(a, b));
   return *reinterpret_cast<const uint32_t*>(&y);
 }
+// One channel of a tile's V, converted already, times what its keys' exponents have below 2^-60.  Rare, and out of line: the
+// conversion is inlined in three places (tree of two levels, quantised: 39.9 us without this, 39.1 so, 40.4 inlined, 48.5
+// with a test per page in the conversion's loop).
+template <int D, int kRawBlk>
+__device__ __noinline__ void take_rest(unsigned char* v, const unsigned char* raw0, const unsigned char* raw1, int n, int keys) {
+#pragma unroll 1
+  for (int x = 0; 16 * x < keys; ++x) {
+    const uint4 e = *reinterpret_cast<const uint4*>((x < 4 ? raw0 : raw1) + (x & 3) * kRawBlk + 2 * kPage * D + kPage);
+    unsigned char* row = v + (x >> 2) * (128 * 128) + n * 128;
+    uint4* lo = reinterpret_cast<uint4*>(row + (((2 * x & 7) ^ (n & 7)) << 4));
+    uint4* hi = reinterpret_cast<uint4*>(row + (((2 * x & 7) + 1 ^ (n & 7)) << 4));
+    *lo = make_uint4(times_rest(lo->x, e.x), times_rest(lo->y, e.x >> 16), times_rest(lo->z, e.y), times_rest(lo->w, e.y >> 16));
+    *hi = make_uint4(times_rest(hi->x, e.z), times_rest(hi->y, e.z >> 16), times_rest(hi->z, e.w), times_rest(hi->w, e.w >> 16));
+  }
+}
 __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t x) {
   uint32_t d;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(__uint_as_float(x & 0xffff0000u)), "f"(__uint_as_float(x << 16)));
@@ -490,17 +505,7 @@ decode_shared_tc_kernel(const __grid_constant__ CUtensorMap pages, const __grid_
         *reinterpret_cast<uint4*>(to + ((at ^ (n & 7)) << 4)) = lo;
         *reinterpret_cast<uint4*>(to + (((at + 1) ^ (n & 7)) << 4)) = hi;
       }
-      if (low) {   // (over again: with a test per page in the loop above a tree took 49 us for 42, like this 41.3 for 40.8 without)
-#pragma unroll 1
-        for (int x = 0; 16 * x < min(left, kTile); ++x) {
-          const uint4 e = *reinterpret_cast<const uint4*>(raw[x >> 2] + (x & 3) * L::kRawBlk + 2 * kPage * D + kPage);
-          unsigned char* row = gbase + L::kSmV + (G & 1) * L::kTileBytes + (x >> 2) * (128 * 128) + n * 128;
-          uint4* lo = reinterpret_cast<uint4*>(row + (((2 * x & 7) ^ (n & 7)) << 4));
-          uint4* hi = reinterpret_cast<uint4*>(row + (((2 * x & 7) + 1 ^ (n & 7)) << 4));
-          *lo = make_uint4(times_rest(lo->x, e.x), times_rest(lo->y, e.x >> 16), times_rest(lo->z, e.y), times_rest(lo->w, e.y >> 16));
-          *hi = make_uint4(times_rest(hi->x, e.z), times_rest(hi->y, e.z >> 16), times_rest(hi->z, e.w), times_rest(hi->w, e.w >> 16));
-        }
-      }
+      if (low) take_rest<D, L::kRawBlk>(gbase + L::kSmV + (G & 1) * L::kTileBytes, raw[0], raw[1], n, min(left, kTile));
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) {
