@@ -32,17 +32,18 @@ static_assert(MIXATTN_MAX_RULE_TOKENS <= (int)kCountMask && MIXATTN_MAX_RULE_BIA
 // What a row divides by, as a factor.  bf16 results take the product with the reciprocal, one more rounding of 2^-24
 // beside their 2^-8.  fp32 results take the reciprocal in two terms, cut off and not rounded in the first, so that the
 // second is positive (for an infinity): x hi + x lo, rounded once, is the quotient within half a step (1 + 2^-21).
-// (fp32 rows with lists of 2000 tokens, 512 x 131072: 114 us with products, 117 so, 126 corrected by the quotient's residual,
-// 154 with divisions; penalties alone in place 120, 135.)  Divisors at the ends of fp32's range, whose reciprocal is none or an inexact one, are left to the
-// division itself: their rows go one logit at a time.
-__device__ __forceinline__ bool ordinary(float by) { return by >= 0x1p-120f && by <= 0x1p60f; }
+// (fp32 rows with lists of 2000 tokens, 512 x 131072: 114 us with products, 121 so, 126 corrected by the quotient's residual,
+// 154 with divisions; penalties alone in place 120, 136.)  Divisors at the ends of fp32's range, whose reciprocal is none or an inexact one, are left to the
+// division itself: their rows go one logit at a time.  (0 is no divisor; it multiplies by fp32's largest number, so that
+// a logit of 0 does not turn into a NaN.)
+__device__ __forceinline__ bool ordinary(float by) { return (by >= 0x1p-120f && by <= 0x1p60f) || by == 0.f; }
 __device__ __forceinline__ float cut_off_reciprocal(float x) { return __frcp_rz(x); }
 template <bool kExact>
 struct Inverse {
   float hi, lo;
   Inverse() = default;
-  __device__ __forceinline__ explicit Inverse(float by) : hi(kExact ? cut_off_reciprocal(by) : 1.f / by), lo(0.f) {
-    if (kExact) lo = fmaxf(fmaf(-by, hi, 1.f) / by, 0x1p-149f);
+  __device__ __forceinline__ explicit Inverse(float by) : hi(fminf(kExact ? cut_off_reciprocal(by) : 1.f / by, 3.4028235e38f)), lo(0.f) {
+    if (kExact) lo = by == 0.f ? 0x1p-149f : fmaxf(fmaf(-by, hi, 1.f) / by, 0x1p-149f);
   }
   __device__ __forceinline__ float times(float x) const { return kExact ? fmaf(x, hi, x * lo) : x * hi; }
 };

@@ -85,3 +85,20 @@ def test_divisors_from_end_to_end(ti, to, rule):
     else:
         bound = torch.finfo(to).eps / 2 * want.abs() * 1.001 + 4 * 2.0 ** -24 * want.abs() + 2.0 ** -134 + 2.0 ** -149
         assert ((out.double() - want).abs()[~near] <= bound[~near]).all()
+
+
+@pytest.mark.parametrize("ti,to", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32)])
+def test_a_divisor_of_zero_leaves_no_nan(ti, to):
+    """It is none, but loops that set it for their greedy rows keep the order of what fp32 can tell apart."""
+    mx, ctx = context()
+    gen = torch.Generator("cuda").manual_seed(7)
+    logits = (torch.randn(3, 4097, generator=gen, device="cuda") * 2).to(ti)
+    logits[:, ::9] = 0.0
+    zero = torch.tensor([0.0, 1.0, 0.0], device="cuda")
+    out = torch.empty(3, 4097, device="cuda", dtype=to)
+    ctx.adjust_logits(logits, out, temperature=zero)
+    want = logits.float() * torch.where(zero == 0, torch.finfo(torch.float32).max, 1.0)[:, None]
+    assert torch.equal(out, want.to(to))
+    everything = torch.arange(4097, device="cuda", dtype=torch.int32).repeat(3, 1)
+    ctx.adjust_logits(logits, out, tokens=everything, repetition=zero)
+    assert not torch.isnan(out).any() and torch.equal(out[1], logits[1].to(to))
